@@ -16,19 +16,27 @@
 #include <vector>
 
 #include "../../include/ic_cache.h"
+#include "host_util.h"
 #include "kernels.h"
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
 
-int fail(int code, const char* fmt, ...) {
+int icc::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof g_err, fmt, ap);
   va_end(ap);
   return code;
 }
+
+namespace {
+
+using icc::DeviceGuard;
+using icc::EncodeTiledFn;
+using icc::fail;
+using icc::is_device_ptr;
 
 constexpr int WINDOW_MAX_NQ = 1024;   // queries scored per pass over the slab
 constexpr int QUERY_TILE = 128;       // tcgen05 path: queries per CTA (MMA M)
@@ -60,26 +68,10 @@ unsigned next_epoch() {
   return e;
 }
 
-struct DeviceGuard {
-  int prev = -1;
-  bool changed = false;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) == cudaSuccess && prev != dev) changed = (cudaSetDevice(dev) == cudaSuccess);
-  }
-  ~DeviceGuard() {
-    if (changed) cudaSetDevice(prev);
-  }
-};
-
 struct Buffer {
   void* p = nullptr;
   size_t bytes = 0;
 };
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                                  CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
-                                  CUtensorMapFloatOOBfill);
 
 }  // namespace
 
@@ -128,16 +120,6 @@ struct ic_cache {
 namespace {
 
 size_t in_elem_bytes(const ic_cache* c) { return c->input_dtype == IC_F32 ? 4 : 2; }
-
-bool is_device_ptr(const void* p, int device) {
-  cudaPointerAttributes a;
-  if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
-    cudaGetLastError();
-    return false;
-  }
-  if (a.type == cudaMemoryTypeManaged) return true;
-  return a.type == cudaMemoryTypeDevice && a.device == device;
-}
 
 int ensure(ic_cache* c, Buffer& b, size_t bytes, const char* what) {
   if (bytes <= b.bytes) return IC_OK;

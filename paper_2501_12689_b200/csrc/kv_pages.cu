@@ -1,0 +1,480 @@
+// Page operations of the paged key-value cache: reserve, write, fork, free, compact.
+//
+// The state is three integer arrays on the device (page tables, lengths, reference counts) and there is
+// no free list beside them: a page is free if its count is 0, and pages are handed out lowest number
+// first.  That makes the tables a function of the calls alone, needs nothing rebuilt after a restore, and
+// costs one pass over the counts per allocation, 4 bytes a page.
+#include "common.cuh"
+#include "kv.h"
+
+namespace icc {
+
+namespace {
+
+constexpr int PLAN_THREADS = 1024;        // planning kernels: one CTA, so that its barriers order the steps
+constexpr int PAGES_PER_THREAD = 32;      // counts that a thread of a planning kernel looks at per round
+constexpr int COPY_THREADS = 256;
+constexpr int COPY_UNIT = COPY_THREADS * 16 * 4;   // bytes of a page that a CTA copies at a time
+constexpr int ROW_UNIT = 1024;            // table entries that a CTA updates at a time
+
+// Exclusive prefix sum over the CTA; *total gets the sum.  Unsigned, so that two packed counters may be
+// summed at once.  `sums`: 33 words of shared memory; ends with a barrier.
+__device__ __forceinline__ unsigned block_scan(unsigned x, unsigned* sums, unsigned* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned inc = x;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const unsigned y = __shfl_up_sync(FULL_MASK, inc, d);
+    if (lane >= d) inc += y;
+  }
+  if (lane == 31) sums[warp] = inc;
+  __syncthreads();
+  if (warp == 0) {
+    const unsigned w = lane < (int)(blockDim.x >> 5) ? sums[lane] : 0u;
+    unsigned winc = w;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const unsigned y = __shfl_up_sync(FULL_MASK, winc, d);
+      if (lane >= d) winc += y;
+    }
+    sums[lane] = winc - w;
+    if (lane == 31) sums[32] = winc;
+  }
+  __syncthreads();
+  const unsigned before = sums[warp] + inc - x;
+  *total = sums[32];
+  __syncthreads();
+  return before;
+}
+
+// Bit b of the result: page p0 + b exists and its reference count is 0.
+__device__ __forceinline__ unsigned free_mask(const int* refs, int n_pages, int p0) {
+  unsigned m = 0;
+  if (p0 + PAGES_PER_THREAD <= n_pages) {
+    int4 r[PAGES_PER_THREAD / 4];
+#pragma unroll
+    for (int j = 0; j < PAGES_PER_THREAD / 4; ++j) r[j] = reinterpret_cast<const int4*>(refs + p0)[j];
+#pragma unroll
+    for (int j = 0; j < PAGES_PER_THREAD / 4; ++j)
+      m |= ((r[j].x == 0 ? 1u : 0u) | (r[j].y == 0 ? 2u : 0u) | (r[j].z == 0 ? 4u : 0u) | (r[j].w == 0 ? 8u : 0u)) << (4 * j);
+  } else {
+    for (int b = 0; p0 + b < n_pages; ++b) m |= (refs[p0 + b] == 0 ? 1u : 0u) << b;
+  }
+  return m;
+}
+
+// The lowest `need` free pages, in order, into `list`; returns how many were found (at least `need` if
+// there are that many).  Whole CTA; ends with a barrier.
+__device__ int take_free_pages(const KvView& v, int need, int* list, unsigned* sums) {
+  int found = 0;
+  for (int base = 0; base < v.n_pages && found < need; base += PLAN_THREADS * PAGES_PER_THREAD) {
+    const int p0 = base + threadIdx.x * PAGES_PER_THREAD;
+    unsigned m = p0 < v.n_pages ? free_mask(v.refs, v.n_pages, p0) : 0u;
+    unsigned total;
+    int r = found + (int)block_scan(__popc(m), sums, &total);
+    while (m && r < need) {
+      list[r++] = p0 + __ffs(m) - 1;
+      m &= m - 1;
+    }
+    found += (int)total;
+  }
+  __syncthreads();
+  return found;
+}
+
+// Which of begin[0..n) holds rank r (begin ascends; entries without pages repeat their successor's value).
+__device__ __forceinline__ int owner_of(const int* begin, int n, int r) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (begin[mid] <= r) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// ---------------------------------------------------------------- reserve
+// One CTA: check the arguments and sum up the pages they need, find that many free pages, and only then
+// write tables, counts and lengths.
+__global__ void __launch_bounds__(PLAN_THREADS) kv_reserve_kernel(const KvView v, const int* __restrict__ seqs,
+                                                                  const int* __restrict__ counts, int n) {
+  extern __shared__ int begin[];          // [n] rank of a sequence's first fresh page
+  __shared__ unsigned sums[33];
+  __shared__ int bad;
+  if (*v.err != KV_OK) return;
+  if (threadIdx.x == 0) bad = KV_OK;
+  __syncthreads();
+  long long need = 0;
+  for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
+    const int i = i0 + threadIdx.x;
+    unsigned mine = 0;
+    if (i < n) {
+      const int s = seqs[i], c = counts[i];
+      if (s < 0 || s >= v.max_seqs || c < 0) {
+        bad = KV_INVALID;
+      } else if (atomicExch(&v.mark[s], 1) != 0) {
+        bad = KV_INVALID;
+      } else {
+        const int had = v.lengths[s];
+        const long long will = (long long)had + c;
+        if (had < 0 || will > ((long long)v.max_pages << v.page_shift)) atomicCAS(&bad, KV_OK, KV_FULL);
+        else mine = kv_pages_of((int)will, v.page_shift) - kv_pages_of(had, v.page_shift);
+      }
+    }
+    unsigned total;
+    const unsigned before = block_scan(mine, sums, &total);
+    if (i < n) begin[i] = (int)min(need + before, 0x7fffffffll);
+    need += total;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += PLAN_THREADS) {
+    const int s = seqs[i];
+    if (s >= 0 && s < v.max_seqs) v.mark[s] = 0;
+  }
+  int why = bad;
+  if (why == KV_OK && need > v.n_pages) why = KV_FULL;
+  if (why == KV_OK && need > 0 && take_free_pages(v, (int)need, v.fresh, sums) < need) why = KV_FULL;
+  if (why != KV_OK) {
+    if (threadIdx.x == 0) kv_report(v, why);
+    return;
+  }
+  for (int r = threadIdx.x; r < (int)need; r += PLAN_THREADS) {
+    const int i = owner_of(begin, n, r), s = seqs[i], page = v.fresh[r];
+    v.tables[(size_t)s * v.max_pages + kv_pages_of(v.lengths[s], v.page_shift) + (r - begin[i])] = page;
+    v.refs[page] = 1;
+  }
+  __syncthreads();                        // every old length has been read
+  for (int i = threadIdx.x; i < n; i += PLAN_THREADS) v.lengths[seqs[i]] += counts[i];
+}
+
+// ---------------------------------------------------------------- write
+// TOKENS tokens per CTA.  The first threads find their token's place (sequence, position, page); then all
+// threads move 16-byte pieces.  A head's rows of one page are contiguous, so the pieces of neighbouring
+// tokens fill whole lines.
+template <int TOKENS>
+__global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, int layer, const uint4* __restrict__ k,
+                                                                const uint4* __restrict__ val, int64_t token_stride, int64_t head_stride,
+                                                                const int* __restrict__ seqs, const int* __restrict__ starts, int n,
+                                                                int64_t n_tokens) {
+  __shared__ unsigned char* place[TOKENS];   // first byte of the token's key row of head 0, or null
+  if (*v.err != KV_OK) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
+  for (int x = warp; x < TOKENS; x += COPY_THREADS / 32) {
+    const int64_t t = t0 + x;
+    unsigned char* at = nullptr;
+    if (t < n_tokens) {
+      // sequence of token t: the last one that starts at or before it
+      int i = (int)t, begin = (int)t, end = (int)t + 1;
+      if (starts) {
+        int below = 0;
+        for (int j = lane; j - lane < n; j += 32) below += __popc(__ballot_sync(FULL_MASK, j < n && starts[j] <= t));
+        i = below - 1;
+        begin = i >= 0 ? starts[i] : 0;
+        end = i >= 0 ? starts[i + 1] : 0;
+      }
+      const int s = i >= 0 ? seqs[i] : -1;
+      bool fine = s >= 0 && s < v.max_seqs && t < end;
+      if (fine) {
+        const int64_t pos = (int64_t)v.lengths[s] - end + t;
+        fine = pos >= 0 && begin >= 0 && pos < ((int64_t)v.max_pages << v.page_shift);
+        if (fine) {
+          const int page = v.tables[(size_t)s * v.max_pages + (size_t)(pos >> v.page_shift)];
+          fine = page >= 0 && page < v.n_pages;
+          const size_t row = (size_t)layer * 2 * v.n_kv_heads << v.page_shift;
+          at = v.pool + (size_t)page * v.page_bytes + (row + (size_t)(pos & ((1 << v.page_shift) - 1))) * v.head_dim * 2;
+        }
+      }
+      if (!fine) {
+        at = nullptr;
+        if (lane == 0) kv_report(v, KV_INVALID);
+      }
+    }
+    if (lane == 0) place[x] = at;
+  }
+  __syncthreads();
+  const int pieces = v.head_dim >> 3, per_token = v.n_kv_heads * pieces;
+  const size_t block = ((size_t)v.head_dim * 2) << v.page_shift;      // bytes of one head's keys in a page
+  for (int u = threadIdx.x; u < TOKENS * 2 * per_token; u += COPY_THREADS) {
+    const int x = u / (2 * per_token), r = u - x * 2 * per_token;
+    const int is_v = r >= per_token, hp = is_v ? r - per_token : r;
+    const int h = hp / pieces, piece = hp - h * pieces;
+    unsigned char* at = place[x];
+    if (!at) continue;
+    const uint4 w = (is_v ? val : k)[((t0 + x) * token_stride + h * head_stride) / 8 + piece];
+    *reinterpret_cast<uint4*>(at + (size_t)(is_v * v.n_kv_heads + h) * block + (size_t)piece * 16) = w;
+  }
+}
+
+// An owned table entry names a page of the pool.  One that does not (borrowed tables that are not an
+// earlier cache's) is reported and left alone.
+__device__ __forceinline__ bool page_exists(const KvView& v, int page) {
+  if ((unsigned)page < (unsigned)v.n_pages) return true;
+  kv_report(v, KV_INVALID);
+  return false;
+}
+
+// ---------------------------------------------------------------- copying whole pages
+// All CTAs of the grid share the pages jobs[0..n_jobs), a COPY_UNIT at a time.
+__device__ __forceinline__ void copy_pages(const KvView& v, int n_jobs) {
+  const long long units_per_page = (long long)((v.page_bytes + COPY_UNIT - 1) / COPY_UNIT);
+  for (long long u = blockIdx.x; u < n_jobs * units_per_page; u += gridDim.x) {
+    const int j = (int)(u / units_per_page);
+    const size_t off = (size_t)(u - j * units_per_page) * COPY_UNIT + threadIdx.x * 16;
+    const int2 job = v.jobs[j];
+    const unsigned char* from = v.pool + (size_t)job.x * v.page_bytes;
+    unsigned char* to = v.pool + (size_t)job.y * v.page_bytes;
+    uint4 w[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (off + x * COPY_THREADS * 16 < v.page_bytes) w[x] = ld_stream_16B(from + off + x * COPY_THREADS * 16);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (off + x * COPY_THREADS * 16 < v.page_bytes) __stcs(reinterpret_cast<uint4*>(to + off + x * COPY_THREADS * 16), w[x]);
+  }
+}
+
+// ---------------------------------------------------------------- fork
+// Three launches: a plan by one CTA (arguments, pages needed, free pages), the children's new rows made
+// beside the old ones while all parents still stand, and the exchange of rows with the copies.
+__global__ void __launch_bounds__(PLAN_THREADS) kv_fork_plan_kernel(const KvView v, const int* __restrict__ parents,
+                                                                    const int* __restrict__ children, const int* __restrict__ upto,
+                                                                    int n, int copy) {
+  __shared__ unsigned sums[33];
+  __shared__ int bad;
+  if (threadIdx.x == 0) {
+    bad = KV_OK;
+    v.meta[0] = 0;
+  }
+  __syncthreads();
+  if (*v.err != KV_OK) return;
+  long long need = 0;
+  for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
+    const int i = i0 + threadIdx.x;
+    unsigned mine = 0;
+    if (i < n) {
+      const int a = parents[i], b = children[i];
+      if (a < 0 || a >= v.max_seqs || b < 0 || b >= v.max_seqs || atomicExch(&v.mark[b], 1) != 0) {
+        bad = KV_INVALID;
+      } else {
+        const int len = v.lengths[a], want = upto ? upto[i] : len;
+        if (want < 0 || want > len || len > ((long long)v.max_pages << v.page_shift)) {
+          bad = KV_INVALID;
+        } else {
+          const bool nothing = !copy && a == b && want == len;
+          const int pages = kv_pages_of(want, v.page_shift);
+          const int shared = copy ? 0 : (nothing ? pages : want >> v.page_shift);
+          v.had[i] = v.lengths[b];
+          v.upto[i] = nothing ? -1 : want;
+          v.shared[i] = shared;
+          mine = pages - shared;
+        }
+      }
+    }
+    unsigned total;
+    const unsigned before = block_scan(mine, sums, &total);
+    if (i < n) v.begin[i] = (int)min(need + before, 0x7fffffffll);
+    need += total;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += PLAN_THREADS) {
+    const int b = children[i];
+    if (b >= 0 && b < v.max_seqs) v.mark[b] = 0;
+  }
+  int why = bad;
+  if (why == KV_OK && need > v.n_pages) why = KV_FULL;
+  if (why == KV_OK && need > 0 && take_free_pages(v, (int)need, v.fresh, sums) < need) why = KV_FULL;
+  if (threadIdx.x == 0) {
+    if (why != KV_OK) {
+      kv_report(v, why);
+    } else {
+      v.meta[0] = 1;
+      v.meta[1] = (int)need;
+    }
+  }
+}
+
+__global__ void __launch_bounds__(COPY_THREADS) kv_fork_stage_kernel(const KvView v, const int* __restrict__ parents, int n) {
+  if (v.meta[0] == 0) return;
+  const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
+  for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
+    const int i = (int)(u / chunks), c0 = (int)(u - (long long)i * chunks) * ROW_UNIT;
+    const int want = v.upto[i];
+    if (want < 0) continue;
+    const int end = min(kv_pages_of(want, v.page_shift), c0 + ROW_UNIT), shared = v.shared[i], begin = v.begin[i];
+    const int* row = v.tables + (size_t)parents[i] * v.max_pages;
+    int* to = v.staged + (size_t)i * v.max_pages;
+    for (int c = c0 + threadIdx.x; c < end; c += COPY_THREADS) {
+      const int page = row[c];
+      if (!page_exists(v, page)) continue;
+      if (c < shared) {
+        atomicAdd(&v.refs[page], 1);
+        to[c] = page;
+      } else {
+        const int r = begin + c - shared, mine = v.fresh[r];
+        v.refs[mine] = 1;
+        v.jobs[r] = make_int2(page, mine);
+        to[c] = mine;
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(COPY_THREADS) kv_fork_apply_kernel(const KvView v, const int* __restrict__ children, int n) {
+  if (v.meta[0] == 0) return;
+  const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
+  for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
+    const int i = (int)(u / chunks), c0 = (int)(u - (long long)i * chunks) * ROW_UNIT;
+    const int want = v.upto[i];
+    if (want < 0) continue;
+    const int b = children[i], left = kv_pages_of(v.had[i], v.page_shift), pages = kv_pages_of(want, v.page_shift);
+    const int end = min(max(left, pages), c0 + ROW_UNIT);
+    int* row = v.tables + (size_t)b * v.max_pages;
+    const int* from = v.staged + (size_t)i * v.max_pages;
+    for (int c = c0 + threadIdx.x; c < end; c += COPY_THREADS) {
+      if (c < left && page_exists(v, row[c])) atomicSub(&v.refs[row[c]], 1);
+      if (c < pages) row[c] = from[c];
+    }
+    if (c0 == 0 && threadIdx.x == 0) v.lengths[b] = want;
+  }
+  copy_pages(v, v.meta[1]);
+}
+
+// ---------------------------------------------------------------- free
+// A CTA per sequence.  Whoever takes the length away owns the release, so a number that comes twice counts once.
+__global__ void __launch_bounds__(COPY_THREADS) kv_free_kernel(const KvView v, const int* __restrict__ seqs, int n) {
+  __shared__ int had;
+  if (*v.err != KV_OK) return;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int s = seqs[i];
+    if (s < 0 || s >= v.max_seqs) {
+      if (threadIdx.x == 0) kv_report(v, KV_INVALID);
+      continue;
+    }
+    if (threadIdx.x == 0) had = atomicExch(&v.lengths[s], 0);
+    __syncthreads();
+    const int pages = kv_pages_of(had, v.page_shift);
+    const int* row = v.tables + (size_t)s * v.max_pages;
+    for (int c = threadIdx.x; c < pages; c += COPY_THREADS)
+      if (page_exists(v, row[c])) atomicSub(&v.refs[row[c]], 1);
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- compact
+// The plan: count the live pages, then give the holes below that number and the live pages above it
+// their ranks; rank r's page moves to rank r's hole.
+__global__ void __launch_bounds__(PLAN_THREADS) kv_compact_plan_kernel(const KvView v) {
+  __shared__ unsigned sums[33];
+  if (threadIdx.x == 0) v.meta[0] = 0;
+  if (*v.err != KV_OK) return;
+  constexpr int ROUND = PLAN_THREADS * PAGES_PER_THREAD;
+  int n_free = 0;
+  for (int base = 0; base < v.n_pages; base += ROUND) {
+    const int p0 = base + threadIdx.x * PAGES_PER_THREAD;
+    unsigned total;
+    block_scan(p0 < v.n_pages ? __popc(free_mask(v.refs, v.n_pages, p0)) : 0, sums, &total);
+    n_free += (int)total;
+  }
+  const int n_live = v.n_pages - n_free;
+  int holes = 0, movers = 0;
+  for (int base = 0; base < v.n_pages; base += ROUND) {
+    const int p0 = base + threadIdx.x * PAGES_PER_THREAD;
+    unsigned hole = 0, move = 0;
+    if (p0 < v.n_pages) {
+      const unsigned f = free_mask(v.refs, v.n_pages, p0);
+      const int here = min(PAGES_PER_THREAD, v.n_pages - p0), below = max(0, min(PAGES_PER_THREAD, n_live - p0));
+      const unsigned exist = here == 32 ? ~0u : (1u << here) - 1u, low = below == 32 ? ~0u : (1u << below) - 1u;
+      hole = f & low;
+      move = ~f & exist & ~low;
+    }
+    unsigned total;      // two counts in one scan: at most 32,768 pages a round, so neither overflows its half
+    const unsigned before = block_scan((unsigned)__popc(hole) | ((unsigned)__popc(move) << 16), sums, &total);
+    int r = holes + (int)(before & 0xffffu);
+    for (unsigned m = hole; m; m &= m - 1) v.jobs[r++].y = p0 + __ffs(m) - 1;
+    r = movers + (int)(before >> 16);
+    for (unsigned m = move; m; m &= m - 1) {
+      const int p = p0 + __ffs(m) - 1;
+      v.jobs[r].x = p;
+      v.fresh[p] = r++;
+    }
+    holes += (int)(total & 0xffffu);
+    movers += (int)(total >> 16);
+  }
+  if (threadIdx.x == 0) {
+    v.meta[0] = 1;
+    v.meta[1] = movers;
+    v.meta[2] = n_live;
+  }
+}
+
+__global__ void __launch_bounds__(COPY_THREADS) kv_compact_apply_kernel(const KvView v) {
+  if (v.meta[0] == 0) return;
+  const int n_jobs = v.meta[1], n_live = v.meta[2];
+  if (n_jobs == 0) return;
+  const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
+  for (long long u = blockIdx.x; u < (long long)v.max_seqs * chunks; u += gridDim.x) {
+    const int s = (int)(u / chunks), c0 = (int)(u - (long long)s * chunks) * ROW_UNIT;
+    const int end = min(kv_pages_of(v.lengths[s], v.page_shift), c0 + ROW_UNIT);
+    int* row = v.tables + (size_t)s * v.max_pages;
+    for (int c = c0 + threadIdx.x; c < end; c += COPY_THREADS) {
+      const int page = row[c];
+      if (page >= n_live && page < v.n_pages) row[c] = v.jobs[v.fresh[page]].y;
+    }
+  }
+  for (int r = blockIdx.x * COPY_THREADS + threadIdx.x; r < n_jobs; r += gridDim.x * COPY_THREADS) {
+    const int2 job = v.jobs[r];
+    v.refs[job.y] = v.refs[job.x];
+    v.refs[job.x] = 0;
+  }
+  copy_pages(v, n_jobs);
+}
+
+}  // namespace
+
+cudaError_t kv_pages_configure(int smem_optin) {
+  (void)smem_optin;
+  return cudaFuncSetAttribute(kv_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 16384 * 4);
+}
+
+cudaError_t kv_reserve_launch(const KvView& v, const int* seqs, const int* counts, int n, cudaStream_t st) {
+  kv_reserve_kernel<<<1, PLAN_THREADS, (size_t)n * 4, st>>>(v, seqs, counts, n);
+  return cudaGetLastError();
+}
+
+cudaError_t kv_write_launch(const KvView& v, int layer, const void* k, const void* val, int64_t token_stride, int64_t head_stride,
+                            const int* seqs, const int* starts, int n, int64_t n_tokens, int sm_count, cudaStream_t st) {
+  const uint4* k4 = static_cast<const uint4*>(k);
+  const uint4* v4 = static_cast<const uint4*>(val);
+  if (n_tokens <= 4 * sm_count)
+    kv_write_kernel<1><<<(unsigned)n_tokens, COPY_THREADS, 0, st>>>(v, layer, k4, v4, token_stride, head_stride, seqs, starts, n, n_tokens);
+  else
+    kv_write_kernel<8><<<(unsigned)((n_tokens + 7) / 8), COPY_THREADS, 0, st>>>(v, layer, k4, v4, token_stride, head_stride, seqs, starts, n,
+                                                                               n_tokens);
+  return cudaGetLastError();
+}
+
+cudaError_t kv_fork_launch(const KvView& v, const int* parents, const int* children, const int* upto, int n, int copy,
+                           int sm_count, int* launches, cudaStream_t st) {
+  const long long rows = (long long)n * ((v.max_pages + ROW_UNIT - 1) / ROW_UNIT);
+  const int most = 8 * sm_count;
+  kv_fork_plan_kernel<<<1, PLAN_THREADS, 0, st>>>(v, parents, children, upto, n, copy);
+  kv_fork_stage_kernel<<<(int)(rows < most ? rows : most), COPY_THREADS, 0, st>>>(v, parents, n);
+  kv_fork_apply_kernel<<<most, COPY_THREADS, 0, st>>>(v, children, n);
+  *launches = 3;
+  return cudaGetLastError();
+}
+
+cudaError_t kv_free_launch(const KvView& v, const int* seqs, int n, int sm_count, cudaStream_t st) {
+  kv_free_kernel<<<n < 8 * sm_count ? n : 8 * sm_count, COPY_THREADS, 0, st>>>(v, seqs, n);
+  return cudaGetLastError();
+}
+
+cudaError_t kv_compact_launch(const KvView& v, int sm_count, int* launches, cudaStream_t st) {
+  kv_compact_plan_kernel<<<1, PLAN_THREADS, 0, st>>>(v);
+  kv_compact_apply_kernel<<<8 * sm_count, COPY_THREADS, 0, st>>>(v);
+  *launches = 2;
+  return cudaGetLastError();
+}
+
+}  // namespace icc
