@@ -55,9 +55,15 @@ struct KvAttendParams {
   const int* seqs;
   const int* starts;        // null: one token per sequence
   int n, n_heads, group, layer;
-  int64_t n_tokens;
+  int64_t n_tokens;         // of the whole call: `starts` and first_token index its q
+  int first_token;          // starts null: the token of this launch's first sequence
   int window, sinks;
   float scale_log2;         // scale * log2(e): the softmax works in powers of two
+  // pieces of items that span CTAs: two slots per CTA, and per CTA how many pieces of the item that
+  // begins in it and goes on have arrived (zero between launches)
+  float* partials;
+  int* arrivals;
+  size_t partial_floats;    // of one slot
 };
 
 cudaError_t kv_reserve_launch(const KvView& v, const int* seqs, const int* counts, int n, cudaStream_t st);
@@ -69,6 +75,11 @@ cudaError_t kv_free_launch(const KvView& v, const int* seqs, int n, int sm_count
 cudaError_t kv_compact_launch(const KvView& v, int sm_count, int* launches, cudaStream_t st);
 cudaError_t kv_pages_configure(int smem_optin);
 
-cudaError_t kv_attend_simple_launch(const KvAttendParams& p, bool f16, cudaStream_t st);
+cudaError_t kv_rows_configure(int smem_optin);
+size_t kv_rows_partial_floats(int head_dim);
+// tmap: the pool as rows of head_dim elements, box of 64 elements x min(page_size, 64) rows, 128-byte swizzle.
+cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int rows_per_seq, int sm_count, int smem_optin,
+                           cudaStream_t st);
+constexpr int KV_BATCH = 512;   // sequences per attention launch
 
 }  // namespace icc

@@ -25,6 +25,10 @@ struct ic_kv {
   void* own_workspace = nullptr;
   int* h_status = nullptr;
   int64_t launches = 0;
+  CUtensorMap tmap;                // the pool, row by row
+  float* partials = nullptr;       // in the workspace: pieces of attention split over a cache's length
+  int* arrivals = nullptr;
+  size_t partial_floats = 0;
 };
 
 namespace {
@@ -50,8 +54,10 @@ int check_opts(const ic_kv_opts_t* o) {
   return IC_OK;
 }
 
-// Pieces of the workspace, in order; `at` (may be null) gets their addresses.
-size_t carve(const ic_kv_opts_t* o, unsigned char* base, icc::KvView* at) {
+constexpr int MAX_CTAS = 160;   // attention kernels run one CTA per SM, of which there are at most this many
+
+// Pieces of the workspace, in order; `kv` (may be null) gets their addresses.
+size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
     unsigned char* p = base ? base + off : nullptr;
@@ -60,6 +66,7 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, icc::KvView* at) {
   };
   auto ints = [&](size_t n) { return reinterpret_cast<int*>(take(n * 4)); };
   int* err = ints(64);
+  int* arrivals = ints(MAX_CTAS);
   int* mark = ints(o->max_seqs);
   int* had = ints(o->max_seqs);
   int* upto = ints(o->max_seqs);
@@ -68,7 +75,13 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, icc::KvView* at) {
   int* fresh = ints(o->n_pages);
   int2* jobs = reinterpret_cast<int2*>(take((size_t)o->n_pages * 8));
   int* staged = ints((size_t)o->max_seqs * o->max_pages);
-  if (at) {
+  const size_t partial_floats = icc::kv_rows_partial_floats(o->head_dim);
+  float* partials = reinterpret_cast<float*>(take(2 * MAX_CTAS * partial_floats * 4));
+  if (kv) {
+    icc::KvView* at = &kv->v;
+    kv->arrivals = arrivals;
+    kv->partials = partials;
+    kv->partial_floats = partial_floats;
     at->err = err;
     at->meta = err + 32;
     at->mark = mark;
@@ -82,8 +95,8 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, icc::KvView* at) {
   }
   return off;
 }
-// The words at the head of the workspace that start out as zeros: error, plan, marks.
-size_t zero_bytes(const ic_kv_opts_t* o) { return 256 + up256((size_t)o->max_seqs * 4); }
+// The words at the head of the workspace that start out as zeros: error, plan, arrivals, marks.
+size_t zero_bytes(const ic_kv_opts_t* o) { return 256 + up256(MAX_CTAS * 4) + up256((size_t)o->max_seqs * 4); }
 
 int read_opts(const ic_kv_opts_t* opts, ic_kv_opts_t* o) {
   memset(o, 0, sizeof *o);
@@ -125,6 +138,28 @@ int check_list(const ic_kv* kv, const int32_t* p, const char* what) {
 int check_n(const ic_kv* kv, int32_t n) {
   if (n < 0 || n > kv->v.max_seqs) return fail(IC_ERR_INVALID, "n = %d outside [0, max_seqs = %d]", n, kv->v.max_seqs);
   return IC_OK;
+}
+
+// The pool as rows of head_dim elements; a box is 64 elements (128 bytes, swizzled) of the rows of a page, at
+// most 64 of them; what lies beyond head_dim reads as zero.
+int encode_pool(ic_kv* kv) {
+  cudaDriverEntryPointQueryResult qres;
+  void* fn = nullptr;
+  const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+  if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) {
+    cudaGetLastError();
+    return fail(IC_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
+  }
+  const icc::KvView& v = kv->v;
+  const int page = 1 << v.page_shift;
+  cuuint64_t dims[2] = {(cuuint64_t)v.head_dim, (cuuint64_t)v.n_pages * v.n_layers * 2 * v.n_kv_heads * page};
+  cuuint64_t strides[1] = {(cuuint64_t)v.head_dim * 2};
+  cuuint32_t box[2] = {64, (cuuint32_t)(page < 64 ? page : 64)};
+  cuuint32_t estr[2] = {1, 1};
+  const CUresult r = reinterpret_cast<icc::EncodeTiledFn>(fn)(
+      &kv->tmap, kv->f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.pool, dims, strides, box, estr,
+      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? IC_OK : fail(IC_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
 }
 
 int launched(ic_kv* kv, cudaError_t e, int n, const char* what) {
@@ -172,8 +207,8 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
     fail(IC_ERR_CUDA, "reading the device's attributes failed");
     return nullptr;
   }
-  if (major != 10) {
-    fail(IC_ERR_UNSUPPORTED, "device %d is sm_%d%d; this library is built for sm_100a only", dev, major, minor);
+  if (major != 10 || sms > MAX_CTAS) {
+    fail(IC_ERR_UNSUPPORTED, "device %d is sm_%d%d with %d multiprocessors; this library is built for sm_100a only", dev, major, minor, sms);
     return nullptr;
   }
   ic_kv* kv = new (std::nothrow) ic_kv();
@@ -250,7 +285,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
   } else if (ok) {
     ok = allocate(&kv->own_workspace, need, clear, "workspace");
   }
-  if (ok) carve(&o, static_cast<unsigned char*>(o.workspace ? o.workspace : kv->own_workspace), &v);
+  if (ok) carve(&o, static_cast<unsigned char*>(o.workspace ? o.workspace : kv->own_workspace), kv);
   if (ok) {
     e = cudaHostAlloc(reinterpret_cast<void**>(&kv->h_status), sizeof(int), cudaHostAllocMapped);
     if (e == cudaSuccess) {
@@ -258,6 +293,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
       e = cudaHostGetDevicePointer(reinterpret_cast<void**>(&v.host_status), kv->h_status, 0);
     }
     if (e == cudaSuccess) e = icc::kv_pages_configure(smem);
+    if (e == cudaSuccess) e = icc::kv_rows_configure(smem);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the cleared words are there for any stream
     if (e != cudaSuccess) {
       cudaGetLastError();
@@ -265,6 +301,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
       ok = false;
     }
   }
+  if (ok) ok = encode_pool(kv) == IC_OK;
   if (!ok) {
     char keep[512];
     strncpy(keep, ic_cache_last_error(), sizeof keep - 1);
@@ -355,8 +392,19 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
   p.window = a.window;
   p.sinks = a.window ? a.sinks : 0;
   p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.partials = kv->partials;
+  p.arrivals = kv->arrivals;
+  p.partial_floats = kv->partial_floats;
   DeviceGuard guard(kv->device);
-  return launched(kv, icc::kv_attend_simple_launch(p, kv->f16, kv->stream), 1, "attention");
+  const int64_t rows = (a.n_tokens + a.n - 1) / a.n * p.group;      // query rows of a sequence and kv head, on average
+  for (int off = 0; off < a.n && rc == IC_OK; off += icc::KV_BATCH) {
+    p.first_token = off;
+    p.seqs = a.seqs + off;
+    p.starts = a.starts ? a.starts + off : nullptr;
+    p.n = a.n - off < icc::KV_BATCH ? a.n - off : icc::KV_BATCH;
+    rc = launched(kv, icc::kv_rows_launch(p, kv->tmap, kv->f16, (int)(rows < 64 ? rows : 64), kv->sm_count, kv->smem_optin, kv->stream), 1, "attention");
+  }
+  return rc;
 }
 
 int ic_kv_fork(ic_kv_t* kv, const int32_t* parents, const int32_t* children, const int32_t* upto, int32_t n, int32_t copy) {

@@ -1,0 +1,581 @@
+// Attention over the paged cache for few query rows per sequence and kv head: decoding (one token, `group`
+// query heads), a handful of new tokens behind a long cached prefix, and any head_dim above 128.
+//
+// What bounds it: every key and value is read once per row tile and used for at most 64 rows, so
+// it is the read of the cache.  The kernel is therefore built around the loads.  One CTA per SM; a
+// producer warp fetches 64-key tiles, one tensor-map box per page, 64-element column chunk and keys/values,
+// into a ring of shared-memory stages (128-byte swizzle, so that the fragment loads below have no bank
+// conflicts) and looks up page numbers two tiles ahead.  Eight warps consume: the 16-row tiles of the
+// query (RT of them) times key groups; even and odd tiles go to different halves of the warps, so
+// two tiles are being worked on at any time.  Scores and weighted values are m16n8k16 products with
+// fp32 accumulation; each warp keeps its own running maximum and sum and its own accumulator for its keys,
+// which are merged once per item through shared memory.
+//
+// The weights are rounded to the cache's 16-bit type for the second product.  To lose nothing by that
+// they are split in two such numbers (high part, remainder): twice the products, which are not the bound.
+#include <cuda_fp16.h>
+
+#include <type_traits>
+
+#include "kv_schedule.cuh"
+#include "pipeline.cuh"
+
+namespace icc {
+
+namespace {
+
+constexpr int KEYS = 64;                 // keys per tile
+constexpr int WARPS = 8;                 // consumer warps
+constexpr int THREADS = WARPS * 32 + 128;   // and a warpgroup of which one warp produces
+// Registers: launched with 168 a thread (the most that 384 threads can have); the producers' warpgroup gives
+// its share to the two that hold accumulators.  384 x 168 = 256 x 216 + 128 x 72.
+constexpr int PRODUCER_REGS = 72, CONSUMER_REGS = 216;
+constexpr int MAX_STAGES = 12;
+
+struct RowsTail {
+  uint64_t full[MAX_STAGES], empty[MAX_STAGES];
+  float m[WARPS][16], l[WARPS][16];      // per consumer warp: its rows' maxima and sums
+  float scale[64];                       // factors of the final step
+  int abort_flag, last;
+  KvBatch batch;
+};
+
+__host__ __device__ constexpr int stage_bytes(int dch) { return 2 * dch * KEYS * 128; }
+__host__ __device__ constexpr int merge_stride(int dch) { return dch * 64 + 8; }    // floats; rows 8 banks apart: the quads of a fragment row spread out
+__host__ __device__ constexpr int merge_bytes(int dch, int rt) { return 16 * rt * merge_stride(dch) * 4; }
+int rows_smem(int dch, int rt, int stages) { return 1024 + stages * stage_bytes(dch) + merge_bytes(dch, rt) + (int)sizeof(RowsTail); }
+
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+template <bool F16>
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (F16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Two floats as a pair of 16-bit numbers, and what the rounding left over as another pair.
+template <bool F16>
+__device__ __forceinline__ void split2(float x, float y, uint32_t* high, uint32_t* rest) {
+  if (F16) {
+    const __half2 h = __floats2half2_rn(x, y);
+    const float2 f = __half22float2(h);
+    const __half2 r = __floats2half2_rn(x - f.x, y - f.y);
+    *high = *reinterpret_cast<const uint32_t*>(&h);
+    *rest = *reinterpret_cast<const uint32_t*>(&r);
+  } else {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    const float2 f = __bfloat1622float2(h);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(x - f.x, y - f.y);
+    *high = *reinterpret_cast<const uint32_t*>(&h);
+    *rest = *reinterpret_cast<const uint32_t*>(&r);
+  }
+}
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  if (F16) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <int I, int N, typename F>
+__device__ __forceinline__ void static_for(F f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<I + 1, N>(f);
+  }
+}
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+template <bool F16, int DCH, int RT>
+__global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParams p, const __grid_constant__ CUtensorMap tmap, int n_stages) {
+  constexpr int ROWS = 16 * RT;
+  constexpr int KG = WARPS / RT;                     // key groups: SLICES of a tile, times even and odd tiles
+  constexpr int SLICES = KG / 2;
+  constexpr int STEPS = KEYS / 16 / SLICES;          // 16-key steps of a warp in a tile
+  constexpr int CHUNK = KEYS * 128;                  // bytes of one 64-element column chunk of a tile
+  constexpr int KV_BYTES = DCH * CHUNK;              // keys of a tile; the values follow
+  constexpr int STAGE = 2 * KV_BYTES;
+  constexpr int PITCH = merge_stride(DCH);
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  float* merge = reinterpret_cast<float*>(ring + n_stages * STAGE);
+  RowsTail* t = reinterpret_cast<RowsTail*>(reinterpret_cast<unsigned char*>(merge) + merge_bytes(DCH, RT));
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const KvView& v = p.v;
+  if (tid == 0) {
+    for (int s = 0; s < n_stages; ++s) {
+      mbar_init(&t->full[s], 1);
+      mbar_init(&t->empty[s], WARPS / 2);
+    }
+    t->abort_flag = 0;
+    mbar_fence_init();
+    prefetch_tmap(&tmap);
+  }
+  kv_load_batch<ROWS, KEYS>(p, &t->batch);
+  __syncthreads();
+  KvWalk<ROWS, KEYS> walk(p, t->batch, blockIdx.x, gridDim.x);
+  if (walk.done()) return;
+
+  if (warp >= WARPS) {
+    // ------------------------------------------------------------ producer
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRODUCER_REGS));
+    if (warp > WARPS) return;
+    const int per_tile = max(1, KEYS >> v.page_shift);     // pages of a tile
+    const int box_rows = min(KEYS, 1 << v.page_shift);
+    const uint32_t box_bytes = (uint32_t)box_rows * 128;
+    // Row of the tensor map where this lane's page of the tile begins, or -1 if nothing is to be loaded.
+    int k = walk.from();
+    bool more = true;
+    auto look = [&]() {
+      int y = -1;
+      if (more) {
+        const KvSeq& s = t->batch.seq[walk.i];
+        const int key0 = walk.r.tile(k) * KEYS;
+        const int entry = (key0 >> v.page_shift) + lane;
+        if (lane < per_tile && entry < kv_pages_of(s.length, v.page_shift)) {
+          const int page = v.tables[(size_t)s.slot * v.max_pages + entry];
+          if ((unsigned)page < (unsigned)v.n_pages)
+            y = ((((page * v.n_layers + p.layer) * 2) * v.n_kv_heads + walk.head) << v.page_shift) + (key0 & ((1 << v.page_shift) - 1));
+          else
+            kv_report(v, KV_INVALID);
+        }
+        if (++k >= walk.to()) {
+          walk.next();
+          more = !walk.done();
+          if (more) k = walk.from();
+        }
+      }
+      return y;
+    };
+    const int n_tiles = (int)(walk.end - walk.at);
+    const int to_values = v.n_kv_heads << v.page_shift;
+    int y0 = look(), y1 = look(), y2 = look();
+    int s = 0, lt = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (; lt < n_tiles; ++lt) {
+      ok = mbar_wait(&t->empty[s], ph ^ 1u, &t->abort_flag);
+      ok = __all_sync(FULL_MASK, ok);
+      if (!ok) break;
+      const unsigned who = __ballot_sync(FULL_MASK, y0 >= 0);
+      if (lane == 0) mbar_arrive_expect_tx(&t->full[s], (uint32_t)__popc(who) * 2 * DCH * box_bytes);
+      __syncwarp();
+      if (y0 >= 0) {
+        unsigned char* dst = ring + s * STAGE + lane * box_bytes;
+#pragma unroll
+        for (int c = 0; c < DCH; ++c) tma_load_2d(dst + c * CHUNK, &tmap, c * 64, y0, &t->full[s]);
+#pragma unroll
+        for (int c = 0; c < DCH; ++c) tma_load_2d(dst + KV_BYTES + c * CHUNK, &tmap, c * 64, y0 + to_values, &t->full[s]);
+      }
+      y0 = y1;
+      y1 = y2;
+      y2 = look();
+      if (++s == n_stages) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+    if (!ok) {
+      if (lane == 0) {
+        kv_report(v, KV_TIMEOUT);
+        // what is in flight lands before the CTA leaves
+        for (int j = max(0, lt - n_stages); j < lt; ++j) {
+          const long long t0 = clock64();
+          while (!mbar_try_wait(&t->full[j % n_stages], (uint32_t)((j / n_stages) & 1)) && clock64() - t0 < WAIT_LIMIT_CYCLES) {
+          }
+        }
+      }
+    }
+    return;
+  }
+
+  // -------------------------------------------------------------- consumers
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(CONSUMER_REGS));
+  const int rtile = warp % RT, kg = warp / RT;       // 16-row tile and key group
+  const int half = kg / SLICES, slice = kg % SLICES; // even or odd tiles, and where in them
+  const int key_in_tile = slice * (STEPS * 16);
+  const uint32_t ring_addr = smem_u32(ring);
+  const int qr = lane >> 2, qc = (lane & 3) * 2;     // row and column pair of this thread in a fragment
+  // ldmatrix: lane l gives the address of row (l & 7) of matrix l >> 3
+  //   keys: matrices (keys 0-7, dims 0-7), (keys 0-7, dims 8-15), (keys 8-15, dims 0-7), (keys 8-15, dims 8-15)
+  const int k_row = key_in_tile + (lane & 7) + ((lane >> 4) << 3), k_col = (lane >> 3) & 1;
+  //   values, transposed: (keys 0-7, dims 0-7), (keys 8-15, dims 0-7), (keys 0-7, dims 8-15), (keys 8-15, dims 8-15)
+  const int v_row = key_in_tile + (lane & 7) + (((lane >> 3) & 1) << 3), v_col = lane >> 4;
+  int lt = 0, s = 0;                                 // tiles seen, and their stage and parity
+  uint32_t ph = 0;
+  bool ok = true;
+
+  for (; !walk.done(); walk.next()) {
+    const KvSeq seq = t->batch.seq[walk.i];
+    const int rows = seq.count * p.group - walk.rt * ROWS;        // rows of this tile, if below ROWS
+    int pos[2];                                                   // positions of this thread's two rows; -1 = no row
+    uint32_t q[DCH * 4][4];
+    {
+      const uint16_t* qrow[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int r = rtile * 16 + qr + x * 8;
+        const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
+        pos[x] = r < rows ? seq.length - seq.count + tok : -1;
+        qrow[x] = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(seq.first + tok) * p.q_token_stride + (int64_t)hq * p.q_head_stride;
+        if (r >= rows) qrow[x] = nullptr;
+      }
+#pragma unroll
+      for (int c = 0; c < DCH * 4; ++c)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int d = c * 16 + qc + (x >> 1) * 8;
+          const uint16_t* from = qrow[x & 1];
+          q[c][x] = (from && d < v.head_dim) ? *reinterpret_cast<const uint32_t*>(from + d) : 0u;
+        }
+    }
+    // positions of the first and last row of the warp's 16
+    int lowest = 0x7fffffff, highest = -1;
+    {
+      const int r0 = rtile * 16, r1 = min(r0 + 16, rows) - 1;
+      if (r0 < rows) {
+        lowest = seq.length - seq.count + (walk.rt * ROWS + r0) / p.group;
+        highest = seq.length - seq.count + (walk.rt * ROWS + r1) / p.group;
+      }
+    }
+    float o[DCH * 8][4];
+#pragma unroll
+    for (int c = 0; c < DCH * 8; ++c)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[c][x] = 0.0f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+
+    const int to = walk.to();
+    for (int k = walk.from(); k < to; ++k, ++lt) {
+      if ((lt & 1) == half) {
+        if (ok) ok = mbar_wait(&t->full[s], ph, &t->abort_flag);
+        const int key0 = walk.r.tile(k) * KEYS + key_in_tile;
+        const uint32_t kbase = ring_addr + s * STAGE + k_row * 128, vbase = ring_addr + s * STAGE + KV_BYTES + v_row * 128;
+        float sc[STEPS][2][4];
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) sc[st][0][x] = sc[st][1][x] = 0.0f;
+#pragma unroll
+          for (int c = 0; c < DCH * 4; ++c) {
+            uint32_t b[4];
+            ldmatrix_x4(b, kbase + (c >> 2) * CHUNK + st * 2048 + (((((c & 3) << 1) | k_col) ^ (k_row & 7)) << 4));
+            mma16816<F16>(sc[st][0], q[c], b[0], b[1]);
+            mma16816<F16>(sc[st][1], q[c], b[2], b[3]);
+          }
+        }
+        // all of the warp's keys seen by all of its rows?
+        const int last = key0 + STEPS * 16 - 1;
+        const bool clear = last <= lowest && highest >= 0 && (!p.window || key0 > highest - p.window || last < p.sinks);
+        float top[2] = {m[0], m[1]};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              float y = sc[st][nt][x] * p.scale_log2;
+              if (!clear) {
+                const int j = key0 + st * 16 + nt * 8 + qc + (x & 1), pr = pos[x >> 1];
+                const bool seen = j <= pr && (!p.window || j > pr - p.window || j < p.sinks);
+                y = seen ? y : -INFINITY;
+              }
+              sc[st][nt][x] = y;
+              top[x >> 1] = fmaxf(top[x >> 1], y);
+            }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          top[x] = fmaxf(top[x], __shfl_xor_sync(FULL_MASK, top[x], 1));
+          top[x] = fmaxf(top[x], __shfl_xor_sync(FULL_MASK, top[x], 2));
+        }
+        if (__any_sync(FULL_MASK, top[0] > m[0] || top[1] > m[1])) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float shrink = m[x] == -INFINITY ? 0.0f : exp2_fast(m[x] - top[x]);
+            m[x] = top[x];
+            l[x] *= shrink;
+#pragma unroll
+            for (int c = 0; c < DCH * 8; ++c) {
+              o[c][2 * x] *= shrink;
+              o[c][2 * x + 1] *= shrink;
+            }
+          }
+        }
+        // (a NaN score is no maximum; it reaches the sum and the result through its weight)
+        const float base[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              sc[st][nt][x] = exp2_fast(sc[st][nt][x] - base[x >> 1]);
+              l[x >> 1] += sc[st][nt][x];
+            }
+            split2<F16>(sc[st][nt][0], sc[st][nt][1], &hi[2 * nt], &lo[2 * nt]);
+            split2<F16>(sc[st][nt][2], sc[st][nt][3], &hi[2 * nt + 1], &lo[2 * nt + 1]);
+          }
+          // values of keys that none of the rows sees count as zeros, whatever they hold
+          uint32_t keep[2] = {~0u, ~0u};
+          if (!clear) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int j = key0 + st * 16 + qc + x * 8;
+              keep[x] = 0;
+              if (j <= highest && (!p.window || j > lowest - p.window || j < p.sinks)) keep[x] |= 0xffffu;
+              if (j + 1 <= highest && (!p.window || j + 1 > lowest - p.window || j + 1 < p.sinks)) keep[x] |= 0xffff0000u;
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < DCH * 4; ++c) {
+            uint32_t b[4];
+            ldmatrix_x4_trans(b, vbase + (c >> 2) * CHUNK + st * 2048 + (((((c & 3) << 1) | v_col) ^ (v_row & 7)) << 4));
+            b[0] &= keep[0];
+            b[1] &= keep[1];
+            b[2] &= keep[0];
+            b[3] &= keep[1];
+            mma16816<F16>(o[2 * c], hi, b[0], b[1]);
+            mma16816<F16>(o[2 * c], lo, b[0], b[1]);
+            mma16816<F16>(o[2 * c + 1], hi, b[2], b[3]);
+            mma16816<F16>(o[2 * c + 1], lo, b[2], b[3]);
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&t->empty[s]);
+      }
+      if (++s == n_stages) {
+        s = 0;
+        ph ^= 1u;
+      }
+    }
+
+    // ---- merge the key groups: common maximum per row, then the accumulators column group by column group
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      l[x] += __shfl_xor_sync(FULL_MASK, l[x], 1);
+      l[x] += __shfl_xor_sync(FULL_MASK, l[x], 2);
+    }
+    if ((lane & 3) == 0) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        t->m[warp][qr + 8 * x] = m[x];
+        t->l[warp][qr + 8 * x] = l[x];
+      }
+    }
+    consumers_sync();
+    float big[2], sum[2], part[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      big[x] = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < KG; ++g) big[x] = fmaxf(big[x], t->m[g * RT + rtile][qr + 8 * x]);
+      const float b0 = big[x] == -INFINITY ? 0.0f : big[x];
+      sum[x] = 0.0f;
+#pragma unroll
+      for (int g = 0; g < KG; ++g) sum[x] += t->l[g * RT + rtile][qr + 8 * x] * exp2_fast(t->m[g * RT + rtile][qr + 8 * x] - b0);
+      part[x] = exp2_fast(m[x] - b0);
+    }
+    // round r: group kg adds its columns of part (kg + r) mod KG, so that all warps work and none collide
+    constexpr int CT = DCH * 8 / KG;                 // 8-column tiles per part
+#pragma unroll 1
+    for (int r = 0; r < KG; ++r) {
+      static_for<0, KG>([&](auto part_no) {
+        constexpr int c0 = decltype(part_no)::value;
+        if (((kg + r) & (KG - 1)) == c0) {
+          asm volatile("" ::"n"(c0));                // keeps the branches apart: merged, they would index registers at run time
+#pragma unroll
+          for (int c = c0 * CT; c < (c0 + 1) * CT; ++c)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float2* at = reinterpret_cast<float2*>(merge + (rtile * 16 + qr + 8 * x) * PITCH + c * 8 + qc);
+              float2 w = make_float2(o[c][2 * x] * part[x], o[c][2 * x + 1] * part[x]);
+              if (r > 0) {
+                const float2 have = *at;
+                w.x += have.x;
+                w.y += have.y;
+              }
+              *at = w;
+            }
+        }
+      });
+      if (r == 0 && kg == 0 && (lane & 3) == 0) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) t->scale[rtile * 16 + qr + 8 * x] = sum[x];
+      }
+      consumers_sync();
+    }
+    if (kg == 0 && (lane & 3) == 0) {                // the rows' common maxima, for a partial result (read after the next barrier)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) t->m[warp][qr + 8 * x] = big[x];
+    }
+
+    const bool whole = walk.whole();
+    float* slot = p.partials + (size_t)(blockIdx.x * 2 + (walk.at == walk.begin_of(blockIdx.x) ? 0 : 1)) * p.partial_floats;
+    const int live = min(rows, ROWS);
+    auto put = [&](int r, int d, float a, float b) {              // two values of one row of the result
+      const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
+      uint16_t* to16 = reinterpret_cast<uint16_t*>(p.out) + (int64_t)(seq.first + tok) * p.out_token_stride + (int64_t)hq * p.out_head_stride + d;
+      *reinterpret_cast<uint32_t*>(to16) = pack2<F16>(a, b);
+    };
+    if (whole) {
+      for (int r = warp; r < live; r += WARPS) {
+        const float total = t->scale[r], inv = total == 0.0f ? 0.0f : 1.0f / total;
+        for (int d = lane * 2; d < v.head_dim; d += 64) {
+          const float2 w = *reinterpret_cast<const float2*>(merge + r * PITCH + d);
+          put(r, d, w.x * inv, w.y * inv);
+        }
+      }
+    } else {
+      consumers_sync();
+      // layout of a partial result: ROWS maxima, ROWS sums, ROWS x 64 * DCH values
+      for (int r = warp; r < live; r += WARPS) {
+        if (lane == 0) {
+          slot[r] = t->m[r >> 4][r & 15];
+          slot[ROWS + r] = t->scale[r];
+        }
+        for (int d = lane * 2; d < v.head_dim; d += 64)
+          *reinterpret_cast<float2*>(slot + 2 * ROWS + r * (DCH * 64) + d) = *reinterpret_cast<const float2*>(merge + r * PITCH + d);
+      }
+      __threadfence();
+      consumers_sync();
+      const int c0 = walk.cta_of(walk.item_at), c1 = walk.cta_of(walk.item_at + walk.r.n - 1);
+      if (tid == 0) {
+        const int arrived = atomicAdd(&p.arrivals[c0], 1);
+        t->last = arrived == c1 - c0;
+        if (t->last) p.arrivals[c0] = 0;             // ready for the next launch
+        __threadfence();
+      }
+      consumers_sync();
+      if (t->last) {
+        // join the pieces, in the order of the CTAs
+        const int first_slot = c0 * 2 + (walk.item_at == walk.begin_of(c0) ? 0 : 1), n_parts = c1 - c0 + 1;
+        for (int r = warp; r < live; r += WARPS) {
+          float top = -INFINITY;
+          for (int c = lane; c < n_parts; c += 32)
+            top = fmaxf(top, __ldcg(p.partials + (size_t)(c == 0 ? first_slot : (c0 + c) * 2) * p.partial_floats + r));
+#pragma unroll
+          for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
+          const float b0 = top == -INFINITY ? 0.0f : top;
+          float total = 0.0f;
+          float2 acc[DCH];
+#pragma unroll
+          for (int x = 0; x < DCH; ++x) acc[x] = make_float2(0.0f, 0.0f);
+          for (int cb = 0; cb < n_parts; cb += 32) {
+            float w = 0.0f;
+            if (cb + lane < n_parts) {
+              const float* part_at = p.partials + (size_t)(cb + lane == 0 ? first_slot : (c0 + cb + lane) * 2) * p.partial_floats;
+              w = exp2_fast(__ldcg(part_at + r) - b0);
+              total += w * __ldcg(part_at + ROWS + r);
+            }
+            const int some = min(32, n_parts - cb);
+#pragma unroll 4
+            for (int c = 0; c < some; ++c) {
+              const float wc = __shfl_sync(FULL_MASK, w, c);
+              const float* part_at = p.partials + (size_t)(cb + c == 0 ? first_slot : (c0 + cb + c) * 2) * p.partial_floats + 2 * ROWS + r * (DCH * 64);
+#pragma unroll
+              for (int x = 0; x < DCH; ++x) {
+                if (x * 64 + lane * 2 < v.head_dim) {
+                  const float2 y = __ldcg(reinterpret_cast<const float2*>(part_at + x * 64 + lane * 2));
+                  acc[x].x += wc * y.x;
+                  acc[x].y += wc * y.y;
+                }
+              }
+            }
+          }
+#pragma unroll
+          for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(FULL_MASK, total, d);
+          const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+          for (int x = 0; x < DCH; ++x)
+            if (x * 64 + lane * 2 < v.head_dim) put(r, x * 64 + lane * 2, acc[x].x * inv, acc[x].y * inv);
+        }
+      }
+    }
+  }
+  if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
+}
+
+template <bool F16, int DCH, int RT>
+cudaError_t configure_one(int smem_optin) {
+  return cudaFuncSetAttribute(kv_rows_kernel<F16, DCH, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
+}
+
+template <bool F16, int DCH, int RT>
+cudaError_t launch_one(const KvAttendParams& p, const CUtensorMap& tmap, int sm_count, int smem_optin, cudaStream_t st) {
+  int stages = 2;
+  while (stages < MAX_STAGES && rows_smem(DCH, RT, stages + 1) <= smem_optin) ++stages;
+  kv_rows_kernel<F16, DCH, RT><<<sm_count, THREADS, rows_smem(DCH, RT, stages), st>>>(p, tmap, stages);
+  return cudaGetLastError();
+}
+
+template <bool F16, int DCH>
+cudaError_t launch_rt(const KvAttendParams& p, const CUtensorMap& tmap, int rt, int sm_count, int smem_optin, cudaStream_t st) {
+  if (rt == 1) return launch_one<F16, DCH, 1>(p, tmap, sm_count, smem_optin, st);
+  if (rt == 2 || DCH > 2) return launch_one<F16, DCH, 2>(p, tmap, sm_count, smem_optin, st);
+  return launch_one<F16, DCH, DCH <= 2 ? 4 : 2>(p, tmap, sm_count, smem_optin, st);
+}
+
+template <bool F16>
+cudaError_t launch_dch(const KvAttendParams& p, const CUtensorMap& tmap, int rt, int sm_count, int smem_optin, cudaStream_t st) {
+  switch ((p.v.head_dim + 63) / 64) {
+    case 1: return launch_rt<F16, 1>(p, tmap, rt, sm_count, smem_optin, st);
+    case 2: return launch_rt<F16, 2>(p, tmap, rt, sm_count, smem_optin, st);
+    case 3: return launch_rt<F16, 3>(p, tmap, rt, sm_count, smem_optin, st);
+    default: return launch_rt<F16, 4>(p, tmap, rt, sm_count, smem_optin, st);
+  }
+}
+
+template <bool F16, int DCH>
+cudaError_t configure_dch(int smem_optin) {
+  cudaError_t e = configure_one<F16, DCH, 1>(smem_optin);
+  if (e == cudaSuccess) e = configure_one<F16, DCH, 2>(smem_optin);
+  if (e == cudaSuccess) e = configure_one<F16, DCH, DCH <= 2 ? 4 : 2>(smem_optin);
+  return e;
+}
+template <bool F16>
+cudaError_t configure_all(int smem_optin) {
+  cudaError_t e = configure_dch<F16, 1>(smem_optin);
+  if (e == cudaSuccess) e = configure_dch<F16, 2>(smem_optin);
+  if (e == cudaSuccess) e = configure_dch<F16, 3>(smem_optin);
+  if (e == cudaSuccess) e = configure_dch<F16, 4>(smem_optin);
+  return e;
+}
+
+}  // namespace
+
+cudaError_t kv_rows_configure(int smem_optin) {
+  const cudaError_t e = configure_all<false>(smem_optin);
+  return e == cudaSuccess ? configure_all<true>(smem_optin) : e;
+}
+
+size_t kv_rows_partial_floats(int head_dim) {
+  const int dch = (head_dim + 63) / 64, rows = dch <= 2 ? 64 : 32;
+  return (size_t)rows * (2 + dch * 64);
+}
+
+cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int rows_per_seq, int sm_count, int smem_optin,
+                           cudaStream_t st) {
+  const int rt = rows_per_seq <= 16 ? 1 : (rows_per_seq <= 32 ? 2 : 4);
+  return f16 ? launch_dch<true>(p, tmap, rt, sm_count, smem_optin, st) : launch_dch<false>(p, tmap, rt, sm_count, smem_optin, st);
+}
+
+}  // namespace icc

@@ -1,0 +1,181 @@
+// How the attention kernels divide their work.
+//
+// The query rows of one sequence and kv head are its tokens times the query heads of that kv head
+// (row = token * group + head in group), cut into tiles of ROWS rows.  A tile's work is the tiles of KEYS
+// keys that any of its rows sees.  All of a launch's key tiles, in the order sequence, kv head, row
+// tile, key tile, form one line, and each CTA takes an equal stretch of it, whatever the lengths: a CTA
+// holds whole (row tile, head) items and at most two pieces of items, and the pieces of an item that
+// spans CTAs are joined by the CTA that finishes last.  Lengths live on the device, so the CTAs work the
+// line out for themselves; sequences are few and their data sits in shared memory.
+#pragma once
+#include "common.cuh"
+#include "kv.h"
+
+namespace icc {
+
+struct KvSeq {
+  int slot, length, first, count;        // table row, tokens, first row of q, number of q's rows
+};
+
+// What the CTAs of one launch share about the batch, in shared memory.
+struct KvBatch {
+  KvSeq seq[KV_BATCH];
+  long long before[KV_BATCH + 1];  // key tiles of the sequences before this one, all heads
+};
+
+// The key tiles of one row tile: the sinks' tiles [0, sink_tiles) and then [first, end).
+struct KvRange {
+  int sink_tiles, first, n;              // n = tiles in all, at least 1
+  __device__ __forceinline__ int tile(int k) const { return k < sink_tiles ? k : first + (k - sink_tiles); }
+};
+
+template <int ROWS, int KEYS>
+struct KvSchedule {
+  const KvAttendParams& p;
+  const KvBatch& b;
+  __device__ KvSchedule(const KvAttendParams& p_, const KvBatch& b_) : p(p_), b(b_) {}
+
+  __device__ __forceinline__ int row_tiles(const KvSeq& s) const { return (int)(((long long)s.count * p.group + ROWS - 1) / ROWS); }
+
+  // Positions of the first and the last row of row tile rt.
+  __device__ __forceinline__ void positions(const KvSeq& s, int rt, int* lowest, int* highest) const {
+    const long long r0 = (long long)rt * ROWS, r1 = min(r0 + ROWS, (long long)s.count * p.group) - 1;
+    *lowest = s.length - s.count + (int)(r0 / p.group);
+    *highest = s.length - s.count + (int)(r1 / p.group);
+  }
+
+  __device__ __forceinline__ KvRange range(const KvSeq& s, int rt) const {
+    int lowest, highest;
+    positions(s, rt, &lowest, &highest);
+    KvRange r;
+    const int end = highest < 0 ? 0 : highest / KEYS + 1;
+    r.first = (p.window && lowest >= p.window) ? (lowest - p.window + 1) / KEYS : 0;
+    // the sinks' tiles, as far as they lie before the window's
+    const int sink_tiles = (int)(((long long)p.sinks + KEYS - 1) / KEYS);
+    r.sink_tiles = min(sink_tiles, r.first);
+    r.n = max(1, r.sink_tiles + end - r.first);      // a row tile that sees nothing writes zeros
+    return r;
+  }
+
+  __device__ __forceinline__ long long tiles_of(const KvSeq& s) const {
+    const int n = row_tiles(s);
+    long long sum = 0;
+    for (int rt = 0; rt < n; ++rt) sum += range(s, rt).n;
+    return sum;
+  }
+};
+
+// Fill the batch table; all threads of the CTA, which synchronise afterwards.
+template <int ROWS, int KEYS>
+__device__ __forceinline__ void kv_load_batch(const KvAttendParams& p, KvBatch* b) {
+  const KvSchedule<ROWS, KEYS> sched(p, *b);
+  for (int i = threadIdx.x; i < p.n; i += blockDim.x) {
+    KvSeq s;
+    s.slot = p.seqs[i];
+    bool fine = s.slot >= 0 && s.slot < p.v.max_seqs;
+    s.length = fine ? p.v.lengths[s.slot] : 0;
+    long long first = p.first_token + i, end = first + 1;
+    if (p.starts) {
+      first = p.starts[i];
+      end = p.starts[i + 1];
+    }
+    if (first < 0 || first > end || end > p.n_tokens) {
+      fine = false;
+      first = 0;
+      end = 0;
+    }
+    s.first = (int)first;
+    s.count = (int)(end - first);
+    if (s.length < 0 || s.length > ((long long)p.v.max_pages << p.v.page_shift)) {
+      fine = false;
+      s.length = 0;
+    }
+    if (s.count > s.length && (p.starts || s.length > 0)) fine = false;     // (the one token of an empty sequence sees nothing)
+    if (!fine && blockIdx.x == 0) kv_report(p.v, KV_INVALID);
+    b->seq[i] = s;
+    b->before[i + 1] = sched.tiles_of(s) * p.v.n_kv_heads;
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    long long sum = 0;
+    for (int i0 = 0; i0 < p.n; i0 += 32) {
+      const int i = i0 + threadIdx.x;
+      long long x = i < p.n ? b->before[i + 1] : 0;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const long long y = __shfl_up_sync(FULL_MASK, x, d);
+        if ((int)threadIdx.x >= d) x += y;
+      }
+      if (i < p.n) b->before[i + 1] = sum + x;
+      sum += __shfl_sync(FULL_MASK, x, 31);
+    }
+    if (threadIdx.x == 0) b->before[0] = 0;
+  }
+}
+
+// Walks a CTA's stretch of the line, item by item.
+template <int ROWS, int KEYS>
+struct KvWalk {
+  KvSchedule<ROWS, KEYS> sched;
+  long long total, n_ctas, at, end;      // next key tile of the line, end of the stretch
+  int i, head, rt;                       // the item that `at` lies in
+  KvRange r;
+  long long item_at;                     // first key tile of the item
+
+  // Stretch of CTA c; n_ctas is capped so that none is empty.
+  __device__ KvWalk(const KvAttendParams& p, const KvBatch& b, int c, int grid) : sched(p, b) {
+    total = b.before[p.n];
+    n_ctas = min((long long)grid, total);
+    if (c >= n_ctas) {
+      at = end = 0;
+      return;
+    }
+    at = begin_of(c);
+    end = begin_of(c + 1);
+    int lo = 0, hi = p.n - 1;            // the last sequence that begins at or before `at`
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (b.before[mid] <= at) lo = mid;
+      else hi = mid - 1;
+    }
+    i = lo;
+    const long long per_head = (b.before[i + 1] - b.before[i]) / p.v.n_kv_heads;
+    head = (int)((at - b.before[i]) / per_head);
+    item_at = b.before[i] + head * per_head;
+    rt = 0;
+    r = sched.range(b.seq[i], 0);
+    while (at >= item_at + r.n) {
+      item_at += r.n;
+      r = sched.range(b.seq[i], ++rt);
+    }
+  }
+  __device__ __forceinline__ long long begin_of(long long c) const { return total * c / n_ctas; }
+  __device__ __forceinline__ bool done() const { return at >= end; }
+  // key tiles of the item within the stretch: [from, to)
+  __device__ __forceinline__ int from() const { return (int)(at - item_at); }
+  __device__ __forceinline__ int to() const { return (int)(min(end, item_at + r.n) - item_at); }
+  __device__ __forceinline__ bool whole() const { return from() == 0 && to() == r.n; }
+  // On to the next item of the stretch.
+  __device__ __forceinline__ void next() {
+    item_at += r.n;
+    at = item_at;
+    if (at >= end) return;
+    if (++rt >= sched.row_tiles(sched.b.seq[i])) {
+      rt = 0;
+      if (++head >= sched.p.v.n_kv_heads) {
+        head = 0;
+        do ++i; while (sched.b.seq[i].count == 0);
+      }
+    }
+    r = sched.range(sched.b.seq[i], rt);
+  }
+  // The CTA whose stretch holds key tile u.
+  __device__ __forceinline__ int cta_of(long long u) const {
+    long long c = u * n_ctas / total;
+    while (c + 1 < n_ctas && begin_of(c + 1) <= u) ++c;
+    while (c > 0 && begin_of(c) > u) --c;
+    return (int)c;
+  }
+};
+
+}  // namespace icc
