@@ -75,11 +75,15 @@ cudaError_t kv_free_launch(const KvView& v, const int* seqs, int n, int sm_count
 cudaError_t kv_compact_launch(const KvView& v, int sm_count, int* launches, cudaStream_t st);
 cudaError_t kv_pages_configure(int smem_optin);
 
+cudaError_t kv_decode_configure(int smem_optin);
+// two: 16 rows per item instead of 8.
+cudaError_t kv_decode_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, bool two, int sm_count, int smem_optin, cudaStream_t st);
 cudaError_t kv_rows_configure(int smem_optin);
 size_t kv_rows_partial_floats(int head_dim);
 // tmap: the pool as rows of head_dim elements, box of 64 elements x min(page_size, 64) rows, 128-byte swizzle.
 cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int rows_per_seq, int sm_count, int smem_optin,
                            cudaStream_t st);
-constexpr int KV_BATCH = 512;   // sequences per attention launch
+constexpr int KV_BATCH = 256;      // sequences per attention launch
+constexpr int KV_MAX_CTAS = 160;   // attention kernels run one CTA per SM, of which there are at most this many
 
 }  // namespace icc

@@ -54,8 +54,6 @@ int check_opts(const ic_kv_opts_t* o) {
   return IC_OK;
 }
 
-constexpr int MAX_CTAS = 160;   // attention kernels run one CTA per SM, of which there are at most this many
-
 // Pieces of the workspace, in order; `kv` (may be null) gets their addresses.
 size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   size_t off = 0;
@@ -66,7 +64,7 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   };
   auto ints = [&](size_t n) { return reinterpret_cast<int*>(take(n * 4)); };
   int* err = ints(64);
-  int* arrivals = ints(MAX_CTAS);
+  int* arrivals = ints(icc::KV_MAX_CTAS);
   int* mark = ints(o->max_seqs);
   int* had = ints(o->max_seqs);
   int* upto = ints(o->max_seqs);
@@ -76,7 +74,7 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   int2* jobs = reinterpret_cast<int2*>(take((size_t)o->n_pages * 8));
   int* staged = ints((size_t)o->max_seqs * o->max_pages);
   const size_t partial_floats = icc::kv_rows_partial_floats(o->head_dim);
-  float* partials = reinterpret_cast<float*>(take(2 * MAX_CTAS * partial_floats * 4));
+  float* partials = reinterpret_cast<float*>(take(2 * icc::KV_MAX_CTAS * partial_floats * 4));
   if (kv) {
     icc::KvView* at = &kv->v;
     kv->arrivals = arrivals;
@@ -96,7 +94,7 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   return off;
 }
 // The words at the head of the workspace that start out as zeros: error, plan, arrivals, marks.
-size_t zero_bytes(const ic_kv_opts_t* o) { return 256 + up256(MAX_CTAS * 4) + up256((size_t)o->max_seqs * 4); }
+size_t zero_bytes(const ic_kv_opts_t* o) { return 256 + up256(icc::KV_MAX_CTAS * 4) + up256((size_t)o->max_seqs * 4); }
 
 int read_opts(const ic_kv_opts_t* opts, ic_kv_opts_t* o) {
   memset(o, 0, sizeof *o);
@@ -207,7 +205,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
     fail(IC_ERR_CUDA, "reading the device's attributes failed");
     return nullptr;
   }
-  if (major != 10 || sms > MAX_CTAS) {
+  if (major != 10 || sms > icc::KV_MAX_CTAS) {
     fail(IC_ERR_UNSUPPORTED, "device %d is sm_%d%d with %d multiprocessors; this library is built for sm_100a only", dev, major, minor, sms);
     return nullptr;
   }
@@ -293,6 +291,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
       e = cudaHostGetDevicePointer(reinterpret_cast<void**>(&v.host_status), kv->h_status, 0);
     }
     if (e == cudaSuccess) e = icc::kv_pages_configure(smem);
+    if (e == cudaSuccess) e = icc::kv_decode_configure(smem);
     if (e == cudaSuccess) e = icc::kv_rows_configure(smem);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the cleared words are there for any stream
     if (e != cudaSuccess) {
@@ -402,7 +401,9 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
     p.seqs = a.seqs + off;
     p.starts = a.starts ? a.starts + off : nullptr;
     p.n = a.n - off < icc::KV_BATCH ? a.n - off : icc::KV_BATCH;
-    rc = launched(kv, icc::kv_rows_launch(p, kv->tmap, kv->f16, (int)(rows < 64 ? rows : 64), kv->sm_count, kv->smem_optin, kv->stream), 1, "attention");
+    const cudaError_t e = rows <= 16 ? icc::kv_decode_launch(p, kv->tmap, kv->f16, rows > 8, kv->sm_count, kv->smem_optin, kv->stream)
+                                     : icc::kv_rows_launch(p, kv->tmap, kv->f16, (int)(rows < 64 ? rows : 64), kv->sm_count, kv->smem_optin, kv->stream);
+    rc = launched(kv, e, 1, "attention");
   }
   return rc;
 }

@@ -5,7 +5,9 @@
 // first.  That makes the tables a function of the calls alone, needs nothing rebuilt after a restore, and
 // costs one pass over the counts per allocation, 4 bytes a page.
 #include "common.cuh"
+#include "kernels.h"
 #include "kv.h"
+#include "pipeline.cuh"
 
 namespace icc {
 

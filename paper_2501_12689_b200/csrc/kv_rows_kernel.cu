@@ -13,10 +13,10 @@
 //
 // The weights are rounded to the cache's 16-bit type for the second product.  To lose nothing by that
 // they are split in two such numbers (high part, remainder): twice the products, which are not the bound.
-#include <cuda_fp16.h>
-
 #include <type_traits>
 
+#include "kernels.h"
+#include "kv_mma.cuh"
 #include "kv_schedule.cuh"
 #include "pipeline.cuh"
 
@@ -26,14 +26,15 @@ namespace {
 
 constexpr int KEYS = 64;                 // keys per tile
 constexpr int WARPS = 8;                 // consumer warps
-constexpr int THREADS = WARPS * 32 + 128;   // and a warpgroup of which one warp produces
+constexpr int Q_WARPS = 3;               // warps that fetch query rows
+constexpr int THREADS = WARPS * 32 + 32 + Q_WARPS * 32;
 // Registers: launched with 168 a thread (the most that 384 threads can have); the producers' warpgroup gives
-// its share to the two that hold accumulators.  384 x 168 = 256 x 216 + 128 x 72.
+// part of its share to the two that hold accumulators.  384 x 168 = 256 x 216 + 128 x 72.
 constexpr int PRODUCER_REGS = 72, CONSUMER_REGS = 216;
 constexpr int MAX_STAGES = 12;
 
 struct RowsTail {
-  uint64_t full[MAX_STAGES], empty[MAX_STAGES];
+  uint64_t full[MAX_STAGES], empty[MAX_STAGES], q_full, q_empty;
   float m[WARPS][16], l[WARPS][16];      // per consumer warp: its rows' maxima and sums
   float scale[64];                       // factors of the final step
   int abort_flag, last;
@@ -43,58 +44,12 @@ struct RowsTail {
 __host__ __device__ constexpr int stage_bytes(int dch) { return 2 * dch * KEYS * 128; }
 __host__ __device__ constexpr int merge_stride(int dch) { return dch * 64 + 8; }    // floats; rows 8 banks apart: the quads of a fragment row spread out
 __host__ __device__ constexpr int merge_bytes(int dch, int rt) { return 16 * rt * merge_stride(dch) * 4; }
-int rows_smem(int dch, int rt, int stages) { return 1024 + stages * stage_bytes(dch) + merge_bytes(dch, rt) + (int)sizeof(RowsTail); }
+__host__ __device__ constexpr int q_pitch(int dch) { return dch * 128 + 16; }           // bytes of a query row in shared memory
+__host__ __device__ constexpr int q_bytes(int dch, int rt) { return 16 * rt * q_pitch(dch); }
+int rows_smem(int dch, int rt, int stages) {
+  return 1024 + stages * stage_bytes(dch) + merge_bytes(dch, rt) + q_bytes(dch, rt) + (int)sizeof(RowsTail);
+}
 
-__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr));
-}
-template <bool F16>
-__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if (F16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// Two floats as a pair of 16-bit numbers, and what the rounding left over as another pair.
-template <bool F16>
-__device__ __forceinline__ void split2(float x, float y, uint32_t* high, uint32_t* rest) {
-  if (F16) {
-    const __half2 h = __floats2half2_rn(x, y);
-    const float2 f = __half22float2(h);
-    const __half2 r = __floats2half2_rn(x - f.x, y - f.y);
-    *high = *reinterpret_cast<const uint32_t*>(&h);
-    *rest = *reinterpret_cast<const uint32_t*>(&r);
-  } else {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-    const float2 f = __bfloat1622float2(h);
-    const __nv_bfloat162 r = __floats2bfloat162_rn(x - f.x, y - f.y);
-    *high = *reinterpret_cast<const uint32_t*>(&h);
-    *rest = *reinterpret_cast<const uint32_t*>(&r);
-  }
-}
-template <bool F16>
-__device__ __forceinline__ uint32_t pack2(float x, float y) {
-  if (F16) {
-    const __half2 h = __floats2half2_rn(x, y);
-    return *reinterpret_cast<const uint32_t*>(&h);
-  }
-  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 template <int I, int N, typename F>
 __device__ __forceinline__ void static_for(F f) {
   if constexpr (I < N) {
@@ -117,7 +72,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
   extern __shared__ unsigned char smem_raw[];
   unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   float* merge = reinterpret_cast<float*>(ring + n_stages * STAGE);
-  RowsTail* t = reinterpret_cast<RowsTail*>(reinterpret_cast<unsigned char*>(merge) + merge_bytes(DCH, RT));
+  unsigned char* q_smem = reinterpret_cast<unsigned char*>(merge) + merge_bytes(DCH, RT);
+  RowsTail* t = reinterpret_cast<RowsTail*>(q_smem + q_bytes(DCH, RT));
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const KvView& v = p.v;
   if (tid == 0) {
@@ -125,10 +81,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
       mbar_init(&t->full[s], 1);
       mbar_init(&t->empty[s], WARPS / 2);
     }
+    mbar_init(&t->q_full, Q_WARPS);
+    mbar_init(&t->q_empty, WARPS);
     t->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tmap);
   }
+  grid_dep_launch_dependents();
+  grid_dep_wait();   // queries, tables and pages come from earlier kernels in the stream
   kv_load_batch<ROWS, KEYS>(p, &t->batch);
   __syncthreads();
   KvWalk<ROWS, KEYS> walk(p, t->batch, blockIdx.x, gridDim.x);
@@ -137,37 +97,63 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
   if (warp >= WARPS) {
     // ------------------------------------------------------------ producer
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PRODUCER_REGS));
-    if (warp > WARPS) return;
+    if (warp > WARPS) {
+      // ---------------------------------------------------------- query rows: an item's are fetched while the one before it is worked on
+      constexpr int PIECES = DCH * 8;                        // 16-byte pieces of a row
+      uint32_t ph = 1;
+      for (; !walk.done(); walk.next(), ph ^= 1u) {
+        const KvSeq& seq = t->batch.seq[walk.i];
+        const int rows = seq.count * p.group - walk.rt * ROWS;
+        if (!mbar_wait(&t->q_empty, ph, &t->abort_flag)) {
+          if (lane == 0) kv_report(v, KV_TIMEOUT);
+          break;
+        }
+#pragma unroll 4
+        for (int u = (warp - WARPS - 1) * 32 + lane; u < ROWS * PIECES; u += Q_WARPS * 32) {
+          const int r = u / PIECES, piece = u - r * PIECES;
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (r < rows && piece * 8 < v.head_dim) {
+            const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
+            w = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(seq.first + tok) * p.q_token_stride +
+                                                (int64_t)hq * p.q_head_stride + piece * 8);
+          }
+          *reinterpret_cast<uint4*>(q_smem + r * q_pitch(DCH) + piece * 16) = w;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&t->q_full);
+      }
+      return;
+    }
     const int per_tile = max(1, KEYS >> v.page_shift);     // pages of a tile
     const int box_rows = min(KEYS, 1 << v.page_shift);
     const uint32_t box_bytes = (uint32_t)box_rows * 128;
-    // Row of the tensor map where this lane's page of the tile begins, or -1 if nothing is to be loaded.
-    int k = walk.from();
+    const int page_rows = (v.n_layers * 2 * v.n_kv_heads) << v.page_shift;   // rows of the tensor map per page
+    // What this lane loads of the next tile: its page (-1: nothing) and the first row in it.  The page number is
+    // looked at only when the tile is issued, three tiles later, so that nothing waits for the table here.
+    struct Ahead {
+      int page, row;
+    };
+    const int n_tiles = walk.left;
+    int k = walk.from;
     bool more = true;
     auto look = [&]() {
-      int y = -1;
+      Ahead a{-1, 0};
       if (more) {
         const KvSeq& s = t->batch.seq[walk.i];
         const int key0 = walk.r.tile(k) * KEYS;
         const int entry = (key0 >> v.page_shift) + lane;
-        if (lane < per_tile && entry < kv_pages_of(s.length, v.page_shift)) {
-          const int page = v.tables[(size_t)s.slot * v.max_pages + entry];
-          if ((unsigned)page < (unsigned)v.n_pages)
-            y = ((((page * v.n_layers + p.layer) * 2) * v.n_kv_heads + walk.head) << v.page_shift) + (key0 & ((1 << v.page_shift) - 1));
-          else
-            kv_report(v, KV_INVALID);
-        }
-        if (++k >= walk.to()) {
+        if (lane < per_tile && entry < kv_pages_of(s.length, v.page_shift)) a.page = v.tables[(size_t)s.slot * v.max_pages + entry];
+        a.row = ((p.layer * 2 * v.n_kv_heads + walk.head) << v.page_shift) + (key0 & ((1 << v.page_shift) - 1));
+        if (++k >= walk.to) {
           walk.next();
           more = !walk.done();
-          if (more) k = walk.from();
+          if (more) k = walk.from;
         }
       }
-      return y;
+      return a;
     };
-    const int n_tiles = (int)(walk.end - walk.at);
     const int to_values = v.n_kv_heads << v.page_shift;
-    int y0 = look(), y1 = look(), y2 = look();
+    Ahead a0 = look(), a1 = look(), a2 = look();
     int s = 0, lt = 0;
     uint32_t ph = 0;
     bool ok = true;
@@ -175,19 +161,22 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
       ok = mbar_wait(&t->empty[s], ph ^ 1u, &t->abort_flag);
       ok = __all_sync(FULL_MASK, ok);
       if (!ok) break;
-      const unsigned who = __ballot_sync(FULL_MASK, y0 >= 0);
+      const bool mine = (unsigned)a0.page < (unsigned)v.n_pages;
+      const unsigned who = __ballot_sync(FULL_MASK, mine);
+      if (a0.page != -1 && !mine) kv_report(v, KV_INVALID);      // a borrowed table's entry that names no page
       if (lane == 0) mbar_arrive_expect_tx(&t->full[s], (uint32_t)__popc(who) * 2 * DCH * box_bytes);
       __syncwarp();
-      if (y0 >= 0) {
+      if (mine) {
+        const int y0 = a0.page * page_rows + a0.row;
         unsigned char* dst = ring + s * STAGE + lane * box_bytes;
 #pragma unroll
         for (int c = 0; c < DCH; ++c) tma_load_2d(dst + c * CHUNK, &tmap, c * 64, y0, &t->full[s]);
 #pragma unroll
         for (int c = 0; c < DCH; ++c) tma_load_2d(dst + KV_BYTES + c * CHUNK, &tmap, c * 64, y0 + to_values, &t->full[s]);
       }
-      y0 = y1;
-      y1 = y2;
-      y2 = look();
+      a0 = a1;
+      a1 = a2;
+      a2 = look();
       if (++s == n_stages) {
         s = 0;
         ph ^= 1u;
@@ -219,34 +208,29 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
   const int k_row = key_in_tile + (lane & 7) + ((lane >> 4) << 3), k_col = (lane >> 3) & 1;
   //   values, transposed: (keys 0-7, dims 0-7), (keys 8-15, dims 0-7), (keys 0-7, dims 8-15), (keys 8-15, dims 8-15)
   const int v_row = key_in_tile + (lane & 7) + (((lane >> 3) & 1) << 3), v_col = lane >> 4;
+  //   queries: matrices (rows 0-7, dims 0-7), (rows 8-15, dims 0-7), (rows 0-7, dims 8-15), (rows 8-15, dims 8-15)
+  const uint32_t q_addr = smem_u32(q_smem) + (rtile * 16 + (lane & 7) + (((lane >> 3) & 1) << 3)) * q_pitch(DCH) + (lane >> 4) * 16;
   int lt = 0, s = 0;                                 // tiles seen, and their stage and parity
-  uint32_t ph = 0;
+  uint32_t ph = 0, q_ph = 0;
   bool ok = true;
 
   for (; !walk.done(); walk.next()) {
     const KvSeq seq = t->batch.seq[walk.i];
     const int rows = seq.count * p.group - walk.rt * ROWS;        // rows of this tile, if below ROWS
     int pos[2];                                                   // positions of this thread's two rows; -1 = no row
-    uint32_t q[DCH * 4][4];
-    {
-      const uint16_t* qrow[2];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int r = rtile * 16 + qr + x * 8;
-        const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
-        pos[x] = r < rows ? seq.length - seq.count + tok : -1;
-        qrow[x] = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(seq.first + tok) * p.q_token_stride + (int64_t)hq * p.q_head_stride;
-        if (r >= rows) qrow[x] = nullptr;
-      }
-#pragma unroll
-      for (int c = 0; c < DCH * 4; ++c)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int d = c * 16 + qc + (x >> 1) * 8;
-          const uint16_t* from = qrow[x & 1];
-          q[c][x] = (from && d < v.head_dim) ? *reinterpret_cast<const uint32_t*>(from + d) : 0u;
-        }
+    for (int x = 0; x < 2; ++x) {
+      const int r = rtile * 16 + qr + x * 8;
+      pos[x] = r < rows ? seq.length - seq.count + (walk.rt * ROWS + r) / p.group : -1;
     }
+    uint32_t q[DCH * 4][4];
+    if (ok) ok = mbar_wait(&t->q_full, q_ph, &t->abort_flag);
+    q_ph ^= 1u;
+#pragma unroll
+    for (int c = 0; c < DCH * 4; ++c)
+      ldmatrix_x4(q[c], q_addr + c * 32);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&t->q_empty);
     // positions of the first and last row of the warp's 16
     int lowest = 0x7fffffff, highest = -1;
     {
@@ -263,8 +247,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
       for (int x = 0; x < 4; ++x) o[c][x] = 0.0f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
 
-    const int to = walk.to();
-    for (int k = walk.from(); k < to; ++k, ++lt) {
+    const int to = walk.to;
+    for (int k = walk.from; k < to; ++k, ++lt) {
       if ((lt & 1) == half) {
         if (ok) ok = mbar_wait(&t->full[s], ph, &t->abort_flag);
         const int key0 = walk.r.tile(k) * KEYS + key_in_tile;
@@ -429,7 +413,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
     }
 
     const bool whole = walk.whole();
-    float* slot = p.partials + (size_t)(blockIdx.x * 2 + (walk.at == walk.begin_of(blockIdx.x) ? 0 : 1)) * p.partial_floats;
+    float* slot = p.partials + (size_t)walk.my_slot(blockIdx.x) * p.partial_floats;
     const int live = min(rows, ROWS);
     auto put = [&](int r, int d, float a, float b) {              // two values of one row of the result
       const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
@@ -457,56 +441,82 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
       }
       __threadfence();
       consumers_sync();
-      const int c0 = walk.cta_of(walk.item_at), c1 = walk.cta_of(walk.item_at + walk.r.n - 1);
+      const auto pieces = walk.pieces();
+      const int c0 = pieces.first, n_parts = pieces.n;
       if (tid == 0) {
         const int arrived = atomicAdd(&p.arrivals[c0], 1);
-        t->last = arrived == c1 - c0;
+        t->last = arrived == n_parts - 1;
         if (t->last) p.arrivals[c0] = 0;             // ready for the next launch
         __threadfence();
       }
       consumers_sync();
       if (t->last) {
-        // join the pieces, in the order of the CTAs
-        const int first_slot = c0 * 2 + (walk.item_at == walk.begin_of(c0) ? 0 : 1), n_parts = c1 - c0 + 1;
+        // Join the pieces, in the order of the CTAs: a warp per row, lanes along the row, JOIN loads in
+        // flight per lane (the pieces come from L2, a microsecond away).
+        constexpr int VPL = (DCH + 1) / 2;           // 16-byte vectors of a row per lane
+        constexpr int SIDE = DCH == 1 ? 2 : 1;       // pieces side by side in a warp
+        constexpr int JOIN = 16 / VPL;
+        auto part_at = [&](int c) { return p.partials + (size_t)pieces.slot(c) * p.partial_floats; };
+        const int side = SIDE == 2 ? lane >> 4 : 0, col = (SIDE == 2 ? lane & 15 : lane) * 4;
         for (int r = warp; r < live; r += WARPS) {
-          float top = -INFINITY;
-          for (int c = lane; c < n_parts; c += 32)
-            top = fmaxf(top, __ldcg(p.partials + (size_t)(c == 0 ? first_slot : (c0 + c) * 2) * p.partial_floats + r));
+          float w[KV_MAX_CTAS / 32], total = 0.0f, top = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < KV_MAX_CTAS / 32; ++x) w[x] = x * 32 + lane < n_parts ? __ldcg(part_at(x * 32 + lane) + r) : -INFINITY;
+#pragma unroll
+          for (int x = 0; x < KV_MAX_CTAS / 32; ++x) top = fmaxf(top, w[x]);
 #pragma unroll
           for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, d));
           const float b0 = top == -INFINITY ? 0.0f : top;
-          float total = 0.0f;
-          float2 acc[DCH];
 #pragma unroll
-          for (int x = 0; x < DCH; ++x) acc[x] = make_float2(0.0f, 0.0f);
-          for (int cb = 0; cb < n_parts; cb += 32) {
-            float w = 0.0f;
-            if (cb + lane < n_parts) {
-              const float* part_at = p.partials + (size_t)(cb + lane == 0 ? first_slot : (c0 + cb + lane) * 2) * p.partial_floats;
-              w = exp2_fast(__ldcg(part_at + r) - b0);
-              total += w * __ldcg(part_at + ROWS + r);
-            }
-            const int some = min(32, n_parts - cb);
-#pragma unroll 4
-            for (int c = 0; c < some; ++c) {
-              const float wc = __shfl_sync(FULL_MASK, w, c);
-              const float* part_at = p.partials + (size_t)(cb + c == 0 ? first_slot : (c0 + cb + c) * 2) * p.partial_floats + 2 * ROWS + r * (DCH * 64);
+          for (int x = 0; x < KV_MAX_CTAS / 32; ++x) {
+            w[x] = exp2_fast(w[x] - b0);
+            if (x * 32 + lane < n_parts) total += w[x] * __ldcg(part_at(x * 32 + lane) + ROWS + r);
+          }
+          float4 acc[VPL];
 #pragma unroll
-              for (int x = 0; x < DCH; ++x) {
-                if (x * 64 + lane * 2 < v.head_dim) {
-                  const float2 y = __ldcg(reinterpret_cast<const float2*>(part_at + x * 64 + lane * 2));
-                  acc[x].x += wc * y.x;
-                  acc[x].y += wc * y.y;
+          for (int x = 0; x < VPL; ++x) acc[x] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int x = 0; x < KV_MAX_CTAS / 32; ++x) {
+            for (int cb = 0; cb < 32 && x * 32 + cb < n_parts; cb += JOIN * SIDE) {
+              float4 y[JOIN][VPL];
+#pragma unroll
+              for (int u = 0; u < JOIN; ++u)
+#pragma unroll
+                for (int z = 0; z < VPL; ++z) {
+                  const int c = x * 32 + cb + u * SIDE + side, d = z * 128 + col;
+                  y[u][z] = (c < n_parts && d < v.head_dim) ? __ldcg(reinterpret_cast<const float4*>(part_at(c) + 2 * ROWS + r * (DCH * 64) + d))
+                                                            : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
+#pragma unroll
+              for (int u = 0; u < JOIN; ++u) {
+                const float wc = __shfl_sync(FULL_MASK, w[x], (cb + u * SIDE + side) & 31);
+#pragma unroll
+                for (int z = 0; z < VPL; ++z) {
+                  acc[z].x += wc * y[u][z].x;
+                  acc[z].y += wc * y[u][z].y;
+                  acc[z].z += wc * y[u][z].z;
+                  acc[z].w += wc * y[u][z].w;
                 }
               }
             }
           }
 #pragma unroll
           for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(FULL_MASK, total, d);
+          if (SIDE == 2) {
+            acc[0].x += __shfl_xor_sync(FULL_MASK, acc[0].x, 16);
+            acc[0].y += __shfl_xor_sync(FULL_MASK, acc[0].y, 16);
+            acc[0].z += __shfl_xor_sync(FULL_MASK, acc[0].z, 16);
+            acc[0].w += __shfl_xor_sync(FULL_MASK, acc[0].w, 16);
+          }
           const float inv = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
-          for (int x = 0; x < DCH; ++x)
-            if (x * 64 + lane * 2 < v.head_dim) put(r, x * 64 + lane * 2, acc[x].x * inv, acc[x].y * inv);
+          for (int z = 0; z < VPL; ++z) {
+            const int d = z * 128 + col;
+            if (side == 0 && d < v.head_dim) {
+              put(r, d, acc[z].x * inv, acc[z].y * inv);
+              put(r, d + 2, acc[z].z * inv, acc[z].w * inv);
+            }
+          }
         }
       }
     }
@@ -521,10 +531,11 @@ cudaError_t configure_one(int smem_optin) {
 
 template <bool F16, int DCH, int RT>
 cudaError_t launch_one(const KvAttendParams& p, const CUtensorMap& tmap, int sm_count, int smem_optin, cudaStream_t st) {
+  // An even number of stages, so that a stage always belongs to the same half of the consumers: a warp that met
+  // a stage's barrier at every other round only could not tell a round's parity from that of two rounds before.
   int stages = 2;
-  while (stages < MAX_STAGES && rows_smem(DCH, RT, stages + 1) <= smem_optin) ++stages;
-  kv_rows_kernel<F16, DCH, RT><<<sm_count, THREADS, rows_smem(DCH, RT, stages), st>>>(p, tmap, stages);
-  return cudaGetLastError();
+  while (stages + 2 <= MAX_STAGES && rows_smem(DCH, RT, stages + 2) <= smem_optin) stages += 2;
+  return launch_overlapped(kv_rows_kernel<F16, DCH, RT>, dim3(sm_count), dim3(THREADS), rows_smem(DCH, RT, stages), st, 1, p, tmap, stages);
 }
 
 template <bool F16, int DCH>

@@ -113,25 +113,33 @@ __device__ __forceinline__ void kv_load_batch(const KvAttendParams& p, KvBatch* 
   }
 }
 
-// Walks a CTA's stretch of the line, item by item.
+// 64-bit division, which is a long sequence of instructions, only where 32 bits do not do.
+__device__ __forceinline__ long long kv_div(long long a, long long b) {
+  return (a >> 31) == 0 ? (long long)((unsigned)a / (unsigned)min(b, 0xffffffffll)) : a / b;
+}
+
+// Walks a CTA's stretch of the line, item by item.  The present item's key tiles within the stretch are
+// [from, to); `left` tiles of the stretch begin with them.
 template <int ROWS, int KEYS>
 struct KvWalk {
   KvSchedule<ROWS, KEYS> sched;
-  long long total, n_ctas, at, end;      // next key tile of the line, end of the stretch
-  int i, head, rt;                       // the item that `at` lies in
+  int i, head, rt;                       // the item: sequence of the batch, kv head, row tile
   KvRange r;
-  long long item_at;                     // first key tile of the item
+  int from, to, left;
+  long long end;                         // where the stretch ends
+  long long base;                        // each CTA's stretch is `base` long, the first `extra` ones' one more
+  int extra;
 
-  // Stretch of CTA c; n_ctas is capped so that none is empty.
   __device__ KvWalk(const KvAttendParams& p, const KvBatch& b, int c, int grid) : sched(p, b) {
-    total = b.before[p.n];
-    n_ctas = min((long long)grid, total);
-    if (c >= n_ctas) {
-      at = end = 0;
-      return;
-    }
-    at = begin_of(c);
+    const long long total = b.before[p.n];
+    const int n_ctas = (int)min((long long)grid, total);     // none is empty
+    left = 0;
+    if (c >= n_ctas) return;
+    base = kv_div(total, n_ctas);
+    extra = (int)(total - base * n_ctas);
+    const long long at = begin_of(c);
     end = begin_of(c + 1);
+    left = (int)(end - at);
     int lo = 0, hi = p.n - 1;            // the last sequence that begins at or before `at`
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -139,27 +147,27 @@ struct KvWalk {
       else hi = mid - 1;
     }
     i = lo;
-    const long long per_head = (b.before[i + 1] - b.before[i]) / p.v.n_kv_heads;
-    head = (int)((at - b.before[i]) / per_head);
-    item_at = b.before[i] + head * per_head;
+    long long into = at - b.before[i];
+    const long long per_head = kv_div(b.before[i + 1] - b.before[i], p.v.n_kv_heads);
+    head = (int)kv_div(into, per_head);
+    into -= head * per_head;
     rt = 0;
     r = sched.range(b.seq[i], 0);
-    while (at >= item_at + r.n) {
-      item_at += r.n;
+    while (into >= r.n) {
+      into -= r.n;
       r = sched.range(b.seq[i], ++rt);
     }
+    from = (int)into;
+    to = min(r.n, from + left);
   }
-  __device__ __forceinline__ long long begin_of(long long c) const { return total * c / n_ctas; }
-  __device__ __forceinline__ bool done() const { return at >= end; }
-  // key tiles of the item within the stretch: [from, to)
-  __device__ __forceinline__ int from() const { return (int)(at - item_at); }
-  __device__ __forceinline__ int to() const { return (int)(min(end, item_at + r.n) - item_at); }
-  __device__ __forceinline__ bool whole() const { return from() == 0 && to() == r.n; }
+  __device__ __forceinline__ long long begin_of(int c) const { return base * c + min(c, extra); }
+  __device__ __forceinline__ bool done() const { return left == 0; }
+  __device__ __forceinline__ bool whole() const { return from == 0 && to == r.n; }
+  __device__ __forceinline__ long long item_at() const { return end - left - from; }     // first key tile of the item
   // On to the next item of the stretch.
   __device__ __forceinline__ void next() {
-    item_at += r.n;
-    at = item_at;
-    if (at >= end) return;
+    left -= to - from;
+    if (left == 0) return;
     if (++rt >= sched.row_tiles(sched.b.seq[i])) {
       rt = 0;
       if (++head >= sched.p.v.n_kv_heads) {
@@ -168,14 +176,29 @@ struct KvWalk {
       }
     }
     r = sched.range(sched.b.seq[i], rt);
+    from = 0;
+    to = min(r.n, left);
   }
   // The CTA whose stretch holds key tile u.
   __device__ __forceinline__ int cta_of(long long u) const {
-    long long c = u * n_ctas / total;
-    while (c + 1 < n_ctas && begin_of(c + 1) <= u) ++c;
-    while (c > 0 && begin_of(c) > u) --c;
-    return (int)c;
+    const long long longer = (base + 1) * extra;
+    return u < longer ? (int)kv_div(u, base + 1) : extra + (int)kv_div(u - longer, base);
   }
+  // The pieces of the present item lie with CTAs [first, first + n), in slots of the partial results.
+  struct Pieces {
+    int first, n, first_slot;
+    __device__ __forceinline__ int slot(int c) const { return c == 0 ? first_slot : (first + c) * 2; }
+  };
+  __device__ __forceinline__ Pieces pieces() const {
+    const long long u = item_at();
+    Pieces x;
+    x.first = cta_of(u);
+    x.n = cta_of(u + r.n - 1) - x.first + 1;
+    x.first_slot = x.first * 2 + (u == begin_of(x.first) ? 0 : 1);
+    return x;
+  }
+  // Slot for this CTA's piece: 0 for the item its stretch begins with, else 1 (the item that goes on past its end).
+  __device__ __forceinline__ int my_slot(int c) const { return c * 2 + (end - left == begin_of(c) ? 0 : 1); }
 };
 
 }  // namespace icc
