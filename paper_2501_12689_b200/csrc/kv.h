@@ -59,8 +59,8 @@ struct KvAttendParams {
   int first_token;          // starts null: the token of this launch's first sequence
   int window, sinks;
   float scale_log2;         // scale * log2(e): the softmax works in powers of two
-  // pieces of items that span CTAs: two slots per CTA, and per CTA how many pieces of the item that
-  // begins in it and goes on have arrived (zero between launches)
+  // pieces of items that span CTAs: two slots per CTA, and per CTA (and row tile, where an item has two)
+  // how many pieces of the item that begins in it and goes on have arrived (zero between launches)
   float* partials;
   int* arrivals;
   size_t partial_floats;    // of one slot
@@ -83,6 +83,9 @@ size_t kv_rows_partial_floats(int head_dim);
 // tmap: the pool as rows of head_dim elements, box of 64 elements x min(page_size, 64) rows, 128-byte swizzle.
 cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int rows_per_seq, int sm_count, int smem_optin,
                            cudaStream_t st);
+cudaError_t kv_extend_configure(int smem_optin);
+size_t kv_extend_partial_floats(int head_dim);
+cudaError_t kv_extend_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int sm_count, int smem_optin, cudaStream_t st);
 constexpr int KV_BATCH = 256;      // sequences per attention launch
 constexpr int KV_MAX_CTAS = 160;   // attention kernels run one CTA per SM, of which there are at most this many
 

@@ -64,7 +64,7 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   };
   auto ints = [&](size_t n) { return reinterpret_cast<int*>(take(n * 4)); };
   int* err = ints(64);
-  int* arrivals = ints(icc::KV_MAX_CTAS);
+  int* arrivals = ints(2 * icc::KV_MAX_CTAS);
   int* mark = ints(o->max_seqs);
   int* had = ints(o->max_seqs);
   int* upto = ints(o->max_seqs);
@@ -73,7 +73,8 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   int* fresh = ints(o->n_pages);
   int2* jobs = reinterpret_cast<int2*>(take((size_t)o->n_pages * 8));
   int* staged = ints((size_t)o->max_seqs * o->max_pages);
-  const size_t partial_floats = icc::kv_rows_partial_floats(o->head_dim);
+  size_t partial_floats = icc::kv_rows_partial_floats(o->head_dim);
+  if (partial_floats < icc::kv_extend_partial_floats(o->head_dim)) partial_floats = icc::kv_extend_partial_floats(o->head_dim);
   float* partials = reinterpret_cast<float*>(take(2 * icc::KV_MAX_CTAS * partial_floats * 4));
   if (kv) {
     icc::KvView* at = &kv->v;
@@ -94,7 +95,7 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   return off;
 }
 // The words at the head of the workspace that start out as zeros: error, plan, arrivals, marks.
-size_t zero_bytes(const ic_kv_opts_t* o) { return 256 + up256(icc::KV_MAX_CTAS * 4) + up256((size_t)o->max_seqs * 4); }
+size_t zero_bytes(const ic_kv_opts_t* o) { return 256 + up256(2 * icc::KV_MAX_CTAS * 4) + up256((size_t)o->max_seqs * 4); }
 
 int read_opts(const ic_kv_opts_t* opts, ic_kv_opts_t* o) {
   memset(o, 0, sizeof *o);
@@ -293,6 +294,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
     if (e == cudaSuccess) e = icc::kv_pages_configure(smem);
     if (e == cudaSuccess) e = icc::kv_decode_configure(smem);
     if (e == cudaSuccess) e = icc::kv_rows_configure(smem);
+    if (e == cudaSuccess) e = icc::kv_extend_configure(smem);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the cleared words are there for any stream
     if (e != cudaSuccess) {
       cudaGetLastError();
@@ -402,6 +404,7 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
     p.starts = a.starts ? a.starts + off : nullptr;
     p.n = a.n - off < icc::KV_BATCH ? a.n - off : icc::KV_BATCH;
     const cudaError_t e = rows <= 16 ? icc::kv_decode_launch(p, kv->tmap, kv->f16, rows > 8, kv->sm_count, kv->smem_optin, kv->stream)
+                          : p.v.head_dim <= 128 ? icc::kv_extend_launch(p, kv->tmap, kv->f16, kv->sm_count, kv->smem_optin, kv->stream)
                                      : icc::kv_rows_launch(p, kv->tmap, kv->f16, (int)(rows < 64 ? rows : 64), kv->sm_count, kv->smem_optin, kv->stream);
     rc = launched(kv, e, 1, "attention");
   }
