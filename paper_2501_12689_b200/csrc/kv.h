@@ -58,6 +58,8 @@ struct KvAttendParams {
   int64_t n_tokens;         // of the whole call: `starts` and first_token index its q
   int first_token;          // starts null: the token of this launch's first sequence
   int window, sinks;
+  unsigned group_magic;     // x / group = x * group_magic >> group_shift for 0 <= x < 2^31
+  int group_shift;
   float scale_log2;         // scale * log2(e): the softmax works in powers of two
   // pieces of items that span CTAs: two slots per CTA, and per CTA (and row tile, where an item has two)
   // how many pieces of the item that begins in it and goes on have arrived (zero between launches)
@@ -65,6 +67,10 @@ struct KvAttendParams {
   int* arrivals;
   size_t partial_floats;    // of one slot
 };
+
+__device__ __forceinline__ int kv_token_of(const KvAttendParams& p, int row) {
+  return (int)(((unsigned long long)(unsigned)row * p.group_magic) >> p.group_shift);
+}
 
 cudaError_t kv_reserve_launch(const KvView& v, const int* seqs, const int* counts, int n, cudaStream_t st);
 cudaError_t kv_write_launch(const KvView& v, int layer, const void* k, const void* val, int64_t token_stride, int64_t head_stride,

@@ -388,6 +388,11 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
   p.n = a.n;
   p.n_heads = a.n_heads;
   p.group = a.n_heads / kv->v.n_kv_heads;
+  // division by the group as a product: with 2^b >= group, ceil(2^(31 + b) / group) is exact for 31-bit numerators
+  int bits = 0;
+  while ((1ll << bits) < p.group) ++bits;
+  p.group_shift = 31 + bits;
+  p.group_magic = (unsigned)(((1ull << p.group_shift) + p.group - 1) / p.group);
   p.layer = a.layer;
   p.n_tokens = a.n_tokens;
   p.window = a.window;

@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
         const int r = u / PIECES, piece = u - r * PIECES;
         uint4 w = make_uint4(0, 0, 0, 0);
         if (r < rows && piece * 8 < v.head_dim) {
-          const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
+          const int rr = walk.rt * ROWS + r, tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
           w = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(seq.first + tok) * p.q_token_stride +
                                               (int64_t)hq * p.q_head_stride + piece * 8);
         }
@@ -221,10 +221,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int r = b * 8 + fc + x;
-        pos[b][x] = r < rows ? first_pos + (walk.rt * ROWS + r) / p.group : -1;
+        pos[b][x] = r < rows ? first_pos + kv_token_of(p, walk.rt * ROWS + r) : -1;
       }
     const int live = min(rows, ROWS);
-    const int lowest = first_pos + walk.rt * ROWS / p.group, highest = first_pos + (walk.rt * ROWS + live - 1) / p.group;
+    const int lowest = first_pos + kv_token_of(p, walk.rt * ROWS), highest = first_pos + kv_token_of(p, walk.rt * ROWS + live - 1);
     uint32_t q[Q_IN_REGISTERS ? DCH * 2 : 1][NB][4];              // two 16-element steps each
     if (ok) ok = mbar_wait(&t->q_full, q_ph, &t->abort_flag);
     q_ph ^= 1u;
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
       for (int x = 0; x < 4; ++x) {
         const int r = r0 + x;
         if (r >= live) break;
-        const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
+        const int rr = walk.rt * ROWS + r, tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
         reinterpret_cast<uint16_t*>(p.out)[(int64_t)(seq.first + tok) * p.out_token_stride + (int64_t)hq * p.out_head_stride + d] = round16<F16>(e[x]);
       }
     };

@@ -100,6 +100,8 @@ __device__ __forceinline__ void cp_async_16(uint32_t smem_dst, const void* src, 
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// The lowest n bits, n <= 0: none, n >= 32: all.
+__device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); }
 __device__ __forceinline__ void warpgroup_sync(int which) {
   if (which == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
   else asm volatile("bar.sync 2, 128;" ::: "memory");
@@ -257,9 +259,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       };
       for (; !walk.done() && ok; walk.next()) {
         const KvSeq& seq = t->batch.seq[walk.i];
-        const bool two = (long long)seq.count * p.group - (long long)walk.rt * ROWS > 128;
-        int lowest, highest;
-        walk.sched.positions(seq, walk.rt, &lowest, &highest);
+        const bool two = seq.count * p.group - walk.rt * ROWS > 128;
+        // what the call's tokens of this sequence see: keys below `sinks` and from `first_seen` on
+        const int first_seen = p.window ? max(0, seq.length - seq.count - p.window + 1) : 0;
         ok = mbar_wait(&t->q_full, q_ph, &t->abort_flag) && mbar_wait(&t->full[s], ph, &t->abort_flag);
         q_ph ^= 1u;
         if (!__all_sync(FULL_MASK, ok)) {
@@ -281,14 +283,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           ok = __all_sync(FULL_MASK, mbar_wait(&t->full[s], ph, &t->abort_flag));
           if (!ok) break;
           advance();
-          // Values of keys that none of the rows sees count as zeros, whatever is there: a weight of zero
-          // would not undo an infinity or a NaN.  Only the tiles at the ends of what is visible hold such keys.
+          // Values of keys that no token of the call sees count as zeros, whatever is there (slots past the
+          // end, tokens that have left the window): a weight of zero would not undo an infinity or a NaN.
           const int key0 = walk.r.tile(k) * KEYS;
-          if (key0 + KEYS - 1 > highest || (p.window && key0 <= lowest - p.window && key0 + KEYS > p.sinks)) {
-            for (int r = 0; r < KEYS; ++r) {
-              const int j = key0 + r;
-              if (j <= highest && (!p.window || j > lowest - p.window || j < p.sinks)) continue;
-              if (lane < DCH * 8) *reinterpret_cast<uint4*>(ring + sv * SLOT + (lane >> 3) * CHUNK + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
+          const int gap = max(key0, p.sinks), gap_end = min(key0 + KEYS, first_seen), tail = max(key0, seq.length);
+          if (gap < gap_end || tail < key0 + KEYS) {
+            constexpr int PIECES = DCH * 8;
+            for (int u = lane; u < KEYS * PIECES; u += 32) {
+              const int r = u / PIECES, j = key0 + r, piece = u % PIECES;
+              if ((j >= gap && j < gap_end) || j >= tail)
+                *reinterpret_cast<uint4*>(ring + sv * SLOT + (piece >> 3) * CHUNK + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
             }
             fence_async_shared();
             __syncwarp();
@@ -334,18 +338,21 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       uint32_t ph = 1;
       for (; !walk.done(); walk.next(), ph ^= 1u) {
         const KvSeq& seq = t->batch.seq[walk.i];
-        const int rows = (int)min((long long)ROWS, (long long)seq.count * p.group - (long long)walk.rt * ROWS);
+        const int rows = min(ROWS, seq.count * p.group - walk.rt * ROWS);
         if (!mbar_wait(&t->q_empty, ph, &t->abort_flag)) {
           if (lane == 0) kv_report(v, KV_TIMEOUT);
           break;
         }
         const int fill = rows > 128 ? 256 : 128;     // the rest of a tile is zeros
-        for (int u = (warp - 10) * 32 + lane; u < fill * PIECES; u += 64) {
-          const int r = u / PIECES, piece = u - r * PIECES;
-          const bool there = r < rows && piece * 8 < v.head_dim;
-          const int rr = walk.rt * ROWS + (there ? r : 0), tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
-          const uint16_t* from = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(seq.first + tok) * p.q_token_stride +
-                                 (int64_t)hq * p.q_head_stride + (there ? piece * 8 : 0);
+        const int first = (warp - 10) * 32 + lane, piece = first % PIECES;     // a thread's pieces are in one column
+        const bool column = piece * 8 < v.head_dim;
+        const uint16_t* base = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)seq.first * p.q_token_stride +
+                               (int64_t)walk.head * p.group * p.q_head_stride + (column ? piece * 8 : 0);
+#pragma unroll 4
+        for (int r = first / PIECES; r < fill; r += 64 / PIECES) {
+          const bool there = r < rows && column;
+          const int rr = walk.rt * ROWS + (there ? r : 0), tok = kv_token_of(p, rr);
+          const uint16_t* from = base + (int64_t)tok * p.q_token_stride + (int64_t)(rr - tok * p.group) * p.q_head_stride;
           cp_async_16(q_addr + (r >> 7) * Q_TILE + (piece >> 3) * CHUNK + (r & 127) * 128 + (((piece & 7) ^ (r & 7)) << 4), from, there);
         }
         cp_async_wait_all();
@@ -364,13 +371,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     bool ok = true;
     for (; !walk.done(); walk.next()) {
       const KvSeq seq = t->batch.seq[walk.i];
-      const long long rows = (long long)seq.count * p.group - (long long)walk.rt * ROWS - x * 128;   // of this row tile, if below 128
+      const int rows = seq.count * p.group - walk.rt * ROWS - x * 128;        // of this row tile, if below 128
       if (rows <= 0) continue;
-      const int rr = walk.rt * ROWS + x * 128 + row, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
       const bool live = row < rows;
-      const int pos = live ? seq.length - seq.count + tok : -1;
-      // positions of the warp's first and last rows; a warp with rows missing never takes the short way
-      const int lowest = __shfl_sync(FULL_MASK, pos, 0), highest = __shfl_sync(FULL_MASK, pos, 31);
+      // a row that is not there goes along with the last one that is, and is not written
+      const int rr = walk.rt * ROWS + x * 128 + min(row, rows - 1), tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
+      const int pos = seq.length - seq.count + tok;
+      const int lowest = __shfl_sync(FULL_MASK, pos, 0), highest = __shfl_sync(FULL_MASK, pos, 31);     // of the warp's rows
       float m = -INFINITY, l = 0.0f;
       for (int k = walk.from; k < walk.to; ++k) {
         if (ok) ok = mbar_wait(&t->s_full[x], s_ph, &t->abort_flag);
@@ -383,21 +390,21 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         tmem_ld_wait_for(va);
         tmem_ld_wait_for(vb);
         const int key0 = walk.r.tile(k) * KEYS, last = key0 + KEYS - 1;
-        const bool clear = last <= lowest && highest >= 0 && (!p.window || key0 > highest - p.window || last < p.sinks);
+        const bool clear = last <= lowest && (!p.window || key0 > highest - p.window || last < p.sinks);
         float scale = p.scale_log2;
         if (!clear) {
-          const int from = p.window ? pos - p.window : -1;       // seen: from < j <= pos, or j < sinks
+          // one bit per key: at or before the row's position, and in its window or a sink
+          uint32_t seen[4];
 #pragma unroll
-          for (int i = 0; i < 64; ++i) {
-            const int j = key0 + i;
-            const bool seen = j <= pos && (j > from || j < p.sinks);
-            va[i] = __float_as_uint(seen ? __uint_as_float(va[i]) * scale : -INFINITY);
+          for (int y = 0; y < 4; ++y) {
+            const int j = key0 + y * 32;
+            seen[y] = bits_below(pos - j + 1);
+            if (p.window) seen[y] &= ~bits_below(pos - p.window + 1 - j) | bits_below(p.sinks - j);
           }
 #pragma unroll
           for (int i = 0; i < 64; ++i) {
-            const int j = key0 + 64 + i;
-            const bool seen = j <= pos && (j > from || j < p.sinks);
-            vb[i] = __float_as_uint(seen ? __uint_as_float(vb[i]) * scale : -INFINITY);
+            va[i] = (seen[i >> 5] >> (i & 31)) & 1u ? __float_as_uint(__uint_as_float(va[i]) * scale) : 0xff800000u;
+            vb[i] = (seen[2 + (i >> 5)] >> (i & 31)) & 1u ? __float_as_uint(__uint_as_float(vb[i]) * scale) : 0xff800000u;
           }
           scale = 1.0f;
         }

@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
           const int r = u / PIECES, piece = u - r * PIECES;
           uint4 w = make_uint4(0, 0, 0, 0);
           if (r < rows && piece * 8 < v.head_dim) {
-            const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
+            const int rr = walk.rt * ROWS + r, tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
             w = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(seq.first + tok) * p.q_token_stride +
                                                 (int64_t)hq * p.q_head_stride + piece * 8);
           }
@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int r = rtile * 16 + qr + x * 8;
-      pos[x] = r < rows ? seq.length - seq.count + (walk.rt * ROWS + r) / p.group : -1;
+      pos[x] = r < rows ? seq.length - seq.count + kv_token_of(p, walk.rt * ROWS + r) : -1;
     }
     uint32_t q[DCH * 4][4];
     if (ok) ok = mbar_wait(&t->q_full, q_ph, &t->abort_flag);
@@ -236,8 +236,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
     {
       const int r0 = rtile * 16, r1 = min(r0 + 16, rows) - 1;
       if (r0 < rows) {
-        lowest = seq.length - seq.count + (walk.rt * ROWS + r0) / p.group;
-        highest = seq.length - seq.count + (walk.rt * ROWS + r1) / p.group;
+        lowest = seq.length - seq.count + kv_token_of(p, walk.rt * ROWS + r0);
+        highest = seq.length - seq.count + kv_token_of(p, walk.rt * ROWS + r1);
       }
     }
     float o[DCH * 8][4];
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
     float* slot = p.partials + (size_t)walk.my_slot(blockIdx.x) * p.partial_floats;
     const int live = min(rows, ROWS);
     auto put = [&](int r, int d, float a, float b) {              // two values of one row of the result
-      const int rr = walk.rt * ROWS + r, tok = rr / p.group, hq = walk.head * p.group + (rr - tok * p.group);
+      const int rr = walk.rt * ROWS + r, tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
       uint16_t* to16 = reinterpret_cast<uint16_t*>(p.out) + (int64_t)(seq.first + tok) * p.out_token_stride + (int64_t)hq * p.out_head_stride + d;
       *reinterpret_cast<uint32_t*>(to16) = pack2<F16>(a, b);
     };

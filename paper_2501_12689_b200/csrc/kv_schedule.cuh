@@ -35,13 +35,13 @@ struct KvSchedule {
   const KvBatch& b;
   __device__ KvSchedule(const KvAttendParams& p_, const KvBatch& b_) : p(p_), b(b_) {}
 
-  __device__ __forceinline__ int row_tiles(const KvSeq& s) const { return (int)(((long long)s.count * p.group + ROWS - 1) / ROWS); }
+  __device__ __forceinline__ int row_tiles(const KvSeq& s) const { return (int)(((unsigned)s.count * (unsigned)p.group + ROWS - 1u) / ROWS); }
 
   // Positions of the first and the last row of row tile rt.
   __device__ __forceinline__ void positions(const KvSeq& s, int rt, int* lowest, int* highest) const {
-    const long long r0 = (long long)rt * ROWS, r1 = min(r0 + ROWS, (long long)s.count * p.group) - 1;
-    *lowest = s.length - s.count + (int)(r0 / p.group);
-    *highest = s.length - s.count + (int)(r1 / p.group);
+    const unsigned r0 = (unsigned)rt * ROWS, r1 = min(r0 + ROWS, (unsigned)s.count * (unsigned)p.group) - 1u;
+    *lowest = s.length - s.count + kv_token_of(p, (int)r0);
+    *highest = s.length - s.count + kv_token_of(p, (int)r1);
   }
 
   __device__ __forceinline__ KvRange range(const KvSeq& s, int rt) const {
@@ -51,17 +51,10 @@ struct KvSchedule {
     const int end = highest < 0 ? 0 : highest / KEYS + 1;
     r.first = (p.window && lowest >= p.window) ? (lowest - p.window + 1) / KEYS : 0;
     // the sinks' tiles, as far as they lie before the window's
-    const int sink_tiles = (int)(((long long)p.sinks + KEYS - 1) / KEYS);
+    const int sink_tiles = (int)(((unsigned)p.sinks + KEYS - 1u) / KEYS);
     r.sink_tiles = min(sink_tiles, r.first);
     r.n = max(1, r.sink_tiles + end - r.first);      // a row tile that sees nothing writes zeros
     return r;
-  }
-
-  __device__ __forceinline__ long long tiles_of(const KvSeq& s) const {
-    const int n = row_tiles(s);
-    long long sum = 0;
-    for (int rt = 0; rt < n; ++rt) sum += range(s, rt).n;
-    return sum;
   }
 };
 
@@ -93,7 +86,21 @@ __device__ __forceinline__ void kv_load_batch(const KvAttendParams& p, KvBatch* 
     if (s.count > s.length && (p.starts || s.length > 0)) fine = false;     // (the one token of an empty sequence sees nothing)
     if (!fine && blockIdx.x == 0) kv_report(p.v, KV_INVALID);
     b->seq[i] = s;
-    b->before[i + 1] = sched.tiles_of(s) * p.v.n_kv_heads;
+    const int n = sched.row_tiles(s);
+    b->before[i + 1] = n == 0 ? 0 : (n == 1 ? (long long)sched.range(s, 0).n * p.v.n_kv_heads : -1);
+  }
+  __syncthreads();
+  // sequences of several row tiles: a warp each
+  for (int i = threadIdx.x >> 5; i < p.n; i += blockDim.x >> 5) {
+    if (b->before[i + 1] >= 0) continue;
+    const KvSeq s = b->seq[i];
+    const int n = sched.row_tiles(s), lane = threadIdx.x & 31;
+    long long sum = 0;
+    for (int rt = lane; rt < n; rt += 32) sum += sched.range(s, rt).n;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(FULL_MASK, sum, d);
+    __syncwarp();
+    if (lane == 0) b->before[i + 1] = sum * p.v.n_kv_heads;
   }
   __syncthreads();
   if (threadIdx.x < 32) {
@@ -151,12 +158,30 @@ struct KvWalk {
     const long long per_head = kv_div(b.before[i + 1] - b.before[i], p.v.n_kv_heads);
     head = (int)kv_div(into, per_head);
     into -= head * per_head;
+    // the row tile that `into` lies in: the warp looks at 32 of them at a time
+    const int n = sched.row_tiles(b.seq[i]);
     rt = 0;
-    r = sched.range(b.seq[i], 0);
-    while (into >= r.n) {
-      into -= r.n;
-      r = sched.range(b.seq[i], ++rt);
+    if (n > 1) {
+      for (int rt0 = 0;; rt0 += 32) {
+        const int mine = rt0 + (threadIdx.x & 31);
+        long long upto = mine < n ? sched.range(b.seq[i], mine).n : 0;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const long long y = __shfl_up_sync(FULL_MASK, upto, d);
+          if ((int)(threadIdx.x & 31) >= d) upto += y;
+        }
+        const unsigned past = __ballot_sync(FULL_MASK, upto > into);       // never empty in the last round
+        if (past || rt0 + 32 >= n) {
+          const int at_lane = past ? __ffs(past) - 1 : 31;
+          rt = rt0 + at_lane;
+          const long long before_it = __shfl_sync(FULL_MASK, upto, max(at_lane - 1, 0));
+          into -= at_lane > 0 ? before_it : 0;
+          break;
+        }
+        into -= __shfl_sync(FULL_MASK, upto, 31);
+      }
     }
+    r = sched.range(b.seq[i], rt);
     from = (int)into;
     to = min(r.n, from + left);
   }
