@@ -8,10 +8,17 @@
 // each for both row tiles); neither may wait for the other.  Hence the two row tiles: while one's scores are turned
 // into weights, the tensor cores work for the other one.
 //
-//   warps 0-3, 4-7   softmax of row tile A, B: a thread owns a row (a tensor-memory lane)
+//   warps 0-3, 4-7   softmax of row tile A, B: a thread owns a row (a tensor-memory lane), and copies the row's
+//                    query into the swizzled layout of the left operand, an item ahead
 //   warp 8           loads of keys and values: one tensor-map box per page (or 64 rows) and 64-element chunk
-//   warp 9           issues the products: PV_A(j), S_A(j+1), PV_B(j), S_B(j+1), ...
-//   warps 10, 11     query rows of the next item, into the swizzled layout of the left operand
+//   warps 9, 10      issue the products of row tile A, B: PV(j), S(j+1), ..., so that neither waits in the other's
+//                    queue.  They take turns with the products that the softmax waits for: left alone both
+//                    row tiles fall into step, and then compete for the tensor cores and for the
+//                    special-function units at the same times
+//   warp 11          zeros in place of values that nobody sees
+//
+// The chain softmax - PV - S of one row tile is what a tile takes when all goes well, so it is kept short: weights
+// go to the tensor cores in two halves of 64 keys.
 //
 // A row's maximum is only raised when it is exceeded by more than 2^8: O is rescaled a few times per item and not
 // per tile, and weights of up to 256 are as exact as those up to 1.  Weights are rounded to the cache's
@@ -36,8 +43,8 @@ constexpr float RAISE = 8.0f;            // how far (log2) a row's scores may ex
 constexpr int AHEAD = 3;                 // batches of page numbers under way
 
 struct ExtendTail {
-  uint64_t full[MAX_SLOTS], empty[MAX_SLOTS], q_full, q_empty;
-  uint64_t s_full[2], p_full[2], o_full[2], drain;
+  uint64_t full[MAX_SLOTS], empty[MAX_SLOTS], clean[MAX_SLOTS], turn[2];
+  uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2], drain[2];       // per row tile; p_full: keys 0-63 and 64-127
   uint32_t tmem_base;
   int abort_flag, last[2];
   KvBatch batch;
@@ -61,15 +68,49 @@ __device__ __forceinline__ uint64_t desc_mn_major_sw128(uint32_t smem_addr, uint
   d |= (uint64_t)2 << 61;
   return d;
 }
-// D[tmem] (+)= A[tmem] * B[smem], issued by one thread.
-__device__ __forceinline__ void umma_from_tmem(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t id, uint32_t accumulate) {
+// Products and their completion, executed by a whole warp and issued by the one lane whose `on` is not 0, so that the
+// warp never has to leave for a branch of one lane.
+__device__ __forceinline__ void product_smem(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t id, uint32_t accumulate, uint32_t on) {
   asm volatile(
       "{\n"
-      ".reg .pred p;\n"
+      ".reg .pred p, q;\n"
       "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
       "}\n" ::"r"(tmem_d),
-      "r"(tmem_a), "l"(desc_b), "r"(id), "r"(accumulate)
+      "l"(desc_a), "l"(desc_b), "r"(id), "r"(accumulate), "r"(on)
+      : "memory");
+}
+// The left operand in tensor memory.
+__device__ __forceinline__ void product_tmem(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t id, uint32_t accumulate, uint32_t on) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "}\n" ::"r"(tmem_d),
+      "r"(tmem_a), "l"(desc_b), "r"(id), "r"(accumulate), "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void commit_products(uint64_t* bar, uint32_t on) {
+  asm volatile(
+      "{\n"
+      ".reg .pred q;\n"
+      "setp.ne.b32 q, %1, 0;\n"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n"
+      "}\n" ::"r"(smem_u32(bar)),
+      "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void arrive_one(uint64_t* bar, uint32_t on) {
+  asm volatile(
+      "{\n"
+      ".reg .pred q;\n"
+      "setp.ne.b32 q, %1, 0;\n"
+      "@q mbarrier.arrive.shared::cta.b64 _, [%0];\n"
+      "}\n" ::"r"(smem_u32(bar)),
+      "r"(on)
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t* v) {
@@ -100,12 +141,62 @@ __device__ __forceinline__ void cp_async_16(uint32_t smem_dst, const void* src, 
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// A wait of a whole warp.  All lanes ask together: a lane that waits by itself, inside a branch, wakes up to 200 cycles
+// later (measured: 54 against 70 to 240 cycles from the arrival).
+__device__ __forceinline__ bool mbar_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  return __all_sync(FULL_MASK, mbar_wait(bar, parity, abort_flag)) != 0;
+}
 // The lowest n bits, n <= 0: none, n >= 32: all.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); }
 __device__ __forceinline__ void warpgroup_sync(int which) {
   if (which == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
   else asm volatile("bar.sync 2, 128;" ::: "memory");
 }
+
+// ---------------------------------------------------------------- pairs of floats in one instruction
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ void split_pair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma_pairs(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_pairs(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// Weights 2^(scale s - base) of 64 scores, packed to the cache's type; their sum is added to sum2.
+template <bool F16>
+__device__ __forceinline__ void weights(const uint32_t (&s)[64], uint64_t scale2, uint64_t base2, uint64_t (&sum2)[2], uint32_t (&w)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const uint64_t x2 = fma_pairs(pair_of(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), scale2, base2);
+    float a, b;
+    split_pair(x2, &a, &b);
+    a = exp2_fast(a);
+    b = exp2_fast(b);
+    sum2[i & 1] = add_pairs(sum2[i & 1], pair_of(a, b));
+    w[i] = pack2<F16>(a, b);
+  }
+}
+
+// Keys that no token of the call sees: between the sinks and the first token's window, and past the end (slots of
+// the last page without tokens).  Whatever stands there must not reach a product: a weight of zero would not undo an
+// infinity or a NaN.
+struct Hidden {
+  int sinks, first_seen, length;
+  __device__ __forceinline__ Hidden(const KvAttendParams& p, const KvSeq& s)
+      : sinks(p.sinks), first_seen(p.window ? max(0, s.length - s.count - p.window + 1) : 0), length(s.length) {}
+  __device__ __forceinline__ bool is(int key) const { return (key >= sinks && key < first_seen) || key >= length; }
+  __device__ __forceinline__ bool any(int key0) const {          // among the keys of a tile
+    return max(key0, sinks) < min(key0 + KEYS, first_seen) || key0 + KEYS > length;
+  }
+};
 
 template <bool F16, int DCH>
 __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendParams p, const __grid_constant__ CUtensorMap tmap, int n_slots) {
@@ -123,16 +214,18 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
   if (tid == 0) {
     for (int s = 0; s < n_slots; ++s) {
       mbar_init(&t->full[s], 1);
-      mbar_init(&t->empty[s], 1);
+      mbar_init(&t->empty[s], 2 + (s & 1));          // row tiles A and B; and warp 11 for values, which take the odd slots
+      mbar_init(&t->clean[s], 1);
     }
-    mbar_init(&t->q_full, 2);
-    mbar_init(&t->q_empty, 1);
     for (int x = 0; x < 2; ++x) {
+      mbar_init(&t->q_full[x], 4);
       mbar_init(&t->s_full[x], 1);
-      mbar_init(&t->p_full[x], 4);
+      mbar_init(&t->p_full[x][0], 4);
+      mbar_init(&t->p_full[x][1], 4);
       mbar_init(&t->o_full[x], 1);
+      mbar_init(&t->drain[x], 1);
+      mbar_init(&t->turn[x], 1);
     }
-    mbar_init(&t->drain, 1);
     t->abort_flag = 0;
     mbar_fence_init();
     prefetch_tmap(&tmap);
@@ -204,7 +297,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           const unsigned who = __ballot_sync(FULL_MASK, y >= 0);
           if (y >= 0) y += key & page_mask;
           for (int values = 0; values < 2; ++values) {
-            ok = __all_sync(FULL_MASK, mbar_wait(&t->empty[s], ph ^ 1u, &t->abort_flag));
+            ok = mbar_warp_wait(&t->empty[s], ph ^ 1u, &t->abort_flag);
             if (!ok) break;
             if (lane == 0) mbar_arrive_expect_tx(&t->full[s], (uint32_t)__popc(who) * DCH * box_bytes);
             __syncwarp();
@@ -229,137 +322,141 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           }
         }
       }
-    } else if (warp == 9) {
+    } else if (warp <= 10) {
       // ---------------------------------------------------------- products
-      constexpr uint32_t id_s = idesc(F16, KEYS, false), id_o = idesc(F16, DIM, true);
-      const uint32_t q_addr = smem_u32(q_smem), ring_addr = smem_u32(ring);
-      int s = 0;                                     // next slot of the ring
-      uint32_t ph = 0, q_ph = 0, p_ph[2] = {0, 0};
-      bool ok = true;
-      auto advance = [&]() {
-        if (++s == n_slots) {
-          s = 0;
-          ph ^= 1u;
-        }
-      };
-      auto scores = [&](int x, int slot) {           // S_x = Q_x K^T
+      {
+        constexpr uint32_t id_s = idesc(F16, KEYS, false), id_o = idesc(F16, DIM, true);
+        const int x = warp - 9;                      // row tile
+        const uint32_t on = lane == 0;
+        const uint32_t s_at = tmem + x * 128, o_at = tmem + TMEM_O + x * 128;
+        const uint64_t q_desc = umma_desc_k_major_sw128(smem_u32(q_smem) + x * Q_TILE), k_desc = umma_desc_k_major_sw128(smem_u32(ring)),
+                       v_desc = desc_mn_major_sw128(smem_u32(ring), CHUNK);
+        int s = 0;                                   // next slot of the ring
+        uint32_t ph = 0, q_ph = 0, p_ph = 0, clean_ph = 0, turn_ph = x ^ 1;
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_warp_wait(bar, parity, &t->abort_flag); };
+        auto advance = [&]() {
+          if (++s == n_slots) {
+            s = 0;
+            ph ^= 1u;
+          }
+        };
+        auto scores = [&](int slot) {                // S = Q K^T
+          const uint64_t db = k_desc + slot * (SLOT >> 4);
 #pragma unroll
-        for (int c = 0; c < DCH; ++c) {
-          const uint64_t da = umma_desc_k_major_sw128(q_addr + x * Q_TILE + c * CHUNK), db = umma_desc_k_major_sw128(ring_addr + slot * SLOT + c * CHUNK);
+          for (int c = 0; c < DCH; ++c)
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) umma_bf16(tmem + x * 128, da + kk * 2, db + kk * 2, id_s, (c | kk) != 0 ? 1u : 0u);
-        }
-        umma_commit(&t->s_full[x]);
-      };
-      auto values = [&](int x, int slot, bool add) { // O_x (+)= P_x V
-        const uint64_t db = desc_mn_major_sw128(ring_addr + slot * SLOT, CHUNK);
+            for (int kk = 0; kk < 4; ++kk)
+              product_smem(s_at, q_desc + (c * (CHUNK >> 4) + kk * 2), db + (c * (CHUNK >> 4) + kk * 2), id_s, (c | kk) != 0 ? 1u : 0u, on);
+          commit_products(&t->s_full[x], on);
+        };
+        auto values = [&](int slot, int half, bool add) {        // O (+)= P V, 64 of the keys
+          const uint64_t db = v_desc + slot * (SLOT >> 4);
 #pragma unroll
-        for (int kk = 0; kk < KEYS / 16; ++kk)       // 16 keys further: 8 columns of P, 2048 bytes of V
-          umma_from_tmem(tmem + TMEM_O + x * 128, tmem + x * 128 + kk * 8, db + kk * 128, id_o, (add || kk != 0) ? 1u : 0u);
-      };
-      for (; !walk.done() && ok; walk.next()) {
-        const KvSeq& seq = t->batch.seq[walk.i];
-        const bool two = seq.count * p.group - walk.rt * ROWS > 128;
-        // what the call's tokens of this sequence see: keys below `sinks` and from `first_seen` on
-        const int first_seen = p.window ? max(0, seq.length - seq.count - p.window + 1) : 0;
-        ok = mbar_wait(&t->q_full, q_ph, &t->abort_flag) && mbar_wait(&t->full[s], ph, &t->abort_flag);
-        q_ph ^= 1u;
-        if (!__all_sync(FULL_MASK, ok)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after_sync();
-        if (lane == 0) {
-          scores(0, s);
-          if (two) scores(1, s);
-          umma_commit(&t->empty[s]);
-          if (walk.from + 1 == walk.to) umma_commit(&t->q_empty);
-        }
-        __syncwarp();
-        advance();
-        for (int k = walk.from; k < walk.to; ++k) {
-          const bool more = k + 1 < walk.to;
-          const int sv = s;
-          ok = __all_sync(FULL_MASK, mbar_wait(&t->full[s], ph, &t->abort_flag));
+          for (int i = 0; i < KEYS / 32; ++i) {      // 16 keys further: 8 columns of P, 2048 bytes of V
+            const int kk = half * (KEYS / 32) + i;
+            product_tmem(o_at, s_at + kk * 8, db + kk * 128, id_o, (add || kk != 0) ? 1u : 0u, on);
+          }
+        };
+        // A slot is free when both row tiles are done with it; one that has no rows in the item says so at once.
+        auto done_with = [&](int slot, bool mine) {
+          if (mine) commit_products(&t->empty[slot], on);
+          else arrive_one(&t->empty[slot], on);
+        };
+        for (; !walk.done() && ok; walk.next()) {
+          const KvSeq& seq = t->batch.seq[walk.i];
+          const int rows = seq.count * p.group - walk.rt * ROWS, n = walk.to - walk.from;
+          const bool mine = rows > x * 128, two = rows > 128;
+          const Hidden hidden(p, seq);
+          ok = wait(&t->full[s], ph);
+          if (mine && ok) {
+            ok = wait(&t->q_full[x], q_ph);
+            q_ph ^= 1u;
+            tc_fence_after_sync();
+            if (ok) scores(s);
+          }
           if (!ok) break;
+          done_with(s, mine);
           advance();
-          // Values of keys that no token of the call sees count as zeros, whatever is there (slots past the
-          // end, tokens that have left the window): a weight of zero would not undo an infinity or a NaN.
+          for (int j = 0; j < n; ++j) {
+            const bool more = j + 1 < n;
+            const int sv = s;
+            const bool cleaned = hidden.any(walk.r.tile(walk.from + j) * KEYS);
+            ok = wait(&t->full[s], ph);
+            if (ok && cleaned) {
+              ok = wait(&t->clean[sv], (clean_ph >> sv) & 1u);   // a slot's barrier turns at each use that is cleaned
+              clean_ph ^= 1u << sv;
+            }
+            if (!ok) break;
+            advance();
+            if (mine) {
+              ok = wait(&t->p_full[x][0], p_ph);
+              if (!ok) break;
+              tc_fence_after_sync();
+              values(sv, 0, j > 0);
+            }
+            if (more) ok = wait(&t->full[s], ph);
+            if (mine && ok) {
+              ok = wait(&t->p_full[x][1], p_ph);
+              p_ph ^= 1u;
+              if (ok && two) {
+                ok = wait(&t->turn[x], turn_ph);
+                turn_ph ^= 1u;
+              }
+              if (!ok) break;
+              tc_fence_after_sync();
+              values(sv, 1, true);
+              done_with(sv, true);
+              if (more) scores(s);
+              else commit_products(&t->o_full[x], on);
+              if (two) arrive_one(&t->turn[x ^ 1], on);
+            }
+            if (!ok) break;
+            if (!mine) done_with(sv, false);
+            if (more) {
+              done_with(s, mine);
+              advance();
+            }
+          }
+        }
+        // nothing issued is still running when tensor memory is released
+        commit_products(&t->drain[x], on);
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&t->drain[x], 0) && clock64() - t0 < WAIT_LIMIT_CYCLES) {
+        }
+        if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
+      }
+    } else {
+      // ---------------------------------------------------------- values that no token of the call sees count as zeros
+      // (it looks at every tile and has a say in its slot's release, or it could lose count of the rounds)
+      int s = 1;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (; !walk.done() && ok; walk.next()) {
+        const Hidden hidden(p, t->batch.seq[walk.i]);
+        for (int k = walk.from; k < walk.to; ++k) {
           const int key0 = walk.r.tile(k) * KEYS;
-          const int gap = max(key0, p.sinks), gap_end = min(key0 + KEYS, first_seen), tail = max(key0, seq.length);
-          if (gap < gap_end || tail < key0 + KEYS) {
+          ok = mbar_warp_wait(&t->full[s], ph, &t->abort_flag);
+          if (!ok) break;
+          if (hidden.any(key0)) {
             constexpr int PIECES = DCH * 8;
             for (int u = lane; u < KEYS * PIECES; u += 32) {
-              const int r = u / PIECES, j = key0 + r, piece = u % PIECES;
-              if ((j >= gap && j < gap_end) || j >= tail)
-                *reinterpret_cast<uint4*>(ring + sv * SLOT + (piece >> 3) * CHUNK + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
+              const int r = u / PIECES, piece = u % PIECES;
+              if (hidden.is(key0 + r))
+                *reinterpret_cast<uint4*>(ring + s * SLOT + (piece >> 3) * CHUNK + r * 128 + (piece & 7) * 16) = make_uint4(0, 0, 0, 0);
             }
             fence_async_shared();
             __syncwarp();
+            if (lane == 0) mbar_arrive(&t->clean[s]);
           }
-          if (more) {
-            ok = __all_sync(FULL_MASK, mbar_wait(&t->full[s], ph, &t->abort_flag));
-            if (!ok) break;
+          if (lane == 0) mbar_arrive(&t->empty[s]);
+          if ((s += 2) >= n_slots) {
+            s = 1;
+            ph ^= 1u;
           }
-          for (int x = 0; x < (two ? 2 : 1) && ok; ++x) {
-            ok = __all_sync(FULL_MASK, mbar_wait(&t->p_full[x], p_ph[x], &t->abort_flag));
-            if (!ok) break;
-            p_ph[x] ^= 1u;
-            tc_fence_after_sync();
-            if (lane == 0) {
-              values(x, sv, k > walk.from);
-              if (more) scores(x, s);
-              else umma_commit(&t->o_full[x]);
-            }
-            __syncwarp();
-          }
-          if (!ok) break;
-          if (lane == 0) {
-            umma_commit(&t->empty[sv]);
-            if (more) umma_commit(&t->empty[s]);
-            if (k + 2 == walk.to) umma_commit(&t->q_empty);      // the last scores of the item are under way
-          }
-          __syncwarp();
-          if (more) advance();
         }
       }
-      if (lane == 0) {
-        // nothing issued is still running when tensor memory is released
-        umma_commit(&t->drain);
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&t->drain, 0) && clock64() - t0 < WAIT_LIMIT_CYCLES) {
-        }
-        if (!ok) kv_report(v, KV_TIMEOUT);
-      }
-    } else {
-      // ---------------------------------------------------------- query rows
-      constexpr int PIECES = DCH * 8;
-      const uint32_t q_addr = smem_u32(q_smem);
-      uint32_t ph = 1;
-      for (; !walk.done(); walk.next(), ph ^= 1u) {
-        const KvSeq& seq = t->batch.seq[walk.i];
-        const int rows = min(ROWS, seq.count * p.group - walk.rt * ROWS);
-        if (!mbar_wait(&t->q_empty, ph, &t->abort_flag)) {
-          if (lane == 0) kv_report(v, KV_TIMEOUT);
-          break;
-        }
-        const int fill = rows > 128 ? 256 : 128;     // the rest of a tile is zeros
-        const int first = (warp - 10) * 32 + lane, piece = first % PIECES;     // a thread's pieces are in one column
-        const bool column = piece * 8 < v.head_dim;
-        const uint16_t* base = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)seq.first * p.q_token_stride +
-                               (int64_t)walk.head * p.group * p.q_head_stride + (column ? piece * 8 : 0);
-#pragma unroll 4
-        for (int r = first / PIECES; r < fill; r += 64 / PIECES) {
-          const bool there = r < rows && column;
-          const int rr = walk.rt * ROWS + (there ? r : 0), tok = kv_token_of(p, rr);
-          const uint16_t* from = base + (int64_t)tok * p.q_token_stride + (int64_t)(rr - tok * p.group) * p.q_head_stride;
-          cp_async_16(q_addr + (r >> 7) * Q_TILE + (piece >> 3) * CHUNK + (r & 127) * 128 + (((piece & 7) ^ (r & 7)) << 4), from, there);
-        }
-        cp_async_wait_all();
-        fence_async_shared();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&t->q_full);
-      }
+      if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
     }
   } else {
     // ------------------------------------------------------------ softmax
@@ -369,60 +466,88 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + TMEM_O + x * 128;
     uint32_t s_ph = 0, o_ph = 0;
     bool ok = true;
-    for (; !walk.done(); walk.next()) {
+    using Walk = KvWalk<ROWS, KEYS>;
+    // Rows of this row tile in an item, if below 128; items without any are passed over.
+    auto rows_of = [&](const Walk& w) { return t->batch.seq[w.i].count * p.group - w.rt * ROWS - x * 128; };
+    auto skip = [&](Walk& w) {
+      while (!w.done() && rows_of(w) <= 0) w.next();
+    };
+    // A row that is not there goes along with the last one that is, and is not written.
+    auto row_at = [&](const Walk& w) { return w.rt * ROWS + x * 128 + min(row, rows_of(w) - 1); };
+    auto fetch_q = [&](const Walk& w) {
+      const int rr = row_at(w), tok = kv_token_of(p, rr);
+      const uint16_t* from = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(t->batch.seq[w.i].first + tok) * p.q_token_stride +
+                             (int64_t)(w.head * p.group + (rr - tok * p.group)) * p.q_head_stride;
+      const uint32_t to = smem_u32(q_smem) + x * Q_TILE + row * 128;
+#pragma unroll
+      for (int piece = 0; piece < DCH * 8; ++piece) {
+        const bool there = piece * 8 < v.head_dim;
+        cp_async_16(to + (piece >> 3) * CHUNK + (((piece & 7) ^ (row & 7)) << 4), from + (there ? piece * 8 : 0), there);
+      }
+    };
+    auto q_ready = [&]() {
+      cp_async_wait_all();
+      fence_async_shared();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&t->q_full[x]);
+    };
+    skip(walk);
+    if (!walk.done()) {
+      fetch_q(walk);
+      q_ready();
+    }
+    while (!walk.done()) {
       const KvSeq seq = t->batch.seq[walk.i];
-      const int rows = seq.count * p.group - walk.rt * ROWS - x * 128;        // of this row tile, if below 128
-      if (rows <= 0) continue;
-      const bool live = row < rows;
-      // a row that is not there goes along with the last one that is, and is not written
-      const int rr = walk.rt * ROWS + x * 128 + min(row, rows - 1), tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
+      const bool live = row < rows_of(walk);
+      const int rr = row_at(walk), tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
       const int pos = seq.length - seq.count + tok;
       const int lowest = __shfl_sync(FULL_MASK, pos, 0), highest = __shfl_sync(FULL_MASK, pos, 31);     // of the warp's rows
+      Walk after = walk;
+      after.next();
+      skip(after);
       float m = -INFINITY, l = 0.0f;
       for (int k = walk.from; k < walk.to; ++k) {
-        if (ok) ok = mbar_wait(&t->s_full[x], s_ph, &t->abort_flag);
+        if (ok) ok = mbar_warp_wait(&t->s_full[x], s_ph, &t->abort_flag);
         s_ph ^= 1u;
         __syncwarp();
         tc_fence_after_sync();
         uint32_t va[64], vb[64];
         tmem_ld_32x64(s_addr, va);
-        tmem_ld_32x64(s_addr + 64, vb);
-        tmem_ld_wait_for(va);
-        tmem_ld_wait_for(vb);
+        const bool fetch = k + 1 == walk.to && !after.done();
+        if (fetch) fetch_q(after);                   // the item's last scores are there: its query is no longer read
         const int key0 = walk.r.tile(k) * KEYS, last = key0 + KEYS - 1;
         const bool clear = last <= lowest && (!p.window || key0 > highest - p.window || last < p.sinks);
-        float scale = p.scale_log2;
-        if (!clear) {
-          // one bit per key: at or before the row's position, and in its window or a sink
-          uint32_t seen[4];
+        // Tiles with hidden keys (and negative scales, which turn the order round): scaled here, hidden keys to
+        // minus infinity.  One bit per key: at or before the row's position, and in its window or a sink.
+        const bool plain = clear && p.scale_log2 >= 0.0f;
+        const float scale = plain ? p.scale_log2 : 1.0f;
+        auto hide = [&](uint32_t (&v64)[64], int j0) {
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int j = key0 + y * 32;
-            seen[y] = bits_below(pos - j + 1);
-            if (p.window) seen[y] &= ~bits_below(pos - p.window + 1 - j) | bits_below(p.sinks - j);
+          for (int y = 0; y < 2; ++y) {
+            const int j = j0 + y * 32;
+            uint32_t seen = bits_below(pos - j + 1);
+            if (p.window) seen &= ~bits_below(pos - p.window + 1 - j) | bits_below(p.sinks - j);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              v64[y * 32 + i] = (seen >> i) & 1u ? __float_as_uint(__uint_as_float(v64[y * 32 + i]) * p.scale_log2) : 0xff800000u;
           }
+        };
+        float g[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        auto largest = [&](const uint32_t (&v64)[64]) {
 #pragma unroll
-          for (int i = 0; i < 64; ++i) {
-            va[i] = (seen[i >> 5] >> (i & 31)) & 1u ? __float_as_uint(__uint_as_float(va[i]) * scale) : 0xff800000u;
-            vb[i] = (seen[2 + (i >> 5)] >> (i & 31)) & 1u ? __float_as_uint(__uint_as_float(vb[i]) * scale) : 0xff800000u;
+          for (int i = 0; i < 64; i += 8) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) g[y] = fmax3(g[y], __uint_as_float(v64[i + 2 * y]), __uint_as_float(v64[i + 2 * y + 1]));
           }
-          scale = 1.0f;
-        }
-        float top;
-        if (scale >= 0.0f) {
-          float g[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int i = 0; i < 64; i += 4) {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) g[y] = fmax3(g[y], __uint_as_float(va[i + y]), __uint_as_float(vb[i + y]));
-          }
-          top = fmaxf(fmax3(g[0], g[1], g[2]), g[3]) * scale;
-        } else {
-          float g = INFINITY;
-#pragma unroll
-          for (int i = 0; i < 64; ++i) g = fminf(g, fminf(__uint_as_float(va[i]), __uint_as_float(vb[i])));
-          top = g * scale;
-        }
+        };
+        tmem_ld_wait_for(va);
+        tmem_ld_32x64(s_addr + 64, vb);
+        if (!plain) hide(va, key0);
+        largest(va);
+        tmem_ld_wait_for(vb);
+        if (!plain) hide(vb, key0 + 64);
+        largest(vb);
+        const float top = fmaxf(fmax3(g[0], g[1], g[2]), g[3]) * scale;
         const bool raise = top > m + RAISE || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(FULL_MASK, raise)) {
           const float now = raise ? top : m;
@@ -442,32 +567,33 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           }
         }
         const float base = m == -INFINITY ? 0.0f : m;
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const uint64_t scale2 = pair_of(scale, scale), base2 = pair_of(-base, -base);
+        uint64_t sum2[2] = {0, 0};
+        auto hand_over = [&](int half) {             // 64 keys' weights go to the tensor cores
+          tmem_st_wait();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&t->p_full[x][half]);
+        };
+        // The second half is fetched again: held in registers meanwhile, its exponentials would be scheduled ahead
+        // of the first half's hand-over (seen as that coming 900 cycles late).
         uint32_t w[32];
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float a = exp2_fast(fmaf(__uint_as_float(va[2 * i]), scale, -base)), b = exp2_fast(fmaf(__uint_as_float(va[2 * i + 1]), scale, -base));
-          sum[(2 * i) & 3] += a;
-          sum[(2 * i + 1) & 3] += b;
-          w[i] = pack2<F16>(a, b);
-        }
+        weights<F16>(va, scale2, base2, sum2, w);
         tmem_st_32x32(s_addr, w);
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float a = exp2_fast(fmaf(__uint_as_float(vb[2 * i]), scale, -base)), b = exp2_fast(fmaf(__uint_as_float(vb[2 * i + 1]), scale, -base));
-          sum[(2 * i) & 3] += a;
-          sum[(2 * i + 1) & 3] += b;
-          w[i] = pack2<F16>(a, b);
-        }
+        tmem_ld_32x64(s_addr + 64, vb);
+        hand_over(0);
+        tmem_ld_wait_for(vb);
+        if (!plain) hide(vb, key0 + 64);
+        weights<F16>(vb, scale2, base2, sum2, w);
         tmem_st_32x32(s_addr + 32, w);
-        tmem_st_wait();
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&t->p_full[x]);
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        hand_over(1);
+        float sa, sb;
+        split_pair(add_pairs(sum2[0], sum2[1]), &sa, &sb);
+        l += sa + sb;
+        if (fetch) q_ready();
       }
       // ---- the result, or a piece of it
-      if (ok) ok = mbar_wait(&t->o_full[x], o_ph, &t->abort_flag);
+      if (ok) ok = mbar_warp_wait(&t->o_full[x], o_ph, &t->abort_flag);
       o_ph ^= 1u;
       __syncwarp();
       tc_fence_after_sync();
@@ -519,8 +645,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         warpgroup_sync(x);
         if (t->last[x]) {                            // join the pieces, in the order of the CTAs
           float top = -INFINITY, total = 0.0f;
+#pragma unroll 4
           for (int c = 0; c < pieces.n; ++c) top = fmaxf(top, __ldcg(p.partials + (size_t)pieces.slot(c) * p.partial_floats + r));
           if (top == -INFINITY) top = 0.0f;
+#pragma unroll 4
           for (int c = 0; c < pieces.n; ++c) {
             const float* from = p.partials + (size_t)pieces.slot(c) * p.partial_floats + r;
             total += exp2_fast(__ldcg(from) - top) * __ldcg(from + ROWS);
@@ -556,6 +684,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           }
         }
       }
+      walk = after;
     }
     if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
   }
@@ -569,8 +698,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
 
 template <bool F16, int DCH>
 cudaError_t launch_one(const KvAttendParams& p, const CUtensorMap& tmap, int sm_count, int smem_optin, cudaStream_t st) {
-  int slots = 2;
-  while (slots < MAX_SLOTS && extend_smem(DCH, slots + 1) <= smem_optin) ++slots;
+  int slots = 2;                                     // an even number: keys take the even slots, values the odd ones
+  while (slots + 2 <= MAX_SLOTS && extend_smem(DCH, slots + 2) <= smem_optin) slots += 2;
   return launch_overlapped(kv_extend_kernel<F16, DCH>, dim3(sm_count), dim3(THREADS), extend_smem(DCH, slots), st, 1, p, tmap, slots);
 }
 

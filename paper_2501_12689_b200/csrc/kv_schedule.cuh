@@ -31,17 +31,17 @@ struct KvRange {
 
 template <int ROWS, int KEYS>
 struct KvSchedule {
-  const KvAttendParams& p;
-  const KvBatch& b;
-  __device__ KvSchedule(const KvAttendParams& p_, const KvBatch& b_) : p(p_), b(b_) {}
+  const KvAttendParams* p;
+  const KvBatch* b;
+  __device__ KvSchedule(const KvAttendParams& p_, const KvBatch& b_) : p(&p_), b(&b_) {}
 
-  __device__ __forceinline__ int row_tiles(const KvSeq& s) const { return (int)(((unsigned)s.count * (unsigned)p.group + ROWS - 1u) / ROWS); }
+  __device__ __forceinline__ int row_tiles(const KvSeq& s) const { return (int)(((unsigned)s.count * (unsigned)p->group + ROWS - 1u) / ROWS); }
 
   // Positions of the first and the last row of row tile rt.
   __device__ __forceinline__ void positions(const KvSeq& s, int rt, int* lowest, int* highest) const {
-    const unsigned r0 = (unsigned)rt * ROWS, r1 = min(r0 + ROWS, (unsigned)s.count * (unsigned)p.group) - 1u;
-    *lowest = s.length - s.count + kv_token_of(p, (int)r0);
-    *highest = s.length - s.count + kv_token_of(p, (int)r1);
+    const unsigned r0 = (unsigned)rt * ROWS, r1 = min(r0 + ROWS, (unsigned)s.count * (unsigned)p->group) - 1u;
+    *lowest = s.length - s.count + kv_token_of(*p, (int)r0);
+    *highest = s.length - s.count + kv_token_of(*p, (int)r1);
   }
 
   __device__ __forceinline__ KvRange range(const KvSeq& s, int rt) const {
@@ -49,9 +49,9 @@ struct KvSchedule {
     positions(s, rt, &lowest, &highest);
     KvRange r;
     const int end = highest < 0 ? 0 : highest / KEYS + 1;
-    r.first = (p.window && lowest >= p.window) ? (lowest - p.window + 1) / KEYS : 0;
+    r.first = (p->window && lowest >= p->window) ? (lowest - p->window + 1) / KEYS : 0;
     // the sinks' tiles, as far as they lie before the window's
-    const int sink_tiles = (int)(((unsigned)p.sinks + KEYS - 1u) / KEYS);
+    const int sink_tiles = (int)(((unsigned)p->sinks + KEYS - 1u) / KEYS);
     r.sink_tiles = min(sink_tiles, r.first);
     r.n = max(1, r.sink_tiles + end - r.first);      // a row tile that sees nothing writes zeros
     return r;
@@ -193,14 +193,14 @@ struct KvWalk {
   __device__ __forceinline__ void next() {
     left -= to - from;
     if (left == 0) return;
-    if (++rt >= sched.row_tiles(sched.b.seq[i])) {
+    if (++rt >= sched.row_tiles(sched.b->seq[i])) {
       rt = 0;
-      if (++head >= sched.p.v.n_kv_heads) {
+      if (++head >= sched.p->v.n_kv_heads) {
         head = 0;
-        do ++i; while (sched.b.seq[i].count == 0);
+        do ++i; while (sched.b->seq[i].count == 0);
       }
     }
-    r = sched.range(sched.b.seq[i], rt);
+    r = sched.range(sched.b->seq[i], rt);
     from = 0;
     to = min(r.n, left);
   }
