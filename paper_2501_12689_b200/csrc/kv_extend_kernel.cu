@@ -47,6 +47,7 @@ struct ExtendTail {
   uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2], drain[2];       // per row tile; p_full: keys 0-63 and 64-127
   uint32_t tmem_base;
   int abort_flag, last[2];
+  alignas(16) unsigned char turn_rows[SOFTMAX_WARPS][32 * 80];
   KvBatch batch;
 };
 
@@ -57,6 +58,7 @@ int extend_smem(int dch, int slots) { return 1024 + ROWS * dch * 128 + slots * s
 __host__ __device__ constexpr uint32_t idesc(bool f16, int n, bool b_mn_major) {
   return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | (b_mn_major ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | ((128u >> 4) << 24);
 }
+constexpr uint32_t NEGATE_A = 1u << 13;
 // Operand whose rows (keys) are the summed dimension: 64-element chunks of the other one `chunk` bytes apart, groups of
 // eight rows 1024 bytes apart, 128-byte swizzle.
 __device__ __forceinline__ uint64_t desc_mn_major_sw128(uint32_t smem_addr, uint32_t chunk) {
@@ -183,6 +185,25 @@ __device__ __forceinline__ void weights(const uint32_t (&s)[64], uint64_t scale2
     sum2[i & 1] = add_pairs(sum2[i & 1], pair_of(a, b));
     w[i] = pack2<F16>(a, b);
   }
+}
+
+// 32 columns of a warp's 32 rows to the result: each thread has its row's four 16-byte pieces; turned round in shared
+// memory (rows 80 bytes apart: no bank conflicts) so that four lanes write a row's 64 bytes side by side, a quarter
+// of the lines per store.  `mine`: where this thread's row of the result begins, 0 = not to be written.
+constexpr int TURN_PITCH = 80;
+__device__ __forceinline__ void store_rows(unsigned char* turn, const uint4 (&w)[4], unsigned long long mine, int column, int head_dim, int lane) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(turn + lane * TURN_PITCH + i * 16) = w[i];
+  __syncwarp();
+  const int piece = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = i * 8 + (lane >> 2);
+    const unsigned long long to = __shfl_sync(FULL_MASK, mine, r);
+    const uint4 y = *reinterpret_cast<const uint4*>(turn + r * TURN_PITCH + piece * 16);
+    if (to && column + piece * 8 < head_dim) *reinterpret_cast<uint4*>(to + (column + piece * 8) * 2) = y;
+  }
+  __syncwarp();
 }
 
 // Keys that no token of the call sees: between the sinks and the first token's window, and past the end (slots of
@@ -325,7 +346,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     } else if (warp <= 10) {
       // ---------------------------------------------------------- products
       {
-        constexpr uint32_t id_s = idesc(F16, KEYS, false), id_o = idesc(F16, DIM, true);
+        // (a negative scale: the product with -Q, and the scale's magnitude)
+        const uint32_t id_s = idesc(F16, KEYS, false) | (p.scale_log2 < 0.0f ? NEGATE_A : 0u);
+        constexpr uint32_t id_o = idesc(F16, DIM, true);
         const int x = warp - 9;                      // row tile
         const uint32_t on = lane == 0;
         const uint32_t s_at = tmem + x * 128, o_at = tmem + TMEM_O + x * 128;
@@ -462,8 +485,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     // ------------------------------------------------------------ softmax
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     const int x = warp >> 2, row = tid & 127;        // row tile, and row (tensor-memory lane) of this thread
+    unsigned char* turn_smem = t->turn_rows[warp];
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + TMEM_O + x * 128;
+    // A scale of zero must not make NaN of the minus infinity that stands for a hidden key.
+    const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);
     uint32_t s_ph = 0, o_ph = 0;
     bool ok = true;
     using Walk = KvWalk<ROWS, KEYS>;
@@ -474,15 +500,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     };
     // A row that is not there goes along with the last one that is, and is not written.
     auto row_at = [&](const Walk& w) { return w.rt * ROWS + x * 128 + min(row, rows_of(w) - 1); };
-    auto fetch_q = [&](const Walk& w) {
+    auto fetch_q = [&](const Walk& w) {              // a warp's 32 rows, LANES lanes along a row
+      constexpr int LANES = DCH * 8, AT_ONCE = 32 / LANES;
       const int rr = row_at(w), tok = kv_token_of(p, rr);
-      const uint16_t* from = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(t->batch.seq[w.i].first + tok) * p.q_token_stride +
+      const uint16_t* mine = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(t->batch.seq[w.i].first + tok) * p.q_token_stride +
                              (int64_t)(w.head * p.group + (rr - tok * p.group)) * p.q_head_stride;
-      const uint32_t to = smem_u32(q_smem) + x * Q_TILE + row * 128;
-#pragma unroll
-      for (int piece = 0; piece < DCH * 8; ++piece) {
-        const bool there = piece * 8 < v.head_dim;
-        cp_async_16(to + (piece >> 3) * CHUNK + (((piece & 7) ^ (row & 7)) << 4), from + (there ? piece * 8 : 0), there);
+      const int piece = lane % LANES, sub = lane / LANES;
+      const bool there = piece * 8 < v.head_dim;
+      const uint32_t to = smem_u32(q_smem) + x * Q_TILE + (piece >> 3) * CHUNK;
+#pragma unroll 4
+      for (int i = 0; i < 32; i += AT_ONCE) {
+        const uint16_t* from = reinterpret_cast<const uint16_t*>(__shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(mine), i + sub));
+        const int r = (warp & 3) * 32 + i + sub;
+        cp_async_16(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + (there ? piece * 8 : 0), there);
       }
     };
     auto q_ready = [&]() {
@@ -517,10 +547,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         if (fetch) fetch_q(after);                   // the item's last scores are there: its query is no longer read
         const int key0 = walk.r.tile(k) * KEYS, last = key0 + KEYS - 1;
         const bool clear = last <= lowest && (!p.window || key0 > highest - p.window || last < p.sinks);
-        // Tiles with hidden keys (and negative scales, which turn the order round): scaled here, hidden keys to
-        // minus infinity.  One bit per key: at or before the row's position, and in its window or a sink.
-        const bool plain = clear && p.scale_log2 >= 0.0f;
-        const float scale = plain ? p.scale_log2 : 1.0f;
+        // Tiles with hidden keys: those become minus infinity.  One bit per key: at or before the row's position, and
+        // in its window or a sink.
         auto hide = [&](uint32_t (&v64)[64], int j0) {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
@@ -529,7 +557,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
             if (p.window) seen &= ~bits_below(pos - p.window + 1 - j) | bits_below(p.sinks - j);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              v64[y * 32 + i] = (seen >> i) & 1u ? __float_as_uint(__uint_as_float(v64[y * 32 + i]) * p.scale_log2) : 0xff800000u;
+              if (!(seen & (1u << i))) v64[y * 32 + i] = 0xff800000u;
           }
         };
         float g[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -542,10 +570,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         };
         tmem_ld_wait_for(va);
         tmem_ld_32x64(s_addr + 64, vb);
-        if (!plain) hide(va, key0);
+        if (!clear) hide(va, key0);
         largest(va);
         tmem_ld_wait_for(vb);
-        if (!plain) hide(vb, key0 + 64);
+        if (!clear) hide(vb, key0 + 64);
         largest(vb);
         const float top = fmaxf(fmax3(g[0], g[1], g[2]), g[3]) * scale;
         const bool raise = top > m + RAISE || (m == -INFINITY && top > -INFINITY);
@@ -583,7 +611,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         tmem_ld_32x64(s_addr + 64, vb);
         hand_over(0);
         tmem_ld_wait_for(vb);
-        if (!plain) hide(vb, key0 + 64);
+        if (!clear) hide(vb, key0 + 64);
         weights<F16>(vb, scale2, base2, sum2, w);
         tmem_st_32x32(s_addr + 32, w);
         hand_over(1);
@@ -600,20 +628,21 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       uint16_t* to = reinterpret_cast<uint16_t*>(p.out) + (int64_t)(seq.first + tok) * p.out_token_stride + (int64_t)hq * p.out_head_stride;
       if (walk.whole()) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const unsigned long long mine = live ? reinterpret_cast<unsigned long long>(to) : 0ull;
 #pragma unroll 1
         for (int c = 0; c < DIM; c += 32) {
           uint32_t o[32];
           tmem_ld_32x32(o_addr + c, o);
           tmem_ld_wait_for32(o);
+          uint4 w[4];
 #pragma unroll
-          for (int i = 0; i < 32; i += 8) {
-            uint4 w;
-            w.x = pack2<F16>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-            w.y = pack2<F16>(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-            w.z = pack2<F16>(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-            w.w = pack2<F16>(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-            if (live && c + i < v.head_dim) *reinterpret_cast<uint4*>(to + c + i) = w;
+          for (int i = 0; i < 4; ++i) {
+            w[i].x = pack2<F16>(__uint_as_float(o[8 * i]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
+            w[i].y = pack2<F16>(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
+            w[i].z = pack2<F16>(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
+            w[i].w = pack2<F16>(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
           }
+          store_rows(turn_smem, w, mine, c, v.head_dim, lane);
         }
         tc_fence_before_sync();
       } else {
@@ -672,15 +701,15 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
                 acc[i].w += w * y.w;
               }
             }
+            uint4 w[4];
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              uint4 w;
-              w.x = pack2<F16>(acc[i].x, acc[i].y);
-              w.y = pack2<F16>(acc[i].z, acc[i].w);
-              w.z = pack2<F16>(acc[i + 1].x, acc[i + 1].y);
-              w.w = pack2<F16>(acc[i + 1].z, acc[i + 1].w);
-              if (live && c32 + i * 4 < v.head_dim) *reinterpret_cast<uint4*>(to + c32 + i * 4) = w;
+            for (int i = 0; i < 4; ++i) {
+              w[i].x = pack2<F16>(acc[2 * i].x, acc[2 * i].y);
+              w[i].y = pack2<F16>(acc[2 * i].z, acc[2 * i].w);
+              w[i].z = pack2<F16>(acc[2 * i + 1].x, acc[2 * i + 1].y);
+              w[i].w = pack2<F16>(acc[2 * i + 1].z, acc[2 * i + 1].w);
             }
+            store_rows(turn_smem, w, live ? reinterpret_cast<unsigned long long>(to) : 0ull, c32, v.head_dim, lane);
           }
         }
       }
