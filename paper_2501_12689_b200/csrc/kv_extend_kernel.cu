@@ -1,27 +1,24 @@
 // Attention over the paged cache for many query rows: prompts, on the tensor cores (tcgen05), head_dim <= 128.
 //
-// An item is 256 rows of one sequence and kv head (tokens times query heads of the kv head), two tiles A and
-// B of 128 that share every key and value fetched.  Per 128-key tile and row tile there are two products,
-// S = Q K^T and O += P V, of 128 x 128 x head_dim each, with S, P and O in tensor memory (512 columns: S_A, S_B,
-// O_A, O_B; P, 16 bit, takes the first 64 columns of its S).  The same work needs 128 x 128 exponentials, for
-// which the special-function units take as long as the tensor cores do for the products (2,048 cycles
-// each for both row tiles); neither may wait for the other.  Hence the two row tiles: while one's scores are turned
-// into weights, the tensor cores work for the other one.
+// An item is 256 rows of one sequence and kv head (tokens times query heads of the kv head), two row tiles A and
+// B of 128 that share every key and value fetched.  Per 64 keys (a unit) and row tile there are two products,
+// S = Q K^T and O += P V, with S, P and O in tensor memory (512 columns: two units' S of A and of B, O_A, O_B; a
+// unit's P, 16 bit, takes the first half of its S).  The same work needs 128 x 64 exponentials, for which the
+// special-function units take as long as the tensor cores do for the products, so neither may wait for the
+// other: two row tiles in flight, and of each the scores of the next unit while the present one's become
+// weights.  (Units of 128 keys fit only once per row tile; then a row tile's chain softmax - PV - S is exposed:
+// 4,300 cycles for both row tiles and 128 keys, of which the tensor cores work 2,048.)  The price is that
+// S with 64 columns is bound by shared memory: 48 cycles a product where the tensor cores need 32.
 //
 //   warps 0-3, 4-7   softmax of row tile A, B: a thread owns a row (a tensor-memory lane), and copies the row's
 //                    query into the swizzled layout of the left operand, an item ahead
-//   warp 8           loads of keys and values: one tensor-map box per page (or 64 rows) and 64-element chunk
-//   warps 9, 10      issue the products of row tile A, B: PV(j), S(j+1), ..., so that neither waits in the other's
-//                    queue.  They take turns with the products that the softmax waits for: left alone both
-//                    row tiles fall into step, and then compete for the tensor cores and for the
-//                    special-function units at the same times
+//   warp 8           loads of keys and values, 128 of each a slot: one tensor-map box per page (or 64 rows) and
+//                    64-element chunk
+//   warps 9, 10      issue the products of row tile A, B: PV(u), S(u + 2), ...
 //   warp 11          zeros in place of values that nobody sees
 //
-// The chain softmax - PV - S of one row tile is what a tile takes when all goes well, so it is kept short: weights
-// go to the tensor cores in two halves of 64 keys.
-//
 // A row's maximum is only raised when it is exceeded by more than 2^8: O is rescaled a few times per item and not
-// per tile, and weights of up to 256 are as exact as those up to 1.  Weights are rounded to the cache's
+// per unit, and weights of up to 256 are as exact as those up to 1.  Weights are rounded to the cache's
 // 16-bit type (the tensor cores take both operands in one type); their sum is taken before the rounding.
 #include "kernels.h"
 #include "kv_mma.cuh"
@@ -32,7 +29,7 @@ namespace icc {
 
 namespace {
 
-constexpr int KEYS = 128;                // keys per tile
+constexpr int KEYS = 128;                // keys per tile (a slot of the ring), two units of 64
 constexpr int ROWS = 256;                // rows per item
 constexpr int SOFTMAX_WARPS = 8;
 constexpr int THREADS = 384;
@@ -43,8 +40,8 @@ constexpr float RAISE = 8.0f;            // how far (log2) a row's scores may ex
 constexpr int AHEAD = 3;                 // batches of page numbers under way
 
 struct ExtendTail {
-  uint64_t full[MAX_SLOTS], empty[MAX_SLOTS], clean[MAX_SLOTS], turn[2];
-  uint64_t q_full[2], s_full[2], p_full[2][2], o_full[2], drain[2];       // per row tile; p_full: keys 0-63 and 64-127
+  uint64_t full[MAX_SLOTS], empty[MAX_SLOTS], clean[MAX_SLOTS];
+  uint64_t q_full[2], s_full[2][2], p_full[2][2], o_last[2], o_full[2], drain[2];     // per row tile (and unit of a tile)
   uint32_t tmem_base;
   int abort_flag, last[2];
   alignas(16) unsigned char turn_rows[SOFTMAX_WARPS][32 * 80];
@@ -225,7 +222,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
   constexpr int CHUNK = KEYS * 128;                  // bytes of a 64-element column chunk of 128 rows
   constexpr int SLOT = slot_bytes(DCH);
   constexpr int Q_TILE = DCH * CHUNK;                // bytes of a row tile of the query
-  constexpr uint32_t TMEM_O = 256;                   // first column of O_A; S_A at 0, S_B at 128, O_B at 256 + 128
+  constexpr uint32_t TMEM_O = 256;                   // first column of O_A; S of A's units at 0 and 64, of B's at 128 and 192, O_B at 256 + 128
   extern __shared__ unsigned char smem_raw[];
   unsigned char* q_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char* ring = q_smem + 2 * Q_TILE;
@@ -240,12 +237,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     }
     for (int x = 0; x < 2; ++x) {
       mbar_init(&t->q_full[x], 4);
-      mbar_init(&t->s_full[x], 1);
-      mbar_init(&t->p_full[x][0], 4);
-      mbar_init(&t->p_full[x][1], 4);
+      for (int h = 0; h < 2; ++h) {
+        mbar_init(&t->s_full[x][h], 1);
+        mbar_init(&t->p_full[x][h], 4);
+      }
+      mbar_init(&t->o_last[x], 1);
       mbar_init(&t->o_full[x], 1);
       mbar_init(&t->drain[x], 1);
-      mbar_init(&t->turn[x], 1);
     }
     t->abort_flag = 0;
     mbar_fence_init();
@@ -347,7 +345,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       // ---------------------------------------------------------- products
       {
         // (a negative scale: the product with -Q, and the scale's magnitude)
-        const uint32_t id_s = idesc(F16, KEYS, false) | (p.scale_log2 < 0.0f ? NEGATE_A : 0u);
+        const uint32_t id_s = idesc(F16, KEYS / 2, false) | (p.scale_log2 < 0.0f ? NEGATE_A : 0u);
         constexpr uint32_t id_o = idesc(F16, DIM, true);
         const int x = warp - 9;                      // row tile
         const uint32_t on = lane == 0;
@@ -355,7 +353,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         const uint64_t q_desc = umma_desc_k_major_sw128(smem_u32(q_smem) + x * Q_TILE), k_desc = umma_desc_k_major_sw128(smem_u32(ring)),
                        v_desc = desc_mn_major_sw128(smem_u32(ring), CHUNK);
         int s = 0;                                   // next slot of the ring
-        uint32_t ph = 0, q_ph = 0, p_ph = 0, clean_ph = 0, turn_ph = x ^ 1;
+        uint32_t ph = 0, q_ph = 0, p_ph = 0, clean_ph = 0;
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_warp_wait(bar, parity, &t->abort_flag); };
         auto advance = [&]() {
@@ -364,22 +362,21 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
             ph ^= 1u;
           }
         };
-        auto scores = [&](int slot) {                // S = Q K^T
-          const uint64_t db = k_desc + slot * (SLOT >> 4);
+        auto scores = [&](int slot, int half) {      // S = Q K^T, 64 of the keys
+          const uint64_t db = k_desc + (slot * (SLOT >> 4) + half * (64 * 128 >> 4));
 #pragma unroll
           for (int c = 0; c < DCH; ++c)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              product_smem(s_at, q_desc + (c * (CHUNK >> 4) + kk * 2), db + (c * (CHUNK >> 4) + kk * 2), id_s, (c | kk) != 0 ? 1u : 0u, on);
-          commit_products(&t->s_full[x], on);
+              product_smem(s_at + half * 64, q_desc + (c * (CHUNK >> 4) + kk * 2), db + (c * (CHUNK >> 4) + kk * 2), id_s,
+                           (c | kk) != 0 ? 1u : 0u, on);
+          commit_products(&t->s_full[x][half], on);
         };
         auto values = [&](int slot, int half, bool add) {        // O (+)= P V, 64 of the keys
-          const uint64_t db = v_desc + slot * (SLOT >> 4);
+          const uint64_t db = v_desc + (slot * (SLOT >> 4) + half * (64 * 128 >> 4));
 #pragma unroll
-          for (int i = 0; i < KEYS / 32; ++i) {      // 16 keys further: 8 columns of P, 2048 bytes of V
-            const int kk = half * (KEYS / 32) + i;
-            product_tmem(o_at, s_at + kk * 8, db + kk * 128, id_o, (add || kk != 0) ? 1u : 0u, on);
-          }
+          for (int kk = 0; kk < 4; ++kk)             // 16 keys further: 8 columns of P, 2048 bytes of V
+            product_tmem(o_at, s_at + half * 64 + kk * 8, db + kk * 128, id_o, (add || kk != 0) ? 1u : 0u, on);
         };
         // A slot is free when both row tiles are done with it; one that has no rows in the item says so at once.
         auto done_with = [&](int slot, bool mine) {
@@ -389,14 +386,17 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         for (; !walk.done() && ok; walk.next()) {
           const KvSeq& seq = t->batch.seq[walk.i];
           const int rows = seq.count * p.group - walk.rt * ROWS, n = walk.to - walk.from;
-          const bool mine = rows > x * 128, two = rows > 128;
+          const bool mine = rows > x * 128;
           const Hidden hidden(p, seq);
           ok = wait(&t->full[s], ph);
           if (mine && ok) {
             ok = wait(&t->q_full[x], q_ph);
             q_ph ^= 1u;
             tc_fence_after_sync();
-            if (ok) scores(s);
+            if (ok) {
+              scores(s, 0);
+              scores(s, 1);
+            }
           }
           if (!ok) break;
           done_with(s, mine);
@@ -417,22 +417,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
               if (!ok) break;
               tc_fence_after_sync();
               values(sv, 0, j > 0);
+              if (!more) commit_products(&t->o_last[x], on);
             }
             if (more) ok = wait(&t->full[s], ph);
             if (mine && ok) {
+              if (more) scores(s, 0);
               ok = wait(&t->p_full[x][1], p_ph);
               p_ph ^= 1u;
-              if (ok && two) {
-                ok = wait(&t->turn[x], turn_ph);
-                turn_ph ^= 1u;
-              }
               if (!ok) break;
               tc_fence_after_sync();
               values(sv, 1, true);
               done_with(sv, true);
-              if (more) scores(s);
+              if (more) scores(s, 1);
               else commit_products(&t->o_full[x], on);
-              if (two) arrive_one(&t->turn[x ^ 1], on);
             }
             if (!ok) break;
             if (!mine) done_with(sv, false);
@@ -536,45 +533,39 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       after.next();
       skip(after);
       float m = -INFINITY, l = 0.0f;
-      for (int k = walk.from; k < walk.to; ++k) {
-        if (ok) ok = mbar_warp_wait(&t->s_full[x], s_ph, &t->abort_flag);
-        s_ph ^= 1u;
+      const int units = 2 * (walk.to - walk.from);
+      bool last_seen = false;
+      for (int u = 0; u < units; ++u) {
+        const int half = u & 1;
+        if (ok) ok = mbar_warp_wait(&t->s_full[x][half], s_ph, &t->abort_flag);
         __syncwarp();
         tc_fence_after_sync();
-        uint32_t va[64], vb[64];
-        tmem_ld_32x64(s_addr, va);
-        const bool fetch = k + 1 == walk.to && !after.done();
+        uint32_t va[64];
+        tmem_ld_32x64(s_addr + half * 64, va);
+        const bool fetch = u + 1 == units && !after.done();
         if (fetch) fetch_q(after);                   // the item's last scores are there: its query is no longer read
-        const int key0 = walk.r.tile(k) * KEYS, last = key0 + KEYS - 1;
+        const int key0 = walk.r.tile(walk.from + (u >> 1)) * KEYS + half * 64, last = key0 + 63;
         const bool clear = last <= lowest && (!p.window || key0 > highest - p.window || last < p.sinks);
-        // Tiles with hidden keys: those become minus infinity.  One bit per key: at or before the row's position, and
-        // in its window or a sink.
-        auto hide = [&](uint32_t (&v64)[64], int j0) {
+        tmem_ld_wait_for(va);
+        if (!clear) {
+          // Hidden keys become minus infinity.  One bit per key: at or before the row's position, and in its window
+          // or a sink.
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const int j = j0 + y * 32;
+            const int j = key0 + y * 32;
             uint32_t seen = bits_below(pos - j + 1);
             if (p.window) seen &= ~bits_below(pos - p.window + 1 - j) | bits_below(p.sinks - j);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (!(seen & (1u << i))) v64[y * 32 + i] = 0xff800000u;
+              if (!(seen & (1u << i))) va[y * 32 + i] = 0xff800000u;
           }
-        };
+        }
         float g[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        auto largest = [&](const uint32_t (&v64)[64]) {
 #pragma unroll
-          for (int i = 0; i < 64; i += 8) {
+        for (int i = 0; i < 64; i += 8) {
 #pragma unroll
-            for (int y = 0; y < 4; ++y) g[y] = fmax3(g[y], __uint_as_float(v64[i + 2 * y]), __uint_as_float(v64[i + 2 * y + 1]));
-          }
-        };
-        tmem_ld_wait_for(va);
-        tmem_ld_32x64(s_addr + 64, vb);
-        if (!clear) hide(va, key0);
-        largest(va);
-        tmem_ld_wait_for(vb);
-        if (!clear) hide(vb, key0 + 64);
-        largest(vb);
+          for (int y = 0; y < 4; ++y) g[y] = fmax3(g[y], __uint_as_float(va[i + 2 * y]), __uint_as_float(va[i + 2 * y + 1]));
+        }
         const float top = fmaxf(fmax3(g[0], g[1], g[2]), g[3]) * scale;
         const bool raise = top > m + RAISE || (m == -INFINITY && top > -INFINITY);
         if (__any_sync(FULL_MASK, raise)) {
@@ -582,7 +573,18 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           const float shrink = raise ? (m == -INFINITY ? 0.0f : exp2_fast(m - now)) : 1.0f;
           m = now;
           l *= shrink;
-          if (k > walk.from) {                       // S(k) is complete, and with it everything issued before it: PV(k - 1) too
+          if (u > 0) {
+            // All products into O so far have to be complete: those before the scores of unit u + 1 are when these
+            // are there; for the last unit there is a barrier of its own.
+            if (ok) {
+              if (u + 1 < units) {
+                ok = mbar_warp_wait(&t->s_full[x][half ^ 1], s_ph ^ (uint32_t)half, &t->abort_flag);
+              } else {
+                ok = mbar_warp_wait(&t->o_last[x], o_ph, &t->abort_flag);
+                last_seen = true;
+              }
+            }
+            tc_fence_after_sync();
 #pragma unroll 1
             for (int c = 0; c < DIM; c += 32) {
               uint32_t o[32];
@@ -597,29 +599,20 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         const float base = m == -INFINITY ? 0.0f : m;
         const uint64_t scale2 = pair_of(scale, scale), base2 = pair_of(-base, -base);
         uint64_t sum2[2] = {0, 0};
-        auto hand_over = [&](int half) {             // 64 keys' weights go to the tensor cores
-          tmem_st_wait();
-          tc_fence_before_sync();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&t->p_full[x][half]);
-        };
-        // The second half is fetched again: held in registers meanwhile, its exponentials would be scheduled ahead
-        // of the first half's hand-over (seen as that coming 900 cycles late).
         uint32_t w[32];
         weights<F16>(va, scale2, base2, sum2, w);
-        tmem_st_32x32(s_addr, w);
-        tmem_ld_32x64(s_addr + 64, vb);
-        hand_over(0);
-        tmem_ld_wait_for(vb);
-        if (!clear) hide(vb, key0 + 64);
-        weights<F16>(vb, scale2, base2, sum2, w);
-        tmem_st_32x32(s_addr + 32, w);
-        hand_over(1);
+        tmem_st_32x32(s_addr + half * 64, w);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&t->p_full[x][half]);
         float sa, sb;
         split_pair(add_pairs(sum2[0], sum2[1]), &sa, &sb);
         l += sa + sb;
         if (fetch) q_ready();
+        s_ph ^= (uint32_t)half;                      // both halves' barriers turn once per tile
       }
+      if (!last_seen && ok) ok = mbar_warp_wait(&t->o_last[x], o_ph, &t->abort_flag);      // (keeps count of its rounds)
       // ---- the result, or a piece of it
       if (ok) ok = mbar_warp_wait(&t->o_full[x], o_ph, &t->abort_flag);
       o_ph ^= 1u;
