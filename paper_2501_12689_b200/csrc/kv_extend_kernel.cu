@@ -44,6 +44,7 @@ struct ExtendTail {
   uint64_t q_full[2], s_full[2][2], p_full[2][2], o_last[2], o_full[2], drain[2];     // per row tile (and unit of a tile)
   uint32_t tmem_base;
   int abort_flag, last[2];
+  float zero;
   alignas(16) unsigned char turn_rows[SOFTMAX_WARPS][32 * 80];
   KvBatch batch;
 };
@@ -139,7 +140,9 @@ __device__ __forceinline__ void cp_async_16(uint32_t smem_dst, const void* src, 
   const int bytes = there ? 16 : 0;      // the rest is filled with zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 // A wait of a whole warp.  All lanes ask together: a lane that waits by itself, inside a branch, wakes up to 200 cycles
 // later (measured: 54 against 70 to 240 cycles from the arrival).
 __device__ __forceinline__ bool mbar_warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
@@ -147,6 +150,9 @@ __device__ __forceinline__ bool mbar_warp_wait(uint64_t* bar, uint32_t parity, v
 }
 // The lowest n bits, n <= 0: none, n >= 32: all.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); }
+// Turns between warp w of row tile A and warp w + 4 of B: barriers 3 .. 6 call A's warp, 7 .. 10 B's.
+__device__ __forceinline__ void pair_wait(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(3 + warp) : "memory"); }
+__device__ __forceinline__ void pair_pass(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(3 + (warp ^ 4)) : "memory"); }
 __device__ __forceinline__ void warpgroup_sync(int which) {
   if (which == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
   else asm volatile("bar.sync 2, 128;" ::: "memory");
@@ -236,7 +242,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       mbar_init(&t->clean[s], 1);
     }
     for (int x = 0; x < 2; ++x) {
-      mbar_init(&t->q_full[x], 4);
+      mbar_init(&t->q_full[x], 128);
       for (int h = 0; h < 2; ++h) {
         mbar_init(&t->s_full[x][h], 1);
         mbar_init(&t->p_full[x][h], 4);
@@ -246,6 +252,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       mbar_init(&t->drain[x], 1);
     }
     t->abort_flag = 0;
+    t->zero = 0.0f;
     mbar_fence_init();
     prefetch_tmap(&tmap);
   }
@@ -392,6 +399,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           if (mine && ok) {
             ok = wait(&t->q_full[x], q_ph);
             q_ph ^= 1u;
+            fence_async_shared();                    // the query's copies were ordinary writes
             tc_fence_after_sync();
             if (ok) {
               scores(s, 0);
@@ -511,18 +519,10 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         const int r = (warp & 3) * 32 + i + sub;
         cp_async_16(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + (there ? piece * 8 : 0), there);
       }
-    };
-    auto q_ready = [&]() {
-      cp_async_wait_all();
-      fence_async_shared();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&t->q_full[x]);
+      cp_async_arrive(&t->q_full[x]);                // when this thread's copies have landed
     };
     skip(walk);
-    if (!walk.done()) {
-      fetch_q(walk);
-      q_ready();
-    }
+    if (!walk.done()) fetch_q(walk);
     while (!walk.done()) {
       const KvSeq seq = t->batch.seq[walk.i];
       const bool live = row < rows_of(walk);
@@ -534,6 +534,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       skip(after);
       float m = -INFINITY, l = 0.0f;
       const int units = 2 * (walk.to - walk.from);
+      // The two row tiles' warps on one scheduler take turns with their exponentials: at the same time they would
+      // both have them, and then both load scores and look for maxima while the special-function unit has
+      // nothing to do.  A begins; what B passes on after its last unit of an item would be one too many.
+      const bool paired = seq.count * p.group - walk.rt * ROWS > 128;
+      if (paired && x == 1) pair_pass(warp);
       bool last_seen = false;
       for (int u = 0; u < units; ++u) {
         const int half = u & 1;
@@ -596,12 +601,19 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
             }
           }
         }
-        const float base = m == -INFINITY ? 0.0f : m;
+        float base = m == -INFINITY ? 0.0f : m;
+        if (paired) {
+          // (the zero that is read behind the barrier keeps the exponentials behind it too: nothing else would; on
+          // the other side the store of the weights does)
+          pair_wait(warp);
+          base -= *reinterpret_cast<volatile float*>(&t->zero);
+        }
         const uint64_t scale2 = pair_of(scale, scale), base2 = pair_of(-base, -base);
         uint64_t sum2[2] = {0, 0};
         uint32_t w[32];
         weights<F16>(va, scale2, base2, sum2, w);
         tmem_st_32x32(s_addr + half * 64, w);
+        if (paired && (x == 0 || u + 1 < units)) pair_pass(warp);
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
@@ -609,7 +621,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         float sa, sb;
         split_pair(add_pairs(sum2[0], sum2[1]), &sa, &sb);
         l += sa + sb;
-        if (fetch) q_ready();
         s_ph ^= (uint32_t)half;                      // both halves' barriers turn once per tile
       }
       if (!last_seen && ok) ok = mbar_warp_wait(&t->o_last[x], o_ph, &t->abort_flag);      // (keeps count of its rounds)
