@@ -15,7 +15,7 @@
 //   warp 8           loads of keys and values, 128 of each a slot: one tensor-map box per page (or 64 rows) and
 //                    64-element chunk
 //   warps 9, 10      issue the products of row tile A, B: PV(u), S(u + 2), ...
-//   warp 11          zeros in place of values that nobody sees
+//   warp 11          zeros in place of values that nobody sees; tells the softmax warps what the next items are
 //
 // A row's maximum is only raised when it is exceeded by more than 2^8: O is rescaled a few times per item and not
 // per unit, and weights of up to 256 are as exact as those up to 1.  Weights are rounded to the cache's
@@ -39,13 +39,28 @@ constexpr int OTHER_REGS = 72, SOFTMAX_REGS = 216;
 constexpr float RAISE = 8.0f;            // how far (log2) a row's scores may exceed its maximum before O is rescaled
 constexpr int AHEAD = 3;                 // batches of page numbers under way
 
+// What the softmax warps need to know of an item: worked out by warp 11, ITEMS ahead at most.
+constexpr int ITEMS = 8;
+struct alignas(16) Item {
+  int more;                              // 0: there are no more
+  int rows;                              // query rows from the item's first one to the sequence's last
+  int row0, first_pos;                   // first row; position of the call's first token of the sequence
+  int q_first, head0;                    // that token's row of q; first query head
+  int from, to, sink_tiles, first_tile;  // key tiles, as in KvWalk and KvRange
+  int whole, my_slot;                    // 0: a piece of an item, and where the partial result goes
+  int piece_first, pieces, piece_slot;   // which CTAs have the others (KvWalk::Pieces)
+  int unused;
+};
+
 struct ExtendTail {
+  Item item[ITEMS];
+  uint64_t item_full[ITEMS], item_empty[ITEMS];
+  uint64_t group_sync[2];                // the four warps of a row tile (with a limit, as all waits here)
   uint64_t full[MAX_SLOTS], empty[MAX_SLOTS], clean[MAX_SLOTS];
   uint64_t q_full[2], s_full[2][2], p_full[2][2], o_last[2], o_full[2], drain[2];     // per row tile (and unit of a tile)
   uint32_t tmem_base;
-  int abort_flag, last[2];
+  int abort_flag, last[2], left[SOFTMAX_WARPS];
   float zero;
-  alignas(16) unsigned char turn_rows[SOFTMAX_WARPS][32 * 80];
   KvBatch batch;
 };
 
@@ -150,13 +165,10 @@ __device__ __forceinline__ bool mbar_warp_wait(uint64_t* bar, uint32_t parity, v
 }
 // The lowest n bits, n <= 0: none, n >= 32: all.
 __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n >= 32 ? ~0u : (1u << n) - 1u); }
-// Turns between warp w of row tile A and warp w + 4 of B: barriers 3 .. 6 call A's warp, 7 .. 10 B's.
-__device__ __forceinline__ void pair_wait(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(3 + warp) : "memory"); }
-__device__ __forceinline__ void pair_pass(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(3 + (warp ^ 4)) : "memory"); }
-__device__ __forceinline__ void warpgroup_sync(int which) {
-  if (which == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
-  else asm volatile("bar.sync 2, 128;" ::: "memory");
-}
+// Turns between warp w of row tile A and warp w + 4 of B, on the hardware's barriers (110 cycles a turn quicker than a
+// barrier in shared memory): 3 .. 6 call A's warp, 7 .. 10 B's.
+__device__ __forceinline__ void turn_wait(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(3 + warp) : "memory"); }
+__device__ __forceinline__ void turn_pass(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(3 + (warp ^ 4)) : "memory"); }
 
 // ---------------------------------------------------------------- pairs of floats in one instruction
 __device__ __forceinline__ uint64_t pair_of(float a, float b) {
@@ -190,23 +202,19 @@ __device__ __forceinline__ void weights(const uint32_t (&s)[64], uint64_t scale2
   }
 }
 
-// 32 columns of a warp's 32 rows to the result: each thread has its row's four 16-byte pieces; turned round in shared
-// memory (rows 80 bytes apart: no bank conflicts) so that four lanes write a row's 64 bytes side by side, a quarter
-// of the lines per store.  `mine`: where this thread's row of the result begins, 0 = not to be written.
-constexpr int TURN_PITCH = 80;
-__device__ __forceinline__ void store_rows(unsigned char* turn, const uint4 (&w)[4], unsigned long long mine, int column, int head_dim, int lane) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(turn + lane * TURN_PITCH + i * 16) = w[i];
-  __syncwarp();
-  const int piece = lane & 3;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = i * 8 + (lane >> 2);
-    const unsigned long long to = __shfl_sync(FULL_MASK, mine, r);
-    const uint4 y = *reinterpret_cast<const uint4*>(turn + r * TURN_PITCH + piece * 16);
-    if (to && column + piece * 8 < head_dim) *reinterpret_cast<uint4*>(to + (column + piece * 8) * 2) = y;
+// 16 columns of a thread's row to the result: 32 bytes at a time where the address allows (a whole sector per lane; halves
+// of sectors from different instructions cost as many passes as whole ones).
+template <bool F16>
+__device__ __forceinline__ void store_row(uint16_t* to, int column, int head_dim, const uint32_t (&w)[8]) {
+  uint16_t* at = to + column;
+  if (column + 16 <= head_dim && (reinterpret_cast<uintptr_t>(at) & 31) == 0) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+  } else {
+    if (column < head_dim) *reinterpret_cast<uint4*>(at) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (column + 8 < head_dim) *reinterpret_cast<uint4*>(at + 8) = make_uint4(w[4], w[5], w[6], w[7]);
   }
-  __syncwarp();
 }
 
 // Keys that no token of the call sees: between the sinks and the first token's window, and past the end (slots of
@@ -248,11 +256,17 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         mbar_init(&t->p_full[x][h], 4);
       }
       mbar_init(&t->o_last[x], 1);
+      mbar_init(&t->group_sync[x], 4);
       mbar_init(&t->o_full[x], 1);
       mbar_init(&t->drain[x], 1);
     }
     t->abort_flag = 0;
     t->zero = 0.0f;
+    for (int i = 0; i < ITEMS; ++i) {
+      mbar_init(&t->item_full[i], 1);
+      mbar_init(&t->item_empty[i], SOFTMAX_WARPS);
+    }
+    for (int w = 0; w < SOFTMAX_WARPS; ++w) t->left[w] = 0;
     mbar_fence_init();
     prefetch_tmap(&tmap);
   }
@@ -457,10 +471,46 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     } else {
       // ---------------------------------------------------------- values that no token of the call sees count as zeros
       // (it looks at every tile and has a say in its slot's release, or it could lose count of the rounds)
-      int s = 1;
+      int s = 1, n_items = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (; !walk.done() && ok; walk.next()) {
+      auto publish = [&](const KvWalk<ROWS, KEYS>& w) {
+        const int at = n_items % ITEMS;
+        if (ok) ok = mbar_warp_wait(&t->item_empty[at], ((n_items / ITEMS) & 1) ^ 1, &t->abort_flag);
+        if (lane == 0) {
+          Item d = {};
+          if (!w.done()) {
+            const KvSeq& seq = t->batch.seq[w.i];
+            d.more = 1;
+            d.row0 = w.rt * ROWS;
+            d.rows = seq.count * p.group - d.row0;
+            d.first_pos = seq.length - seq.count;
+            d.q_first = seq.first;
+            d.head0 = w.head * p.group;
+            d.from = w.from;
+            d.to = w.to;
+            d.sink_tiles = w.r.sink_tiles;
+            d.first_tile = w.r.first;
+            d.whole = w.whole();
+            if (!d.whole) {
+              const auto pieces = w.pieces();
+              d.my_slot = w.my_slot(blockIdx.x);
+              d.piece_first = pieces.first;
+              d.pieces = pieces.n;
+              d.piece_slot = pieces.first_slot;
+            }
+          }
+          t->item[at] = d;
+          mbar_arrive(&t->item_full[at]);
+        }
+        __syncwarp();
+        ++n_items;
+      };
+      publish(walk);
+      while (!walk.done() && ok) {
+        KvWalk<ROWS, KEYS> after = walk;
+        after.next();
+        publish(after);
         const Hidden hidden(p, t->batch.seq[walk.i]);
         for (int k = walk.from; k < walk.to; ++k) {
           const int key0 = walk.r.tile(k) * KEYS;
@@ -483,6 +533,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
             ph ^= 1u;
           }
         }
+        walk = after;
       }
       if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
     }
@@ -490,26 +541,33 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     // ------------------------------------------------------------ softmax
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     const int x = warp >> 2, row = tid & 127;        // row tile, and row (tensor-memory lane) of this thread
-    unsigned char* turn_smem = t->turn_rows[warp];
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + lane_base + x * 128, o_addr = tmem + lane_base + TMEM_O + x * 128;
     // A scale of zero must not make NaN of the minus infinity that stands for a hidden key.
     const float scale = fmaxf(fabsf(p.scale_log2), 1e-30f);
-    uint32_t s_ph = 0, o_ph = 0;
+    const uint32_t on = lane == 0;
+    uint32_t s_ph = 0, o_ph = 0, sync_ph = 0;
     bool ok = true;
-    using Walk = KvWalk<ROWS, KEYS>;
-    // Rows of this row tile in an item, if below 128; items without any are passed over.
-    auto rows_of = [&](const Walk& w) { return t->batch.seq[w.i].count * p.group - w.rt * ROWS - x * 128; };
-    auto skip = [&](Walk& w) {
-      while (!w.done() && rows_of(w) <= 0) w.next();
+    int n_items = 0;
+    auto read_item = [&]() {
+      const int at = n_items % ITEMS;
+      if (ok) ok = mbar_warp_wait(&t->item_full[at], (n_items / ITEMS) & 1, &t->abort_flag);
+      Item d = t->item[at];
+      if (!ok) d.more = 0;
+      return d;
+    };
+    auto next_item = [&]() {                         // the present one's place may be used again
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&t->item_empty[n_items % ITEMS]);
+      ++n_items;
     };
     // A row that is not there goes along with the last one that is, and is not written.
-    auto row_at = [&](const Walk& w) { return w.rt * ROWS + x * 128 + min(row, rows_of(w) - 1); };
-    auto fetch_q = [&](const Walk& w) {              // a warp's 32 rows, LANES lanes along a row
+    auto row_of = [&](const Item& d) { return d.row0 + x * 128 + min(row, d.rows - x * 128 - 1); };
+    auto fetch_q = [&](const Item& d) {              // a warp's 32 rows, LANES lanes along a row
       constexpr int LANES = DCH * 8, AT_ONCE = 32 / LANES;
-      const int rr = row_at(w), tok = kv_token_of(p, rr);
-      const uint16_t* mine = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(t->batch.seq[w.i].first + tok) * p.q_token_stride +
-                             (int64_t)(w.head * p.group + (rr - tok * p.group)) * p.q_head_stride;
+      const int rr = row_of(d), tok = kv_token_of(p, rr);
+      const uint16_t* mine = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(d.q_first + tok) * p.q_token_stride +
+                             (int64_t)(d.head0 + (rr - tok * p.group)) * p.q_head_stride;
       const int piece = lane % LANES, sub = lane / LANES;
       const bool there = piece * 8 < v.head_dim;
       const uint32_t to = smem_u32(q_smem) + x * Q_TILE + (piece >> 3) * CHUNK;
@@ -521,24 +579,34 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       }
       cp_async_arrive(&t->q_full[x]);                // when this thread's copies have landed
     };
-    skip(walk);
-    if (!walk.done()) fetch_q(walk);
-    while (!walk.done()) {
-      const KvSeq seq = t->batch.seq[walk.i];
-      const bool live = row < rows_of(walk);
-      const int rr = row_at(walk), tok = kv_token_of(p, rr), hq = walk.head * p.group + (rr - tok * p.group);
-      const int pos = seq.length - seq.count + tok;
+    auto group_sync = [&]() {
+      __syncwarp();
+      arrive_one(&t->group_sync[x], on);
+      if (ok) ok = mbar_warp_wait(&t->group_sync[x], sync_ph, &t->abort_flag);
+      sync_ph ^= 1u;
+    };
+    bool fetched = false;
+    Item item = read_item();
+    while (item.more) {
+      if (item.rows <= x * 128) {                    // none of this row tile's rows
+        next_item();
+        item = read_item();
+        continue;
+      }
+      if (!fetched) fetch_q(item);
+      fetched = false;
+      Item after = {};
+      const bool live = row < item.rows - x * 128;
+      const int rr = row_of(item), tok = kv_token_of(p, rr), hq = item.head0 + (rr - tok * p.group);
+      const int pos = item.first_pos + tok;
       const int lowest = __shfl_sync(FULL_MASK, pos, 0), highest = __shfl_sync(FULL_MASK, pos, 31);     // of the warp's rows
-      Walk after = walk;
-      after.next();
-      skip(after);
       float m = -INFINITY, l = 0.0f;
-      const int units = 2 * (walk.to - walk.from);
+      const int units = 2 * (item.to - item.from);
       // The two row tiles' warps on one scheduler take turns with their exponentials: at the same time they would
       // both have them, and then both load scores and look for maxima while the special-function unit has
       // nothing to do.  A begins; what B passes on after its last unit of an item would be one too many.
-      const bool paired = seq.count * p.group - walk.rt * ROWS > 128;
-      if (paired && x == 1) pair_pass(warp);
+      const bool paired = item.rows > 128;
+      if (paired && x == 1) turn_pass(warp);
       bool last_seen = false;
       for (int u = 0; u < units; ++u) {
         const int half = u & 1;
@@ -547,9 +615,14 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         tc_fence_after_sync();
         uint32_t va[64];
         tmem_ld_32x64(s_addr + half * 64, va);
-        const bool fetch = u + 1 == units && !after.done();
-        if (fetch) fetch_q(after);                   // the item's last scores are there: its query is no longer read
-        const int key0 = walk.r.tile(walk.from + (u >> 1)) * KEYS + half * 64, last = key0 + 63;
+        if (u + 1 == units) {                        // the item's last scores are there: its query is no longer read
+          next_item();
+          after = read_item();
+          fetched = after.more && after.rows > x * 128;
+          if (fetched) fetch_q(after);
+        }
+        const int k = item.from + (u >> 1);
+        const int key0 = (k < item.sink_tiles ? k : item.first_tile + (k - item.sink_tiles)) * KEYS + half * 64, last = key0 + 63;
         const bool clear = last <= lowest && (!p.window || key0 > highest - p.window || last < p.sinks);
         tmem_ld_wait_for(va);
         if (!clear) {
@@ -603,9 +676,9 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         }
         float base = m == -INFINITY ? 0.0f : m;
         if (paired) {
-          // (the zero that is read behind the barrier keeps the exponentials behind it too: nothing else would; on
+          // (the zero that is read behind the wait keeps the exponentials behind it too: nothing else would; on
           // the other side the store of the weights does)
-          pair_wait(warp);
+          turn_wait(warp);
           base -= *reinterpret_cast<volatile float*>(&t->zero);
         }
         const uint64_t scale2 = pair_of(scale, scale), base2 = pair_of(-base, -base);
@@ -613,11 +686,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         uint32_t w[32];
         weights<F16>(va, scale2, base2, sum2, w);
         tmem_st_32x32(s_addr + half * 64, w);
-        if (paired && (x == 0 || u + 1 < units)) pair_pass(warp);
+        if (paired && (x == 0 || u + 1 < units)) turn_pass(warp);
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&t->p_full[x][half]);
+        arrive_one(&t->p_full[x][half], on);
         float sa, sb;
         split_pair(add_pairs(sum2[0], sum2[1]), &sa, &sb);
         l += sa + sb;
@@ -629,30 +702,28 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       o_ph ^= 1u;
       __syncwarp();
       tc_fence_after_sync();
-      uint16_t* to = reinterpret_cast<uint16_t*>(p.out) + (int64_t)(seq.first + tok) * p.out_token_stride + (int64_t)hq * p.out_head_stride;
-      if (walk.whole()) {
+      uint16_t* to = reinterpret_cast<uint16_t*>(p.out) + (int64_t)(item.q_first + tok) * p.out_token_stride + (int64_t)hq * p.out_head_stride;
+      if (item.whole) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const unsigned long long mine = live ? reinterpret_cast<unsigned long long>(to) : 0ull;
-#pragma unroll 1
-        for (int c = 0; c < DIM; c += 32) {
-          uint32_t o[32];
-          tmem_ld_32x32(o_addr + c, o);
-          tmem_ld_wait_for32(o);
-          uint4 w[4];
+        uint32_t o[DCH][64];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[i].x = pack2<F16>(__uint_as_float(o[8 * i]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
-            w[i].y = pack2<F16>(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
-            w[i].z = pack2<F16>(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
-            w[i].w = pack2<F16>(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
+        for (int c = 0; c < DCH; ++c) tmem_ld_32x64(o_addr + c * 64, o[c]);
+#pragma unroll
+        for (int c = 0; c < DCH; ++c) {
+          tmem_ld_wait_for(o[c]);
+#pragma unroll
+          for (int i = 0; i < 64; i += 16) {
+            uint32_t w[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) w[y] = pack2<F16>(__uint_as_float(o[c][i + 2 * y]) * inv, __uint_as_float(o[c][i + 2 * y + 1]) * inv);
+            if (live) store_row<F16>(to, c * 64 + i, v.head_dim, w);
           }
-          store_rows(turn_smem, w, mine, c, v.head_dim, lane);
         }
         tc_fence_before_sync();
       } else {
         // layout of a piece: 256 maxima, 256 sums, then four columns of all rows at a time
         const int r = x * 128 + row;
-        float* slot = p.partials + (size_t)walk.my_slot(blockIdx.x) * p.partial_floats;
+        float* slot = p.partials + (size_t)item.my_slot * p.partial_floats;
         slot[r] = m;
         slot[ROWS + r] = l;
 #pragma unroll 1
@@ -666,8 +737,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         }
         tc_fence_before_sync();
         __threadfence();
-        warpgroup_sync(x);
-        const auto pieces = walk.pieces();
+        group_sync();
+        const typename KvWalk<ROWS, KEYS>::Pieces pieces{item.piece_first, item.pieces, item.piece_slot};
         if (row == 0) {
           int* arrivals = p.arrivals + pieces.first * 2 + x;
           const int arrived = atomicAdd(arrivals, 1);
@@ -675,51 +746,77 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           if (t->last[x]) *arrivals = 0;             // ready for the next launch
           __threadfence();
         }
-        warpgroup_sync(x);
+        group_sync();
         if (t->last[x]) {                            // join the pieces, in the order of the CTAs
+          // (a row that is not there is not read, either)
           float top = -INFINITY, total = 0.0f;
-#pragma unroll 4
-          for (int c = 0; c < pieces.n; ++c) top = fmaxf(top, __ldcg(p.partials + (size_t)pieces.slot(c) * p.partial_floats + r));
-          if (top == -INFINITY) top = 0.0f;
-#pragma unroll 4
-          for (int c = 0; c < pieces.n; ++c) {
-            const float* from = p.partials + (size_t)pieces.slot(c) * p.partial_floats + r;
-            total += exp2_fast(__ldcg(from) - top) * __ldcg(from + ROWS);
-          }
-          const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-#pragma unroll 1
-          for (int c32 = 0; c32 < DIM; c32 += 32) {
-            float4 acc[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 2
+          if (live) {
+#pragma unroll 8
+            for (int c = 0; c < pieces.n; ++c) top = fmaxf(top, __ldcg(p.partials + (size_t)pieces.slot(c) * p.partial_floats + r));
+            if (top == -INFINITY) top = 0.0f;
+#pragma unroll 8
             for (int c = 0; c < pieces.n; ++c) {
-              const float* from = p.partials + (size_t)pieces.slot(c) * p.partial_floats;
-              const float w = exp2_fast(__ldcg(from + r) - top) * inv;
+              const float* from = p.partials + (size_t)pieces.slot(c) * p.partial_floats + r;
+              total += exp2_fast(__ldcg(from) - top) * __ldcg(from + ROWS);
+            }
+            const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+            constexpr int FLIGHT = 4;                // pieces under way at a time, eight loads of each
+#pragma unroll 1
+            for (int c32 = 0; c32 < DIM; c32 += 32) {
+              float4 acc[8];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float4 y = __ldcg(reinterpret_cast<const float4*>(from + 2 * ROWS + ((c32 / 4 + i) * ROWS + r) * 4));
-                acc[i].x += w * y.x;
-                acc[i].y += w * y.y;
-                acc[i].z += w * y.z;
-                acc[i].w += w * y.w;
+              for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+              for (int c0 = 0; c0 < pieces.n; c0 += FLIGHT) {
+                float4 y[FLIGHT][8];
+                float w[FLIGHT];
+#pragma unroll
+                for (int c = 0; c < FLIGHT; ++c) {
+                  const float* from = p.partials + (size_t)pieces.slot(min(c0 + c, pieces.n - 1)) * p.partial_floats;
+                  w[c] = c0 + c < pieces.n ? __ldcg(from + r) : -INFINITY;
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) y[c][i] = __ldcg(reinterpret_cast<const float4*>(from + 2 * ROWS + ((c32 / 4 + i) * ROWS + r) * 4));
+                }
+#pragma unroll
+                for (int c = 0; c < FLIGHT; ++c) {
+                  const float f = exp2_fast(w[c] - top) * inv;
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) {
+                    acc[i].x += f * y[c][i].x;
+                    acc[i].y += f * y[c][i].y;
+                    acc[i].z += f * y[c][i].z;
+                    acc[i].w += f * y[c][i].w;
+                  }
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                uint32_t w[8];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  w[2 * y] = pack2<F16>(acc[4 * i + y].x, acc[4 * i + y].y);
+                  w[2 * y + 1] = pack2<F16>(acc[4 * i + y].z, acc[4 * i + y].w);
+                }
+                store_row<F16>(to, c32 + 16 * i, v.head_dim, w);
               }
             }
-            uint4 w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              w[i].x = pack2<F16>(acc[2 * i].x, acc[2 * i].y);
-              w[i].y = pack2<F16>(acc[2 * i].z, acc[2 * i].w);
-              w[i].z = pack2<F16>(acc[2 * i + 1].x, acc[2 * i + 1].y);
-              w[i].w = pack2<F16>(acc[2 * i + 1].z, acc[2 * i + 1].w);
-            }
-            store_rows(turn_smem, w, live ? reinterpret_cast<unsigned long long>(to) : 0ull, c32, v.head_dim, lane);
           }
         }
       }
-      walk = after;
+      item = after;
     }
-    if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
+    // A warp that leaves early, because a wait ran out, must not leave its partner in a turn that nobody passes on: it
+    // passes turns on until the partner has left too (whose other waits have limits).
+    __syncwarp();
+    if (lane == 0) *reinterpret_cast<volatile int*>(&t->left[warp]) = 1;
+    if (!ok) {
+      if (lane == 0) kv_report(v, KV_TIMEOUT);
+      const long long t0 = clock64();
+      while (__all_sync(FULL_MASK, *reinterpret_cast<volatile int*>(&t->left[warp ^ 4]) == 0 && clock64() - t0 < 8 * WAIT_LIMIT_CYCLES)) {
+        turn_pass(warp);
+        __nanosleep(1000);
+      }
+    }
   }
   tc_fence_before_sync();
   __syncthreads();
