@@ -87,8 +87,7 @@ cudaError_t kv_decode_launch(const KvAttendParams& p, const CUtensorMap& tmap, b
 cudaError_t kv_rows_configure(int smem_optin);
 size_t kv_rows_partial_floats(int head_dim);
 // tmap: the pool as rows of head_dim elements, box of 64 elements x min(page_size, 64) rows, 128-byte swizzle.
-cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int rows_per_seq, int sm_count, int smem_optin,
-                           cudaStream_t st);
+cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int sm_count, int smem_optin, cudaStream_t st);
 cudaError_t kv_extend_configure(int smem_optin);
 size_t kv_extend_partial_floats(int head_dim);
 cudaError_t kv_extend_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int sm_count, int smem_optin, cudaStream_t st);

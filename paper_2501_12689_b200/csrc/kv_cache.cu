@@ -408,9 +408,10 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
     p.seqs = a.seqs + off;
     p.starts = a.starts ? a.starts + off : nullptr;
     p.n = a.n - off < icc::KV_BATCH ? a.n - off : icc::KV_BATCH;
-    const cudaError_t e = rows <= 16 ? icc::kv_decode_launch(p, kv->tmap, kv->f16, rows > 8, kv->sm_count, kv->smem_optin, kv->stream)
-                          : p.v.head_dim <= 128 ? icc::kv_extend_launch(p, kv->tmap, kv->f16, kv->sm_count, kv->smem_optin, kv->stream)
-                                     : icc::kv_rows_launch(p, kv->tmap, kv->f16, (int)(rows < 64 ? rows : 64), kv->sm_count, kv->smem_optin, kv->stream);
+    cudaError_t e;
+    if (rows <= 16) e = icc::kv_decode_launch(p, kv->tmap, kv->f16, rows > 8, kv->sm_count, kv->smem_optin, kv->stream);
+    else if (p.v.head_dim <= 128) e = icc::kv_extend_launch(p, kv->tmap, kv->f16, kv->sm_count, kv->smem_optin, kv->stream);
+    else e = icc::kv_rows_launch(p, kv->tmap, kv->f16, kv->sm_count, kv->smem_optin, kv->stream);
     rc = launched(kv, e, 1, "attention");
   }
   return rc;

@@ -103,6 +103,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_reserve_kernel(const KvView v
   extern __shared__ int begin[];          // [n] rank of a sequence's first fresh page
   __shared__ unsigned sums[33];
   __shared__ int bad;
+  grid_dep_launch_dependents();
+  grid_dep_wait();   // arguments and state come from earlier kernels in the stream
   if (*v.err != KV_OK) return;
   if (threadIdx.x == 0) bad = KV_OK;
   __syncthreads();
@@ -159,6 +161,8 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, 
                                                                 const int* __restrict__ seqs, const int* __restrict__ starts, int n,
                                                                 int64_t n_tokens) {
   __shared__ unsigned char* place[TOKENS];   // first byte of the token's key row of head 0, or null
+  grid_dep_launch_dependents();
+  grid_dep_wait();
   if (*v.err != KV_OK) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
@@ -244,6 +248,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_fork_plan_kernel(const KvView
                                                                     int n, int copy) {
   __shared__ unsigned sums[33];
   __shared__ int bad;
+  grid_dep_launch_dependents();
+  grid_dep_wait();
   if (threadIdx.x == 0) {
     bad = KV_OK;
     v.meta[0] = 0;
@@ -297,6 +303,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_fork_plan_kernel(const KvView
 }
 
 __global__ void __launch_bounds__(COPY_THREADS) kv_fork_stage_kernel(const KvView v, const int* __restrict__ parents, int n) {
+  grid_dep_launch_dependents();
+  grid_dep_wait();
   if (v.meta[0] == 0) return;
   const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
   for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
@@ -323,6 +331,8 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_fork_stage_kernel(const KvVie
 }
 
 __global__ void __launch_bounds__(COPY_THREADS) kv_fork_apply_kernel(const KvView v, const int* __restrict__ children, int n) {
+  grid_dep_launch_dependents();
+  grid_dep_wait();
   if (v.meta[0] == 0) return;
   const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
   for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
@@ -346,6 +356,8 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_fork_apply_kernel(const KvVie
 // A CTA per sequence.  Whoever takes the length away owns the release, so a number that comes twice counts once.
 __global__ void __launch_bounds__(COPY_THREADS) kv_free_kernel(const KvView v, const int* __restrict__ seqs, int n) {
   __shared__ int had;
+  grid_dep_launch_dependents();
+  grid_dep_wait();
   if (*v.err != KV_OK) return;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int s = seqs[i];
@@ -368,6 +380,8 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_free_kernel(const KvView v, c
 // their ranks; rank r's page moves to rank r's hole.
 __global__ void __launch_bounds__(PLAN_THREADS) kv_compact_plan_kernel(const KvView v) {
   __shared__ unsigned sums[33];
+  grid_dep_launch_dependents();
+  grid_dep_wait();
   if (threadIdx.x == 0) v.meta[0] = 0;
   if (*v.err != KV_OK) return;
   constexpr int ROUND = PLAN_THREADS * PAGES_PER_THREAD;
@@ -411,6 +425,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_compact_plan_kernel(const KvV
 }
 
 __global__ void __launch_bounds__(COPY_THREADS) kv_compact_apply_kernel(const KvView v) {
+  grid_dep_launch_dependents();
+  grid_dep_wait();
   if (v.meta[0] == 0) return;
   const int n_jobs = v.meta[1], n_live = v.meta[2];
   if (n_jobs == 0) return;
@@ -440,8 +456,7 @@ cudaError_t kv_pages_configure(int smem_optin) {
 }
 
 cudaError_t kv_reserve_launch(const KvView& v, const int* seqs, const int* counts, int n, cudaStream_t st) {
-  kv_reserve_kernel<<<1, PLAN_THREADS, (size_t)n * 4, st>>>(v, seqs, counts, n);
-  return cudaGetLastError();
+  return launch_overlapped(kv_reserve_kernel, dim3(1), dim3(PLAN_THREADS), (size_t)n * 4, st, 1, v, seqs, counts, n);
 }
 
 cudaError_t kv_write_launch(const KvView& v, int layer, const void* k, const void* val, int64_t token_stride, int64_t head_stride,
@@ -449,34 +464,32 @@ cudaError_t kv_write_launch(const KvView& v, int layer, const void* k, const voi
   const uint4* k4 = static_cast<const uint4*>(k);
   const uint4* v4 = static_cast<const uint4*>(val);
   if (n_tokens <= 4 * sm_count)
-    kv_write_kernel<1><<<(unsigned)n_tokens, COPY_THREADS, 0, st>>>(v, layer, k4, v4, token_stride, head_stride, seqs, starts, n, n_tokens);
-  else
-    kv_write_kernel<8><<<(unsigned)((n_tokens + 7) / 8), COPY_THREADS, 0, st>>>(v, layer, k4, v4, token_stride, head_stride, seqs, starts, n,
-                                                                               n_tokens);
-  return cudaGetLastError();
+    return launch_overlapped(kv_write_kernel<1>, dim3((unsigned)n_tokens), dim3(COPY_THREADS), 0, st, 1, v, layer, k4, v4, token_stride, head_stride,
+                             seqs, starts, n, n_tokens);
+  return launch_overlapped(kv_write_kernel<8>, dim3((unsigned)((n_tokens + 7) / 8)), dim3(COPY_THREADS), 0, st, 1, v, layer, k4, v4, token_stride,
+                           head_stride, seqs, starts, n, n_tokens);
 }
 
 cudaError_t kv_fork_launch(const KvView& v, const int* parents, const int* children, const int* upto, int n, int copy,
                            int sm_count, int* launches, cudaStream_t st) {
   const long long rows = (long long)n * ((v.max_pages + ROW_UNIT - 1) / ROW_UNIT);
   const int most = 8 * sm_count;
-  kv_fork_plan_kernel<<<1, PLAN_THREADS, 0, st>>>(v, parents, children, upto, n, copy);
-  kv_fork_stage_kernel<<<(int)(rows < most ? rows : most), COPY_THREADS, 0, st>>>(v, parents, n);
-  kv_fork_apply_kernel<<<most, COPY_THREADS, 0, st>>>(v, children, n);
   *launches = 3;
-  return cudaGetLastError();
+  cudaError_t e = launch_overlapped(kv_fork_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, 1, v, parents, children, upto, n, copy);
+  if (e == cudaSuccess)
+    e = launch_overlapped(kv_fork_stage_kernel, dim3((unsigned)(rows < most ? rows : most)), dim3(COPY_THREADS), 0, st, 1, v, parents, n);
+  if (e == cudaSuccess) e = launch_overlapped(kv_fork_apply_kernel, dim3((unsigned)most), dim3(COPY_THREADS), 0, st, 1, v, children, n);
+  return e;
 }
 
 cudaError_t kv_free_launch(const KvView& v, const int* seqs, int n, int sm_count, cudaStream_t st) {
-  kv_free_kernel<<<n < 8 * sm_count ? n : 8 * sm_count, COPY_THREADS, 0, st>>>(v, seqs, n);
-  return cudaGetLastError();
+  return launch_overlapped(kv_free_kernel, dim3((unsigned)(n < 8 * sm_count ? n : 8 * sm_count)), dim3(COPY_THREADS), 0, st, 1, v, seqs, n);
 }
 
 cudaError_t kv_compact_launch(const KvView& v, int sm_count, int* launches, cudaStream_t st) {
-  kv_compact_plan_kernel<<<1, PLAN_THREADS, 0, st>>>(v);
-  kv_compact_apply_kernel<<<8 * sm_count, COPY_THREADS, 0, st>>>(v);
   *launches = 2;
-  return cudaGetLastError();
+  const cudaError_t e = launch_overlapped(kv_compact_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, 1, v);
+  return e == cudaSuccess ? launch_overlapped(kv_compact_apply_kernel, dim3((unsigned)(8 * sm_count)), dim3(COPY_THREADS), 0, st, 1, v) : e;
 }
 
 }  // namespace icc

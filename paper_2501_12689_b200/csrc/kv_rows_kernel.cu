@@ -1,18 +1,17 @@
-// Attention over the paged cache for few query rows per sequence and kv head: decoding (one token, `group`
-// query heads), a handful of new tokens behind a long cached prefix, and any head_dim above 128.
+// Attention over the paged cache for more than 16 query rows per sequence and kv head and a head_dim of 129 to 256,
+// which the tensor-memory kernel (kv_extend_kernel.cu) has no room for.
 //
-// What bounds it: every key and value is read once per row tile and used for at most 64 rows, so
-// it is the read of the cache.  The kernel is therefore built around the loads.  One CTA per SM; a
-// producer warp fetches 64-key tiles, one tensor-map box per page, 64-element column chunk and keys/values,
-// into a ring of shared-memory stages (128-byte swizzle, so that the fragment loads below have no bank
-// conflicts) and looks up page numbers two tiles ahead.  Eight warps consume: the 16-row tiles of the
-// query (RT of them) times key groups; even and odd tiles go to different halves of the warps, so
-// two tiles are being worked on at any time.  Scores and weighted values are m16n8k16 products with
-// fp32 accumulation; each warp keeps its own running maximum and sum and its own accumulator for its keys,
-// which are merged once per item through shared memory.
+// One CTA per SM; an item is 32 query rows (tokens times query heads of a kv head).  A producer warp fetches 64-key
+// tiles, one tensor-map box per page, 64-element column chunk and keys/values, into a ring of shared-memory
+// stages (128-byte swizzle, so that the fragment loads below have no bank conflicts) and looks up page
+// numbers two tiles ahead.  Eight warps consume: two 16-row tiles of the query times four key groups (halves of
+// a tile, even and odd tiles).  Scores and weighted values are m16n8k16 products with fp32 accumulation; each
+// warp keeps its own running maximum and sum and its own accumulator for its keys, which are merged once
+// per item through shared memory.  With 32 rows per fetched key and value it is bound by the fetches from L2 and by
+// these products in about equal parts.
 //
 // The weights are rounded to the cache's 16-bit type for the second product.  To lose nothing by that
-// they are split in two such numbers (high part, remainder): twice the products, which are not the bound.
+// they are split in two such numbers (high part, remainder), twice the second product's instructions.
 #include <type_traits>
 
 #include "kernels.h"
@@ -524,69 +523,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
   if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
 }
 
-template <bool F16, int DCH, int RT>
-cudaError_t configure_one(int smem_optin) {
-  return cudaFuncSetAttribute(kv_rows_kernel<F16, DCH, RT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
-}
-
-template <bool F16, int DCH, int RT>
+template <bool F16, int DCH>
 cudaError_t launch_one(const KvAttendParams& p, const CUtensorMap& tmap, int sm_count, int smem_optin, cudaStream_t st) {
   // An even number of stages, so that a stage always belongs to the same half of the consumers: a warp that met
   // a stage's barrier at every other round only could not tell a round's parity from that of two rounds before.
   int stages = 2;
-  while (stages + 2 <= MAX_STAGES && rows_smem(DCH, RT, stages + 2) <= smem_optin) stages += 2;
-  return launch_overlapped(kv_rows_kernel<F16, DCH, RT>, dim3(sm_count), dim3(THREADS), rows_smem(DCH, RT, stages), st, 1, p, tmap, stages);
-}
-
-template <bool F16, int DCH>
-cudaError_t launch_rt(const KvAttendParams& p, const CUtensorMap& tmap, int rt, int sm_count, int smem_optin, cudaStream_t st) {
-  if (rt == 1) return launch_one<F16, DCH, 1>(p, tmap, sm_count, smem_optin, st);
-  if (rt == 2 || DCH > 2) return launch_one<F16, DCH, 2>(p, tmap, sm_count, smem_optin, st);
-  return launch_one<F16, DCH, DCH <= 2 ? 4 : 2>(p, tmap, sm_count, smem_optin, st);
-}
-
-template <bool F16>
-cudaError_t launch_dch(const KvAttendParams& p, const CUtensorMap& tmap, int rt, int sm_count, int smem_optin, cudaStream_t st) {
-  switch ((p.v.head_dim + 63) / 64) {
-    case 1: return launch_rt<F16, 1>(p, tmap, rt, sm_count, smem_optin, st);
-    case 2: return launch_rt<F16, 2>(p, tmap, rt, sm_count, smem_optin, st);
-    case 3: return launch_rt<F16, 3>(p, tmap, rt, sm_count, smem_optin, st);
-    default: return launch_rt<F16, 4>(p, tmap, rt, sm_count, smem_optin, st);
-  }
-}
-
-template <bool F16, int DCH>
-cudaError_t configure_dch(int smem_optin) {
-  cudaError_t e = configure_one<F16, DCH, 1>(smem_optin);
-  if (e == cudaSuccess) e = configure_one<F16, DCH, 2>(smem_optin);
-  if (e == cudaSuccess) e = configure_one<F16, DCH, DCH <= 2 ? 4 : 2>(smem_optin);
-  return e;
-}
-template <bool F16>
-cudaError_t configure_all(int smem_optin) {
-  cudaError_t e = configure_dch<F16, 1>(smem_optin);
-  if (e == cudaSuccess) e = configure_dch<F16, 2>(smem_optin);
-  if (e == cudaSuccess) e = configure_dch<F16, 3>(smem_optin);
-  if (e == cudaSuccess) e = configure_dch<F16, 4>(smem_optin);
-  return e;
+  while (stages + 2 <= MAX_STAGES && rows_smem(DCH, 2, stages + 2) <= smem_optin) stages += 2;
+  return launch_overlapped(kv_rows_kernel<F16, DCH, 2>, dim3(sm_count), dim3(THREADS), rows_smem(DCH, 2, stages), st, 1, p, tmap, stages);
 }
 
 }  // namespace
 
 cudaError_t kv_rows_configure(int smem_optin) {
-  const cudaError_t e = configure_all<false>(smem_optin);
-  return e == cudaSuccess ? configure_all<true>(smem_optin) : e;
+  cudaError_t e = cudaFuncSetAttribute(kv_rows_kernel<false, 3, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_rows_kernel<false, 4, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_rows_kernel<true, 3, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_rows_kernel<true, 4, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
+  return e;
 }
 
-size_t kv_rows_partial_floats(int head_dim) {
-  const int dch = (head_dim + 63) / 64, rows = dch <= 2 ? 64 : 32;
-  return (size_t)rows * (2 + dch * 64);
-}
+size_t kv_rows_partial_floats(int head_dim) { return (size_t)32 * (2 + (head_dim + 63) / 64 * 64); }
 
-cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int rows_per_seq, int sm_count, int smem_optin,
-                           cudaStream_t st) {
-  const int rt = rows_per_seq <= 16 ? 1 : (rows_per_seq <= 32 ? 2 : 4);
-  return f16 ? launch_dch<true>(p, tmap, rt, sm_count, smem_optin, st) : launch_dch<false>(p, tmap, rt, sm_count, smem_optin, st);
+cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int sm_count, int smem_optin, cudaStream_t st) {
+  if (p.v.head_dim <= 192) return f16 ? launch_one<true, 3>(p, tmap, sm_count, smem_optin, st) : launch_one<false, 3>(p, tmap, sm_count, smem_optin, st);
+  return f16 ? launch_one<true, 4>(p, tmap, sm_count, smem_optin, st) : launch_one<false, 4>(p, tmap, sm_count, smem_optin, st);
 }
 
 }  // namespace icc
