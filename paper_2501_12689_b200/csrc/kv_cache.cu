@@ -3,6 +3,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <mutex>
 #include <new>
 
 #include "../../include/ic_kv.h"
@@ -32,6 +33,50 @@ struct ic_kv {
 };
 
 namespace {
+
+// Mapped host words for the handles' errors.  Allocating pinned memory takes longer than everything else in a
+// creation, so one page of words serves all handles of the process; it is never given back.
+constexpr int STATUS_WORDS = 1024;
+std::mutex g_status_mutex;
+int* g_status_words = nullptr;
+bool g_status_used[STATUS_WORDS] = {};
+
+int* take_status_word() {
+  std::lock_guard<std::mutex> lock(g_status_mutex);
+  if (!g_status_words) {
+    void* p = nullptr;
+    if (cudaHostAlloc(&p, STATUS_WORDS * sizeof(int), cudaHostAllocMapped | cudaHostAllocPortable) != cudaSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    g_status_words = static_cast<int*>(p);
+  }
+  for (int i = 0; i < STATUS_WORDS; ++i)
+    if (!g_status_used[i]) {
+      g_status_used[i] = true;
+      g_status_words[i] = 0;
+      return g_status_words + i;
+    }
+  return nullptr;
+}
+void give_status_word(int* w) {
+  std::lock_guard<std::mutex> lock(g_status_mutex);
+  g_status_used[w - g_status_words] = false;
+}
+
+// The kernels' shared-memory limits, once per device.
+cudaError_t configure_kernels(int dev, int smem) {
+  static std::mutex mutex;
+  static bool done[64] = {};
+  std::lock_guard<std::mutex> lock(mutex);
+  if (dev < 64 && done[dev]) return cudaSuccess;
+  cudaError_t e = icc::kv_pages_configure(smem);
+  if (e == cudaSuccess) e = icc::kv_decode_configure(smem);
+  if (e == cudaSuccess) e = icc::kv_rows_configure(smem);
+  if (e == cudaSuccess) e = icc::kv_extend_configure(smem);
+  if (e == cudaSuccess && dev < 64) done[dev] = true;
+  return e;
+}
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -239,7 +284,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
   };
   auto allocate = [&](void** p, size_t bytes, size_t clear, const char* what) {
     e = cudaMalloc(p, bytes);
-    if (e == cudaSuccess && clear) e = cudaMemset(*p, 0, clear);
+    if (e == cudaSuccess && clear) e = cudaMemsetAsync(*p, 0, clear, kv->stream);
     if (e == cudaSuccess) return true;
     cudaGetLastError();
     fail(IC_ERR_NOMEM, "cudaMalloc of %zu bytes for the %s failed: %s", bytes, what, cudaGetErrorString(e));
@@ -276,7 +321,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
       fail(IC_ERR_NOMEM, "opts.workspace holds %zu bytes, %zu are needed", o.workspace_bytes, need);
       ok = false;
     }
-    if (ok && (cudaMemset(o.workspace, 0, clear) != cudaSuccess)) {
+    if (ok && (cudaMemsetAsync(o.workspace, 0, clear, kv->stream) != cudaSuccess)) {
       cudaGetLastError();
       fail(IC_ERR_CUDA, "clearing the head of opts.workspace failed");
       ok = false;
@@ -286,16 +331,9 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
   }
   if (ok) carve(&o, static_cast<unsigned char*>(o.workspace ? o.workspace : kv->own_workspace), kv);
   if (ok) {
-    e = cudaHostAlloc(reinterpret_cast<void**>(&kv->h_status), sizeof(int), cudaHostAllocMapped);
-    if (e == cudaSuccess) {
-      *kv->h_status = 0;
-      e = cudaHostGetDevicePointer(reinterpret_cast<void**>(&v.host_status), kv->h_status, 0);
-    }
-    if (e == cudaSuccess) e = icc::kv_pages_configure(smem);
-    if (e == cudaSuccess) e = icc::kv_decode_configure(smem);
-    if (e == cudaSuccess) e = icc::kv_rows_configure(smem);
-    if (e == cudaSuccess) e = icc::kv_extend_configure(smem);
-    if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the cleared words are there for any stream
+    kv->h_status = take_status_word();
+    e = kv->h_status ? cudaHostGetDevicePointer(reinterpret_cast<void**>(&v.host_status), kv->h_status, 0) : cudaErrorMemoryAllocation;
+    if (e == cudaSuccess) e = configure_kernels(dev, smem);
     if (e != cudaSuccess) {
       cudaGetLastError();
       fail(IC_ERR_CUDA, "setting up the cache failed: %s", cudaGetErrorString(e));
@@ -321,7 +359,7 @@ void ic_kv_destroy(ic_kv_t* kv) {
   if (kv->own_pool) cudaFree(kv->own_pool);
   if (kv->own_books) cudaFree(kv->own_books);
   if (kv->own_workspace) cudaFree(kv->own_workspace);
-  if (kv->h_status) cudaFreeHost(kv->h_status);
+  if (kv->h_status) give_status_word(kv->h_status);
   delete kv;
 }
 

@@ -474,14 +474,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
         slot[tid] = t->big[tid];
         slot[ROWS + tid] = t->total[tid];
       }
-      __threadfence();
       consumers_sync();
       const auto pieces = walk.pieces();
       if (tid == 0) {
-        const int arrived = atomicAdd(&p.arrivals[pieces.first], 1);
-        t->last = arrived == pieces.n - 1;
+        t->last = kv_arrive(&p.arrivals[pieces.first]) == pieces.n - 1;
         if (t->last) p.arrivals[pieces.first] = 0;   // ready for the next launch
-        __threadfence();
       }
       consumers_sync();
       if (t->last) {

@@ -61,6 +61,7 @@ struct ExtendTail {
   uint32_t tmem_base;
   int abort_flag, last[2], left[SOFTMAX_WARPS];
   float zero;
+  float join_top[2][128], join_inv[2][128];
   KvBatch batch;
 };
 
@@ -721,86 +722,111 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         }
         tc_fence_before_sync();
       } else {
-        // layout of a piece: 256 maxima, 256 sums, then four columns of all rows at a time
+        // layout of a piece: 256 maxima, 256 sums, then four columns of all rows at a time (rows that are not there
+        // are left out)
         const int r = x * 128 + row;
         float* slot = p.partials + (size_t)item.my_slot * p.partial_floats;
-        slot[r] = m;
-        slot[ROWS + r] = l;
-#pragma unroll 1
-        for (int c = 0; c < DIM; c += 32) {
-          uint32_t o[32];
-          tmem_ld_32x32(o_addr + c, o);
-          tmem_ld_wait_for32(o);
+        if (live) {
+          slot[r] = m;
+          slot[ROWS + r] = l;
+        }
+        uint32_t o[DCH][64];
 #pragma unroll
-          for (int i = 0; i < 32; i += 4)
-            *reinterpret_cast<uint4*>(slot + 2 * ROWS + ((c + i) / 4 * ROWS + r) * 4) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        for (int c = 0; c < DCH; ++c) tmem_ld_32x64(o_addr + c * 64, o[c]);
+#pragma unroll
+        for (int c = 0; c < DCH; ++c) {
+          tmem_ld_wait_for(o[c]);
+          if (live) {
+#pragma unroll
+            for (int i = 0; i < 64; i += 4)
+              *reinterpret_cast<uint4*>(slot + 2 * ROWS + ((c * 64 + i) / 4 * ROWS + r) * 4) = make_uint4(o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]);
+          }
         }
         tc_fence_before_sync();
-        __threadfence();
-        group_sync();
         const typename KvWalk<ROWS, KEYS>::Pieces pieces{item.piece_first, item.pieces, item.piece_slot};
+        group_sync();
         if (row == 0) {
           int* arrivals = p.arrivals + pieces.first * 2 + x;
-          const int arrived = atomicAdd(arrivals, 1);
-          t->last[x] = arrived == pieces.n - 1;
+          t->last[x] = kv_arrive(arrivals) == pieces.n - 1;
           if (t->last[x]) *arrivals = 0;             // ready for the next launch
-          __threadfence();
         }
         group_sync();
-        if (t->last[x]) {                            // join the pieces, in the order of the CTAs
-          // (a row that is not there is not read, either)
-          float top = -INFINITY, total = 0.0f;
-          if (live) {
-#pragma unroll 8
-            for (int c = 0; c < pieces.n; ++c) top = fmaxf(top, __ldcg(p.partials + (size_t)pieces.slot(c) * p.partial_floats + r));
-            if (top == -INFINITY) top = 0.0f;
-#pragma unroll 8
-            for (int c = 0; c < pieces.n; ++c) {
-              const float* from = p.partials + (size_t)pieces.slot(c) * p.partial_floats + r;
-              total += exp2_fast(__ldcg(from) - top) * __ldcg(from + ROWS);
+        if (t->last[x]) {
+          // Join the pieces, in the order of the CTAs: first a row per thread for the common maximum and sum, then the
+          // values, four columns of a row at a time, spread over all threads however few rows there are.  They
+          // come from L2, a microsecond away: COLUMNS x FLIGHT loads are under way per thread.
+          const int rows = min(128, item.rows - x * 128);
+          if (live) {                                // (whole batches of loads, the last piece again where there are fewer)
+            float top = -INFINITY, total = 0.0f;
+            for (int c0 = 0; c0 < pieces.n; c0 += 8) {
+              float pm[8], pl[8];
+#pragma unroll
+              for (int c = 0; c < 8; ++c) {
+                const float* from = p.partials + (size_t)pieces.slot(min(c0 + c, pieces.n - 1)) * p.partial_floats + r;
+                pm[c] = __ldcg(from);
+                pl[c] = c0 + c < pieces.n ? __ldcg(from + ROWS) : 0.0f;
+              }
+              float now = top;
+#pragma unroll
+              for (int c = 0; c < 8; ++c) now = fmaxf(now, pm[c]);
+              const float base = now == -INFINITY ? 0.0f : now;
+              total *= exp2_fast(top - base);
+              top = now;
+#pragma unroll
+              for (int c = 0; c < 8; ++c) total += exp2_fast(pm[c] - base) * pl[c];
             }
-            const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-            constexpr int FLIGHT = 4;                // pieces under way at a time, eight loads of each
+            t->join_top[x][row] = top == -INFINITY ? 0.0f : top;
+            t->join_inv[x][row] = total == 0.0f ? 0.0f : 1.0f / total;
+          }
+          group_sync();
+          constexpr int COLUMNS = 4, FLIGHT = 8;
+          const int vecs = rows * (DIM / 4);
 #pragma unroll 1
-            for (int c32 = 0; c32 < DIM; c32 += 32) {
-              float4 acc[8];
+          for (int f0 = row; f0 < vecs; f0 += 128 * COLUMNS) {
+            float4 acc[COLUMNS];
 #pragma unroll
-              for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            for (int i = 0; i < COLUMNS; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
-              for (int c0 = 0; c0 < pieces.n; c0 += FLIGHT) {
-                float4 y[FLIGHT][8];
-                float w[FLIGHT];
+            for (int c0 = 0; c0 < pieces.n; c0 += FLIGHT) {
+              float4 y[FLIGHT][COLUMNS];
+              float w[FLIGHT][COLUMNS];
 #pragma unroll
-                for (int c = 0; c < FLIGHT; ++c) {
-                  const float* from = p.partials + (size_t)pieces.slot(min(c0 + c, pieces.n - 1)) * p.partial_floats;
-                  w[c] = c0 + c < pieces.n ? __ldcg(from + r) : -INFINITY;
+              for (int c = 0; c < FLIGHT; ++c) {
+                const float* from = p.partials + (size_t)pieces.slot(min(c0 + c, pieces.n - 1)) * p.partial_floats + x * 128;
 #pragma unroll
-                  for (int i = 0; i < 8; ++i) y[c][i] = __ldcg(reinterpret_cast<const float4*>(from + 2 * ROWS + ((c32 / 4 + i) * ROWS + r) * 4));
-                }
-#pragma unroll
-                for (int c = 0; c < FLIGHT; ++c) {
-                  const float f = exp2_fast(w[c] - top) * inv;
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) {
-                    acc[i].x += f * y[c][i].x;
-                    acc[i].y += f * y[c][i].y;
-                    acc[i].z += f * y[c][i].z;
-                    acc[i].w += f * y[c][i].w;
-                  }
+                for (int i = 0; i < COLUMNS; ++i) {
+                  const int f = min(f0 + i * 128, vecs - 1), rf = f % rows;
+                  w[c][i] = c0 + c < pieces.n ? __ldcg(from + rf) : -INFINITY;
+                  y[c][i] = __ldcg(reinterpret_cast<const float4*>(from + 2 * ROWS - x * 128 + ((f / rows) * ROWS + x * 128 + rf) * 4));
                 }
               }
 #pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                uint32_t w[8];
+              for (int i = 0; i < COLUMNS; ++i) {
+                const float base = t->join_top[x][min(f0 + i * 128, vecs - 1) % rows];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                  w[2 * y] = pack2<F16>(acc[4 * i + y].x, acc[4 * i + y].y);
-                  w[2 * y + 1] = pack2<F16>(acc[4 * i + y].z, acc[4 * i + y].w);
+                for (int c = 0; c < FLIGHT; ++c) {
+                  const float f = exp2_fast(w[c][i] - base);
+                  acc[i].x += f * y[c][i].x;
+                  acc[i].y += f * y[c][i].y;
+                  acc[i].z += f * y[c][i].z;
+                  acc[i].w += f * y[c][i].w;
                 }
-                store_row<F16>(to, c32 + 16 * i, v.head_dim, w);
               }
+            }
+#pragma unroll
+            for (int i = 0; i < COLUMNS; ++i) {
+              const int f = f0 + i * 128, rf = f % rows, d = f / rows * 4;
+              if (f >= vecs || d >= v.head_dim) continue;
+              const int jr = item.row0 + x * 128 + rf, jt = kv_token_of(p, jr);
+              const float inv = t->join_inv[x][rf];
+              uint2 w;
+              w.x = pack2<F16>(acc[i].x * inv, acc[i].y * inv);
+              w.y = pack2<F16>(acc[i].z * inv, acc[i].w * inv);
+              *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + (int64_t)(item.q_first + jt) * p.out_token_stride +
+                                        (int64_t)(item.head0 + (jr - jt * p.group)) * p.out_head_stride + d) = w;
             }
           }
+          group_sync();                              // join_top and join_inv may be written again
         }
       }
       item = after;

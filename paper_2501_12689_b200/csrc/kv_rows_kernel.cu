@@ -438,15 +438,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
         for (int d = lane * 2; d < v.head_dim; d += 64)
           *reinterpret_cast<float2*>(slot + 2 * ROWS + r * (DCH * 64) + d) = *reinterpret_cast<const float2*>(merge + r * PITCH + d);
       }
-      __threadfence();
       consumers_sync();
       const auto pieces = walk.pieces();
-      const int c0 = pieces.first, n_parts = pieces.n;
+      const int n_parts = pieces.n;
       if (tid == 0) {
-        const int arrived = atomicAdd(&p.arrivals[c0], 1);
-        t->last = arrived == n_parts - 1;
-        if (t->last) p.arrivals[c0] = 0;             // ready for the next launch
-        __threadfence();
+        t->last = kv_arrive(&p.arrivals[pieces.first]) == n_parts - 1;
+        if (t->last) p.arrivals[pieces.first] = 0;   // ready for the next launch
       }
       consumers_sync();
       if (t->last) {

@@ -120,6 +120,14 @@ __device__ __forceinline__ void kv_load_batch(const KvAttendParams& p, KvBatch* 
   }
 }
 
+// One more piece of an item is written: by one thread, after a barrier that the writers have passed.  Returns how many were
+// there before.  Release for the pieces of this CTA, acquire for those of the others.
+__device__ __forceinline__ int kv_arrive(int* arrivals) {
+  int before;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(arrivals) : "memory");
+  return before;
+}
+
 // 64-bit division, which is a long sequence of instructions, only where 32 bits do not do.
 __device__ __forceinline__ long long kv_div(long long a, long long b) {
   return (a >> 31) == 0 ? (long long)((unsigned)a / (unsigned)min(b, 0xffffffffll)) : a / b;

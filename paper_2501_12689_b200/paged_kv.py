@@ -122,12 +122,17 @@ class ICPagedKV:
         self.refs = tensor(refs, (n_pages,), torch.int32, "refs")
         o.device, o.stream = dev, self._stream.cuda_stream or None
         o.pool, o.tables, o.lengths, o.refs = (t.data_ptr() for t in (self.pool, self.tables, self.lengths, self.refs))
-        if workspace is not None:
+        if workspace is None:       # from torch's allocator, which has it ready more often than not
+            workspace = torch.empty(lib.ic_kv_workspace_bytes(ctypes.byref(o)), dtype=torch.uint8, device=self.device)
+            workspace.record_stream(self._stream)
+            made = True
+        else:
+            made = pool is None or tables is None or lengths is None or refs is None
             if not workspace.is_cuda or not workspace.is_contiguous():
                 raise ValueError("workspace must be a contiguous device tensor")
-            o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        o.workspace, o.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         self._workspace = workspace     # borrowed by the handle: keep it alive
-        if pool is None or tables is None or lengths is None or refs is None:
+        if made:
             # what was made here is made before the handle's stream uses it
             self._stream.wait_stream(torch.cuda.current_stream(self.device))
         self._h = lib.ic_kv_create(ctypes.byref(o))
