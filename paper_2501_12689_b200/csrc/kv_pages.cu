@@ -199,16 +199,22 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, 
     if (lane == 0) place[x] = at;
   }
   __syncthreads();
+  // a thread takes one place in the tokens (keys or values, head, piece) at a time and all TOKENS tokens there: their
+  // loads are under way together
   const int pieces = v.head_dim >> 3, per_token = v.n_kv_heads * pieces;
   const size_t block = ((size_t)v.head_dim * 2) << v.page_shift;      // bytes of one head's keys in a page
-  for (int u = threadIdx.x; u < TOKENS * 2 * per_token; u += COPY_THREADS) {
-    const int x = u / (2 * per_token), r = u - x * 2 * per_token;
-    const int is_v = r >= per_token, hp = is_v ? r - per_token : r;
+  for (int u = threadIdx.x; u < 2 * per_token; u += COPY_THREADS) {
+    const int is_v = u >= per_token, hp = is_v ? u - per_token : u;
     const int h = hp / pieces, piece = hp - h * pieces;
-    unsigned char* at = place[x];
-    if (!at) continue;
-    const uint4 w = (is_v ? val : k)[((t0 + x) * token_stride + h * head_stride) / 8 + piece];
-    *reinterpret_cast<uint4*>(at + (size_t)(is_v * v.n_kv_heads + h) * block + (size_t)piece * 16) = w;
+    const uint4* from = (is_v ? val : k) + (t0 * token_stride + h * head_stride) / 8 + piece;
+    const size_t off = (size_t)(is_v * v.n_kv_heads + h) * block + (size_t)piece * 16;
+    uint4 w[TOKENS];
+#pragma unroll
+    for (int x = 0; x < TOKENS; ++x)
+      if (place[x]) w[x] = ld_stream_16B(from + x * (token_stride / 8));
+#pragma unroll
+    for (int x = 0; x < TOKENS; ++x)
+      if (place[x]) *reinterpret_cast<uint4*>(place[x] + off) = w[x];
   }
 }
 
@@ -241,11 +247,51 @@ __device__ __forceinline__ void copy_pages(const KvView& v, int n_jobs) {
 }
 
 // ---------------------------------------------------------------- fork
-// Three launches: a plan by one CTA (arguments, pages needed, free pages), the children's new rows made
-// beside the old ones while all parents still stand, and the exchange of rows with the copies.
+// Three steps: the plan (arguments, pages needed, free pages), by one CTA; the children's new rows, made
+// beside the old ones while all parents still stand; and the exchange of rows, with the copies of pages.  The plan's
+// CTA does the rows too where there are few table entries (SMALL_FORK), which saves a launch; otherwise the rows are
+// spread over CTAs, and each step is a launch.
+constexpr int SMALL_FORK = 8192;          // table entries: eight per thread of the plan's CTA, about what a launch takes
+
+// Entries c0 .. of child i's new row; n_threads threads.
+__device__ __forceinline__ void stage_row(const KvView& v, const int* parents, int i, int c0, int c_end, int thread, int n_threads) {
+  const int want = v.upto[i];
+  if (want < 0) return;
+  const int end = min(kv_pages_of(want, v.page_shift), c_end), shared = v.shared[i], begin = v.begin[i];
+  const int* row = v.tables + (size_t)parents[i] * v.max_pages;
+  int* to = v.staged + (size_t)i * v.max_pages;
+  for (int c = c0 + thread; c < end; c += n_threads) {
+    const int page = row[c];
+    if (!page_exists(v, page)) continue;
+    if (c < shared) {
+      atomicAdd(&v.refs[page], 1);
+      to[c] = page;
+    } else {
+      const int r = begin + c - shared, mine = v.fresh[r];
+      v.refs[mine] = 1;
+      v.jobs[r] = make_int2(page, mine);
+      to[c] = mine;
+    }
+  }
+}
+
+__device__ __forceinline__ void exchange_row(const KvView& v, const int* children, int i, int c0, int c_end, int thread, int n_threads) {
+  const int want = v.upto[i];
+  if (want < 0) return;
+  const int b = children[i], left = kv_pages_of(v.had[i], v.page_shift), pages = kv_pages_of(want, v.page_shift);
+  const int end = min(max(left, pages), c_end);
+  int* row = v.tables + (size_t)b * v.max_pages;
+  const int* from = v.staged + (size_t)i * v.max_pages;
+  for (int c = c0 + thread; c < end; c += n_threads) {
+    if (c < left && page_exists(v, row[c])) atomicSub(&v.refs[row[c]], 1);
+    if (c < pages) row[c] = from[c];
+  }
+  if (c0 == 0 && thread == 0) v.lengths[b] = want;
+}
+
 __global__ void __launch_bounds__(PLAN_THREADS) kv_fork_plan_kernel(const KvView v, const int* __restrict__ parents,
                                                                     const int* __restrict__ children, const int* __restrict__ upto,
-                                                                    int n, int copy) {
+                                                                    int n, int copy, int rows_too) {
   __shared__ unsigned sums[33];
   __shared__ int bad;
   grid_dep_launch_dependents();
@@ -292,13 +338,20 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_fork_plan_kernel(const KvView
   int why = bad;
   if (why == KV_OK && need > v.n_pages) why = KV_FULL;
   if (why == KV_OK && need > 0 && take_free_pages(v, (int)need, v.fresh, sums) < need) why = KV_FULL;
+  if (why != KV_OK) {
+    if (threadIdx.x == 0) kv_report(v, why);
+    return;
+  }
   if (threadIdx.x == 0) {
-    if (why != KV_OK) {
-      kv_report(v, why);
-    } else {
-      v.meta[0] = 1;
-      v.meta[1] = (int)need;
-    }
+    v.meta[0] = 1;
+    v.meta[1] = (int)need;
+  }
+  if (rows_too) {                         // a warp per row
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();
+    for (int i = warp; i < n; i += PLAN_THREADS / 32) stage_row(v, parents, i, 0, v.max_pages, lane, 32);
+    __syncthreads();
+    for (int i = warp; i < n; i += PLAN_THREADS / 32) exchange_row(v, children, i, 0, v.max_pages, lane, 32);
   }
 }
 
@@ -309,45 +362,20 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_fork_stage_kernel(const KvVie
   const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
   for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
     const int i = (int)(u / chunks), c0 = (int)(u - (long long)i * chunks) * ROW_UNIT;
-    const int want = v.upto[i];
-    if (want < 0) continue;
-    const int end = min(kv_pages_of(want, v.page_shift), c0 + ROW_UNIT), shared = v.shared[i], begin = v.begin[i];
-    const int* row = v.tables + (size_t)parents[i] * v.max_pages;
-    int* to = v.staged + (size_t)i * v.max_pages;
-    for (int c = c0 + threadIdx.x; c < end; c += COPY_THREADS) {
-      const int page = row[c];
-      if (!page_exists(v, page)) continue;
-      if (c < shared) {
-        atomicAdd(&v.refs[page], 1);
-        to[c] = page;
-      } else {
-        const int r = begin + c - shared, mine = v.fresh[r];
-        v.refs[mine] = 1;
-        v.jobs[r] = make_int2(page, mine);
-        to[c] = mine;
-      }
-    }
+    stage_row(v, parents, i, c0, c0 + ROW_UNIT, threadIdx.x, COPY_THREADS);
   }
 }
 
-__global__ void __launch_bounds__(COPY_THREADS) kv_fork_apply_kernel(const KvView v, const int* __restrict__ children, int n) {
+__global__ void __launch_bounds__(COPY_THREADS) kv_fork_apply_kernel(const KvView v, const int* __restrict__ children, int n, int rows_done) {
   grid_dep_launch_dependents();
   grid_dep_wait();
   if (v.meta[0] == 0) return;
-  const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
-  for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
-    const int i = (int)(u / chunks), c0 = (int)(u - (long long)i * chunks) * ROW_UNIT;
-    const int want = v.upto[i];
-    if (want < 0) continue;
-    const int b = children[i], left = kv_pages_of(v.had[i], v.page_shift), pages = kv_pages_of(want, v.page_shift);
-    const int end = min(max(left, pages), c0 + ROW_UNIT);
-    int* row = v.tables + (size_t)b * v.max_pages;
-    const int* from = v.staged + (size_t)i * v.max_pages;
-    for (int c = c0 + threadIdx.x; c < end; c += COPY_THREADS) {
-      if (c < left && page_exists(v, row[c])) atomicSub(&v.refs[row[c]], 1);
-      if (c < pages) row[c] = from[c];
+  if (!rows_done) {
+    const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
+    for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
+      const int i = (int)(u / chunks), c0 = (int)(u - (long long)i * chunks) * ROW_UNIT;
+      exchange_row(v, children, i, c0, c0 + ROW_UNIT, threadIdx.x, COPY_THREADS);
     }
-    if (c0 == 0 && threadIdx.x == 0) v.lengths[b] = want;
   }
   copy_pages(v, v.meta[1]);
 }
@@ -472,13 +500,15 @@ cudaError_t kv_write_launch(const KvView& v, int layer, const void* k, const voi
 
 cudaError_t kv_fork_launch(const KvView& v, const int* parents, const int* children, const int* upto, int n, int copy,
                            int sm_count, int* launches, cudaStream_t st) {
+  const bool small = (long long)n * v.max_pages <= SMALL_FORK;
   const long long rows = (long long)n * ((v.max_pages + ROW_UNIT - 1) / ROW_UNIT);
   const int most = 8 * sm_count;
-  *launches = 3;
-  cudaError_t e = launch_overlapped(kv_fork_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, 1, v, parents, children, upto, n, copy);
-  if (e == cudaSuccess)
+  *launches = small ? 2 : 3;
+  cudaError_t e = launch_overlapped(kv_fork_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, 1, v, parents, children, upto, n, copy, (int)small);
+  if (e == cudaSuccess && !small)
     e = launch_overlapped(kv_fork_stage_kernel, dim3((unsigned)(rows < most ? rows : most)), dim3(COPY_THREADS), 0, st, 1, v, parents, n);
-  if (e == cudaSuccess) e = launch_overlapped(kv_fork_apply_kernel, dim3((unsigned)most), dim3(COPY_THREADS), 0, st, 1, v, children, n);
+  if (e == cudaSuccess)
+    e = launch_overlapped(kv_fork_apply_kernel, dim3((unsigned)most), dim3(COPY_THREADS), 0, st, 1, v, children, n, (int)small);
   return e;
 }
 

@@ -140,7 +140,7 @@ class ICPagedKV:
             self._h = None
             raise ICCacheError(IC_ERR_INVALID, ic_cache_last_error())
         self._lib = lib
-        self._raw = self._stream.cuda_stream
+        self._raw, self._index = self._stream.cuda_stream, dev
         self._a = ic_kv_attend_t()
         self._a.struct_size = ctypes.sizeof(ic_kv_attend_t)
         self._ref = ctypes.byref(self._a)
@@ -168,7 +168,7 @@ class ICPagedKV:
     def _call(self, fn, args, *tensors) -> None:
         if self._h is None:
             raise ValueError("the cache is closed")
-        if torch._C._cuda_getCurrentRawStream(self.device.index) == self._raw:
+        if torch._C._cuda_getCurrentRawStream(self._index) == self._raw:
             rc = fn(self._h, *args)
         else:
             # under another stream: the handle's stream takes its turn between that stream's work
@@ -210,27 +210,30 @@ class ICPagedKV:
         self._ints(seqs, n, "seqs")
         if starts is not None:
             self._ints(starts, n + 1, "starts")
-        if k.shape != v.shape or k.dim() != 3 or k.shape[1] != self.n_kv_heads:
-            raise ValueError(f"k and v must have the same shape [tokens, {self.n_kv_heads}, {self.head_dim}]")
         k, v = self._rows(k, "k"), self._rows(v, "v")
-        if k.stride() != v.stride():
-            k, v = k.contiguous(), v.contiguous()
-            if k.stride() != v.stride():      # a dimension of size one keeps any stride
-                k, v = (torch.empty(x.shape, dtype=x.dtype, device=x.device).copy_(x) for x in (k, v))
-        self._call(self._lib.ic_kv_write, (layer, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), seqs.data_ptr(),
-                                           starts.data_ptr() if starts is not None else None, n, k.shape[0]), k, v, seqs, starts)
+        tokens, heads, _ = k.shape
+        if heads != self.n_kv_heads or v.shape != k.shape:
+            raise ValueError(f"k and v must have the same shape [tokens, {self.n_kv_heads}, {self.head_dim}]")
+        strides = k.stride()
+        if strides != v.stride():
+            k, v = (torch.empty(x.shape, dtype=x.dtype, device=x.device).copy_(x) for x in (k, v))
+            strides = k.stride()
+        self._call(self._lib.ic_kv_write, (layer, k.data_ptr(), v.data_ptr(), strides[0], strides[1], seqs.data_ptr(),
+                                           starts.data_ptr() if starts is not None else None, n, tokens), k, v, seqs, starts)
 
     def _attend(self, layer, q, seqs, starts, window, sinks, scale, out):
         n = seqs.shape[0]
         self._ints(seqs, n, "seqs")
         q = self._rows(q, "q")
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
-        given, out = out, self._rows(out, "out")
+        tokens, heads, _ = q.shape
         a = self._a
-        a.layer, a.n, a.n_heads, a.n_tokens = layer, n, q.shape[1], q.shape[0]
+        if out is None:      # (empty_like is the quicker one, where it gives what is wanted)
+            given = out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            if out.shape != q.shape:
+                raise ValueError("out must have the shape of q")
+            given, out = out, self._rows(out, "out")
+        a.layer, a.n, a.n_heads, a.n_tokens = layer, n, heads, tokens
         a.window, a.sinks, a.scale = window, sinks, self._scale if scale is None else scale
         a.q, (a.q_token_stride, a.q_head_stride, _) = q.data_ptr(), q.stride()
         a.out, (a.out_token_stride, a.out_head_stride, _) = out.data_ptr(), out.stride()
