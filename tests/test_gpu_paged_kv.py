@@ -106,6 +106,15 @@ def test_decode_long(hq, hkv, d):
     check(kv, [2, 0], [1, 1], hq, 9000, 4, decode=True)
 
 
+@pytest.mark.parametrize("hq,hkv,d,page,dtype", [(8, 1, 128, 64, F16), (8, 1, 64, 128, BF16), (16, 2, 64, 16, F16), (16, 1, 192, 32, BF16),
+                                                 (4, 1, 256, 128, BF16), (16, 1, 256, 64, F16), (16, 1, 128, 16, BF16)])
+def test_decode_many_tiles_per_cta(hq, hkv, d, page, dtype):
+    """Enough key tiles for every stage of the ring to go round many times in each CTA."""
+    kv = make([120_011, 60_000], hkv=hkv, d=d, page=page, dtype=dtype, layers=1, layer=0)
+    check(kv, [0, 1], [1, 1], hq, layer=0, decode=True)
+    check(kv, [1, 0], [1, 1], hq, 40_000, 70, layer=0, decode=True)
+
+
 def test_decode_same_sequence_twice_and_repeatable():
     kv = make([3000, 17], hkv=2, d=128)
     q = query(4, 8, 128, BF16)
@@ -130,6 +139,47 @@ def test_hidden_values_have_no_influence(value, decode):
             p = int(kv.tables[s, j // 16])
             kv.pool[p, 1, :, :, j % 16] = value
     check(kv, [0, 1, 2, 3], counts, 8, window, sinks, decode=decode)
+
+
+@pytest.mark.parametrize("hq,d,counts", [(8, 64, [40, 3]), (2, 128, [200, 100]), (4, 256, [30, 20]), (1, 64, [1, 1])])
+def test_a_nan_key_reaches_the_queries_that_see_it_and_no_others(hq, d, counts):
+    lens, at = [300, 150], [280, 120]
+    kv = make(lens, hkv=1, d=d)
+    q = query(sum(counts), hq, d, BF16)
+    want, size = attention(kv, 1, q, [0, 1], counts)
+    for s, j in enumerate(at):
+        kv.pool[int(kv.tables[s, j // 16]), 1, 0, :, j % 16, 1] = float("nan")
+    got = kv.extend(1, q, ints([0, 1]), starts_of(counts))
+    kv.sync()
+    t = 0
+    for n, f, j in zip(lens, counts, at):
+        pos = torch.arange(n - f, n, device=DEV)
+        mine = slice(t, t + f)
+        assert got[mine][pos >= j].isnan().all()
+        close(got[mine][pos < j], want[mine][pos < j], size[mine][pos < j])
+        t += f
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [50, 60]])
+def test_infinite_scores(counts):
+    """A score of plus infinity makes NaN of its rows as the formula does; one of minus infinity takes its key out."""
+    kv = make([100, 90], hkv=1, d=64)
+    kv.pool[int(kv.tables[0, 1]), 1, 0, :, 3] = torch.tensor(3e38, dtype=BF16, device=DEV)      # key 19 of sequence 0
+    q = query(sum(counts), 4, 64, BF16).abs()
+    q[:, 2:] = -q[:, 2:]
+    got = kv.extend(1, q, ints([0, 1]), starts_of(counts))
+    kv.sync()
+    a = counts[0]
+    assert got[:a, :2].isnan().all()
+    keep = torch.ones(100, dtype=torch.bool, device=DEV)
+    keep[19] = False
+    k, v = kv_util.gathered(kv, 1, 0, 100)
+    for t in range(a):
+        n = 100 - a + t + 1
+        w = torch.softmax((q[t, 2:].double() @ k[:n, 0].T / 8.0).masked_fill(~keep[:n], float("-inf")), -1)
+        close(got[t:t + 1, 2:], (w @ v[:n, 0])[None], (w @ v[:n, 0].abs())[None])
+    want, size = attention(kv, 1, q[a:], [1], counts[1:])
+    close(got[a:], want, size)
 
 
 def test_large_scores_and_scale():
