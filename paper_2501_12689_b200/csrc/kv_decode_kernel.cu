@@ -27,6 +27,8 @@ constexpr int Q_WARPS = 3;               // warps that fetch query rows
 constexpr int THREADS = (WARPS + 1 + Q_WARPS) * 32;
 constexpr int MAX_STAGES = 12;
 constexpr int AHEAD = 3;                 // batches of page numbers under way
+constexpr int WHOLE = 16;                // items of at most so many tiles are not cut (kv_schedule.cuh).  Cut everywhere | 8 | 16 | 32:
+                                         // a window of 1024, 33 sequences 53 | 49 | 47 | 47 us; of 2095, 35 sequences 64 | 65 | 59 | 61 us
 
 template <int ROWS>
 struct DecodeTail {
@@ -81,7 +83,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
   grid_dep_wait();   // queries, tables and pages come from earlier kernels in the stream
   kv_load_batch<ROWS, KEYS>(p, &t->batch);
   __syncthreads();
-  KvWalk<ROWS, KEYS> walk(p, t->batch, blockIdx.x, gridDim.x);
+  KvWalk<ROWS, KEYS, WHOLE> walk(p, t->batch, blockIdx.x, gridDim.x);
   if (walk.done()) return;
 
   if (warp == WARPS) {

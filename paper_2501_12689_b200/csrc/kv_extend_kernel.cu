@@ -38,6 +38,8 @@ constexpr int MAX_SLOTS = 8;             // of the key/value ring
 constexpr int OTHER_REGS = 72, SOFTMAX_REGS = 216;
 constexpr float RAISE = 8.0f;            // how far (log2) a row's scores may exceed its maximum before O is rescaled
 constexpr int AHEAD = 3;                 // batches of page numbers under way
+constexpr int WHOLE = 8;                 // items of at most so many tiles are not cut (kv_schedule.cuh).  Cut everywhere | 5 | 8 | 12:
+                                         // 40 prompts of up to 1000 tokens 221 | 213 | 213 | 211 us; the window of 1024 143 | 143 | 143 | 152 us
 
 // What the softmax warps need to know of an item: worked out by warp 11, ITEMS ahead at most.
 constexpr int ITEMS = 8;
@@ -48,8 +50,8 @@ struct alignas(16) Item {
   int q_first, head0;                    // that token's row of q; first query head
   int from, to, sink_tiles, first_tile;  // key tiles, as in KvWalk and KvRange
   int whole, my_slot;                    // 0: a piece of an item, and where the partial result goes
-  int piece_first, pieces, piece_slot;   // which CTAs have the others (KvWalk::Pieces)
-  int unused;
+  int piece_first, pieces;               // which CTAs have the others (KvWalk::Pieces)
+  int unused[2];
 };
 
 struct ExtendTail {
@@ -61,7 +63,6 @@ struct ExtendTail {
   uint32_t tmem_base;
   int abort_flag, last[2], left[SOFTMAX_WARPS];
   float zero;
-  float join_top[2][128], join_inv[2][128];
   KvBatch batch;
 };
 
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = t->tmem_base;
-  KvWalk<ROWS, KEYS> walk(p, t->batch, blockIdx.x, gridDim.x);
+  KvWalk<ROWS, KEYS, WHOLE> walk(p, t->batch, blockIdx.x, gridDim.x);
 
   if (warp >= SOFTMAX_WARPS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
@@ -475,7 +476,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       int s = 1, n_items = 0;
       uint32_t ph = 0;
       bool ok = true;
-      auto publish = [&](const KvWalk<ROWS, KEYS>& w) {
+      auto publish = [&](const KvWalk<ROWS, KEYS, WHOLE>& w) {
         const int at = n_items % ITEMS;
         if (ok) ok = mbar_warp_wait(&t->item_empty[at], ((n_items / ITEMS) & 1) ^ 1, &t->abort_flag);
         if (lane == 0) {
@@ -498,7 +499,6 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
               d.my_slot = w.my_slot(blockIdx.x);
               d.piece_first = pieces.first;
               d.pieces = pieces.n;
-              d.piece_slot = pieces.first_slot;
             }
           }
           t->item[at] = d;
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       };
       publish(walk);
       while (!walk.done() && ok) {
-        KvWalk<ROWS, KEYS> after = walk;
+        KvWalk<ROWS, KEYS, WHOLE> after = walk;
         after.next();
         publish(after);
         const Hidden hidden(p, t->batch.seq[walk.i]);
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           }
         }
         tc_fence_before_sync();
-        const typename KvWalk<ROWS, KEYS>::Pieces pieces{item.piece_first, item.pieces, item.piece_slot};
+        const typename KvWalk<ROWS, KEYS, WHOLE>::Pieces pieces{item.piece_first, item.pieces};
         group_sync();
         if (row == 0) {
           int* arrivals = p.arrivals + pieces.first * 2 + x;
@@ -752,12 +752,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         }
         group_sync();
         if (t->last[x]) {
-          // Join the pieces, in the order of the CTAs: first a row per thread for the common maximum and sum, then the
-          // values, four columns of a row at a time, spread over all threads however few rows there are.  They
-          // come from L2, a microsecond away: COLUMNS x FLIGHT loads are under way per thread.
-          const int rows = min(128, item.rows - x * 128);
+          // Join the pieces, in the order of the CTAs: a row per thread, FLIGHT pieces' loads of eight columns' groups
+          // under way at a time (they come from L2, a microsecond away).  Written to be short: code that runs once
+          // costs its own way from memory, and a version that spread few rows over all threads was slower for it.
           if (live) {                                // (whole batches of loads, the last piece again where there are fewer)
             float top = -INFINITY, total = 0.0f;
+#pragma unroll 1
             for (int c0 = 0; c0 < pieces.n; c0 += 8) {
               float pm[8], pl[8];
 #pragma unroll
@@ -775,58 +775,54 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
 #pragma unroll
               for (int c = 0; c < 8; ++c) total += exp2_fast(pm[c] - base) * pl[c];
             }
-            t->join_top[x][row] = top == -INFINITY ? 0.0f : top;
-            t->join_inv[x][row] = total == 0.0f ? 0.0f : 1.0f / total;
-          }
-          group_sync();
-          constexpr int COLUMNS = 4, FLIGHT = 8;
-          const int vecs = rows * (DIM / 4);
+            if (top == -INFINITY) top = 0.0f;
+            const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+            constexpr int FLIGHT = 4;
 #pragma unroll 1
-          for (int f0 = row; f0 < vecs; f0 += 128 * COLUMNS) {
-            float4 acc[COLUMNS];
+            for (int c32 = 0; c32 < DIM; c32 += 32) {
+              float4 acc[8];
 #pragma unroll
-            for (int i = 0; i < COLUMNS; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+              for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 1
-            for (int c0 = 0; c0 < pieces.n; c0 += FLIGHT) {
-              float4 y[FLIGHT][COLUMNS];
-              float w[FLIGHT][COLUMNS];
-#pragma unroll
-              for (int c = 0; c < FLIGHT; ++c) {
-                const float* from = p.partials + (size_t)pieces.slot(min(c0 + c, pieces.n - 1)) * p.partial_floats + x * 128;
-#pragma unroll
-                for (int i = 0; i < COLUMNS; ++i) {
-                  const int f = min(f0 + i * 128, vecs - 1), rf = f % rows;
-                  w[c][i] = c0 + c < pieces.n ? __ldcg(from + rf) : -INFINITY;
-                  y[c][i] = __ldcg(reinterpret_cast<const float4*>(from + 2 * ROWS - x * 128 + ((f / rows) * ROWS + x * 128 + rf) * 4));
-                }
-              }
-#pragma unroll
-              for (int i = 0; i < COLUMNS; ++i) {
-                const float base = t->join_top[x][min(f0 + i * 128, vecs - 1) % rows];
+              for (int c0 = 0; c0 < pieces.n; c0 += FLIGHT) {
+                float4 y[FLIGHT][8];
+                float w[FLIGHT];
 #pragma unroll
                 for (int c = 0; c < FLIGHT; ++c) {
-                  const float f = exp2_fast(w[c][i] - base);
-                  acc[i].x += f * y[c][i].x;
-                  acc[i].y += f * y[c][i].y;
-                  acc[i].z += f * y[c][i].z;
-                  acc[i].w += f * y[c][i].w;
+                  const float* from = p.partials + (size_t)pieces.slot(c0 + c) * p.partial_floats;
+                  w[c] = -INFINITY;
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) y[c][i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                  if (c0 + c < pieces.n) {
+                    w[c] = __ldcg(from + r);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[c][i] = __ldcg(reinterpret_cast<const float4*>(from + 2 * ROWS + ((c32 / 4 + i) * ROWS + r) * 4));
+                  }
+                }
+#pragma unroll
+                for (int c = 0; c < FLIGHT; ++c) {
+                  const float f = exp2_fast(w[c] - top) * inv;
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) {
+                    acc[i].x += f * y[c][i].x;
+                    acc[i].y += f * y[c][i].y;
+                    acc[i].z += f * y[c][i].z;
+                    acc[i].w += f * y[c][i].w;
+                  }
                 }
               }
-            }
 #pragma unroll
-            for (int i = 0; i < COLUMNS; ++i) {
-              const int f = f0 + i * 128, rf = f % rows, d = f / rows * 4;
-              if (f >= vecs || d >= v.head_dim) continue;
-              const int jr = item.row0 + x * 128 + rf, jt = kv_token_of(p, jr);
-              const float inv = t->join_inv[x][rf];
-              uint2 w;
-              w.x = pack2<F16>(acc[i].x * inv, acc[i].y * inv);
-              w.y = pack2<F16>(acc[i].z * inv, acc[i].w * inv);
-              *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + (int64_t)(item.q_first + jt) * p.out_token_stride +
-                                        (int64_t)(item.head0 + (jr - jt * p.group)) * p.out_head_stride + d) = w;
+              for (int i = 0; i < 2; ++i) {
+                uint32_t w[8];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  w[2 * y] = pack2<F16>(acc[4 * i + y].x, acc[4 * i + y].y);
+                  w[2 * y + 1] = pack2<F16>(acc[4 * i + y].z, acc[4 * i + y].w);
+                }
+                store_row<F16>(to, c32 + 16 * i, v.head_dim, w);
+              }
             }
           }
-          group_sync();                              // join_top and join_inv may be written again
         }
       }
       item = after;

@@ -31,6 +31,8 @@ constexpr int THREADS = WARPS * 32 + 32 + Q_WARPS * 32;
 // part of its share to the two that hold accumulators.  384 x 168 = 256 x 216 + 128 x 72.
 constexpr int PRODUCER_REGS = 72, CONSUMER_REGS = 216;
 constexpr int MAX_STAGES = 12;
+constexpr int WHOLE = 16;                // items of at most so many tiles are not cut (kv_schedule.cuh): 20 prompts of up to 600
+                                         // tokens, head_dim 256, 1380 us cut everywhere, 1358 so
 
 struct RowsTail {
   uint64_t full[MAX_STAGES], empty[MAX_STAGES], q_full, q_empty;
@@ -90,7 +92,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_rows_kernel(const KvAttendParam
   grid_dep_wait();   // queries, tables and pages come from earlier kernels in the stream
   kv_load_batch<ROWS, KEYS>(p, &t->batch);
   __syncthreads();
-  KvWalk<ROWS, KEYS> walk(p, t->batch, blockIdx.x, gridDim.x);
+  KvWalk<ROWS, KEYS, WHOLE> walk(p, t->batch, blockIdx.x, gridDim.x);
   if (walk.done()) return;
 
   if (warp >= WARPS) {

@@ -5,7 +5,9 @@
 // keys that any of its rows sees.  All of a launch's key tiles, in the order sequence, kv head, row
 // tile, key tile, form one line, and each CTA takes an equal stretch of it, whatever the lengths: a CTA
 // holds whole (row tile, head) items and at most two pieces of items, and the pieces of an item that
-// spans CTAs are joined by the CTA that finishes last.  Lengths live on the device, so the CTAs work the
+// spans CTAs are joined by the CTA that finishes last.  A piece costs its way through memory and the join, as much as
+// some key tiles: an item of up to WHOLE tiles, and no longer than a stretch, is not cut (the cut moves to its nearer end).
+// Lengths live on the device, so the CTAs work the
 // line out for themselves; sequences are few and their data sits in shared memory.
 #pragma once
 #include "common.cuh"
@@ -135,35 +137,50 @@ __device__ __forceinline__ long long kv_div(long long a, long long b) {
 
 // Walks a CTA's stretch of the line, item by item.  The present item's key tiles within the stretch are
 // [from, to); `left` tiles of the stretch begin with them.
-template <int ROWS, int KEYS>
+template <int ROWS, int KEYS, int WHOLE>
 struct KvWalk {
   KvSchedule<ROWS, KEYS> sched;
   int i, head, rt;                       // the item: sequence of the batch, kv head, row tile
   KvRange r;
   int from, to, left;
   long long end;                         // where the stretch ends
-  long long base;                        // each CTA's stretch is `base` long, the first `extra` ones' one more
+  long long base;                        // before cuts move, each CTA's stretch is `base` long, the first `extra` ones' one more
   int extra;
 
   __device__ KvWalk(const KvAttendParams& p, const KvBatch& b, int c, int grid) : sched(p, b) {
     const long long total = b.before[p.n];
-    const int n_ctas = (int)min((long long)grid, total);     // none is empty
+    const int n_ctas = (int)min((long long)grid, total);     // no stretch is empty before its cuts move
     left = 0;
     if (c >= n_ctas) return;
     base = kv_div(total, n_ctas);
     extra = (int)(total - base * n_ctas);
-    const long long at = begin_of(c);
-    end = begin_of(c + 1);
+    end = c + 1 == n_ctas ? total : cut(raw_begin(c + 1));
+    const long long at = c == 0 ? 0 : cut(raw_begin(c));
     left = (int)(end - at);
-    int lo = 0, hi = p.n - 1;            // the last sequence that begins at or before `at`
+    if (left == 0) return;
+    locate(at);
+    to = min(r.n, from + left);
+  }
+  __device__ __forceinline__ long long raw_begin(int c) const { return base * c + min(c, extra); }
+  // Where the cut at key tile u of the line is made.
+  __device__ __forceinline__ long long cut(long long u) {
+    locate(u);
+    if (r.n > min((long long)WHOLE, base)) return u;
+    return 2 * from < r.n ? u - from : u - from + r.n;
+  }
+  // The item of key tile u, and `from` = its place in it.  Whole warps.
+  __device__ __forceinline__ void locate(long long u) {
+    const KvBatch& b = *sched.b;
+    int lo = 0, hi = sched.p->n - 1;     // the last sequence that begins at or before u
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (b.before[mid] <= at) lo = mid;
+      if (b.before[mid] <= u) lo = mid;
       else hi = mid - 1;
     }
     i = lo;
-    long long into = at - b.before[i];
-    const long long per_head = kv_div(b.before[i + 1] - b.before[i], p.v.n_kv_heads);
+    long long into = u - b.before[i];
+    const int heads = sched.p->v.n_kv_heads;
+    const long long per_head = kv_div(b.before[i + 1] - b.before[i], heads);
     head = (int)kv_div(into, per_head);
     into -= head * per_head;
     // the row tile that `into` lies in: the warp looks at 32 of them at a time
@@ -191,12 +208,9 @@ struct KvWalk {
     }
     r = sched.range(b.seq[i], rt);
     from = (int)into;
-    to = min(r.n, from + left);
   }
-  __device__ __forceinline__ long long begin_of(int c) const { return base * c + min(c, extra); }
   __device__ __forceinline__ bool done() const { return left == 0; }
   __device__ __forceinline__ bool whole() const { return from == 0 && to == r.n; }
-  __device__ __forceinline__ long long item_at() const { return end - left - from; }     // first key tile of the item
   // On to the next item of the stretch.
   __device__ __forceinline__ void next() {
     left -= to - from;
@@ -212,26 +226,26 @@ struct KvWalk {
     from = 0;
     to = min(r.n, left);
   }
-  // The CTA whose stretch holds key tile u.
+  // The CTA whose stretch holds key tile u of an item that is cut: its own cuts have not moved, and those that
+  // have stay on their side of it.
   __device__ __forceinline__ int cta_of(long long u) const {
     const long long longer = (base + 1) * extra;
     return u < longer ? (int)kv_div(u, base + 1) : extra + (int)kv_div(u - longer, base);
   }
-  // The pieces of the present item lie with CTAs [first, first + n), in slots of the partial results.
+  // The pieces of the present item lie with CTAs [first, first + n).  A CTA has two slots for partial results: for the
+  // item that goes on into its stretch, and for the one that begins there and goes on past its end.
   struct Pieces {
-    int first, n, first_slot;
-    __device__ __forceinline__ int slot(int c) const { return c == 0 ? first_slot : (first + c) * 2; }
+    int first, n;
+    __device__ __forceinline__ int slot(int c) const { return (first + c) * 2 + (c == 0 ? 1 : 0); }
   };
   __device__ __forceinline__ Pieces pieces() const {
-    const long long u = item_at();
+    const long long u = end - left - from;             // first key tile of the item
     Pieces x;
     x.first = cta_of(u);
     x.n = cta_of(u + r.n - 1) - x.first + 1;
-    x.first_slot = x.first * 2 + (u == begin_of(x.first) ? 0 : 1);
     return x;
   }
-  // Slot for this CTA's piece: 0 for the item its stretch begins with, else 1 (the item that goes on past its end).
-  __device__ __forceinline__ int my_slot(int c) const { return c * 2 + (end - left == begin_of(c) ? 0 : 1); }
+  __device__ __forceinline__ int my_slot(int c) const { return c * 2 + (from == 0 ? 1 : 0); }
 };
 
 }  // namespace icc
