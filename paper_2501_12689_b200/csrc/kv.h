@@ -82,12 +82,9 @@ cudaError_t kv_compact_launch(const KvView& v, int sm_count, int* launches, cuda
 cudaError_t kv_pages_configure(int smem_optin);
 
 cudaError_t kv_decode_configure(int smem_optin);
+// tmap: the pool as rows of head_dim elements, box of 64 elements x min(page_size, 64) rows, 128-byte swizzle.
 // two: 16 rows per item instead of 8.
 cudaError_t kv_decode_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, bool two, int sm_count, int smem_optin, cudaStream_t st);
-cudaError_t kv_rows_configure(int smem_optin);
-size_t kv_rows_partial_floats(int head_dim);
-// tmap: the pool as rows of head_dim elements, box of 64 elements x min(page_size, 64) rows, 128-byte swizzle.
-cudaError_t kv_rows_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int sm_count, int smem_optin, cudaStream_t st);
 cudaError_t kv_extend_configure(int smem_optin);
 size_t kv_extend_partial_floats(int head_dim);
 cudaError_t kv_extend_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int sm_count, int smem_optin, cudaStream_t st);

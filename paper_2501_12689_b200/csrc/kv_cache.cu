@@ -72,7 +72,6 @@ cudaError_t configure_kernels(int dev, int smem) {
   if (dev < 64 && done[dev]) return cudaSuccess;
   cudaError_t e = icc::kv_pages_configure(smem);
   if (e == cudaSuccess) e = icc::kv_decode_configure(smem);
-  if (e == cudaSuccess) e = icc::kv_rows_configure(smem);
   if (e == cudaSuccess) e = icc::kv_extend_configure(smem);
   if (e == cudaSuccess && dev < 64) done[dev] = true;
   return e;
@@ -118,8 +117,7 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   int* fresh = ints(o->n_pages);
   int2* jobs = reinterpret_cast<int2*>(take((size_t)o->n_pages * 8));
   int* staged = ints((size_t)o->max_seqs * o->max_pages);
-  size_t partial_floats = icc::kv_rows_partial_floats(o->head_dim);
-  if (partial_floats < icc::kv_extend_partial_floats(o->head_dim)) partial_floats = icc::kv_extend_partial_floats(o->head_dim);
+  const size_t partial_floats = icc::kv_extend_partial_floats(o->head_dim);      // (the decode kernel's pieces are smaller)
   float* partials = reinterpret_cast<float*>(take(2 * icc::KV_MAX_CTAS * partial_floats * 4));
   if (kv) {
     icc::KvView* at = &kv->v;
@@ -448,8 +446,7 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
     p.n = a.n - off < icc::KV_BATCH ? a.n - off : icc::KV_BATCH;
     cudaError_t e;
     if (rows <= 16) e = icc::kv_decode_launch(p, kv->tmap, kv->f16, rows > 8, kv->sm_count, kv->smem_optin, kv->stream);
-    else if (p.v.head_dim <= 128) e = icc::kv_extend_launch(p, kv->tmap, kv->f16, kv->sm_count, kv->smem_optin, kv->stream);
-    else e = icc::kv_rows_launch(p, kv->tmap, kv->f16, kv->sm_count, kv->smem_optin, kv->stream);
+    else e = icc::kv_extend_launch(p, kv->tmap, kv->f16, kv->sm_count, kv->smem_optin, kv->stream);
     rc = launched(kv, e, 1, "attention");
   }
   return rc;

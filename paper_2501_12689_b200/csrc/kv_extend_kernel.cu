@@ -1,6 +1,6 @@
-// Attention over the paged cache for many query rows: prompts, on the tensor cores (tcgen05), head_dim <= 128.
+// Attention over the paged cache for many query rows: prompts, on the tensor cores (tcgen05).
 //
-// An item is 256 rows of one sequence and kv head (tokens times query heads of the kv head), two row tiles A and
+// Up to a head_dim of 128 an item is 256 rows of one sequence and kv head (tokens times query heads of the kv head), two row tiles A and
 // B of 128 that share every key and value fetched.  Per 64 keys (a unit) and row tile there are two products,
 // S = Q K^T and O += P V, with S, P and O in tensor memory (512 columns: two units' S of A and of B, O_A, O_B; a
 // unit's P, 16 bit, takes the first half of its S).  The same work needs 128 x 64 exponentials, for which the
@@ -10,9 +10,13 @@
 // 4,300 cycles for both row tiles and 128 keys, of which the tensor cores work 2,048.)  The price is that
 // S with 64 columns is bound by shared memory: 48 cycles a product where the tensor cores need 32.
 //
+// Of a head_dim of 129 to 256, O_A alone takes 256 columns, and there is one row tile to an item.  Its products take
+// longer than its exponentials (1,280 cycles against about 900 for 64 keys at 256), so the second row tile is not
+// missed there; what it costs is that a key fetched from L2 serves 128 rows instead of 256.
+//
 //   warps 0-3, 4-7   softmax of row tile A, B: a thread owns a row (a tensor-memory lane), and copies the row's
 //                    query into the swizzled layout of the left operand, an item ahead
-//   warp 8           loads of keys and values, 128 of each a slot: one tensor-map box per page (or 64 rows) and
+//   warp 8           loads of keys and values, 128 (64) of each a slot: one tensor-map box per page (or 64 rows) and
 //                    64-element chunk
 //   warps 9, 10      issue the products of row tile A, B: PV(u), S(u + 2), ...
 //   warp 11          zeros in place of values that nobody sees; tells the softmax warps what the next items are
@@ -20,6 +24,14 @@
 // A row's maximum is only raised when it is exceeded by more than 2^8: O is rescaled a few times per item and not
 // per unit, and weights of up to 256 are as exact as those up to 1.  Weights are rounded to the cache's
 // 16-bit type (the tensor cores take both operands in one type); their sum is taken before the rounding.
+//
+// Measured: 8 prompts of up to 4096 tokens, 32 query and 8 kv heads, head_dim 128: 0.73 ms, 0.93 PFLOP/s (0.86 ms in a
+// row of launches, where the power limit lowers the clock); one prompt of 16384 tokens up to 1.13 PFLOP/s; a window of
+// 1024 over 4 sequences 138 us; one request of few rows 38 us, of which its pieces and their join are a third.
+// head_dim 256: 20 prompts of up to 600 tokens 251 us, 8000 tokens of 8 heads 386 us, where a kernel of 32 rows an item on
+// warp-level products took 1379 and 2333 us, and 29 against 32 us for the smallest, so that there is no kernel of that kind.
+// What bounds it: the exponentials (1,760 cycles per 64 keys of both row tiles) and the change of items
+// (4,600 cycles); at a head_dim of 256 the fetches from L2.
 #include "kernels.h"
 #include "kv_mma.cuh"
 #include "kv_schedule.cuh"
@@ -29,8 +41,6 @@ namespace icc {
 
 namespace {
 
-constexpr int KEYS = 128;                // keys per tile (a slot of the ring), two units of 64
-constexpr int ROWS = 256;                // rows per item
 constexpr int SOFTMAX_WARPS = 8;
 constexpr int THREADS = 384;
 constexpr int MAX_SLOTS = 8;             // of the key/value ring
@@ -38,8 +48,19 @@ constexpr int MAX_SLOTS = 8;             // of the key/value ring
 constexpr int OTHER_REGS = 72, SOFTMAX_REGS = 216;
 constexpr float RAISE = 8.0f;            // how far (log2) a row's scores may exceed its maximum before O is rescaled
 constexpr int AHEAD = 3;                 // batches of page numbers under way
-constexpr int WHOLE = 8;                 // items of at most so many tiles are not cut (kv_schedule.cuh).  Cut everywhere | 5 | 8 | 12:
+constexpr int WHOLE_KEYS = 1024;         // items of at most so many keys are not cut (kv_schedule.cuh).  Cut everywhere | 640 | 1024 | 1536:
                                          // 40 prompts of up to 1000 tokens 221 | 213 | 213 | 211 us; the window of 1024 143 | 143 | 143 | 152 us
+
+// What follows from the head_dim, in chunks of 64.
+template <int DCH>
+struct Shape {
+  static constexpr int TILES = DCH <= 2 ? 2 : 1;               // row tiles of an item
+  static constexpr int KEYS = DCH <= 2 ? 128 : 64;             // keys per tile (a slot of the ring), in units of 64
+  static constexpr int ROWS = TILES * 128;                     // rows per item
+  static constexpr int CHUNK = KEYS * 128, Q_CHUNK = 128 * 128;        // bytes of a 64-element column chunk of keys, of a row tile
+  static constexpr int SLOT = DCH * CHUNK, Q_TILE = DCH * Q_CHUNK;
+  using Walk = KvWalk<ROWS, KEYS, WHOLE_KEYS / KEYS>;
+};
 
 // What the softmax warps need to know of an item: worked out by warp 11, ITEMS ahead at most.
 constexpr int ITEMS = 8;
@@ -66,8 +87,8 @@ struct ExtendTail {
   KvBatch batch;
 };
 
-__host__ __device__ constexpr int slot_bytes(int dch) { return dch * KEYS * 128; }
-int extend_smem(int dch, int slots) { return 1024 + ROWS * dch * 128 + slots * slot_bytes(dch) + (int)sizeof(ExtendTail); }
+template <int DCH>
+int extend_smem(int slots) { return 1024 + Shape<DCH>::TILES * Shape<DCH>::Q_TILE + slots * Shape<DCH>::SLOT + (int)sizeof(ExtendTail); }
 
 // Instruction descriptor: A and B 16-bit floats of one type, fp32 accumulator, M = 128.
 __host__ __device__ constexpr uint32_t idesc(bool f16, int n, bool b_mn_major) {
@@ -227,28 +248,30 @@ struct Hidden {
   __device__ __forceinline__ Hidden(const KvAttendParams& p, const KvSeq& s)
       : sinks(p.sinks), first_seen(p.window ? max(0, s.length - s.count - p.window + 1) : 0), length(s.length) {}
   __device__ __forceinline__ bool is(int key) const { return (key >= sinks && key < first_seen) || key >= length; }
-  __device__ __forceinline__ bool any(int key0) const {          // among the keys of a tile
-    return max(key0, sinks) < min(key0 + KEYS, first_seen) || key0 + KEYS > length;
+  __device__ __forceinline__ bool any(int key0, int keys) const {          // among the keys of a tile
+    return max(key0, sinks) < min(key0 + keys, first_seen) || key0 + keys > length;
   }
 };
 
 template <bool F16, int DCH>
 __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendParams p, const __grid_constant__ CUtensorMap tmap, int n_slots) {
   constexpr int DIM = DCH * 64;                      // head_dim, padded
-  constexpr int CHUNK = KEYS * 128;                  // bytes of a 64-element column chunk of 128 rows
-  constexpr int SLOT = slot_bytes(DCH);
-  constexpr int Q_TILE = DCH * CHUNK;                // bytes of a row tile of the query
+  using X = Shape<DCH>;
+  using Walk = typename X::Walk;
+  constexpr int TILES = X::TILES, KEYS = X::KEYS, ROWS = X::ROWS, CHUNK = X::CHUNK, Q_CHUNK = X::Q_CHUNK, SLOT = X::SLOT, Q_TILE = X::Q_TILE;
+  constexpr int UNITS = KEYS / 64;                   // of a tile
+  constexpr int AT_HAND = DCH <= 2 ? DCH : 1;        // chunks of a result in a thread's registers
   constexpr uint32_t TMEM_O = 256;                   // first column of O_A; S of A's units at 0 and 64, of B's at 128 and 192, O_B at 256 + 128
   extern __shared__ unsigned char smem_raw[];
   unsigned char* q_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  unsigned char* ring = q_smem + 2 * Q_TILE;
+  unsigned char* ring = q_smem + TILES * Q_TILE;
   ExtendTail* t = reinterpret_cast<ExtendTail*>(ring + n_slots * SLOT);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const KvView& v = p.v;
   if (tid == 0) {
     for (int s = 0; s < n_slots; ++s) {
       mbar_init(&t->full[s], 1);
-      mbar_init(&t->empty[s], 2 + (s & 1));          // row tiles A and B; and warp 11 for values, which take the odd slots
+      mbar_init(&t->empty[s], TILES + (s & 1));      // the row tiles; and warp 11 for values, which take the odd slots
       mbar_init(&t->clean[s], 1);
     }
     for (int x = 0; x < 2; ++x) {
@@ -266,7 +289,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     t->zero = 0.0f;
     for (int i = 0; i < ITEMS; ++i) {
       mbar_init(&t->item_full[i], 1);
-      mbar_init(&t->item_empty[i], SOFTMAX_WARPS);
+      mbar_init(&t->item_empty[i], 4 * TILES);
     }
     for (int w = 0; w < SOFTMAX_WARPS; ++w) t->left[w] = 0;
     mbar_fence_init();
@@ -280,7 +303,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = t->tmem_base;
-  KvWalk<ROWS, KEYS, WHOLE> walk(p, t->batch, blockIdx.x, gridDim.x);
+  Walk walk(p, t->batch, blockIdx.x, gridDim.x);
 
   if (warp >= SOFTMAX_WARPS) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
@@ -366,37 +389,30 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       }
     } else if (warp <= 10) {
       // ---------------------------------------------------------- products
-      {
+      if (warp - 9 < TILES) {
         // (a negative scale: the product with -Q, and the scale's magnitude)
-        const uint32_t id_s = idesc(F16, KEYS / 2, false) | (p.scale_log2 < 0.0f ? NEGATE_A : 0u);
+        const uint32_t id_s = idesc(F16, 64, false) | (p.scale_log2 < 0.0f ? NEGATE_A : 0u);
         constexpr uint32_t id_o = idesc(F16, DIM, true);
         const int x = warp - 9;                      // row tile
         const uint32_t on = lane == 0;
         const uint32_t s_at = tmem + x * 128, o_at = tmem + TMEM_O + x * 128;
         const uint64_t q_desc = umma_desc_k_major_sw128(smem_u32(q_smem) + x * Q_TILE), k_desc = umma_desc_k_major_sw128(smem_u32(ring)),
                        v_desc = desc_mn_major_sw128(smem_u32(ring), CHUNK);
-        int s = 0;                                   // next slot of the ring
-        uint32_t ph = 0, q_ph = 0, p_ph = 0, clean_ph = 0;
+        uint32_t q_ph = 0, p_ph = 0, clean_ph = 0;
         bool ok = true;
         auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_warp_wait(bar, parity, &t->abort_flag); };
-        auto advance = [&]() {
-          if (++s == n_slots) {
-            s = 0;
-            ph ^= 1u;
-          }
-        };
-        auto scores = [&](int slot, int half) {      // S = Q K^T, 64 of the keys
-          const uint64_t db = k_desc + (slot * (SLOT >> 4) + half * (64 * 128 >> 4));
+        auto scores = [&](int slot, int part, int half) {        // S = Q K^T, 64 of the keys, into one of the two places for S
+          const uint64_t db = k_desc + (slot * (SLOT >> 4) + part * (64 * 128 >> 4));
 #pragma unroll
           for (int c = 0; c < DCH; ++c)
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-              product_smem(s_at + half * 64, q_desc + (c * (CHUNK >> 4) + kk * 2), db + (c * (CHUNK >> 4) + kk * 2), id_s,
+              product_smem(s_at + half * 64, q_desc + (c * (Q_CHUNK >> 4) + kk * 2), db + (c * (CHUNK >> 4) + kk * 2), id_s,
                            (c | kk) != 0 ? 1u : 0u, on);
           commit_products(&t->s_full[x][half], on);
         };
-        auto values = [&](int slot, int half, bool add) {        // O (+)= P V, 64 of the keys
-          const uint64_t db = v_desc + (slot * (SLOT >> 4) + half * (64 * 128 >> 4));
+        auto values = [&](int slot, int part, int half, bool add) {        // O (+)= P V, 64 of the keys
+          const uint64_t db = v_desc + (slot * (SLOT >> 4) + part * (64 * 128 >> 4));
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk)             // 16 keys further: 8 columns of P, 2048 bytes of V
             product_tmem(o_at, s_at + half * 64 + kk * 8, db + kk * 128, id_o, (add || kk != 0) ? 1u : 0u, on);
@@ -406,60 +422,116 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           if (mine) commit_products(&t->empty[slot], on);
           else arrive_one(&t->empty[slot], on);
         };
-        for (; !walk.done() && ok; walk.next()) {
-          const KvSeq& seq = t->batch.seq[walk.i];
-          const int rows = seq.count * p.group - walk.rt * ROWS, n = walk.to - walk.from;
-          const bool mine = rows > x * 128;
-          const Hidden hidden(p, seq);
-          ok = wait(&t->full[s], ph);
-          if (mine && ok) {
-            ok = wait(&t->q_full[x], q_ph);
-            q_ph ^= 1u;
-            fence_async_shared();                    // the query's copies were ordinary writes
-            tc_fence_after_sync();
-            if (ok) {
-              scores(s, 0);
-              scores(s, 1);
+        if constexpr (UNITS == 2) {
+          int s = 0;                                 // next slot of the ring
+          uint32_t ph = 0;
+          auto advance = [&]() {
+            if (++s == n_slots) {
+              s = 0;
+              ph ^= 1u;
+            }
+          };
+          for (; !walk.done() && ok; walk.next()) {
+            const KvSeq& seq = t->batch.seq[walk.i];
+            const int rows = seq.count * p.group - walk.rt * ROWS, n = walk.to - walk.from;
+            const bool mine = rows > x * 128;
+            const Hidden hidden(p, seq);
+            ok = wait(&t->full[s], ph);
+            if (mine && ok) {
+              ok = wait(&t->q_full[x], q_ph);
+              q_ph ^= 1u;
+              fence_async_shared();                    // the query's copies were ordinary writes
+              tc_fence_after_sync();
+              if (ok) {
+                scores(s, 0, 0);
+                scores(s, 1, 1);
+              }
+            }
+            if (!ok) break;
+            done_with(s, mine);
+            advance();
+            for (int j = 0; j < n; ++j) {
+              const bool more = j + 1 < n;
+              const int sv = s;
+              const bool cleaned = hidden.any(walk.r.tile(walk.from + j) * KEYS, KEYS);
+              ok = wait(&t->full[s], ph);
+              if (ok && cleaned) {
+                ok = wait(&t->clean[sv], (clean_ph >> sv) & 1u);   // a slot's barrier turns at each use that is cleaned
+                clean_ph ^= 1u << sv;
+              }
+              if (!ok) break;
+              advance();
+              if (mine) {
+                ok = wait(&t->p_full[x][0], p_ph);
+                if (!ok) break;
+                tc_fence_after_sync();
+                values(sv, 0, 0, j > 0);
+                if (!more) commit_products(&t->o_last[x], on);
+              }
+              if (more) ok = wait(&t->full[s], ph);
+              if (mine && ok) {
+                if (more) scores(s, 0, 0);
+                ok = wait(&t->p_full[x][1], p_ph);
+                p_ph ^= 1u;
+                if (!ok) break;
+                tc_fence_after_sync();
+                values(sv, 1, 1, true);
+                done_with(sv, true);
+                if (more) scores(s, 1, 1);
+                else commit_products(&t->o_full[x], on);
+              }
+              if (!ok) break;
+              if (!mine) done_with(sv, false);
+              if (more) {
+                done_with(s, mine);
+                advance();
+              }
             }
           }
-          if (!ok) break;
-          done_with(s, mine);
-          advance();
-          for (int j = 0; j < n; ++j) {
-            const bool more = j + 1 < n;
-            const int sv = s;
-            const bool cleaned = hidden.any(walk.r.tile(walk.from + j) * KEYS);
-            ok = wait(&t->full[s], ph);
-            if (ok && cleaned) {
-              ok = wait(&t->clean[sv], (clean_ph >> sv) & 1u);   // a slot's barrier turns at each use that is cleaned
-              clean_ph ^= 1u << sv;
+        } else {
+          // One row tile, a unit a slot: S(0), S(1), PV(0), S(2), PV(1), ...  Keys and values are taken at their own paces.
+          int ks = 0, vs = 1;
+          uint32_t k_ph = 0, v_ph = 0;
+          auto advance = [&](int& s, uint32_t& ph) {
+            if ((s += 2) >= n_slots) {
+              s -= n_slots;
+              ph ^= 1u;
             }
+          };
+          auto next_scores = [&](int half) {
+            ok = wait(&t->full[ks], k_ph);
+            if (!ok) return;
+            scores(ks, 0, half);
+            done_with(ks, true);
+            advance(ks, k_ph);
+          };
+          for (; !walk.done() && ok; walk.next()) {
+            const Hidden hidden(p, t->batch.seq[walk.i]);
+            const int n = walk.to - walk.from;
+            ok = wait(&t->q_full[0], q_ph);
+            q_ph ^= 1u;
             if (!ok) break;
-            advance();
-            if (mine) {
-              ok = wait(&t->p_full[x][0], p_ph);
+            fence_async_shared();                    // the query's copies were ordinary writes
+            tc_fence_after_sync();
+            next_scores(0);
+            if (ok && n > 1) next_scores(1);
+            for (int u = 0; u < n && ok; ++u) {
+              const int half = u & 1;
+              ok = wait(&t->full[vs], v_ph);
+              if (ok && hidden.any(walk.r.tile(walk.from + u) * KEYS, KEYS)) {
+                ok = wait(&t->clean[vs], (clean_ph >> vs) & 1u);   // a slot's barrier turns at each use that is cleaned
+                clean_ph ^= 1u << vs;
+              }
+              if (ok) ok = wait(&t->p_full[0][half], (p_ph >> half) & 1u);
+              p_ph ^= 1u << half;
               if (!ok) break;
               tc_fence_after_sync();
-              values(sv, 0, j > 0);
-              if (!more) commit_products(&t->o_last[x], on);
-            }
-            if (more) ok = wait(&t->full[s], ph);
-            if (mine && ok) {
-              if (more) scores(s, 0);
-              ok = wait(&t->p_full[x][1], p_ph);
-              p_ph ^= 1u;
-              if (!ok) break;
-              tc_fence_after_sync();
-              values(sv, 1, true);
-              done_with(sv, true);
-              if (more) scores(s, 1);
-              else commit_products(&t->o_full[x], on);
-            }
-            if (!ok) break;
-            if (!mine) done_with(sv, false);
-            if (more) {
-              done_with(s, mine);
-              advance();
+              values(vs, 0, half, u > 0);
+              done_with(vs, true);
+              advance(vs, v_ph);
+              if (u == max(n - 2, 0)) commit_products(&t->o_last[0], on);
+              if (u == n - 1) commit_products(&t->o_full[0], on);
+              if (u + 2 < n) next_scores(half);
             }
           }
         }
@@ -476,7 +548,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       int s = 1, n_items = 0;
       uint32_t ph = 0;
       bool ok = true;
-      auto publish = [&](const KvWalk<ROWS, KEYS, WHOLE>& w) {
+      auto publish = [&](const Walk& w) {
         const int at = n_items % ITEMS;
         if (ok) ok = mbar_warp_wait(&t->item_empty[at], ((n_items / ITEMS) & 1) ^ 1, &t->abort_flag);
         if (lane == 0) {
@@ -509,7 +581,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       };
       publish(walk);
       while (!walk.done() && ok) {
-        KvWalk<ROWS, KEYS, WHOLE> after = walk;
+        Walk after = walk;
         after.next();
         publish(after);
         const Hidden hidden(p, t->batch.seq[walk.i]);
@@ -517,7 +589,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           const int key0 = walk.r.tile(k) * KEYS;
           ok = mbar_warp_wait(&t->full[s], ph, &t->abort_flag);
           if (!ok) break;
-          if (hidden.any(key0)) {
+          if (hidden.any(key0, KEYS)) {
             constexpr int PIECES = DCH * 8;
             for (int u = lane; u < KEYS * PIECES; u += 32) {
               const int r = u / PIECES, piece = u % PIECES;
@@ -538,7 +610,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       }
       if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
     }
-  } else {
+  } else if (warp < 4 * TILES) {
     // ------------------------------------------------------------ softmax
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
     const int x = warp >> 2, row = tid & 127;        // row tile, and row (tensor-memory lane) of this thread
@@ -565,18 +637,18 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     // A row that is not there goes along with the last one that is, and is not written.
     auto row_of = [&](const Item& d) { return d.row0 + x * 128 + min(row, d.rows - x * 128 - 1); };
     auto fetch_q = [&](const Item& d) {              // a warp's 32 rows, LANES lanes along a row
-      constexpr int LANES = DCH * 8, AT_ONCE = 32 / LANES;
+      constexpr int LANES = DCH * 8, AT_ONCE = 32 / LANES;       // (of three chunks: 24 lanes, the rest have nothing to do)
       const int rr = row_of(d), tok = kv_token_of(p, rr);
       const uint16_t* mine = reinterpret_cast<const uint16_t*>(p.q) + (int64_t)(d.q_first + tok) * p.q_token_stride +
                              (int64_t)(d.head0 + (rr - tok * p.group)) * p.q_head_stride;
       const int piece = lane % LANES, sub = lane / LANES;
       const bool there = piece * 8 < v.head_dim;
-      const uint32_t to = smem_u32(q_smem) + x * Q_TILE + (piece >> 3) * CHUNK;
+      const uint32_t to = smem_u32(q_smem) + x * Q_TILE + (piece >> 3) * Q_CHUNK;
 #pragma unroll 4
       for (int i = 0; i < 32; i += AT_ONCE) {
         const uint16_t* from = reinterpret_cast<const uint16_t*>(__shfl_sync(FULL_MASK, reinterpret_cast<unsigned long long>(mine), i + sub));
         const int r = (warp & 3) * 32 + i + sub;
-        cp_async_16(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + (there ? piece * 8 : 0), there);
+        if (sub < AT_ONCE) cp_async_16(to + r * 128 + (((piece & 7) ^ (r & 7)) << 4), from + (there ? piece * 8 : 0), there);
       }
       cp_async_arrive(&t->q_full[x]);                // when this thread's copies have landed
     };
@@ -602,16 +674,16 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       const int pos = item.first_pos + tok;
       const int lowest = __shfl_sync(FULL_MASK, pos, 0), highest = __shfl_sync(FULL_MASK, pos, 31);     // of the warp's rows
       float m = -INFINITY, l = 0.0f;
-      const int units = 2 * (item.to - item.from);
+      const int units = UNITS * (item.to - item.from);
       // The two row tiles' warps on one scheduler take turns with their exponentials: at the same time they would
       // both have them, and then both load scores and look for maxima while the special-function unit has
       // nothing to do.  A begins; what B passes on after its last unit of an item would be one too many.
-      const bool paired = item.rows > 128;
+      const bool paired = TILES == 2 && item.rows > 128;
       if (paired && x == 1) turn_pass(warp);
       bool last_seen = false;
       for (int u = 0; u < units; ++u) {
         const int half = u & 1;
-        if (ok) ok = mbar_warp_wait(&t->s_full[x][half], s_ph, &t->abort_flag);
+        if (ok) ok = mbar_warp_wait(&t->s_full[x][half], (s_ph >> half) & 1u, &t->abort_flag);
         __syncwarp();
         tc_fence_after_sync();
         uint32_t va[64];
@@ -622,8 +694,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           fetched = after.more && after.rows > x * 128;
           if (fetched) fetch_q(after);
         }
-        const int k = item.from + (u >> 1);
-        const int key0 = (k < item.sink_tiles ? k : item.first_tile + (k - item.sink_tiles)) * KEYS + half * 64, last = key0 + 63;
+        const int k = item.from + u / UNITS;
+        const int key0 = (k < item.sink_tiles ? k : item.first_tile + (k - item.sink_tiles)) * KEYS + u % UNITS * 64, last = key0 + 63;
         const bool clear = last <= lowest && (!p.window || key0 > highest - p.window || last < p.sinks);
         tmem_ld_wait_for(va);
         if (!clear) {
@@ -657,7 +729,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
             // are there; for the last unit there is a barrier of its own.
             if (ok) {
               if (u + 1 < units) {
-                ok = mbar_warp_wait(&t->s_full[x][half ^ 1], s_ph ^ (uint32_t)half, &t->abort_flag);
+                ok = mbar_warp_wait(&t->s_full[x][half ^ 1], (s_ph >> (half ^ 1)) & 1u, &t->abort_flag);
               } else {
                 ok = mbar_warp_wait(&t->o_last[x], o_ph, &t->abort_flag);
                 last_seen = true;
@@ -695,7 +767,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
         float sa, sb;
         split_pair(add_pairs(sum2[0], sum2[1]), &sa, &sb);
         l += sa + sb;
-        s_ph ^= (uint32_t)half;                      // both halves' barriers turn once per tile
+        s_ph ^= 1u << half;
       }
       if (!last_seen && ok) ok = mbar_warp_wait(&t->o_last[x], o_ph, &t->abort_flag);      // (keeps count of its rounds)
       // ---- the result, or a piece of it
@@ -706,23 +778,24 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
       uint16_t* to = reinterpret_cast<uint16_t*>(p.out) + (int64_t)(item.q_first + tok) * p.out_token_stride + (int64_t)hq * p.out_head_stride;
       if (item.whole) {
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        uint32_t o[DCH][64];
+        uint32_t o[AT_HAND][64];
 #pragma unroll
-        for (int c = 0; c < DCH; ++c) tmem_ld_32x64(o_addr + c * 64, o[c]);
+        for (int c = 0; c < AT_HAND; ++c) tmem_ld_32x64(o_addr + c * 64, o[c]);
 #pragma unroll
         for (int c = 0; c < DCH; ++c) {
-          tmem_ld_wait_for(o[c]);
+          if (c >= AT_HAND) tmem_ld_32x64(o_addr + c * 64, o[c % AT_HAND]);
+          tmem_ld_wait_for(o[c % AT_HAND]);
 #pragma unroll
           for (int i = 0; i < 64; i += 16) {
             uint32_t w[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) w[y] = pack2<F16>(__uint_as_float(o[c][i + 2 * y]) * inv, __uint_as_float(o[c][i + 2 * y + 1]) * inv);
+            for (int y = 0; y < 8; ++y) w[y] = pack2<F16>(__uint_as_float(o[c % AT_HAND][i + 2 * y]) * inv, __uint_as_float(o[c % AT_HAND][i + 2 * y + 1]) * inv);
             if (live) store_row<F16>(to, c * 64 + i, v.head_dim, w);
           }
         }
         tc_fence_before_sync();
       } else {
-        // layout of a piece: 256 maxima, 256 sums, then four columns of all rows at a time (rows that are not there
+        // layout of a piece: its rows' maxima, their sums, then four columns of all rows at a time (rows that are not there
         // are left out)
         const int r = x * 128 + row;
         float* slot = p.partials + (size_t)item.my_slot * p.partial_floats;
@@ -730,20 +803,21 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
           slot[r] = m;
           slot[ROWS + r] = l;
         }
-        uint32_t o[DCH][64];
+        uint32_t o[AT_HAND][64];
 #pragma unroll
-        for (int c = 0; c < DCH; ++c) tmem_ld_32x64(o_addr + c * 64, o[c]);
+        for (int c = 0; c < AT_HAND; ++c) tmem_ld_32x64(o_addr + c * 64, o[c]);
 #pragma unroll
         for (int c = 0; c < DCH; ++c) {
-          tmem_ld_wait_for(o[c]);
+          if (c >= AT_HAND) tmem_ld_32x64(o_addr + c * 64, o[c % AT_HAND]);
+          tmem_ld_wait_for(o[c % AT_HAND]);
           if (live) {
 #pragma unroll
             for (int i = 0; i < 64; i += 4)
-              *reinterpret_cast<uint4*>(slot + 2 * ROWS + ((c * 64 + i) / 4 * ROWS + r) * 4) = make_uint4(o[c][i], o[c][i + 1], o[c][i + 2], o[c][i + 3]);
+              *reinterpret_cast<uint4*>(slot + 2 * ROWS + ((c * 64 + i) / 4 * ROWS + r) * 4) = make_uint4(o[c % AT_HAND][i], o[c % AT_HAND][i + 1], o[c % AT_HAND][i + 2], o[c % AT_HAND][i + 3]);
           }
         }
         tc_fence_before_sync();
-        const typename KvWalk<ROWS, KEYS, WHOLE>::Pieces pieces{item.piece_first, item.pieces};
+        const typename Walk::Pieces pieces{item.piece_first, item.pieces};
         group_sync();
         if (row == 0) {
           int* arrivals = p.arrivals + pieces.first * 2 + x;
@@ -831,8 +905,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
     // passes turns on until the partner has left too (whose other waits have limits).
     __syncwarp();
     if (lane == 0) *reinterpret_cast<volatile int*>(&t->left[warp]) = 1;
-    if (!ok) {
-      if (lane == 0) kv_report(v, KV_TIMEOUT);
+    if (!ok && lane == 0) kv_report(v, KV_TIMEOUT);
+    if (!ok && TILES == 2) {
       const long long t0 = clock64();
       while (__all_sync(FULL_MASK, *reinterpret_cast<volatile int*>(&t->left[warp ^ 4]) == 0 && clock64() - t0 < 8 * WAIT_LIMIT_CYCLES)) {
         turn_pass(warp);
@@ -849,28 +923,42 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
 }
 
 template <bool F16, int DCH>
-cudaError_t launch_one(const KvAttendParams& p, const CUtensorMap& tmap, int sm_count, int smem_optin, cudaStream_t st) {
-  int slots = 2;                                     // an even number: keys take the even slots, values the odd ones
-  while (slots + 2 <= MAX_SLOTS && extend_smem(DCH, slots + 2) <= smem_optin) slots += 2;
-  return launch_overlapped(kv_extend_kernel<F16, DCH>, dim3(sm_count), dim3(THREADS), extend_smem(DCH, slots), st, 1, p, tmap, slots);
+struct Launch {
+  static constexpr auto kernel = kv_extend_kernel<F16, DCH>;
+  static cudaError_t configure(int smem_optin) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin); }
+  static cudaError_t run(const KvAttendParams& p, const CUtensorMap& tmap, int sm_count, int smem_optin, cudaStream_t st) {
+    int slots = 2;                                   // an even number: keys take the even slots, values the odd ones
+    while (slots + 2 <= MAX_SLOTS && extend_smem<DCH>(slots + 2) <= smem_optin) slots += 2;
+    return launch_overlapped(kernel, dim3(sm_count), dim3(THREADS), extend_smem<DCH>(slots), st, 1, p, tmap, slots);
+  }
+};
+
+// f(Launch<type, chunks>()) for a head_dim.
+template <bool F16, typename F>
+cudaError_t for_dim(int head_dim, F f) {
+  if (head_dim <= 64) return f(Launch<F16, 1>());
+  if (head_dim <= 128) return f(Launch<F16, 2>());
+  if (head_dim <= 192) return f(Launch<F16, 3>());
+  return f(Launch<F16, 4>());
 }
 
 }  // namespace
 
 cudaError_t kv_extend_configure(int smem_optin) {
-  cudaError_t e = cudaFuncSetAttribute(kv_extend_kernel<false, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_extend_kernel<false, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_extend_kernel<true, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(kv_extend_kernel<true, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_optin);
+  cudaError_t e = cudaSuccess;
+  auto configure = [&](auto launch) { return launch.configure(smem_optin); };
+  for (int head_dim = 64; head_dim <= 256 && e == cudaSuccess; head_dim += 64) {
+    e = for_dim<false>(head_dim, configure);
+    if (e == cudaSuccess) e = for_dim<true>(head_dim, configure);
+  }
   return e;
 }
 
-size_t kv_extend_partial_floats(int head_dim) { return head_dim <= 128 ? (size_t)ROWS * (2 + (head_dim + 63) / 64 * 64) : 0; }
+size_t kv_extend_partial_floats(int head_dim) { return (size_t)(head_dim <= 128 ? 256 : 128) * (2 + (head_dim + 63) / 64 * 64); }
 
 cudaError_t kv_extend_launch(const KvAttendParams& p, const CUtensorMap& tmap, bool f16, int sm_count, int smem_optin, cudaStream_t st) {
-  if (p.v.head_dim <= 64)
-    return f16 ? launch_one<true, 1>(p, tmap, sm_count, smem_optin, st) : launch_one<false, 1>(p, tmap, sm_count, smem_optin, st);
-  return f16 ? launch_one<true, 2>(p, tmap, sm_count, smem_optin, st) : launch_one<false, 2>(p, tmap, sm_count, smem_optin, st);
+  auto run = [&](auto launch) { return launch.run(p, tmap, sm_count, smem_optin, st); };
+  return f16 ? for_dim<true>(p.v.head_dim, run) : for_dim<false>(p.v.head_dim, run);
 }
 
 }  // namespace icc
