@@ -14,9 +14,9 @@
 // they are split in two such numbers (high part and remainder): a few more products, which are not the bound.
 //
 // Measured: 64 sequences of 900 to 8192 tokens, 32 query and 8 kv heads, head_dim 128 (1.2 GB of keys and values):
-// 212 us, 5.65 TB/s, 87 % of a copy's rate.  One sequence of 131,071 tokens, 8 kv heads: 58 us, 4.6 TB/s; of these
+// 212 us, 5.65 TB/s, 87 % of a copy's rate.  One sequence of 131,071 tokens, 4 kv heads: 57 us, 4.7 TB/s; of these
 // about 3 us pass before the first load, 6 us at the join of its pieces, and the SMs' loads end 9 us apart.  One token
-// of a short sequence: 8.8 us a call, 5.6 us of them on the GPU, launch and the chain table - page - keys - sum.
+// of a short sequence: 8.7 us a call, 5.6 us of them on the GPU, launch and the chain table - page - keys - sum.
 #include "kernels.h"
 #include "kv_mma.cuh"
 #include "kv_schedule.cuh"

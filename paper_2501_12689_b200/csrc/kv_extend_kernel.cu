@@ -27,7 +27,7 @@
 //
 // Measured: 8 prompts of up to 4096 tokens, 32 query and 8 kv heads, head_dim 128: 0.73 ms, 0.93 PFLOP/s (0.86 ms in a
 // row of launches, where the power limit lowers the clock); one prompt of 16384 tokens up to 1.13 PFLOP/s; a window of
-// 1024 over 4 sequences 138 us; one request of few rows 38 us, of which its pieces and their join are a third.
+// 1024 over one sequence of 12,289 tokens 138 us; four requests of up to 57 tokens behind up to 6,000 38 us.
 // head_dim 256: 20 prompts of up to 600 tokens 251 us, 8000 tokens of 8 heads 386 us, where a kernel of 32 rows an item on
 // warp-level products took 1379 and 2333 us, and 29 against 32 us for the smallest, so that there is no kernel of that kind.
 // What bounds it: the exponentials (1,760 cycles per 64 keys of both row tiles) and the change of items

@@ -7,7 +7,7 @@
 //
 // Nothing is computed: the bound is the bytes moved, or for few of them the launches, which overlap their predecessors'
 // tails.  Measured (us; the floor at a copy's rate in brackets): 32 K tokens appended 55 (40), forks of 48 examples with
-// copies of all pages 178 (163), a large compaction 92 (72); small calls of each kind 13 to 19, of which the host's own
+// copies of all pages 177 (163), a large compaction 94 (72); small calls of each kind 13 to 19, of which the host's own
 // part of its two to four calls is most.
 #include "common.cuh"
 #include "kernels.h"
