@@ -10,9 +10,9 @@
 // 4,300 cycles for both row tiles and 128 keys, of which the tensor cores work 2,048.)  The price is that
 // S with 64 columns is bound by shared memory: 48 cycles a product where the tensor cores need 32.
 //
-// Of a head_dim of 129 to 256, O_A alone takes 256 columns, and there is one row tile to an item.  Its products take
-// longer than its exponentials (1,280 cycles against about 900 for 64 keys at 256), so the second row tile is not
-// missed there; what it costs is that a key fetched from L2 serves 128 rows instead of 256.
+// Of a head_dim of 129 to 256, O_A alone takes 256 columns, and there is one row tile to an item.  Its products (1,280
+// cycles for 64 keys at 256) take as long as those of two row tiles at 128, but the softmax is one warp's chain of
+// latencies per scheduler, which is what bounds it: tensor cores 31 % busy, L2 22 %.
 //
 //   warps 0-3, 4-7   softmax of row tile A, B: a thread owns a row (a tensor-memory lane), and copies the row's
 //                    query into the swizzled layout of the left operand, an item ahead
@@ -31,7 +31,7 @@
 // head_dim 256: 20 prompts of up to 600 tokens 251 us, 8000 tokens of 8 heads 386 us, where a kernel of 32 rows an item on
 // warp-level products took 1379 and 2333 us, and 29 against 32 us for the smallest, so that there is no kernel of that kind.
 // What bounds it: the exponentials (1,760 cycles per 64 keys of both row tiles) and the change of items
-// (4,600 cycles); at a head_dim of 256 the fetches from L2.
+// (4,600 cycles).
 #include "kernels.h"
 #include "kv_mma.cuh"
 #include "kv_schedule.cuh"
