@@ -223,6 +223,26 @@ def test_extend_long(lens, counts, hq, hkv, d):
     check(kv, list(range(len(lens))), counts, hq, 700, 5)
 
 
+@pytest.mark.parametrize("d,page,dtype", [(136, 16, BF16), (192, 64, F16), (200, 8, F16), (256, 128, BF16)])
+def test_extend_wide_heads(d, page, dtype):
+    kv = make([3001, 1, 64, 65, 700, 0, 128], hkv=2, d=d, page=page, dtype=dtype)
+    seqs = list(range(7))
+    check(kv, seqs, [500, 1, 64, 65, 700, 0, 127], 4)                # odd and even numbers of 64 keys, whole items and pieces
+    check(kv, seqs, [2, 1, 3, 4, 129, 0, 128], 34, 100, 5)
+    check(kv, [0], [9], 8)
+    check(kv, [3, 4], [33, 300], 8, 1, 0)
+
+
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("total", [63, 64, 65, 1023, 1024, 1025, 1100, 2049])
+def test_items_about_the_length_that_is_cut(total, d):
+    lens = [total] * 41 + [7 * total]                               # decode with 1 row a sequence, extend with 20
+    kv = make(lens, hkv=1, d=d, page=64)
+    seqs = list(range(42))
+    check(kv, seqs, [1] * 42, 1, decode=True)
+    check(kv, seqs, [5] * 42, 4)
+
+
 def test_extend_many_sequences():
     rng = random.Random(5)
     lens = [rng.randint(0, 90) for _ in range(1300)]
