@@ -30,6 +30,9 @@
  *     until ic_kv_sync has reported the error and cleared it: IC_ERR_FULL or IC_ERR_INVALID, also
  *     returned by later calls as soon as the host sees it.  (ic_kv_free skips a bad number and frees
  *     the others.)
+ *   - Borrowed tables, lengths and refs are trusted to be a cache's, but where they are not, no kernel
+ *     leaves the pool and the books because of them: a length that the row cannot hold is reported as a
+ *     bad argument of the call that meets it.
  *   - One handle is bound to one stream and is not thread-safe; handles are independent.  Buffers
  *     are borrowed or owned as in ic_cache.h.  There is no CPU fallback.
  */

@@ -100,6 +100,12 @@ __device__ __forceinline__ int owner_of(const int* begin, int n, int r) {
   return lo;
 }
 
+// A length is one that the sequence's row holds.  Lent lengths that are not an earlier cache's may be anything, and
+// the rows' entries are counted by them.
+__device__ __forceinline__ bool length_fits(const KvView& v, int tokens) {
+  return tokens >= 0 && tokens <= (v.max_pages << v.page_shift);
+}
+
 // ---------------------------------------------------------------- reserve
 // One CTA: check the arguments and sum up the pages they need, find that many free pages, and only then
 // write tables, counts and lengths.
@@ -126,7 +132,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_reserve_kernel(const KvView v
       } else {
         const int had = v.lengths[s];
         const long long will = (long long)had + c;
-        if (had < 0 || will > ((long long)v.max_pages << v.page_shift)) atomicCAS(&bad, KV_OK, KV_FULL);
+        if (!length_fits(v, had)) bad = KV_INVALID;
+        else if (will > ((long long)v.max_pages << v.page_shift)) atomicCAS(&bad, KV_OK, KV_FULL);
         else mine = kv_pages_of((int)will, v.page_shift) - kv_pages_of(had, v.page_shift);
       }
     }
@@ -316,14 +323,14 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_fork_plan_kernel(const KvView
       if (a < 0 || a >= v.max_seqs || b < 0 || b >= v.max_seqs || atomicExch(&v.mark[b], 1) != 0) {
         bad = KV_INVALID;
       } else {
-        const int len = v.lengths[a], want = upto ? upto[i] : len;
-        if (want < 0 || want > len || len > ((long long)v.max_pages << v.page_shift)) {
+        const int len = v.lengths[a], had = v.lengths[b], want = upto ? upto[i] : len;
+        if (want < 0 || want > len || !length_fits(v, len) || !length_fits(v, had)) {
           bad = KV_INVALID;
         } else {
           const bool nothing = !copy && a == b && want == len;
           const int pages = kv_pages_of(want, v.page_shift);
           const int shared = copy ? 0 : (nothing ? pages : want >> v.page_shift);
-          v.had[i] = v.lengths[b];
+          v.had[i] = had;
           v.upto[i] = nothing ? -1 : want;
           v.shared[i] = shared;
           mine = pages - shared;
@@ -394,11 +401,11 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_free_kernel(const KvView v, c
   if (*v.err != KV_OK) return;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int s = seqs[i];
-    if (s < 0 || s >= v.max_seqs) {
-      if (threadIdx.x == 0) kv_report(v, KV_INVALID);
-      continue;
+    if (threadIdx.x == 0) {
+      had = 0;
+      if (s < 0 || s >= v.max_seqs || !length_fits(v, v.lengths[s])) kv_report(v, KV_INVALID);
+      else had = atomicExch(&v.lengths[s], 0);
     }
-    if (threadIdx.x == 0) had = atomicExch(&v.lengths[s], 0);
     __syncthreads();
     const int pages = kv_pages_of(had, v.page_shift);
     const int* row = v.tables + (size_t)s * v.max_pages;
@@ -417,6 +424,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_compact_plan_kernel(const KvV
   grid_dep_wait();
   if (threadIdx.x == 0) v.meta[0] = 0;
   if (*v.err != KV_OK) return;
+  int bad = 0;
+  for (int s = threadIdx.x; s < v.max_seqs; s += PLAN_THREADS) bad |= !length_fits(v, v.lengths[s]);
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) kv_report(v, KV_INVALID);
+    return;
+  }
   constexpr int ROUND = PLAN_THREADS * PAGES_PER_THREAD;
   int n_free = 0;
   for (int base = 0; base < v.n_pages; base += ROUND) {

@@ -1,0 +1,76 @@
+"""The paged key-value cache where calls go wrong or reach the ends of a type's range: refused and reported calls leave no trace,
+small weights keep their value, and calls of mixed lengths, in place, on other streams and in graphs agree with the formula."""
+import pytest
+import torch
+
+from test_gpu_paged_kv import DEV, F16, ints
+
+pytestmark = pytest.mark.gpu
+
+
+def reported(kv):
+    """The error that the kernels found, cleared."""
+    from paper_2501_12689_b200 import ICCacheError
+    with pytest.raises(ICCacheError) as e:
+        kv.sync()
+    return e.value.status
+
+
+# ---------------------------------------------------------------- lent books that are not a cache's
+class Lent:
+    """A small cache in lent tensors, each in the middle of a larger one: what surrounds them must stay.  Sequences 0, 1 and 2 of 12, 8
+    and 27 tokens, sequence 3 empty; max_pages decides how many launches a fork of three takes."""
+
+    def __init__(self, max_pages):
+        from paper_2501_12689_b200 import ICPagedKV
+        n_pages, layers, page, d, rows, edge = 24, 2, 8, 8, 4, 1024
+        self.cap = max_pages * page
+        self.all = {"tables": torch.full((rows * max_pages + 2 * edge,), -77, dtype=torch.int32, device=DEV),
+                    "lengths": torch.full((rows + 2 * edge,), -77, dtype=torch.int32, device=DEV),
+                    "refs": torch.full((n_pages + 2 * edge,), -77, dtype=torch.int32, device=DEV)}
+        inner = {name: t[edge:-edge].zero_() for name, t in self.all.items()}
+        around = torch.randn(n_pages + 16, layers, 2, 1, page, d, device=DEV, generator=torch.Generator(device=DEV).manual_seed(5)).to(F16)
+        self.all["pool"] = around
+        self.kv = ICPagedKV(n_pages, layers, 1, page, d, rows, max_pages, dtype=F16, pool=around[8:-8], tables=inner["tables"].view(rows, max_pages),
+                            lengths=inner["lengths"], refs=inner["refs"])
+        self.kv.reserve(ints([0, 1, 2]), ints([12, 8, 27]))
+        self.kv.fork(ints([2]), ints([3]), ints([16]))          # pages 3 and 4 twice
+        self.kv.free(ints([3]))
+        self.kv.sync()
+        self.keep()
+
+    def keep(self):
+        self.before = {name: t.clone() for name, t in self.all.items()}
+
+    def unchanged(self):
+        return all(torch.equal(t, self.before[name]) for name, t in self.all.items())
+
+
+LENT = pytest.mark.parametrize("max_pages", [4, 4096])          # (a fork of three rows in two launches, and in three)
+
+
+@LENT
+@pytest.mark.parametrize("length", [1, -1, 2 ** 31 - 1, -2 ** 31])
+def test_lengths_that_no_row_holds(max_pages, length):
+    from paper_2501_12689_b200 import IC_ERR_INVALID
+    x = Lent(max_pages)
+    kv = x.kv
+    kv.lengths[1] = length = x.cap + 1 if length == 1 else length
+    x.keep()
+    one = torch.ones(1, 1, 8, dtype=F16, device=DEV)
+    for call in (lambda: kv.reserve(ints([1]), ints([1])), lambda: kv.reserve(ints([0, 1]), ints([1, 0])),
+                 lambda: kv.fork(ints([1]), ints([3])), lambda: kv.fork(ints([1]), ints([3]), ints([3])), lambda: kv.fork(ints([0]), ints([1])),
+                 lambda: kv.fork(ints([0, 1, 2]), ints([2, 3, 0])), lambda: kv.fork(ints([0, 2, 0]), ints([0, 1, 3]), copy=True),
+                 lambda: kv.compact(), lambda: kv.free(ints([1])), lambda: kv.free(ints([1, 1])), lambda: kv.write(0, one, one, ints([1])),
+                 lambda: kv.decode(0, one, ints([1])), lambda: kv.extend(0, one.expand(20, 1, 8), ints([1]), ints([0, 20]))):
+        call()
+        assert reported(kv) == IC_ERR_INVALID
+        assert x.unchanged()
+    kv.free(ints([1, 0]))                                       # the others are given back
+    assert reported(kv) == IC_ERR_INVALID
+    assert kv.lengths.tolist() == [0, length, 27, 0] and kv.refs[:3].tolist() == [0, 0, 1] and kv.refs[3:7].tolist() == [1] * 4
+    kv.lengths[1] = 8                                           # as it was: all is well again
+    kv.free(ints([1]))
+    kv.compact()
+    kv.sync()
+    assert kv.lengths.tolist() == [0, 0, 27, 0] and kv.tables[2, :4].tolist() == [3, 0, 1, 2]
