@@ -230,8 +230,8 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, 
   }
 }
 
-// An owned table entry names a page of the pool.  One that does not (borrowed tables that are not an
-// earlier cache's) is reported and left alone.
+// An owned table entry names a page of the pool.  One that does not (lent tables that are not an earlier cache's) is
+// reported.
 __device__ __forceinline__ bool page_exists(const KvView& v, int page) {
   if ((unsigned)page < (unsigned)v.n_pages) return true;
   kv_report(v, KV_INVALID);
@@ -260,43 +260,55 @@ __device__ __forceinline__ void copy_pages(const KvView& v, int n_jobs) {
 
 // ---------------------------------------------------------------- fork
 // Three steps: the plan (arguments, pages needed, free pages), by one CTA; the children's new rows, made
-// beside the old ones while all parents still stand; and the exchange of rows, with the copies of pages.  The plan's
+// beside the old ones while all parents still stand; and the exchange of rows with its counts, and the copies of pages.
+// Only the last step changes the cache, and it is left out if one of the first two has found something wrong.  The plan's
 // CTA does the rows too where there are few table entries (SMALL_FORK), which saves a launch; otherwise the rows are
 // spread over CTAs, and each step is a launch.
 constexpr int SMALL_FORK = 8192;          // table entries: eight per thread of the plan's CTA, about what a launch takes
 
-// Entries c0 .. of child i's new row; n_threads threads.
-__device__ __forceinline__ void stage_row(const KvView& v, const int* parents, int i, int c0, int c_end, int thread, int n_threads) {
+// Entries c0 .. c_end of child i's new row; n_threads threads.  False if an entry that is taken over or given back names no page.
+__device__ __forceinline__ bool stage_row(const KvView& v, const int* parents, const int* children, int i, int c0, int c_end, int thread,
+                                          int n_threads) {
   const int want = v.upto[i];
-  if (want < 0) return;
-  const int end = min(kv_pages_of(want, v.page_shift), c_end), shared = v.shared[i], begin = v.begin[i];
+  if (want < 0) return true;
+  const int left = kv_pages_of(v.had[i], v.page_shift), pages = kv_pages_of(want, v.page_shift);
+  const int end = min(max(left, pages), c_end), shared = v.shared[i], begin = v.begin[i];
   const int* row = v.tables + (size_t)parents[i] * v.max_pages;
+  const int* old = v.tables + (size_t)children[i] * v.max_pages;
   int* to = v.staged + (size_t)i * v.max_pages;
+  bool fine = true;
   for (int c = c0 + thread; c < end; c += n_threads) {
-    const int page = row[c];
-    if (!page_exists(v, page)) continue;
-    if (c < shared) {
-      atomicAdd(&v.refs[page], 1);
-      to[c] = page;
-    } else {
-      const int r = begin + c - shared, mine = v.fresh[r];
-      v.refs[mine] = 1;
-      v.jobs[r] = make_int2(page, mine);
-      to[c] = mine;
+    if (c < left) fine &= page_exists(v, old[c]);
+    if (c < pages) {
+      const int page = row[c];
+      fine &= page_exists(v, page);
+      if (c < shared) {
+        to[c] = page;
+      } else {
+        const int r = begin + c - shared, mine = v.fresh[r];
+        v.jobs[r] = make_int2(page, mine);
+        to[c] = mine;
+      }
     }
   }
+  return fine;
 }
 
 __device__ __forceinline__ void exchange_row(const KvView& v, const int* children, int i, int c0, int c_end, int thread, int n_threads) {
   const int want = v.upto[i];
   if (want < 0) return;
-  const int b = children[i], left = kv_pages_of(v.had[i], v.page_shift), pages = kv_pages_of(want, v.page_shift);
+  const int b = children[i], left = kv_pages_of(v.had[i], v.page_shift), pages = kv_pages_of(want, v.page_shift), shared = v.shared[i];
   const int end = min(max(left, pages), c_end);
   int* row = v.tables + (size_t)b * v.max_pages;
   const int* from = v.staged + (size_t)i * v.max_pages;
   for (int c = c0 + thread; c < end; c += n_threads) {
-    if (c < left && page_exists(v, row[c])) atomicSub(&v.refs[row[c]], 1);
-    if (c < pages) row[c] = from[c];
+    if (c < left) atomicSub(&v.refs[row[c]], 1);
+    if (c < pages) {
+      const int page = from[c];
+      if (c < shared) atomicAdd(&v.refs[page], 1);
+      else v.refs[page] = 1;
+      row[c] = page;
+    }
   }
   if (c0 == 0 && thread == 0) v.lengths[b] = want;
 }
@@ -354,27 +366,29 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_fork_plan_kernel(const KvView
     if (threadIdx.x == 0) kv_report(v, why);
     return;
   }
+  if (rows_too) {                         // a warp per row
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();
+    bool fine = true;
+    for (int i = warp; i < n; i += PLAN_THREADS / 32) fine &= stage_row(v, parents, children, i, 0, v.max_pages, lane, 32);
+    if (!__syncthreads_and(fine)) return;
+    for (int i = warp; i < n; i += PLAN_THREADS / 32) exchange_row(v, children, i, 0, v.max_pages, lane, 32);
+  }
   if (threadIdx.x == 0) {
     v.meta[0] = 1;
     v.meta[1] = (int)need;
   }
-  if (rows_too) {                         // a warp per row
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    __syncthreads();
-    for (int i = warp; i < n; i += PLAN_THREADS / 32) stage_row(v, parents, i, 0, v.max_pages, lane, 32);
-    __syncthreads();
-    for (int i = warp; i < n; i += PLAN_THREADS / 32) exchange_row(v, children, i, 0, v.max_pages, lane, 32);
-  }
 }
 
-__global__ void __launch_bounds__(COPY_THREADS) kv_fork_stage_kernel(const KvView v, const int* __restrict__ parents, int n) {
+__global__ void __launch_bounds__(COPY_THREADS) kv_fork_stage_kernel(const KvView v, const int* __restrict__ parents,
+                                                                     const int* __restrict__ children, int n) {
   grid_dep_launch_dependents();
   grid_dep_wait();
   if (v.meta[0] == 0) return;
   const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
   for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
     const int i = (int)(u / chunks), c0 = (int)(u - (long long)i * chunks) * ROW_UNIT;
-    stage_row(v, parents, i, c0, c0 + ROW_UNIT, threadIdx.x, COPY_THREADS);
+    if (!stage_row(v, parents, children, i, c0, min(c0 + ROW_UNIT, v.max_pages), threadIdx.x, COPY_THREADS)) v.meta[0] = 0;
   }
 }
 
@@ -386,7 +400,7 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_fork_apply_kernel(const KvVie
     const int chunks = (v.max_pages + ROW_UNIT - 1) / ROW_UNIT;
     for (long long u = blockIdx.x; u < (long long)n * chunks; u += gridDim.x) {
       const int i = (int)(u / chunks), c0 = (int)(u - (long long)i * chunks) * ROW_UNIT;
-      exchange_row(v, children, i, c0, c0 + ROW_UNIT, threadIdx.x, COPY_THREADS);
+      exchange_row(v, children, i, c0, min(c0 + ROW_UNIT, v.max_pages), threadIdx.x, COPY_THREADS);
     }
   }
   copy_pages(v, v.meta[1]);
@@ -524,7 +538,7 @@ cudaError_t kv_fork_launch(const KvView& v, const int* parents, const int* child
   *launches = small ? 2 : 3;
   cudaError_t e = launch_overlapped(kv_fork_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, 1, v, parents, children, upto, n, copy, (int)small);
   if (e == cudaSuccess && !small)
-    e = launch_overlapped(kv_fork_stage_kernel, dim3((unsigned)(rows < most ? rows : most)), dim3(COPY_THREADS), 0, st, 1, v, parents, n);
+    e = launch_overlapped(kv_fork_stage_kernel, dim3((unsigned)(rows < most ? rows : most)), dim3(COPY_THREADS), 0, st, 1, v, parents, children, n);
   if (e == cudaSuccess)
     e = launch_overlapped(kv_fork_apply_kernel, dim3((unsigned)most), dim3(COPY_THREADS), 0, st, 1, v, children, n, (int)small);
   return e;

@@ -3,6 +3,7 @@ small weights keep their value, and calls of mixed lengths, in place, on other s
 import pytest
 import torch
 
+import kv_util
 from test_gpu_paged_kv import DEV, F16, ints
 
 pytestmark = pytest.mark.gpu
@@ -74,3 +75,53 @@ def test_lengths_that_no_row_holds(max_pages, length):
     kv.compact()
     kv.sync()
     assert kv.lengths.tolist() == [0, 0, 27, 0] and kv.tables[2, :4].tolist() == [3, 0, 1, 2]
+
+
+ENTRIES = pytest.mark.parametrize("entry", [-1, 24, 2 ** 31 - 1, -2 ** 31])
+
+
+@LENT
+@ENTRIES
+@pytest.mark.parametrize("at", [0, 1, 3])                       # shared pages of sequence 2, and its last one, which is copied
+def test_a_fork_of_entries_that_name_no_page(max_pages, entry, at):
+    from paper_2501_12689_b200 import IC_ERR_INVALID
+    x = Lent(max_pages)
+    kv = x.kv
+    right = int(kv.tables[2, at])
+    kv.tables[2, at] = entry
+    x.keep()
+    for call in (lambda: kv.fork(ints([2]), ints([3])), lambda: kv.fork(ints([2]), ints([3]), copy=True),
+                 lambda: kv.fork(ints([0, 2, 1]), ints([1, 3, 0])), lambda: kv.fork(ints([2, 2, 2]), ints([0, 1, 2]), copy=True),
+                 lambda: kv.fork(ints([0]), ints([2])), lambda: kv.fork(ints([0, 0, 1]), ints([2, 3, 0]), copy=True),
+                 lambda: kv.fork(ints([2]), ints([2]), ints([26]))):
+        call()
+        assert reported(kv) == IC_ERR_INVALID
+        assert x.unchanged()
+    kv.fork(ints([2, 2]), ints([3, 2]), ints([8 * at, 27]))     # what does not reach the entry is not concerned
+    kv.sync()
+    assert kv.lengths.tolist() == [12, 8, 27, 8 * at] and kv.tables[3, :at].tolist() == kv.tables[2, :at].tolist()
+    kv.fork(ints([1]), ints([3]), ints([0]))
+    kv.tables[2, at] = right
+    kv.fork(ints([2]), ints([3]))
+    kv.sync()
+    a, b = kv_util.gathered(kv, 1, 2, 27), kv_util.gathered(kv, 1, 3, 27)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert torch.equal(x.all["pool"][:8], x.before["pool"][:8]) and torch.equal(x.all["pool"][-8:], x.before["pool"][-8:])
+
+
+@LENT
+@ENTRIES
+def test_other_calls_on_entries_that_name_no_page(max_pages, entry):
+    """free leaves such an entry alone, and write the token."""
+    from paper_2501_12689_b200 import IC_ERR_INVALID
+    x = Lent(max_pages)
+    kv = x.kv
+    kv.tables[2, 3] = entry
+    x.keep()
+    one = torch.ones(1, 1, 8, dtype=F16, device=DEV)
+    kv.write(0, one, one, ints([2]))
+    assert reported(kv) == IC_ERR_INVALID
+    assert x.unchanged()
+    kv.free(ints([2, 0]))
+    assert reported(kv) == IC_ERR_INVALID
+    assert kv.lengths.tolist() == [0, 8, 0, 0] and kv.refs.tolist() == [0, 0, 1, 0, 0, 0, 1] + [0] * 17
