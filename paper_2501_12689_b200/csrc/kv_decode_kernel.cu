@@ -102,12 +102,13 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
     // A batch: tiles of one item that follow each other.  The lanes' page numbers are looked at only when the
     // batch is issued, so that nothing waits for the table before that.
     struct Batch {
-      int page;             // this lane's page number, -1 = none
+      int page;             // this lane's page number,
+      bool owned;           // if there is one
       int key, n, row;      // first key, tiles, first row of the head in a page
     };
     int k = walk.from;
     auto look = [&]() {
-      Batch b{-1, 0, 0, 0};
+      Batch b{0, false, 0, 0, 0};
       if (!walk.done()) {
         const KvSeq& s = t->batch.seq[walk.i];
         const int stop = k < walk.r.sink_tiles ? min(walk.to, walk.r.sink_tiles) : walk.to;
@@ -115,7 +116,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
         b.n = min(stop - k, per_batch);
         b.row = (p.layer * 2 * v.n_kv_heads + walk.head) << v.page_shift;
         const int entry = (b.key >> v.page_shift) + lane;
-        if (entry < kv_pages_of(s.length, v.page_shift)) b.page = v.tables[(size_t)s.slot * v.max_pages + entry];
+        b.owned = entry < kv_pages_of(s.length, v.page_shift);
+        if (b.owned) b.page = v.tables[(size_t)s.slot * v.max_pages + entry];
         k += b.n;
         if (k >= walk.to) {
           walk.next();
@@ -136,8 +138,8 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
       for (int x = 0; x + 1 < AHEAD; ++x) ahead[x] = ahead[x + 1];
       ahead[AHEAD - 1] = look();
       left -= b.n;
-      const bool exists = (unsigned)b.page < (unsigned)v.n_pages;
-      if (b.page != -1 && !exists) kv_report(v, KV_INVALID);     // a borrowed table's entry that names no page
+      const bool exists = b.owned && (unsigned)b.page < (unsigned)v.n_pages;
+      if (b.owned && !exists) kv_report(v, KV_INVALID);     // a borrowed table's entry that names no page
       const int y_page = exists ? b.page * page_rows + b.row : -1;
       const int e0 = b.key >> v.page_shift;
       for (int j = 0; j < b.n; ++j) {

@@ -125,3 +125,19 @@ def test_other_calls_on_entries_that_name_no_page(max_pages, entry):
     kv.free(ints([2, 0]))
     assert reported(kv) == IC_ERR_INVALID
     assert kv.lengths.tolist() == [0, 8, 0, 0] and kv.refs.tolist() == [0, 0, 1, 0, 0, 0, 1] + [0] * 17
+
+
+@LENT
+@ENTRIES
+@pytest.mark.parametrize("at", [0, 3])
+def test_attention_over_entries_that_name_no_page(max_pages, entry, at):
+    from paper_2501_12689_b200 import IC_ERR_INVALID
+    x = Lent(max_pages)
+    kv = x.kv
+    kv.tables[2, at] = entry
+    x.keep()
+    one = torch.ones(1, 1, 8, dtype=F16, device=DEV)
+    for call in (lambda: kv.decode(0, one, ints([2])), lambda: kv.extend(0, one.expand(27, 1, 8), ints([2]), ints([0, 27]))):
+        call()
+        assert reported(kv) == IC_ERR_INVALID
+        assert x.unchanged()
