@@ -497,7 +497,12 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_compact_apply_kernel(const Kv
     int* row = v.tables + (size_t)s * v.max_pages;
     for (int c = c0 + threadIdx.x; c < end; c += COPY_THREADS) {
       const int page = row[c];
-      if (page >= n_live && page < v.n_pages) row[c] = v.jobs[v.fresh[page]].y;
+      if (!page_exists(v, page) || page < n_live) continue;
+      // (an entry of lent tables may name a page that nobody holds: it has no rank, and its word of `fresh` may be anything)
+      const int r = v.fresh[page];
+      const int2 job = (unsigned)r < (unsigned)n_jobs ? v.jobs[r] : make_int2(-1, -1);
+      if (job.x == page) row[c] = job.y;
+      else kv_report(v, KV_INVALID);
     }
   }
   for (int r = blockIdx.x * COPY_THREADS + threadIdx.x; r < n_jobs; r += gridDim.x * COPY_THREADS) {

@@ -141,3 +141,21 @@ def test_attention_over_entries_that_name_no_page(max_pages, entry, at):
         call()
         assert reported(kv) == IC_ERR_INVALID
         assert x.unchanged()
+
+
+@LENT
+@pytest.mark.parametrize("entry", [-1, 24, 2 ** 31 - 1, -2 ** 31, 23])      # no page, and one that nobody holds
+def test_compaction_of_entries_that_do_not_move(max_pages, entry):
+    from paper_2501_12689_b200 import IC_ERR_INVALID
+    x = Lent(max_pages)
+    kv = x.kv
+    kv.free(ints([0]))                                          # 0 and 1 are free: pages 5 and 6 move there
+    kv.tables[1, 0] = entry
+    pages = kv.pool.clone()
+    kv.compact()
+    assert reported(kv) == IC_ERR_INVALID
+    assert kv.tables[1, 0] == entry and kv.tables[2, :4].tolist() == [3, 4, 0, 1] and kv.lengths.tolist() == [0, 8, 27, 0]
+    assert kv.refs.tolist() == [1] * 5 + [0] * 19
+    assert torch.equal(kv.pool[:2], pages[5:7]) and torch.equal(kv.pool[2:], pages[2:])
+    for name, edge in (("tables", 1024), ("lengths", 1024), ("refs", 1024), ("pool", 8)):
+        assert torch.equal(x.all[name][:edge], x.before[name][:edge]) and torch.equal(x.all[name][-edge:], x.before[name][-edge:])
