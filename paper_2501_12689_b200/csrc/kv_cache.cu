@@ -137,8 +137,9 @@ size_t carve(const ic_kv_opts_t* o, unsigned char* base, ic_kv* kv) {
   }
   return off;
 }
-// The words at the head of the workspace that start out as zeros: error, plan, arrivals, marks.
-size_t zero_bytes(const ic_kv_opts_t* o) { return 256 + up256(2 * icc::KV_MAX_CTAS * 4) + up256((size_t)o->max_seqs * 4); }
+// The words at the head of the workspace that start out as zeros, and that a kernel which gave up may leave otherwise:
+// error, plan, arrivals, marks.
+size_t zero_bytes(int max_seqs) { return 256 + up256(2 * icc::KV_MAX_CTAS * 4) + up256((size_t)max_seqs * 4); }
 
 int read_opts(const ic_kv_opts_t* opts, ic_kv_opts_t* o) {
   memset(o, 0, sizeof *o);
@@ -312,7 +313,7 @@ ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
     v.refs = place(o.refs, rb);
   }
   // scratch
-  const size_t need = carve(&o, nullptr, nullptr), clear = zero_bytes(&o);
+  const size_t need = carve(&o, nullptr, nullptr), clear = zero_bytes(o.max_seqs);
   if (ok && o.workspace) {
     ok = lent(o.workspace, 256, "workspace");
     if (ok && o.workspace_bytes < need) {
@@ -495,7 +496,7 @@ int ic_kv_sync(ic_kv_t* kv) {
   const int code = *reinterpret_cast<volatile int*>(kv->h_status);
   if (code == icc::KV_OK) return IC_OK;
   *kv->h_status = 0;
-  e = cudaMemsetAsync(kv->v.err, 0, sizeof(int), kv->stream);
+  e = cudaMemsetAsync(kv->v.err, 0, zero_bytes(kv->v.max_seqs), kv->stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize(kv->stream);
   if (e != cudaSuccess) return fail(IC_ERR_CUDA, "clearing the error failed: %s", cudaGetErrorString(e));
   return reported(code);

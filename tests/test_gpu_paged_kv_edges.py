@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import kv_util
-from test_gpu_paged_kv import DEV, F16, ints
+from kv_util import attention, close
+from test_gpu_paged_kv import BF16, DEV, F16, ints, make, query, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -159,3 +160,25 @@ def test_compaction_of_entries_that_do_not_move(max_pages, entry):
     assert torch.equal(kv.pool[:2], pages[5:7]) and torch.equal(kv.pool[2:], pages[2:])
     for name, edge in (("tables", 1024), ("lengths", 1024), ("refs", 1024), ("pool", 8)):
         assert torch.equal(x.all[name][:edge], x.before[name][:edge]) and torch.equal(x.all[name][-edge:], x.before[name][-edge:])
+
+
+# ---------------------------------------------------------------- after an error
+@pytest.mark.parametrize("counts", [[1, 1], [9, 7]])    # either kernel
+def test_an_error_that_is_cleared_leaves_nothing_in_the_scratch(counts):
+    """A kernel that gives up in the middle leaves counts of arrived pieces behind (the words after the first 256 bytes of the
+    workspace).  Once the error is reported and cleared, attention that is split over the length is right again: with counts
+    that are too high nobody would join the pieces, and the result would not be written."""
+    from paper_2501_12689_b200 import IC_ERR_INVALID, ICPagedKV, ic_kv_workspace_bytes
+    made = make([30_000, 7], hkv=1, d=64)
+    sizes = (made.n_pages, 2, 1, 16, 64, 2, made.max_pages)
+    space = torch.zeros(ic_kv_workspace_bytes(*sizes), dtype=torch.uint8, device=DEV)
+    kv = ICPagedKV(*sizes, pool=made.pool, tables=made.tables, lengths=made.lengths, refs=made.refs, workspace=space)
+    space[256:256 + 2 * 160 * 4].view(torch.int32).fill_(1000)
+    kv.reserve(ints([5]), ints([1]))                    # no such sequence
+    assert reported(kv) == IC_ERR_INVALID
+    q = query(sum(counts), 8, 64, BF16)
+    out = torch.full_like(q, float("nan"))
+    kv.extend(1, q, ints([0, 1]), starts_of(counts), out=out)
+    kv.sync()
+    want, size = attention(kv, 1, q, [0, 1], counts)
+    close(out, want, size)
