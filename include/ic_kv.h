@@ -109,7 +109,11 @@ int ic_kv_write(ic_kv_t* kv, int32_t layer, const void* k, const void* v, int64_
  * (all earlier tokens; or a sliding window and the first `sinks` tokens, which stay visible).
  *     out = sum_j softmax_j(scale * q.k_j) v_j        query head h reads kv head h / (n_heads / n_kv_heads)
  * A token that sees nothing (an empty sequence) gets zeros.  Scores, the softmax's maximum and sum, and
- * the weighted sum are held in fp32.
+ * the weighted sum are held in fp32.  The weights are rounded to the cache's type for the product with the
+ * values.  A call of at most 16 query rows (tokens x query heads per kv head) per sequence on average keeps
+ * what the rounding leaves over as a second number; a call of more rows does not, so that a token's last
+ * bits depend on the call that it is in.  In fp16 a key has no weight if its score is 27 nats (22 in a
+ * call of more rows) below the largest one.
  * A value that no query of the call sees (a page's unused slots, keys outside the window) has no
  * influence, whatever it holds, infinities and NaN included.
  */

@@ -10,8 +10,11 @@
 // (8 or 16 of them) are the short side: scores^T = K q^T, out^T = V^T p^T.  A warp keeps the running maximum and
 // sum of its own keys and its own out^T; they are merged once per item through shared memory.
 //
-// The weights are rounded to the cache's 16-bit type for the second product.  To lose nothing by that
-// they are split in two such numbers (high part and remainder): a few more products, which are not the bound.
+// The weights are rounded to the cache's 16-bit type for the second product.  They are split in two such numbers (high
+// part and remainder), 16 bits of each weight in bf16: a few more products, which are not the bound.  fp16 has 22 bits, but
+// no step finer than 2^-24; so there all weights carry a factor of 2^LIFT, which cancels in the division by their sum.
+// Without it, keys 10 nats below the maximum were down to 11 bits and those 17.3 nats below it had no weight at all, however many
+// they were.  With it that is so 20 and 27.7 nats below, where the result itself comes to the end of fp16.
 //
 // Measured: 64 sequences of 900 to 8192 tokens, 32 query and 8 kv heads, head_dim 128 (1.2 GB of keys and values):
 // 212 us, 5.65 TB/s, 87 % of a copy's rate.  One sequence of 131,071 tokens, 4 kv heads: 57 us, 4.7 TB/s; of these
@@ -34,6 +37,9 @@ constexpr int MAX_STAGES = 12;
 constexpr int AHEAD = 3;                 // batches of page numbers under way
 constexpr int WHOLE = 16;                // items of at most so many tiles are not cut (kv_schedule.cuh).  Cut everywhere | 8 | 16 | 32:
                                          // a window of 1024, 33 sequences 53 | 49 | 47 | 47 us; of 2095, 35 sequences 64 | 65 | 59 | 61 us
+
+template <bool F16>
+constexpr float LIFT = F16 ? 15.0f : 0.0f;          // the largest weight is 2^LIFT (fp16 ends below 2^16)
 
 template <int ROWS>
 struct DecodeTail {
@@ -336,7 +342,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_decode_kernel(const KvAttendPar
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const float base = m[b][x & 1] == -INFINITY ? 0.0f : m[b][x & 1];
+            const float base = (m[b][x & 1] == -INFINITY ? 0.0f : m[b][x & 1]) - LIFT<F16>;
             sc[b][x] = exp2_fast(sc[b][x] - base);
             l[b][x & 1] += sc[b][x];
           }

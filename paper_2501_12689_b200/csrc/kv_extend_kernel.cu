@@ -23,7 +23,8 @@
 //
 // A row's maximum is only raised when it is exceeded by more than 2^8: O is rescaled a few times per item and not
 // per unit, and weights of up to 256 are as exact as those up to 1.  Weights are rounded to the cache's
-// 16-bit type (the tensor cores take both operands in one type); their sum is taken before the rounding.
+// 16-bit type (the tensor cores take both operands in one type), once: the second number that the decode kernel adds to it would
+// double the products with the values, half of what the tensor cores do here.  Their sum is taken before the rounding.
 //
 // Measured: 8 prompts of up to 4096 tokens, 32 query and 8 kv heads, head_dim 128: 0.73 ms, 0.93 PFLOP/s (0.86 ms in a
 // row of launches, where the power limit lowers the clock); one prompt of 16384 tokens up to 1.13 PFLOP/s; a window of
@@ -47,6 +48,11 @@ constexpr int MAX_SLOTS = 8;             // of the key/value ring
 // Registers: launched with 168 a thread; the softmax warpgroups take from the third: 384 x 168 = 256 x 216 + 128 x 72.
 constexpr int OTHER_REGS = 72, SOFTMAX_REGS = 216;
 constexpr float RAISE = 8.0f;            // how far (log2) a row's scores may exceed its maximum before O is rescaled
+// fp16 has no step finer than 2^-24 and ends below 2^16: there all weights carry a factor of 2^LIFT, which cancels in the division by
+// their sum.  They keep 11 bits down to 14.5 nats below the maximum and vanish 22 nats below it (without the factor: 9.7 and 17.3).
+// A smaller RAISE would leave room for a larger factor: 6 and 9, 1.4 nats more, cost 5 % of 8 prompts of up to 4096 tokens, 4 and 11 25 %.
+template <bool F16>
+constexpr float LIFT = F16 ? 7.0f : 0.0f;
 constexpr int AHEAD = 3;                 // batches of page numbers under way
 constexpr int WHOLE_KEYS = 1024;         // items of at most so many keys are not cut (kv_schedule.cuh).  Cut everywhere | 640 | 1024 | 1536:
                                          // 40 prompts of up to 1000 tokens 221 | 213 | 213 | 211 us; the window of 1024 143 | 143 | 143 | 152 us
@@ -749,7 +755,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_extend_kernel(const KvAttendPar
             }
           }
         }
-        float base = m == -INFINITY ? 0.0f : m;
+        float base = (m == -INFINITY ? 0.0f : m) - LIFT<F16>;
         if (paired) {
           // (the zero that is read behind the wait keeps the exponentials behind it too: nothing else would; on
           // the other side the store of the weights does)

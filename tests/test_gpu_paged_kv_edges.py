@@ -182,3 +182,37 @@ def test_an_error_that_is_cleared_leaves_nothing_in_the_scratch(counts):
     kv.sync()
     want, size = attention(kv, 1, q, [0, 1], counts)
     close(out, want, size)
+
+
+# ---------------------------------------------------------------- range of the weights
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("gap", [12.0, 15.0, 16.0, 17.0, 17.5, 18.0])
+@pytest.mark.parametrize("group,count", [(2, 1), (16, 1), (4, 10)])
+def test_one_key_far_above_many(group, count, gap, dtype):
+    """A key whose score lies `gap` above 6,000 others and whose value is zero: the result is what the others add up to.  37
+    sequences of 4 kv heads are an item per SM, so that no join gives the others a maximum of their own.
+
+    The bound of `close` holds weights that are rounded once, to a unit roundoff of themselves.  In fp16 that takes a factor:
+    18 is 26 powers of two, and a weight of 2**-26 is nothing.  With 2**15, as single tokens have it, it is off by 2**-14 of
+    itself at most.  With 2**7 it stands at 2**-19, 32 steps of 2**-24, and is off by up to 2**-6, but each by its own share: the
+    spread of 0.3 nats goes over ten steps, and the mean of 6,000 such errors is 2**-6 / sqrt(3 * 6000) = 1.2e-4, a tenth of
+    the bound of 2 u + 2e-4."""
+    n, hkv, d = 6000, 4, 64
+    kv = make([n] * 37, hkv=hkv, d=d, page=64, layers=1, layer=0, dtype=dtype, poison=False)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    kv.pool[:, 0, 0] = 0.0
+    kv.pool[:, 0, 0, :, :, 1] = (0.3 * torch.randn(kv.n_pages, hkv, 64, device=DEV, generator=g)).to(dtype)
+    kv.pool[:, 0, 1] = (0.5 + torch.rand(kv.n_pages, hkv, 64, d, device=DEV, generator=g)).to(dtype)
+    first = kv.tables[:, 0].long()
+    kv.pool[first, 0, 0, :, 0, 0] = gap
+    kv.pool[first, 0, 1, :, 0] = 0.0
+    seqs, counts = list(range(37)), [count] * 37
+    q = torch.zeros(37 * count, hkv * group, d, dtype=dtype, device=DEV)
+    q[..., :2] = 1.0
+    if count == 1:
+        got = kv.decode(0, q, ints(seqs), scale=1.0)
+    else:
+        got = kv.extend(0, q, ints(seqs), starts_of(counts), scale=1.0)
+    kv.sync()
+    want, size = attention(kv, 0, q, seqs, counts, scale=1.0)
+    close(got, want, size)
