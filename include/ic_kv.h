@@ -114,6 +114,7 @@ int ic_kv_write(ic_kv_t* kv, int32_t layer, const void* k, const void* v, int64_
  * what the rounding leaves over as a second number; a call of more rows does not, so that a token's last
  * bits depend on the call that it is in.  In fp16 a key has no weight if its score is 27 nats (22 in a
  * call of more rows) below the largest one.
+ * Rows of `out` that `starts` leaves out are not written; that is reported.  Bad sequences get zeros.
  * A value that no query of the call sees (a page's unused slots, keys outside the window) has no
  * influence, whatever it holds, infinities and NaN included.
  */

@@ -55,8 +55,8 @@ struct KvAttendParams {
   const int* seqs;
   const int* starts;        // null: one token per sequence
   int n, n_heads, group, layer;
-  int64_t n_tokens;         // of the whole call: `starts` and first_token index its q
-  int first_token;          // starts null: the token of this launch's first sequence
+  int64_t n_tokens;         // of the whole call: `starts` and first_seq index its q
+  int first_seq, n_seqs;    // where in the call this launch's sequences begin (starts null: its first token), and how many that has
   int window, sinks;
   unsigned group_magic;     // x / group = x * group_magic >> group_shift for 0 <= x < 2^31
   int group_shift;

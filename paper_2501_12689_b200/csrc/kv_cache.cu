@@ -422,7 +422,7 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
   p.out_head_stride = a.out_head_stride;
   p.seqs = a.seqs;
   p.starts = a.starts;
-  p.n = a.n;
+  p.n = p.n_seqs = a.n;
   p.n_heads = a.n_heads;
   p.group = a.n_heads / kv->v.n_kv_heads;
   // division by the group as a product: with 2^b >= group, ceil(2^(31 + b) / group) is exact for 31-bit numerators
@@ -441,7 +441,7 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
   DeviceGuard guard(kv->device);
   const int64_t rows = (a.n_tokens + a.n - 1) / a.n * p.group;      // query rows of a sequence and kv head, on average
   for (int off = 0; off < a.n && rc == IC_OK; off += icc::KV_BATCH) {
-    p.first_token = off;
+    p.first_seq = off;
     p.seqs = a.seqs + off;
     p.starts = a.starts ? a.starts + off : nullptr;
     p.n = a.n - off < icc::KV_BATCH ? a.n - off : icc::KV_BATCH;

@@ -69,8 +69,11 @@ __device__ __forceinline__ void kv_load_batch(const KvAttendParams& p, KvBatch* 
     s.slot = p.seqs[i];
     bool fine = s.slot >= 0 && s.slot < p.v.max_seqs;
     s.length = fine ? p.v.lengths[s.slot] : 0;
-    long long first = p.first_token + i, end = first + 1;
+    long long first = p.first_seq + i, end = first + 1;
+    bool covered = true;               // no token is left out before the first or after the last sequence
     if (p.starts) {
+      covered = first > 0 || p.starts[i] == 0;
+      covered &= end < p.n_seqs || p.starts[i + 1] == p.n_tokens;
       first = p.starts[i];
       end = p.starts[i + 1];
     }
@@ -86,7 +89,7 @@ __device__ __forceinline__ void kv_load_batch(const KvAttendParams& p, KvBatch* 
       s.length = 0;
     }
     if (s.count > s.length && (p.starts || s.length > 0)) fine = false;     // (the one token of an empty sequence sees nothing)
-    if (!fine && blockIdx.x == 0) kv_report(p.v, KV_INVALID);
+    if (!(fine && covered) && blockIdx.x == 0) kv_report(p.v, KV_INVALID);
     b->seq[i] = s;
     const int n = sched.row_tiles(s);
     b->before[i + 1] = n == 0 ? 0 : (n == 1 ? (long long)sched.range(s, 0).n * p.v.n_kv_heads : -1);

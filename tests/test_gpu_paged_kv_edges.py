@@ -216,3 +216,27 @@ def test_one_key_far_above_many(group, count, gap, dtype):
     kv.sync()
     want, size = attention(kv, 0, q, seqs, counts, scale=1.0)
     close(got, want, size)
+
+
+# ---------------------------------------------------------------- starts that do not cover the tokens
+@pytest.mark.parametrize("n", [2, 300])                 # (one launch, and two)
+@pytest.mark.parametrize("group", [1, 40])              # either kernel
+@pytest.mark.parametrize("wrong", ["begin", "end", "past"])
+def test_starts_that_do_not_cover_the_tokens_are_reported(n, group, wrong):
+    from paper_2501_12689_b200 import IC_ERR_INVALID
+    kv = make([5] * n, hkv=1, d=64)
+    starts = starts_of([1] * n)
+    q = query(n, group, 64, BF16)
+    good = kv.extend(1, q, ints(list(range(n))), starts)
+    kv.sync()
+    if wrong == "begin":
+        starts[0] = 1
+    elif wrong == "end":
+        starts[n] = n - 1
+    else:
+        starts[n] = n + 1
+    got = kv.extend(1, q, ints(list(range(n))), starts)
+    assert reported(kv) == IC_ERR_INVALID
+    assert torch.equal(got[1:n - 1], good[1:n - 1])
+    assert torch.equal(kv.extend(1, q, ints(list(range(n))), starts_of([1] * n)), good)
+    kv.sync()
