@@ -404,7 +404,7 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
     return fail(IC_ERR_INVALID, "n_heads %d must be a multiple of n_kv_heads %d, at most 65535", a.n_heads, kv->v.n_kv_heads);
   if (a.window < 0 || a.sinks < 0) return fail(IC_ERR_INVALID, "window %d and sinks %d must not be negative", a.window, a.sinks);
   if (!isfinite(a.scale)) return fail(IC_ERR_INVALID, "scale must be finite");
-  if (a.n_tokens < 0 || a.n_tokens * (int64_t)a.n_heads > 0x7fffffffll || (!a.starts && a.n_tokens != a.n))
+  if (a.n_tokens < 0 || a.n_tokens > 0x7fffffffll / a.n_heads || (!a.starts && a.n_tokens != a.n))
     return fail(IC_ERR_INVALID, "n_tokens = %lld does not fit n = %d and n_heads = %d", (long long)a.n_tokens, a.n, a.n_heads);
   if (a.n == 0 && a.n_tokens > 0) return fail(IC_ERR_INVALID, "tokens without sequences");
   if (a.n_tokens == 0) return IC_OK;

@@ -1,5 +1,7 @@
 """The paged key-value cache where calls go wrong or reach the ends of a type's range: refused and reported calls leave no trace,
 small weights keep their value, and calls of mixed lengths, in place, on other streams and in graphs agree with the formula."""
+import ctypes
+
 import pytest
 import torch
 
@@ -239,4 +241,21 @@ def test_starts_that_do_not_cover_the_tokens_are_reported(n, group, wrong):
     assert reported(kv) == IC_ERR_INVALID
     assert torch.equal(got[1:n - 1], good[1:n - 1])
     assert torch.equal(kv.extend(1, q, ints(list(range(n))), starts_of([1] * n)), good)
+    kv.sync()
+
+
+def test_more_tokens_than_32_bits_are_refused():
+    from paper_2501_12689_b200 import IC_ERR_INVALID, paged_kv
+    kv = make([5], hkv=1, d=64)
+    q, seqs, starts = query(1, 4, 64, BF16), ints([0]), ints([0, 1])
+    a = paged_kv.ic_kv_attend_t()
+    a.struct_size = ctypes.sizeof(a)
+    a.layer, a.n, a.n_heads, a.n_tokens, a.scale = 1, 1, 4, 1 << 62, 1.0       # times 4 heads: 0 in 64 bits
+    a.q = a.out = q.data_ptr()
+    a.q_token_stride = a.out_token_stride = 256
+    a.q_head_stride = a.out_head_stride = 64
+    a.seqs, a.starts = seqs.data_ptr(), starts.data_ptr()
+    assert kv._lib.ic_kv_attend(kv._h, ctypes.byref(a)) == IC_ERR_INVALID
+    a.n_tokens = 1
+    assert kv._lib.ic_kv_attend(kv._h, ctypes.byref(a)) == 0
     kv.sync()
