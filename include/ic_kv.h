@@ -33,7 +33,8 @@
  *   - Borrowed tables, lengths and refs are trusted to be a cache's, but where they are not, no kernel
  *     leaves the pool and the books because of them: a length that the row cannot hold, or an owned entry
  *     that names no page, is reported as a bad argument of the call that meets it.  (Where it is an
- *     entry, ic_kv_free, ic_kv_write and ic_kv_compact pass over it and do the rest.)
+ *     entry, ic_kv_free and ic_kv_compact pass over it and do the rest; ic_kv_write may have stored other
+ *     tokens.)
  *   - One handle is bound to one stream and is not thread-safe; handles are independent.  Buffers
  *     are borrowed or owned as in ic_cache.h.  There is no CPU fallback.
  */

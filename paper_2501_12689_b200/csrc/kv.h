@@ -74,7 +74,7 @@ __device__ __forceinline__ int kv_token_of(const KvAttendParams& p, int row) {
 
 cudaError_t kv_reserve_launch(const KvView& v, const int* seqs, const int* counts, int n, cudaStream_t st);
 cudaError_t kv_write_launch(const KvView& v, int layer, const void* k, const void* val, int64_t token_stride, int64_t head_stride,
-                            const int* seqs, const int* starts, int n, int64_t n_tokens, int sm_count, cudaStream_t st);
+                            const int* seqs, const int* starts, int n, int64_t n_tokens, int sm_count, int* launches, cudaStream_t st);
 cudaError_t kv_fork_launch(const KvView& v, const int* parents, const int* children, const int* upto, int n, int copy,
                            int sm_count, int* launches, cudaStream_t st);
 cudaError_t kv_free_launch(const KvView& v, const int* seqs, int n, int sm_count, cudaStream_t st);

@@ -385,8 +385,10 @@ int ic_kv_write(ic_kv_t* kv, int32_t layer, const void* k, const void* v, int64_
       (rc = check_list(kv, seqs, "seqs")) != IC_OK || (starts && (rc = check_list(kv, starts, "starts")) != IC_OK))
     return rc;
   DeviceGuard guard(kv->device);
-  return launched(kv, icc::kv_write_launch(kv->v, layer, k, v, token_stride, head_stride, seqs, starts, n, n_tokens, kv->sm_count, kv->stream), 1,
-                  "write");
+  int launches = 0;
+  const cudaError_t e =
+      icc::kv_write_launch(kv->v, layer, k, v, token_stride, head_stride, seqs, starts, n, n_tokens, kv->sm_count, &launches, kv->stream);
+  return launched(kv, e, launches, "write");
 }
 
 int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {

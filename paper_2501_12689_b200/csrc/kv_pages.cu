@@ -106,6 +106,14 @@ __device__ __forceinline__ bool length_fits(const KvView& v, int tokens) {
   return tokens >= 0 && tokens <= (v.max_pages << v.page_shift);
 }
 
+// An owned table entry names a page of the pool.  One that does not (lent tables that are not an earlier cache's) is
+// reported.
+__device__ __forceinline__ bool page_exists(const KvView& v, int page) {
+  if ((unsigned)page < (unsigned)v.n_pages) return true;
+  kv_report(v, KV_INVALID);
+  return false;
+}
+
 // ---------------------------------------------------------------- reserve
 // One CTA: check the arguments and sum up the pages they need, find that many free pages, and only then
 // write tables, counts and lengths.
@@ -164,53 +172,91 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_reserve_kernel(const KvView v
 }
 
 // ---------------------------------------------------------------- write
-// TOKENS tokens per CTA.  The first threads find their token's place (sequence, position, page); then all
-// threads move 16-byte pieces.  A head's rows of one page are contiguous, so the pieces of neighbouring
-// tokens fill whole lines.
-template <int TOKENS>
+// What a write needs to be right of sequence i of the call: the sequence, where its tokens begin and end, and its length.
+struct WriteSeq {
+  int s, length;
+  int64_t begin, end;
+  bool fine;
+  __device__ __forceinline__ WriteSeq(const KvView& v, const int* seqs, const int* starts, int i, int n, int64_t n_tokens) {
+    s = seqs[i];
+    begin = starts ? starts[i] : i;
+    end = starts ? starts[i + 1] : i + 1;
+    length = 0;
+    fine = s >= 0 && s < v.max_seqs && begin <= end && (i > 0 || begin == 0) && (i + 1 < n || end == n_tokens);
+    if (fine) {
+      length = v.lengths[s];
+      fine = length_fits(v, length) && end - begin <= length;
+    }
+  }
+};
+
+__global__ void __launch_bounds__(COPY_THREADS) kv_write_check_kernel(const KvView v, const int* __restrict__ seqs, const int* __restrict__ starts,
+                                                                      int n, int64_t n_tokens) {
+  grid_dep_launch_dependents();
+  grid_dep_wait();
+  const int i = blockIdx.x * COPY_THREADS + threadIdx.x;
+  if (*v.err != KV_OK || i >= n) return;
+  if (!WriteSeq(v, seqs, starts, i, n, n_tokens).fine) kv_report(v, KV_INVALID);
+}
+
+// First byte of a token's key row of head 0, or null.
+__device__ __forceinline__ unsigned char* token_place(const KvView& v, int layer, int s, int pos) {
+  const int page = v.tables[(size_t)s * v.max_pages + (pos >> v.page_shift)];
+  if (!page_exists(v, page)) return nullptr;
+  const size_t row = (size_t)layer * 2 * v.n_kv_heads << v.page_shift;
+  return v.pool + (size_t)page * v.page_bytes + (row + (size_t)(pos & ((1 << v.page_shift) - 1))) * v.head_dim * 2;
+}
+
+// TOKENS tokens per CTA.  A bad sequence anywhere in the call means that nothing is stored, so every CTA looks over all of them,
+// one per thread, and on its way finds the places of its own tokens; more than COPY_THREADS sequences are CHECKED by a
+// kernel of their own before this one.  (Looked over here | before, us a write: 1,024 single tokens 5.4 | 5.2, 4,096 11.7 | 6.6,
+// 16,384 99 | 25; 256 and fewer take 2.2 to 2.9 here, and a launch more would add 1.2.)  Then all threads move 16-byte pieces.
+// A head's rows of one page are contiguous, so the pieces of neighbouring tokens fill whole lines.
+template <int TOKENS, bool CHECKED>
 __global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, int layer, const uint4* __restrict__ k,
                                                                 const uint4* __restrict__ val, int64_t token_stride, int64_t head_stride,
                                                                 const int* __restrict__ seqs, const int* __restrict__ starts, int n,
                                                                 int64_t n_tokens) {
-  __shared__ unsigned char* place[TOKENS];   // first byte of the token's key row of head 0, or null
+  __shared__ unsigned char* place[TOKENS];
+  __shared__ int row_of[TOKENS], pos_of[TOKENS];
   grid_dep_launch_dependents();
   grid_dep_wait();
   if (*v.err != KV_OK) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
-  for (int x = warp; x < TOKENS; x += COPY_THREADS / 32) {
-    const int64_t t = t0 + x;
-    unsigned char* at = nullptr;
-    if (t < n_tokens) {
-      // sequence of token t: the last one that starts at or before it
-      int i = (int)t, begin = (int)t, end = (int)t + 1;
-      if (starts) {
-        int below = 0;
-        for (int j = lane; j - lane < n; j += 32) below += __popc(__ballot_sync(FULL_MASK, j < n && starts[j] <= t));
-        i = below - 1;
-        begin = i >= 0 ? starts[i] : 0;
-        end = i >= 0 ? starts[i + 1] : 0;
+  if (CHECKED) {
+    const int64_t t = t0 + threadIdx.x;
+    if (threadIdx.x < TOKENS) {
+      unsigned char* at = nullptr;
+      if (t < n_tokens) {
+        const WriteSeq seq(v, seqs, starts, starts ? owner_of(starts, n, (int)t) : (int)t, n, n_tokens);
+        at = token_place(v, layer, seq.s, (int)(seq.length - seq.end + t));
       }
-      const int s = i >= 0 ? seqs[i] : -1;
-      bool fine = s >= 0 && s < v.max_seqs && t < end;
-      if (fine) {
-        const int64_t pos = (int64_t)v.lengths[s] - end + t;
-        fine = pos >= 0 && begin >= 0 && pos < ((int64_t)v.max_pages << v.page_shift);
-        if (fine) {
-          const int page = v.tables[(size_t)s * v.max_pages + (size_t)(pos >> v.page_shift)];
-          fine = page >= 0 && page < v.n_pages;
-          const size_t row = (size_t)layer * 2 * v.n_kv_heads << v.page_shift;
-          at = v.pool + (size_t)page * v.page_bytes + (row + (size_t)(pos & ((1 << v.page_shift) - 1))) * v.head_dim * 2;
-        }
-      }
-      if (!fine) {
-        at = nullptr;
-        if (lane == 0) kv_report(v, KV_INVALID);
-      }
+      place[threadIdx.x] = at;
     }
-    if (lane == 0) place[x] = at;
+  } else {
+    bool fine = true;
+    const int i = threadIdx.x;
+    if (i < n) {
+      const WriteSeq seq(v, seqs, starts, i, n, n_tokens);
+      fine = seq.fine;
+      if (fine)
+        for (int64_t t = max(seq.begin, t0); t < min(seq.end, t0 + TOKENS); ++t) {
+          const int pos = (int)(seq.length - seq.end + t);
+          if (TOKENS == 1) {
+            place[0] = token_place(v, layer, seq.s, pos);
+          } else {
+            row_of[t - t0] = seq.s;
+            pos_of[t - t0] = pos;
+          }
+        }
+    }
+    if (!__syncthreads_and(fine)) {
+      if (threadIdx.x == 0) kv_report(v, KV_INVALID);
+      return;
+    }
+    if (TOKENS > 1 && i < TOKENS) place[i] = t0 + i < n_tokens ? token_place(v, layer, row_of[i], pos_of[i]) : nullptr;
   }
-  __syncthreads();
+  if (CHECKED || TOKENS > 1) __syncthreads();
   // a thread takes one place in the tokens (keys or values, head, piece) at a time and all TOKENS tokens there: their
   // loads are under way together
   const int pieces = v.head_dim >> 3, per_token = v.n_kv_heads * pieces;
@@ -228,14 +274,6 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, 
     for (int x = 0; x < TOKENS; ++x)
       if (place[x]) *reinterpret_cast<uint4*>(place[x] + off) = w[x];
   }
-}
-
-// An owned table entry names a page of the pool.  One that does not (lent tables that are not an earlier cache's) is
-// reported.
-__device__ __forceinline__ bool page_exists(const KvView& v, int page) {
-  if ((unsigned)page < (unsigned)v.n_pages) return true;
-  kv_report(v, KV_INVALID);
-  return false;
 }
 
 // ---------------------------------------------------------------- copying whole pages
@@ -525,13 +563,18 @@ cudaError_t kv_reserve_launch(const KvView& v, const int* seqs, const int* count
 }
 
 cudaError_t kv_write_launch(const KvView& v, int layer, const void* k, const void* val, int64_t token_stride, int64_t head_stride,
-                            const int* seqs, const int* starts, int n, int64_t n_tokens, int sm_count, cudaStream_t st) {
+                            const int* seqs, const int* starts, int n, int64_t n_tokens, int sm_count, int* launches, cudaStream_t st) {
   const uint4* k4 = static_cast<const uint4*>(k);
   const uint4* v4 = static_cast<const uint4*>(val);
-  if (n_tokens <= 4 * sm_count)
-    return launch_overlapped(kv_write_kernel<1>, dim3((unsigned)n_tokens), dim3(COPY_THREADS), 0, st, 1, v, layer, k4, v4, token_stride, head_stride,
-                             seqs, starts, n, n_tokens);
-  return launch_overlapped(kv_write_kernel<8>, dim3((unsigned)((n_tokens + 7) / 8)), dim3(COPY_THREADS), 0, st, 1, v, layer, k4, v4, token_stride,
+  const bool checked = n > COPY_THREADS, single = n_tokens <= 4 * sm_count;
+  *launches = checked ? 2 : 1;
+  if (checked) {
+    const cudaError_t e = launch_overlapped(kv_write_check_kernel, dim3((unsigned)((n + COPY_THREADS - 1) / COPY_THREADS)), dim3(COPY_THREADS), 0, st, 1, v,
+                                            seqs, starts, n, n_tokens);
+    if (e != cudaSuccess) return e;
+  }
+  auto* kernel = single ? (checked ? kv_write_kernel<1, true> : kv_write_kernel<1, false>) : (checked ? kv_write_kernel<8, true> : kv_write_kernel<8, false>);
+  return launch_overlapped(kernel, dim3((unsigned)(single ? n_tokens : (n_tokens + 7) / 8)), dim3(COPY_THREADS), 0, st, 1, v, layer, k4, v4, token_stride,
                            head_stride, seqs, starts, n, n_tokens);
 }
 

@@ -259,3 +259,84 @@ def test_more_tokens_than_32_bits_are_refused():
     a.n_tokens = 1
     assert kv._lib.ic_kv_attend(kv._h, ctypes.byref(a)) == 0
     kv.sync()
+
+
+# ---------------------------------------------------------------- a write that is refused on the device
+@pytest.mark.parametrize("seqs,starts", [
+    ([0, 5, 1], [0, 8, 20, 40]),            # no such sequence
+    ([0, -1, 1], [0, 8, 20, 40]),
+    ([0, 3, 1], [0, 8, 20, 40]),            # an empty sequence has no 12 tokens
+    ([0, 1, 2], [0, 8, 20, 39]),            # a token too few
+    ([0, 1, 2], [0, 8, 20, 41]),            # and too many
+    ([0, 1, 2], [1, 8, 20, 40]),
+    ([0, 1, 2], [0, 20, 8, 40]),
+    ([0, 1, 2], [0, -8, 20, 40]),
+    ([0, 1, 2], [0, 31, 31, 40]),           # more than sequence 0 has
+])
+@pytest.mark.parametrize("many", [1, 40])
+def test_a_write_that_is_reported_stores_nothing(seqs, starts, many):
+    """`many`: how often the 40 tokens are repeated, each time in sequences of their own; the fault is in the last ones."""
+    from paper_2501_12689_b200 import IC_ERR_INVALID, ICPagedKV
+    rows = 3 * many + 1
+    kv = ICPagedKV(rows * 8, 2, 2, 8, 16, rows, 8, dtype=F16, pool=torch.zeros(rows * 8, 2, 2, 2, 8, 16, dtype=F16, device=DEV))
+    kv.reserve(ints(list(range(rows - 1))), ints([30] * (rows - 1)))
+    good_seqs = [3 * i + s for i in range(many) for s in (0, 1, 2)]
+    good_starts = [0]
+    for c in [8, 12, 20] * many:
+        good_starts.append(good_starts[-1] + c)
+    base, at = 3 * (many - 1), 40 * (many - 1)
+    bad_seqs = good_seqs[:-3] + [base + s if 0 <= s < 3 else (rows - 1 if s == 3 else (rows + 1 if s > 0 else s)) for s in seqs]
+    bad_starts = good_starts[:-4] + [at + s for s in starts]
+    if many > 1 and starts[0] == 1:
+        bad_starts = [1] + good_starts[1:]              # the first of all starts
+    elif many > 1 and starts[1] < 0:
+        bad_starts[-3] = at - 8                         # below the start before it
+    k, v = query(40 * many, 2, 16, F16, 7) + 9.0, query(40 * many, 2, 16, F16, 8) - 9.0
+    kv.write(1, k, v, ints(bad_seqs), ints(bad_starts))
+    assert reported(kv) == IC_ERR_INVALID
+    assert not kv.pool.any()
+    kv.write(1, k, v, ints(good_seqs), ints(good_starts))
+    kv.sync()
+    for s in (0, 1, 2, base, base + 2):
+        i = good_seqs.index(s)
+        c = good_starts[i + 1] - good_starts[i]
+        a, b = kv_util.gathered(kv, 1, s, 30)
+        assert torch.equal(a[30 - c:], k[good_starts[i]:good_starts[i + 1]].double()) and not a[:30 - c].any()
+        assert torch.equal(b[30 - c:], v[good_starts[i]:good_starts[i + 1]].double()) and not b[:30 - c].any()
+
+
+@pytest.mark.parametrize("n", [1, 700, 5000])
+def test_a_write_of_single_tokens_that_is_reported_stores_nothing(n):
+    from paper_2501_12689_b200 import IC_ERR_INVALID, ICPagedKV
+    kv = ICPagedKV(n + 1, 1, 1, 8, 16, n + 1, 1, dtype=F16, pool=torch.zeros(n + 1, 1, 2, 1, 8, 16, dtype=F16, device=DEV))
+    kv.reserve(ints(list(range(n))), ints([1] * n))
+    k = query(n, 1, 16, F16) + 9.0
+    for last in (n, n + 1, -7):                         # an empty sequence, and none
+        kv.write(0, k, k, ints(list(range(n - 1)) + [last]))
+        assert reported(kv) == IC_ERR_INVALID
+        assert not kv.pool.any()
+    kv.write(0, k, k, ints(list(range(n))))
+    kv.sync()
+    at = kv.tables[:n, 0].long()
+    assert torch.equal(kv.pool[at, 0, 0, 0, 0], k[:, 0]) and torch.equal(kv.pool[at, 0, 1, 0, 0], k[:, 0])
+
+
+@pytest.mark.parametrize("n", [255, 257, 600, 4099])
+def test_writes_of_many_ragged_sequences(n):
+    from paper_2501_12689_b200 import ICPagedKV
+    g = torch.Generator().manual_seed(n)
+    counts = torch.randint(0, 4, (n,), generator=g)
+    counts[n // 2] = 45
+    seqs = torch.randperm(n, generator=g)
+    kv = ICPagedKV(7 * n, 1, 1, 8, 8, n, 8, dtype=F16)
+    had = torch.randint(0, 12, (n,), generator=g)
+    kv.reserve(ints(list(range(n))), ints(had.tolist()))
+    kv.reserve(ints(seqs.tolist()), ints(counts.tolist()))
+    k, v = query(int(counts.sum()), 1, 8, F16, 7), query(int(counts.sum()), 1, 8, F16, 8)
+    kv.write(0, k, v, ints(seqs.tolist()), starts_of(counts.tolist()))
+    kv.sync()
+    who = seqs.repeat_interleave(counts).to(DEV)
+    first = (counts.cumsum(0) - counts).repeat_interleave(counts)
+    pos = had[who.cpu()].to(DEV) + (torch.arange(len(who)) - first).to(DEV)
+    page = kv.tables[who, pos // 8].long()
+    assert torch.equal(kv.pool[page, 0, 0, 0, pos % 8], k[:, 0]) and torch.equal(kv.pool[page, 0, 1, 0, pos % 8], v[:, 0])
