@@ -132,8 +132,8 @@ typedef struct ic_kv_attend {
   const void* q;        /* [n_tokens, n_heads, head_dim]: token t, head h at element         */
   int64_t q_token_stride; /*   t * q_token_stride + h * q_head_stride; 16-byte aligned,      */
   int64_t q_head_stride;  /*   strides multiples of 8 elements                               */
-  void* out;            /* the same for the result                                           */
-  int64_t out_token_stride;
+  void* out;            /* the same for the result; no two rows may overlap.  q itself, with */
+  int64_t out_token_stride; /* its strides, is fine; any other overlap with q is not         */
   int64_t out_head_stride;
   const int32_t* seqs;  /* [n]                                                               */
   const int32_t* starts;/* [n+1] ascending from 0 to n_tokens; NULL = one token per sequence */

@@ -166,10 +166,28 @@ int check_handle(ic_kv* kv) {
 
 int check_rows(const ic_kv* kv, const void* p, int64_t token_stride, int64_t head_stride, const char* what) {
   if (!p || !is_device_ptr(p, kv->device)) return fail(IC_ERR_INVALID, "%s must be a device pointer on device %d", what, kv->device);
-  if ((reinterpret_cast<uintptr_t>(p) & 15) || token_stride % 8 || head_stride % 8 || token_stride < 0 || head_stride < 0)
+  constexpr int64_t most = 1ll << 46;      // more than an address has, and times 65535 heads a 63-bit number
+  if ((reinterpret_cast<uintptr_t>(p) & 15) || token_stride % 8 || head_stride % 8 || token_stride < 0 || head_stride < 0 || token_stride > most ||
+      head_stride > most)
     return fail(IC_ERR_INVALID, "%s must be 16-byte aligned, its strides (%lld, %lld) non-negative multiples of 8 elements", what,
                 (long long)token_stride, (long long)head_stride);
   return IC_OK;
+}
+
+// Rows of `length` elements at t * token_stride + h * head_stride, t < tokens, h < heads: do two of them share an element?
+bool rows_overlap(int64_t tokens, int64_t heads, int64_t token_stride, int64_t head_stride, int64_t length) {
+  if (tokens > 1 && token_stride < length) return true;
+  if (heads > 1 && head_stride < length) return true;
+  if (tokens <= 1 || heads <= 1) return false;
+  // one within the other, as in a tensor of tokens and heads in either order
+  if ((token_stride - length) / head_stride >= heads - 1 || (head_stride - length) / token_stride >= tokens - 1) return false;
+  // otherwise: a head h further on is d tokens back, give or take less than a row
+  for (int64_t h = 1; h < heads; ++h) {
+    const int64_t d = h * head_stride / token_stride, rest = h * head_stride - d * token_stride;
+    if (d < tokens && d > 0 && rest < length) return true;
+    if (d + 1 < tokens && token_stride - rest < length) return true;
+  }
+  return false;
 }
 
 int check_list(const ic_kv* kv, const int32_t* p, const char* what) {
@@ -414,6 +432,8 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
       (rc = check_rows(kv, a.out, a.out_token_stride, a.out_head_stride, "out")) != IC_OK ||
       (rc = check_list(kv, a.seqs, "seqs")) != IC_OK || (a.starts && (rc = check_list(kv, a.starts, "starts")) != IC_OK))
     return rc;
+  if (rows_overlap(a.n_tokens, a.n_heads, a.out_token_stride, a.out_head_stride, kv->v.head_dim))
+    return fail(IC_ERR_INVALID, "rows of out overlap with strides (%lld, %lld)", (long long)a.out_token_stride, (long long)a.out_head_stride);
   icc::KvAttendParams p;
   p.v = kv->v;
   p.q = static_cast<const unsigned char*>(a.q);

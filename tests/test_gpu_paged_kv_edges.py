@@ -340,3 +340,53 @@ def test_writes_of_many_ragged_sequences(n):
     pos = had[who.cpu()].to(DEV) + (torch.arange(len(who)) - first).to(DEV)
     page = kv.tables[who, pos // 8].long()
     assert torch.equal(kv.pool[page, 0, 0, 0, pos % 8], k[:, 0]) and torch.equal(kv.pool[page, 0, 1, 0, pos % 8], v[:, 0])
+
+
+# ---------------------------------------------------------------- where results go
+@pytest.mark.parametrize("size,stride", [
+    ((3, 8, 64), (0, 64, 1)), ((3, 8, 64), (512, 0, 1)), ((3, 8, 64), (512, 32, 1)), ((3, 8, 64), (64, 64, 1)), ((3, 8, 64), (448, 64, 1)),
+    ((3, 8, 64), (64, 128, 1)), ((3, 8, 64), (192, 136, 1))])
+def test_results_that_overlap_are_refused(size, stride):
+    from paper_2501_12689_b200 import IC_ERR_INVALID, ICCacheError
+    kv = make([100, 33, 5], hkv=2, d=64)
+    q = query(3, 8, 64, BF16)
+    out = torch.zeros(5000, dtype=BF16, device=DEV).as_strided(size, stride)
+    with pytest.raises(ICCacheError) as e:
+        kv.decode(1, q, ints([0, 1, 2]), out=out)
+    assert e.value.status == IC_ERR_INVALID
+    kv.sync()
+
+
+@pytest.mark.parametrize("stride", [(64, 192, 1), (512, 64, 1), (192, 576, 1), (128, 448, 1), (256, 64 * 12 + 128, 1)])
+def test_results_that_interleave_are_taken(stride):
+    """Heads outermost, or tokens and heads in turn, with no value in common."""
+    kv = make([100, 33, 5], hkv=2, d=64)
+    q = query(3, 8, 64, BF16)
+    out = torch.zeros(9000, dtype=BF16, device=DEV).as_strided((3, 8, 64), stride)
+    kv.decode(1, q, ints([0, 1, 2]), out=out)
+    assert torch.equal(out, kv.decode(1, q, ints([0, 1, 2])))
+    kv.sync()
+
+
+def test_results_of_one_token_or_head_may_have_any_stride():
+    kv = make([100], hkv=1, d=64)
+    q = query(1, 4, 64, BF16)
+    out = torch.zeros(256, dtype=BF16, device=DEV).as_strided((1, 4, 64), (0, 64, 1))
+    kv.decode(1, q, ints([0]), out=out)
+    assert torch.equal(out, kv.decode(1, q, ints([0])))
+    one = torch.zeros(64, dtype=BF16, device=DEV).as_strided((1, 1, 64), (0, 0, 1))
+    kv.decode(1, q[:, :1], ints([0]), out=one)
+    assert torch.equal(one, kv.decode(1, q[:, :1], ints([0])))
+    kv.sync()
+
+
+@pytest.mark.parametrize("lens,counts,hq,hkv,d", [([3000, 17, 700], [1, 1, 1], 8, 2, 128), ([40_001, 5], [1, 1], 8, 1, 64),
+                                                  ([3000, 170, 700], [300, 160, 7], 8, 2, 128), ([9000, 100], [50, 100], 16, 2, 256)])
+def test_results_in_the_place_of_the_queries(lens, counts, hq, hkv, d):
+    kv = make(lens, hkv=hkv, d=d)
+    seqs = ints(list(range(len(lens))))
+    q = query(sum(counts), hq, d, BF16)
+    want = kv.extend(1, q, seqs, starts_of(counts))
+    got = kv.extend(1, q, seqs, starts_of(counts), out=q)
+    kv.sync()
+    assert got is q and torch.equal(q, want)
