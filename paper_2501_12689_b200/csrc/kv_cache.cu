@@ -35,33 +35,43 @@ struct ic_kv {
 namespace {
 
 // Mapped host words for the handles' errors.  Allocating pinned memory takes longer than everything else in a
-// creation, so one page of words serves all handles of the process; it is never given back.
-constexpr int STATUS_WORDS = 1024;
+// creation, so a block of words serves many handles of the process; blocks are never given back.
+struct StatusBlock {
+  static constexpr int WORDS = 1024;
+  int* words = nullptr;
+  bool used[WORDS] = {};
+  StatusBlock* next = nullptr;
+};
 std::mutex g_status_mutex;
-int* g_status_words = nullptr;
-bool g_status_used[STATUS_WORDS] = {};
+StatusBlock* g_status_blocks = nullptr;
 
 int* take_status_word() {
   std::lock_guard<std::mutex> lock(g_status_mutex);
-  if (!g_status_words) {
-    void* p = nullptr;
-    if (cudaHostAlloc(&p, STATUS_WORDS * sizeof(int), cudaHostAllocMapped | cudaHostAllocPortable) != cudaSuccess) {
-      cudaGetLastError();
-      return nullptr;
+  for (StatusBlock* b = g_status_blocks;; b = b->next) {
+    if (!b) {
+      void* p = nullptr;
+      b = new (std::nothrow) StatusBlock;
+      if (!b || cudaHostAlloc(&p, StatusBlock::WORDS * sizeof(int), cudaHostAllocMapped | cudaHostAllocPortable) != cudaSuccess) {
+        cudaGetLastError();
+        delete b;
+        return nullptr;
+      }
+      b->words = static_cast<int*>(p);
+      b->next = g_status_blocks;
+      g_status_blocks = b;
     }
-    g_status_words = static_cast<int*>(p);
+    for (int i = 0; i < StatusBlock::WORDS; ++i)
+      if (!b->used[i]) {
+        b->used[i] = true;
+        b->words[i] = 0;
+        return b->words + i;
+      }
   }
-  for (int i = 0; i < STATUS_WORDS; ++i)
-    if (!g_status_used[i]) {
-      g_status_used[i] = true;
-      g_status_words[i] = 0;
-      return g_status_words + i;
-    }
-  return nullptr;
 }
 void give_status_word(int* w) {
   std::lock_guard<std::mutex> lock(g_status_mutex);
-  g_status_used[w - g_status_words] = false;
+  for (StatusBlock* b = g_status_blocks; b; b = b->next)
+    if (w >= b->words && w < b->words + StatusBlock::WORDS) b->used[w - b->words] = false;
 }
 
 // The kernels' shared-memory limits, once per device.

@@ -390,3 +390,24 @@ def test_results_in_the_place_of_the_queries(lens, counts, hq, hkv, d):
     got = kv.extend(1, q, seqs, starts_of(counts), out=q)
     kv.sync()
     assert got is q and torch.equal(q, want)
+
+
+# ---------------------------------------------------------------- many handles
+def test_many_handles_at_once():
+    """More than a thousand caches; an error stays with the one that met it."""
+    from paper_2501_12689_b200 import IC_ERR_FULL, ICPagedKV, ic_kv_workspace_bytes
+    sizes = (2, 1, 1, 8, 8, 1, 2)
+    space = torch.empty(ic_kv_workspace_bytes(*sizes), dtype=torch.uint8, device=DEV)      # lent to all, as they are used in turn
+    all_of = [ICPagedKV(*sizes, dtype=F16, workspace=space) for _ in range(2100)]
+    for i in (0, 1023, 1024, 2099):
+        all_of[i].reserve(ints([0]), ints([9]))
+        all_of[i].sync()
+        all_of[i].reserve(ints([0]), ints([9]))
+        assert reported(all_of[i]) == IC_ERR_FULL
+    for i in (1, 1022, 1025, 2098):
+        all_of[i].sync()
+    for kv in all_of:
+        kv.close()
+    with ICPagedKV(*sizes, dtype=F16, workspace=space) as kv:
+        kv.reserve(ints([0]), ints([9]))
+        kv.sync()
