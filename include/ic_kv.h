@@ -127,7 +127,7 @@ typedef struct ic_kv_attend {
   int64_t n_tokens;     /* tokens in all                                                     */
   int32_t window;       /* >= 0; 0 = no window                                               */
   int32_t sinks;        /* >= 0; without a window it changes nothing                         */
-  float scale;          /* of the scores; 1 / sqrt(head_dim) as a rule                       */
+  float scale;          /* of the scores; 1 / sqrt(head_dim) as a rule, below 2e38 in size    */
   int32_t reserved;     /* 0                                                                 */
   const void* q;        /* [n_tokens, n_heads, head_dim]: token t, head h at element         */
   int64_t q_token_stride; /*   t * q_token_stride + h * q_head_stride; 16-byte aligned,      */

@@ -433,7 +433,8 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
   if (a.n_heads < 1 || a.n_heads % kv->v.n_kv_heads || a.n_heads > 65535)
     return fail(IC_ERR_INVALID, "n_heads %d must be a multiple of n_kv_heads %d, at most 65535", a.n_heads, kv->v.n_kv_heads);
   if (a.window < 0 || a.sinks < 0) return fail(IC_ERR_INVALID, "window %d and sinks %d must not be negative", a.window, a.sinks);
-  if (!isfinite(a.scale)) return fail(IC_ERR_INVALID, "scale must be finite");
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  if (!isfinite(scale_log2)) return fail(IC_ERR_INVALID, "scale %g, and scale * log2(e), must be finite", a.scale);
   if (a.n_tokens < 0 || a.n_tokens > 0x7fffffffll / a.n_heads || (!a.starts && a.n_tokens != a.n))
     return fail(IC_ERR_INVALID, "n_tokens = %lld does not fit n = %d and n_heads = %d", (long long)a.n_tokens, a.n, a.n_heads);
   if (a.n == 0 && a.n_tokens > 0) return fail(IC_ERR_INVALID, "tokens without sequences");
@@ -466,7 +467,7 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
   p.n_tokens = a.n_tokens;
   p.window = a.window;
   p.sinks = a.window ? a.sinks : 0;
-  p.scale_log2 = a.scale * 1.4426950408889634f;
+  p.scale_log2 = scale_log2;
   p.partials = kv->partials;
   p.arrivals = kv->arrivals;
   p.partial_floats = kv->partial_floats;

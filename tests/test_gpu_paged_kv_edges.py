@@ -411,3 +411,18 @@ def test_many_handles_at_once():
     with ICPagedKV(*sizes, dtype=F16, workspace=space) as kv:
         kv.reserve(ints([0]), ints([9]))
         kv.sync()
+
+
+def test_a_scale_that_leaves_the_range_is_refused():
+    """The softmax works in powers of two: scale * log2(e) has to be a finite number."""
+    from paper_2501_12689_b200 import IC_ERR_INVALID, ICCacheError
+    kv = make([40], hkv=1, d=64)
+    q = torch.zeros(1, 4, 64, dtype=BF16, device=DEV)
+    for scale in (2.5e38, -3e38):
+        with pytest.raises(ICCacheError) as e:
+            kv.decode(1, q, ints([0]), scale=scale)
+        assert e.value.status == IC_ERR_INVALID
+    got = kv.decode(1, q, ints([0]), scale=2e38)        # scores of zero, whatever the scale: the mean of the values
+    want, size = attention(kv, 1, q, [0], [1], scale=2e38)
+    kv.sync()
+    close(got, want, size)
