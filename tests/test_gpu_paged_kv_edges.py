@@ -7,7 +7,7 @@ import torch
 
 import kv_util
 from kv_util import attention, close
-from test_gpu_paged_kv import BF16, DEV, F16, ints, make, query, starts_of
+from test_gpu_paged_kv import BF16, DEV, F16, check, ints, make, query, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -426,3 +426,78 @@ def test_a_scale_that_leaves_the_range_is_refused():
     want, size = attention(kv, 1, q, [0], [1], scale=2e38)
     kv.sync()
     close(got, want, size)
+
+
+# ---------------------------------------------------------------- calls of many kinds
+@pytest.mark.parametrize("singles,prompt,hq,hkv,d", [(255, 512, 8, 2, 128), (60, 1500, 8, 2, 64), (3, 900, 4, 1, 256), (300, 40, 8, 2, 128)])
+def test_single_tokens_and_a_prompt_in_one_call(singles, prompt, hq, hkv, d):
+    """A serving step: what a sequence gets does not depend on the others beyond the rounding of its weights."""
+    rng = torch.Generator().manual_seed(singles)
+    lens = torch.randint(1, 700, (singles,), generator=rng).tolist()
+    at = singles // 2
+    lens.insert(at, prompt + 100)
+    counts = [1] * (singles + 1)
+    counts[at] = prompt
+    kv = make(lens, hkv=hkv, d=d)
+    seqs = list(range(singles + 1))
+    check(kv, seqs, counts, hq)
+    check(kv, seqs, counts, hq, 200, 4)
+
+
+def test_a_token_by_either_kernel():
+    """One token alone, and in a call whose average takes the other kernel."""
+    kv = make([3000, 500], hkv=2, d=128)
+    q = query(201, 8, 128, BF16)
+    alone = kv.decode(1, q[:1], ints([0]))
+    among = kv.extend(1, q, ints([0, 1]), ints([0, 1, 201]))[:1]
+    kv.sync()
+    want, size = attention(kv, 1, q[:1], [0], [1])
+    close(alone, want, size)
+    close(among, want, size)
+
+
+@pytest.mark.parametrize("hq,hkv,d,n", [(32, 1, 128, 40_001), (128, 1, 64, 30_000), (64, 2, 256, 20_011), (24, 1, 192, 131_071)])
+def test_decode_of_many_heads_over_a_long_cache(hq, hkv, d, n):
+    kv = make([n, 300], hkv=hkv, d=d, layers=1, layer=0, page=64)
+    check(kv, [0, 1], [1, 1], hq, layer=0, decode=True)
+    check(kv, [1, 0], [1, 1], hq, 9000, 4, layer=0, decode=True)
+
+
+def test_extend_on_another_stream():
+    kv = make([2000, 100], hkv=2, d=128)
+    q, seqs, starts = query(90, 8, 128, BF16), ints([0, 1]), ints([0, 70, 90])
+    want = kv.extend(1, q, seqs, starts)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        late = torch.zeros_like(q)
+        torch.cuda._sleep(20_000_000)
+        late.copy_(q)
+        got = kv.extend(1, late, seqs, starts)
+        del late
+        again = got.clone()
+    torch.cuda.synchronize()
+    assert torch.equal(again, want)
+    kv.sync()
+
+
+def test_extend_in_a_graph():
+    """Drafted tokens: reserve, write and extend captured once and replayed, the lengths growing on the device."""
+    kv = make([400, 17, 3000], hkv=2, d=64, spare=60)
+    seqs, counts, starts = ints([0, 1, 2]), ints([9, 9, 9]), ints([0, 9, 18, 27])
+    k, v, q = query(27, 2, 64, BF16, 3), query(27, 2, 64, BF16, 4), query(27, 8, 64, BF16, 5)
+    side = torch.cuda.Stream()
+    kv.set_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        kv.reserve(seqs, counts)
+        kv.write(1, k, v, seqs, starts)
+        out = kv.extend(1, q, seqs, starts)
+    for step in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert kv.lengths.tolist() == [400 + 9 * (step + 1), 17 + 9 * (step + 1), 3000 + 9 * (step + 1)]
+        want, size = attention(kv, 1, q, [0, 1, 2], [9, 9, 9])
+        close(out, want, size)
+    kv.sync()
