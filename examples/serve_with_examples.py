@@ -5,7 +5,8 @@ values are not computed again but shared.
 
 The "model" is a stand-in (random projections per layer, no weights are to be had offline): what is shown is the order of the
 calls around it.  An example is run through the model once, into a sequence of the paged cache that stays; a request finds its
-example with ICCache, forks from that sequence (full pages shared, the tail copied), appends and attends its own tokens, and
+example with ICCache, forks from that sequence (full pages shared, the tail copied), appends and attends its own tokens (a second
+example would be among them: its keys and values depend on what stands before it), and
 then decodes, here with a few samples per request that fork from the request in turn."""
 from __future__ import annotations
 

@@ -3,10 +3,12 @@
  *
  * Example selection (ic_cache.h) returns the cached examples that go in front of a request's
  * prompt (paper Sec. 4.1; Algorithm 1, GenerateResponse on "examples + request").  The keys and
- * values that a model computed for an example are the same for every request that uses it.  This
+ * values that a causal model computes for the front of a prompt are the same whatever follows.  This
  * cache keeps them in pages of a fixed number of tokens: an example is run through the model
- * once, requests fork from it and share its full pages, append their own tokens, attend to all
- * of it, and give the pages back.
+ * once, requests that begin with it fork from it and share its full pages, append their own tokens, attend
+ * to all of it, and give the pages back.  (What stands behind the first example depends on it: a second
+ * example's keys and values are part of the request's own tokens, unless the pair is kept as a sequence
+ * too.  A sequence has one parent; there is no call that joins two.)
  *
  * Storage, all on the device (bf16 or fp16, int32):
  *   pool    [n_pages, n_layers, 2, n_kv_heads, page_size, head_dim]   index 2: 0 = keys, 1 = values
@@ -80,8 +82,9 @@ typedef struct ic_kv_opts {
  * handle will ever need is allocated here: no later call allocates. */
 ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts);
 
-/* Bytes of workspace for these options (page and batch scratch, partial results of attention that
- * is split over a cache's length).  0 for invalid options. */
+/* Bytes of workspace for these options: 4 for every entry of the page tables, 12 a page, and the partial
+ * results of attention that is split over a cache's length, whatever the model's size: 22 MB for a
+ * head_dim of up to 64, 43 MB up to 128, 32 MB up to 192, 42 MB above.  0 for invalid options. */
 size_t ic_kv_workspace_bytes(const ic_kv_opts_t* opts);
 
 /*
@@ -117,7 +120,8 @@ int ic_kv_write(ic_kv_t* kv, int32_t layer, const void* k, const void* v, int64_
  * call of more rows) below the largest one.
  * Rows of `out` that `starts` leaves out are not written; that is reported.  Bad sequences get zeros.
  * A value that no query of the call sees (a page's unused slots, keys outside the window) has no
- * influence, whatever it holds, infinities and NaN included.
+ * influence, whatever it holds, infinities and NaN included.  An infinite or NaN value that a query sees
+ * may also reach the sequence's other queries in the call, as a weight of zero does not undo it.
  */
 typedef struct ic_kv_attend {
   uint32_t struct_size; /* sizeof(ic_kv_attend_t) of the caller's build                      */

@@ -17,7 +17,7 @@
 // they were.  With it that is so 20 and 27.7 nats below, where the result itself comes to the end of fp16.
 //
 // Measured: 64 sequences of 900 to 8192 tokens, 32 query and 8 kv heads, head_dim 128 (1.2 GB of keys and values):
-// 212 us, 5.65 TB/s, 87 % of a copy's rate.  One sequence of 131,071 tokens, 4 kv heads: 57 us, 4.7 TB/s; of these
+// 212 to 217 us, 5.5 to 5.65 TB/s, 85 to 87 % of a copy's rate.  One sequence of 131,071 tokens, 4 kv heads: 57 us, 4.7 TB/s; of these
 // about 3 us pass before the first load, 6 us at the join of its pieces, and the SMs' loads end 9 us apart.  One token
 // of a short sequence: 8.7 us a call, 5.6 us of them on the GPU, launch and the chain table - page - keys - sum.
 #include "kernels.h"

@@ -12,7 +12,7 @@
 //
 // Of a head_dim of 129 to 256, O_A alone takes 256 columns, and there is one row tile to an item.  Its products (1,280
 // cycles for 64 keys at 256) take as long as those of two row tiles at 128, but the softmax is one warp's chain of
-// latencies per scheduler, which is what bounds it: tensor cores 31 % busy, L2 22 %.
+// latencies per scheduler, which is what bounds it: tensor cores 31 % busy, special-function units 16 %, L2 22 %.
 //
 //   warps 0-3, 4-7   softmax of row tile A, B: a thread owns a row (a tensor-memory lane), and copies the row's
 //                    query into the swizzled layout of the left operand, an item ahead
@@ -26,13 +26,14 @@
 // 16-bit type (the tensor cores take both operands in one type), once: the second number that the decode kernel adds to it would
 // double the products with the values, half of what the tensor cores do here.  Their sum is taken before the rounding.
 //
-// Measured: 8 prompts of up to 4096 tokens, 32 query and 8 kv heads, head_dim 128: 0.73 ms, 0.93 PFLOP/s (0.86 ms in a
-// row of launches, where the power limit lowers the clock); one prompt of 16384 tokens up to 1.13 PFLOP/s; a window of
-// 1024 over one sequence of 12,289 tokens 138 us; four requests of up to 57 tokens behind up to 6,000 38 us.
-// head_dim 256: 20 prompts of up to 600 tokens 251 us, 8000 tokens of 8 heads 386 us, where a kernel of 32 rows an item on
-// warp-level products took 1379 and 2333 us, and 29 against 32 us for the smallest, so that there is no kernel of that kind.
-// What bounds it: the exponentials (1,760 cycles per 64 keys of both row tiles) and the change of items
-// (4,600 cycles).
+// Measured, 32 query and 8 kv heads: 8 prompts of up to 4096 tokens, head_dim 128: 0.73 ms, 0.93 PFLOP/s, by itself behind a cold
+// L2 (0.86 ms in a row of launches, where the power limit lowers the clock); one prompt of 16384 tokens 2.05 ms, 1.07 PFLOP/s; a
+// window of 1024 over one sequence of 12,289 tokens 138 us; four requests of up to 57 tokens behind up to 6,000 38 us; head_dim
+// 256: 20 prompts of 10 to 600 tokens 204 us.  (For wide heads a kernel of 32 rows an item on warp-level products took five to six
+// times as long on two such cases, and 32 against 29 us for the smallest, so that there is no kernel of that kind.)
+// What bounds it: no unit.  64 keys of both row tiles take 1,760 cycles, where their exponentials are 1,024 and their products
+// 1,280; tensor pipe and special-function units are half busy each.  It is the order of the steps (scores, maximum, turn,
+// exponentials, store), and the change of items (4,600 cycles).
 #include "kernels.h"
 #include "kv_mma.cuh"
 #include "kv_schedule.cuh"

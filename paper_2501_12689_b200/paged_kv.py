@@ -245,7 +245,8 @@ class ICPagedKV:
 
     def decode(self, layer: int, q: torch.Tensor, seqs: torch.Tensor, *, window: int = 0, sinks: int = 0,
                scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Attention of the newest token of each sequence: q [n, n_heads, head_dim] -> the same shape."""
+        """Attention of the newest token of each sequence: q [n, n_heads, head_dim] -> the same shape.  out may be q; its rows may
+        not overlap otherwise."""
         if q.shape[0] != seqs.shape[0]:
             raise ValueError("decode takes one token per sequence: use extend for more")
         return self._attend(layer, q, seqs, None, window, sinks, scale, out)
@@ -253,7 +254,8 @@ class ICPagedKV:
     def extend(self, layer: int, q: torch.Tensor, seqs: torch.Tensor, starts: torch.Tensor, *, window: int = 0, sinks: int = 0,
                scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Causal attention of each sequence's newest starts[i + 1] - starts[i] tokens: q [tokens, n_heads, head_dim] -> the same
-        shape.  A token at position p sees the keys j <= p with j > p - window (window 0: all of them) or j < sinks."""
+        shape.  A token at position p sees the keys j <= p with j > p - window (window 0: all of them) or j < sinks.  out: as for
+        decode."""
         self._ints(starts, seqs.shape[0] + 1, "starts")
         return self._attend(layer, q, seqs, starts, window, sinks, scale, out)
 
