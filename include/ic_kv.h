@@ -146,6 +146,81 @@ typedef struct ic_kv_attend {
 int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* a);
 
 /*
+ * Rotary positions.  ic_kv_set_rotary says how the model behind the cache turns its queries and keys: pair i of a
+ * head at position p by the angle p * f_i,
+ *     (a, b) -> magnitude * (a cos - b sin, a sin + b cos),
+ * where (a, b) are the elements i and i + rotary_dim / 2 (halves) or 2 i and 2 i + 1 (neighbours); elements from rotary_dim on are left as
+ * they are.  f_i = base^(-2 i / rotary_dim) radians per token, scaled for contexts longer than the model was trained on:
+ *     LINEAR  f_i / factor
+ *     BASE    with the base  base * factor^(rotary_dim / (rotary_dim - 2))  (rotary_dim 2: no change)
+ *     BANDS   by how many turns r = original * f_i / 2 pi the pair makes over `original` tokens:  w f_i + (1 - w) f_i / factor
+ *             with w = (r - low) / (high - low), between 0 and 1
+ * or `frequencies` gives the f_i themselves.  Angles are exact to 2^-31 of a half turn at every position.  Rows are computed in fp32 and rounded
+ * once to the cache's type.  The call changes the handle only: later calls use it, a captured graph keeps what it was captured with.
+ * ic_kv_rotary_frequencies writes the f_i of these options to host memory (rotary_dim / 2 numbers).
+ */
+enum ic_kv_rotary_layout { IC_KV_ROTARY_HALVES = 0, IC_KV_ROTARY_NEIGHBOURS = 1 };
+enum ic_kv_rotary_scaling { IC_KV_ROTARY_NONE = 0, IC_KV_ROTARY_LINEAR = 1, IC_KV_ROTARY_BASE = 2, IC_KV_ROTARY_BANDS = 3 };
+
+typedef struct ic_kv_rotary {
+  uint32_t struct_size; /* sizeof(ic_kv_rotary_t) of the caller's build                      */
+  int32_t rotary_dim;   /* even, 2 .. head_dim                                               */
+  int32_t layout;       /* ic_kv_rotary_layout                                               */
+  int32_t scaling;      /* ic_kv_rotary_scaling                                              */
+  double base;          /* > 0; 0 = 10000                                                    */
+  double factor;        /* > 0; 0 = 1                                                        */
+  double low;           /* BANDS: 0 <= low < high                                            */
+  double high;
+  double original;      /* BANDS: > 0                                                        */
+  double magnitude;     /* of ic_kv_rotate's results; 0 = 1                                  */
+  const double* frequencies; /* optional HOST array [rotary_dim / 2], instead of base and scaling */
+} ic_kv_rotary_t;
+
+int ic_kv_set_rotary(ic_kv_t* kv, const ic_kv_rotary_t* r);
+int ic_kv_rotary_frequencies(const ic_kv_rotary_t* r, double* frequencies);
+
+/*
+ * Turn new tokens' queries and keys, and store the keys with their values: ic_kv_write with rotary positions, and the queries
+ * of the same tokens on the way.  Without k and v only queries (or any rows) are turned; without q only keys are stored.
+ * A token stands where it stands in its sequence (as for ic_kv_attend), or at positions[t] (any int32, also below 0);
+ * where it is stored does not depend on positions.  Without k and v, and with positions, seqs may be NULL (n = 0).
+ * inverse != 0 turns back: by minus the angle, still times the magnitude.
+ * A bad sequence or start anywhere in the call means that nothing is turned or stored; a bad table entry is met when others are done.
+ */
+typedef struct ic_kv_rotate {
+  uint32_t struct_size; /* sizeof(ic_kv_rotate_t) of the caller's build                      */
+  int32_t layer;        /* that k and v are stored in                                        */
+  int32_t n;            /* sequences                                                         */
+  int32_t n_heads;      /* of q; 0 without                                                   */
+  int64_t n_tokens;     /* tokens in all                                                     */
+  int32_t inverse;
+  int32_t reserved;     /* 0                                                                 */
+  const void* q;        /* [n_tokens, n_heads, head_dim], strides and alignment as for ic_kv_attend */
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  void* out;            /* the same for the result; q itself, with its strides, is fine      */
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+  const void* k;        /* [n_tokens, n_kv_heads, head_dim], as for ic_kv_write              */
+  const void* v;
+  int64_t kv_token_stride;
+  int64_t kv_head_stride;
+  const int32_t* positions; /* [n_tokens], or NULL                                           */
+  const int32_t* seqs;  /* [n]                                                               */
+  const int32_t* starts;/* [n+1] ascending from 0 to n_tokens; NULL = one token per sequence */
+} ic_kv_rotate_t;
+
+int ic_kv_rotate(ic_kv_t* kv, const ic_kv_rotate_t* a);
+
+/*
+ * Move what is cached of sequence seqs[i], i < n (no sequence twice), by by[i] positions: its keys, in all layers, are turned by
+ * by[i] * f_j (without the magnitude, which they have).  For a copy of an example (ic_kv_fork with copy) that stands
+ * elsewhere in the request than where it was computed.  The keys are rounded to the cache's type once more.
+ * Every page of the sequences must be theirs alone: one that is shared is IC_ERR_INVALID (on the device), and nothing is changed.
+ */
+int ic_kv_shift(ic_kv_t* kv, const int32_t* seqs, const int32_t* by, int32_t n);
+
+/*
  * Make sequence children[i] the first upto[i] tokens of sequence parents[i], i < n, all at once: parents
  * are taken as they are before the call, also where they are children themselves (the reordering of
  * a beam search).  No child twice; upto: 0 <= upto[i] <= the parent's length, NULL = the whole parent.

@@ -10,5 +10,5 @@ from .binding import (  # noqa: F401
     IC_BF16, IC_F32, IC_PATH_AUTO, IC_PATH_GENERIC, IC_PATH_SCAN, IC_PATH_UMMA, IC_MAX_K, IC_MAX_DIM,
 )
 from .paged_kv import (  # noqa: F401
-    ICPagedKV, ic_kv_workspace_bytes, IC_KV_BF16, IC_KV_F16, IC_KV_MAX_HEAD_DIM, IC_KV_MAX_PAGE, IC_KV_MAX_SEQS,
+    ICPagedKV, ic_kv_workspace_bytes, rotary_frequencies, IC_KV_BF16, IC_KV_F16, IC_KV_MAX_HEAD_DIM, IC_KV_MAX_PAGE, IC_KV_MAX_SEQS,
 )

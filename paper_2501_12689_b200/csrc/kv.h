@@ -81,6 +81,32 @@ cudaError_t kv_free_launch(const KvView& v, const int* seqs, int n, int sm_count
 cudaError_t kv_compact_launch(const KvView& v, int sm_count, int* launches, cudaStream_t st);
 cudaError_t kv_pages_configure(int smem_optin);
 
+// Rotary positions: pair i turns by turn[i] / 2^64 of a full turn per position.
+constexpr int KV_MAX_ROTARY_PAIRS = 128;
+struct KvRotary {
+  unsigned long long turn[KV_MAX_ROTARY_PAIRS];
+  int dim;                  // elements of a head that turn, even; 0 = not set
+  int neighbours;           // pairs (2 i, 2 i + 1) instead of (i, i + dim / 2)
+  float magnitude;          // factor of the turned elements
+};
+struct KvRotateParams {
+  KvView v;
+  KvRotary r;
+  const unsigned char* q;   // null: no queries (n_heads is 0)
+  unsigned char* out;
+  const unsigned char* k;   // null: no keys and values
+  const unsigned char* val;
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride, kv_token_stride, kv_head_stride;      // elements
+  const int* positions;     // null: as the tokens stand in their sequences
+  const int* seqs;          // null: positions are given, and nothing is stored
+  const int* starts;
+  int n, n_heads, layer, inverse;
+  int64_t n_tokens;
+};
+cudaError_t kv_rotate_launch(const KvRotateParams& p, bool f16, int sm_count, int* launches, cudaStream_t st);
+cudaError_t kv_shift_launch(const KvView& v, const KvRotary& rot, const int* seqs, const int* by, int n, bool f16, int sm_count, int* launches,
+                            cudaStream_t st);
+
 cudaError_t kv_decode_configure(int smem_optin);
 // tmap: the pool as rows of head_dim elements, box of 64 elements x min(page_size, 64) rows, 128-byte swizzle.
 // two: 16 rows per item instead of 8.

@@ -30,6 +30,7 @@ struct ic_kv {
   float* partials = nullptr;       // in the workspace: pieces of attention split over a cache's length
   int* arrivals = nullptr;
   size_t partial_floats = 0;
+  icc::KvRotary rotary = {};       // dim 0: not set
 };
 
 namespace {
@@ -231,6 +232,56 @@ int encode_pool(ic_kv* kv) {
       &kv->tmap, kv->f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, v.pool, dims, strides, box, estr,
       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? IC_OK : fail(IC_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+}
+
+int read_rotary(const ic_kv_rotary_t* opts, ic_kv_rotary_t* r) {
+  memset(r, 0, sizeof *r);
+  if (!opts) return fail(IC_ERR_INVALID, "NULL options");
+  if (opts->struct_size < sizeof(uint32_t) || opts->struct_size > sizeof *r)
+    return fail(IC_ERR_INVALID, "struct_size %u not understood (this build: %zu)", opts->struct_size, sizeof *r);
+  memcpy(r, opts, opts->struct_size);
+  if (r->base == 0.0) r->base = 10000.0;
+  if (r->factor == 0.0) r->factor = 1.0;
+  if (r->magnitude == 0.0) r->magnitude = 1.0;
+  if (r->rotary_dim < 2 || r->rotary_dim > IC_KV_MAX_HEAD_DIM || r->rotary_dim % 2)
+    return fail(IC_ERR_INVALID, "rotary_dim %d must be even and in [2, %d]", r->rotary_dim, IC_KV_MAX_HEAD_DIM);
+  if (r->layout != IC_KV_ROTARY_HALVES && r->layout != IC_KV_ROTARY_NEIGHBOURS) return fail(IC_ERR_INVALID, "unknown layout %d", r->layout);
+  if (!isfinite(static_cast<float>(r->magnitude))) return fail(IC_ERR_INVALID, "magnitude %g must be finite", r->magnitude);
+  if (r->frequencies) {
+    for (int i = 0; i < r->rotary_dim / 2; ++i)
+      if (!isfinite(r->frequencies[i])) return fail(IC_ERR_INVALID, "frequencies[%d] is not finite", i);
+    return IC_OK;
+  }
+  if (!isfinite(r->base) || r->base <= 0.0 || !isfinite(r->factor) || r->factor <= 0.0)
+    return fail(IC_ERR_INVALID, "base %g and factor %g must be finite and above 0", r->base, r->factor);
+  switch (r->scaling) {
+    case IC_KV_ROTARY_NONE:
+    case IC_KV_ROTARY_LINEAR:
+    case IC_KV_ROTARY_BASE: break;
+    case IC_KV_ROTARY_BANDS:
+      if (!(r->low >= 0.0 && r->low < r->high) || !isfinite(r->high) || !isfinite(r->original) || r->original <= 0.0)
+        return fail(IC_ERR_INVALID, "low %g, high %g, original %g: 0 <= low < high and original above 0 are wanted", r->low, r->high, r->original);
+      break;
+    default: return fail(IC_ERR_INVALID, "unknown scaling %d", r->scaling);
+  }
+  return IC_OK;
+}
+
+constexpr long double TWO_PI = 6.283185307179586476925286766559005768L;
+
+// Radians per token of pair i.
+long double frequency(const ic_kv_rotary_t& r, int i) {
+  if (r.frequencies) return r.frequencies[i];
+  const long double dim = r.rotary_dim;
+  long double base = r.base;
+  if (r.scaling == IC_KV_ROTARY_BASE && r.rotary_dim > 2) base *= powl(r.factor, dim / (dim - 2));
+  const long double f = powl(base, -2 * i / dim);
+  if (r.scaling == IC_KV_ROTARY_LINEAR) return f / r.factor;
+  if (r.scaling != IC_KV_ROTARY_BANDS) return f;
+  const long double turns = r.original * f / TWO_PI;
+  long double w = (turns - r.low) / ((long double)r.high - r.low);
+  w = w < 0 ? 0 : w > 1 ? 1 : w;
+  return w * f + (1 - w) * f / r.factor;
 }
 
 int launched(ic_kv* kv, cudaError_t e, int n, const char* what) {
@@ -487,6 +538,108 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* args) {
     rc = launched(kv, e, 1, "attention");
   }
   return rc;
+}
+
+int ic_kv_rotary_frequencies(const ic_kv_rotary_t* opts, double* frequencies) {
+  ic_kv_rotary_t r;
+  const int rc = read_rotary(opts, &r);
+  if (rc != IC_OK) return rc;
+  if (!frequencies) return fail(IC_ERR_INVALID, "NULL frequencies");
+  for (int i = 0; i < r.rotary_dim / 2; ++i) frequencies[i] = (double)frequency(r, i);
+  return IC_OK;
+}
+
+int ic_kv_set_rotary(ic_kv_t* kv, const ic_kv_rotary_t* opts) {
+  if (!kv) return fail(IC_ERR_INVALID, "NULL handle");
+  ic_kv_rotary_t r;
+  const int rc = read_rotary(opts, &r);
+  if (rc != IC_OK) return rc;
+  if (r.rotary_dim > kv->v.head_dim) return fail(IC_ERR_INVALID, "rotary_dim %d exceeds head_dim %d", r.rotary_dim, kv->v.head_dim);
+  icc::KvRotary to = {};
+  for (int i = 0; i < r.rotary_dim / 2; ++i) {
+    long double turn = frequency(r, i) / TWO_PI;
+    if (!isfinite(turn)) return fail(IC_ERR_INVALID, "the frequency of pair %d is not finite", i);
+    turn -= floorl(turn);                                 // whole turns do nothing
+    const long double steps = roundl(turn * 18446744073709551616.0L);
+    to.turn[i] = steps >= 18446744073709551616.0L ? 0 : (unsigned long long)steps;
+  }
+  to.dim = r.rotary_dim;
+  to.neighbours = r.layout == IC_KV_ROTARY_NEIGHBOURS;
+  to.magnitude = static_cast<float>(r.magnitude);
+  kv->rotary = to;
+  return IC_OK;
+}
+
+int ic_kv_rotate(ic_kv_t* kv, const ic_kv_rotate_t* args) {
+  int rc = check_handle(kv);
+  if (rc != IC_OK) return rc;
+  if (!args) return fail(IC_ERR_INVALID, "NULL arguments");
+  ic_kv_rotate_t a;
+  memset(&a, 0, sizeof a);
+  if (args->struct_size < sizeof(uint32_t) || args->struct_size > sizeof a)
+    return fail(IC_ERR_INVALID, "struct_size %u not understood (this build: %zu)", args->struct_size, sizeof a);
+  memcpy(&a, args, args->struct_size);
+  if (kv->rotary.dim == 0) return fail(IC_ERR_INVALID, "ic_kv_set_rotary has not been called");
+  if ((rc = check_n(kv, a.n)) != IC_OK) return rc;
+  if (a.n_tokens == 0) return IC_OK;                          // (arrays of nothing may be NULL)
+  if (!a.q && !a.k) return fail(IC_ERR_INVALID, "neither q nor k is given");
+  if (!a.k != !a.v) return fail(IC_ERR_INVALID, "k and v come together");
+  if (a.k && (a.layer < 0 || a.layer >= kv->v.n_layers)) return fail(IC_ERR_INVALID, "layer %d outside [0, %d)", a.layer, kv->v.n_layers);
+  if (a.q ? (a.n_heads < 1 || a.n_heads > 65535) : a.n_heads != 0) return fail(IC_ERR_INVALID, "n_heads %d must be in [1, 65535], or 0 without q", a.n_heads);
+  const bool alone = !a.k && a.positions && !a.seqs;          // rows at given positions
+  if (a.n_tokens < 0 || a.n_tokens > 0x7fffffffll / (a.n_heads > 1 ? a.n_heads : 1) || (!alone && !a.starts && a.n_tokens != a.n))
+    return fail(IC_ERR_INVALID, "n_tokens = %lld does not fit n = %d and n_heads = %d", (long long)a.n_tokens, a.n, a.n_heads);
+  if (!alone && a.n == 0 && a.n_tokens > 0) return fail(IC_ERR_INVALID, "tokens without sequences");
+  if (alone && (a.n != 0 || a.starts)) return fail(IC_ERR_INVALID, "n and starts without seqs");
+  if (a.q && ((rc = check_rows(kv, a.q, a.q_token_stride, a.q_head_stride, "q")) != IC_OK ||
+              (rc = check_rows(kv, a.out, a.out_token_stride, a.out_head_stride, "out")) != IC_OK))
+    return rc;
+  if (a.q && rows_overlap(a.n_tokens, a.n_heads, a.out_token_stride, a.out_head_stride, kv->v.head_dim))
+    return fail(IC_ERR_INVALID, "rows of out overlap with strides (%lld, %lld)", (long long)a.out_token_stride, (long long)a.out_head_stride);
+  if (a.k && ((rc = check_rows(kv, a.k, a.kv_token_stride, a.kv_head_stride, "k")) != IC_OK ||
+              (rc = check_rows(kv, a.v, a.kv_token_stride, a.kv_head_stride, "v")) != IC_OK))
+    return rc;
+  if ((a.positions && (rc = check_list(kv, a.positions, "positions")) != IC_OK) || (!alone && (rc = check_list(kv, a.seqs, "seqs")) != IC_OK) ||
+      (a.starts && (rc = check_list(kv, a.starts, "starts")) != IC_OK))
+    return rc;
+  icc::KvRotateParams p;
+  p.v = kv->v;
+  p.r = kv->rotary;
+  p.q = static_cast<const unsigned char*>(a.q);
+  p.out = static_cast<unsigned char*>(a.out);
+  p.k = static_cast<const unsigned char*>(a.k);
+  p.val = static_cast<const unsigned char*>(a.v);
+  p.q_token_stride = a.q_token_stride;
+  p.q_head_stride = a.q_head_stride;
+  p.out_token_stride = a.out_token_stride;
+  p.out_head_stride = a.out_head_stride;
+  p.kv_token_stride = a.kv_token_stride;
+  p.kv_head_stride = a.kv_head_stride;
+  p.positions = a.positions;
+  p.seqs = alone ? nullptr : a.seqs;
+  p.starts = a.starts;
+  p.n = a.n;
+  p.n_heads = a.n_heads;
+  p.layer = a.layer;
+  p.inverse = a.inverse != 0;
+  p.n_tokens = a.n_tokens;
+  DeviceGuard guard(kv->device);
+  int launches = 0;
+  const cudaError_t e = icc::kv_rotate_launch(p, kv->f16, kv->sm_count, &launches, kv->stream);
+  return launched(kv, e, launches, "rotate");
+}
+
+int ic_kv_shift(ic_kv_t* kv, const int32_t* seqs, const int32_t* by, int32_t n) {
+  int rc = check_handle(kv);
+  if (rc == IC_OK) rc = check_n(kv, n);
+  if (rc != IC_OK) return rc;
+  if (kv->rotary.dim == 0) return fail(IC_ERR_INVALID, "ic_kv_set_rotary has not been called");
+  if (n == 0) return IC_OK;
+  if ((rc = check_list(kv, seqs, "seqs")) != IC_OK || (rc = check_list(kv, by, "by")) != IC_OK) return rc;
+  DeviceGuard guard(kv->device);
+  int launches = 0;
+  const cudaError_t e = icc::kv_shift_launch(kv->v, kv->rotary, seqs, by, n, kv->f16, kv->sm_count, &launches, kv->stream);
+  return launched(kv, e, launches, "shift");
 }
 
 int ic_kv_fork(ic_kv_t* kv, const int32_t* parents, const int32_t* children, const int32_t* upto, int32_t n, int32_t copy) {

@@ -12,6 +12,7 @@
 #include "common.cuh"
 #include "kernels.h"
 #include "kv.h"
+#include "kv_pages.cuh"
 #include "pipeline.cuh"
 
 namespace icc {
@@ -23,36 +24,6 @@ constexpr int PAGES_PER_THREAD = 32;      // counts that a thread of a planning 
 constexpr int COPY_THREADS = 256;
 constexpr int COPY_UNIT = COPY_THREADS * 16 * 4;   // bytes of a page that a CTA copies at a time
 constexpr int ROW_UNIT = 1024;            // table entries that a CTA updates at a time
-
-// Exclusive prefix sum over the CTA; *total gets the sum.  Unsigned, so that two packed counters may be
-// summed at once.  `sums`: 33 words of shared memory; ends with a barrier.
-__device__ __forceinline__ unsigned block_scan(unsigned x, unsigned* sums, unsigned* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  unsigned inc = x;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const unsigned y = __shfl_up_sync(FULL_MASK, inc, d);
-    if (lane >= d) inc += y;
-  }
-  if (lane == 31) sums[warp] = inc;
-  __syncthreads();
-  if (warp == 0) {
-    const unsigned w = lane < (int)(blockDim.x >> 5) ? sums[lane] : 0u;
-    unsigned winc = w;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const unsigned y = __shfl_up_sync(FULL_MASK, winc, d);
-      if (lane >= d) winc += y;
-    }
-    sums[lane] = winc - w;
-    if (lane == 31) sums[32] = winc;
-  }
-  __syncthreads();
-  const unsigned before = sums[warp] + inc - x;
-  *total = sums[32];
-  __syncthreads();
-  return before;
-}
 
 // Bit b of the result: page p0 + b exists and its reference count is 0.
 __device__ __forceinline__ unsigned free_mask(const int* refs, int n_pages, int p0) {
@@ -87,31 +58,6 @@ __device__ int take_free_pages(const KvView& v, int need, int* list, unsigned* s
   }
   __syncthreads();
   return found;
-}
-
-// Which of begin[0..n) holds rank r (begin ascends; entries without pages repeat their successor's value).
-__device__ __forceinline__ int owner_of(const int* begin, int n, int r) {
-  int lo = 0, hi = n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (begin[mid] <= r) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
-// A length is one that the sequence's row holds.  Lent lengths that are not an earlier cache's may be anything, and
-// the rows' entries are counted by them.
-__device__ __forceinline__ bool length_fits(const KvView& v, int tokens) {
-  return tokens >= 0 && tokens <= (v.max_pages << v.page_shift);
-}
-
-// An owned table entry names a page of the pool.  One that does not (lent tables that are not an earlier cache's) is
-// reported.
-__device__ __forceinline__ bool page_exists(const KvView& v, int page) {
-  if ((unsigned)page < (unsigned)v.n_pages) return true;
-  kv_report(v, KV_INVALID);
-  return false;
 }
 
 // ---------------------------------------------------------------- reserve
@@ -172,24 +118,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) kv_reserve_kernel(const KvView v
 }
 
 // ---------------------------------------------------------------- write
-// What a write needs to be right of sequence i of the call: the sequence, where its tokens begin and end, and its length.
-struct WriteSeq {
-  int s, length;
-  int64_t begin, end;
-  bool fine;
-  __device__ __forceinline__ WriteSeq(const KvView& v, const int* seqs, const int* starts, int i, int n, int64_t n_tokens) {
-    s = seqs[i];
-    begin = starts ? starts[i] : i;
-    end = starts ? starts[i + 1] : i + 1;
-    length = 0;
-    fine = s >= 0 && s < v.max_seqs && begin <= end && (i > 0 || begin == 0) && (i + 1 < n || end == n_tokens);
-    if (fine) {
-      length = v.lengths[s];
-      fine = length_fits(v, length) && end - begin <= length;
-    }
-  }
-};
-
 __global__ void __launch_bounds__(COPY_THREADS) kv_write_check_kernel(const KvView v, const int* __restrict__ seqs, const int* __restrict__ starts,
                                                                       int n, int64_t n_tokens) {
   grid_dep_launch_dependents();
@@ -197,14 +125,6 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_write_check_kernel(const KvVi
   const int i = blockIdx.x * COPY_THREADS + threadIdx.x;
   if (*v.err != KV_OK || i >= n) return;
   if (!WriteSeq(v, seqs, starts, i, n, n_tokens).fine) kv_report(v, KV_INVALID);
-}
-
-// First byte of a token's key row of head 0, or null.
-__device__ __forceinline__ unsigned char* token_place(const KvView& v, int layer, int s, int pos) {
-  const int page = v.tables[(size_t)s * v.max_pages + (pos >> v.page_shift)];
-  if (!page_exists(v, page)) return nullptr;
-  const size_t row = (size_t)layer * 2 * v.n_kv_heads << v.page_shift;
-  return v.pool + (size_t)page * v.page_bytes + (row + (size_t)(pos & ((1 << v.page_shift) - 1))) * v.head_dim * 2;
 }
 
 // TOKENS tokens per CTA.  A bad sequence anywhere in the call means that nothing is stored, so every CTA looks over all of them,

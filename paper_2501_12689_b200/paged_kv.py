@@ -33,6 +33,20 @@ class ic_kv_attend_t(ctypes.Structure):
                 ("seqs", ctypes.c_void_p), ("starts", ctypes.c_void_p)]
 
 
+class ic_kv_rotary_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [(n, ctypes.c_int32) for n in ("rotary_dim", "layout", "scaling")] + [
+        (n, ctypes.c_double) for n in ("base", "factor", "low", "high", "original", "magnitude")] + [("frequencies", ctypes.c_void_p)]
+
+
+class ic_kv_rotate_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("layer", ctypes.c_int32), ("n", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("n_tokens", ctypes.c_int64), ("inverse", ctypes.c_int32), ("reserved", ctypes.c_int32), ("q", ctypes.c_void_p),
+                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("out", ctypes.c_void_p),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("kv_token_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64), ("positions", ctypes.c_void_p),
+                ("seqs", ctypes.c_void_p), ("starts", ctypes.c_void_p)]
+
+
 _P, _I, _L = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 # name -> (restype, argtypes); also the list the symbol test checks against the header
 SIGNATURES = {
@@ -41,6 +55,10 @@ SIGNATURES = {
     "ic_kv_reserve": (ctypes.c_int, [_P, _P, _P, _I]),
     "ic_kv_write": (ctypes.c_int, [_P, _I, _P, _P, _L, _L, _P, _P, _I, _L]),
     "ic_kv_attend": (ctypes.c_int, [_P, ctypes.POINTER(ic_kv_attend_t)]),
+    "ic_kv_set_rotary": (ctypes.c_int, [_P, ctypes.POINTER(ic_kv_rotary_t)]),
+    "ic_kv_rotary_frequencies": (ctypes.c_int, [ctypes.POINTER(ic_kv_rotary_t), ctypes.POINTER(ctypes.c_double)]),
+    "ic_kv_rotate": (ctypes.c_int, [_P, ctypes.POINTER(ic_kv_rotate_t)]),
+    "ic_kv_shift": (ctypes.c_int, [_P, _P, _P, _I]),
     "ic_kv_fork": (ctypes.c_int, [_P, _P, _P, _P, _I, _I]),
     "ic_kv_free": (ctypes.c_int, [_P, _P, _I]),
     "ic_kv_compact": (ctypes.c_int, [_P]),
@@ -82,6 +100,38 @@ def ic_kv_workspace_bytes(n_pages: int, n_layers: int, n_kv_heads: int, page_siz
     """Bytes of the `workspace` tensor for a cache of these sizes; 0 if they are invalid."""
     return int(_library().ic_kv_workspace_bytes(ctypes.byref(
         _options(n_pages, n_layers, n_kv_heads, page_size, head_dim, max_seqs, max_pages, dtype))))
+
+
+ROTARY_SCALINGS = ("none", "linear", "base", "bands")      # ic_kv_rotary_scaling
+
+
+def _rotary(rotary_dim, base, interleaved, scaling, factor, low, high, original, magnitude, frequencies) -> ic_kv_rotary_t:
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {ROTARY_SCALINGS}")
+    r = ic_kv_rotary_t()
+    r.struct_size = ctypes.sizeof(ic_kv_rotary_t)
+    r.rotary_dim, r.layout, r.scaling = rotary_dim, int(bool(interleaved)), ROTARY_SCALINGS.index(scaling)
+    r.base, r.factor, r.low, r.high, r.original, r.magnitude = base, factor, low, high, original, magnitude
+    if not all((base, factor, magnitude)):
+        raise ValueError("base, factor and magnitude must not be 0")
+    if frequencies is not None:
+        f = [float(x) for x in frequencies]
+        if len(f) != rotary_dim // 2:
+            raise ValueError(f"frequencies must be {rotary_dim // 2} numbers, one a pair")
+        r._kept = (ctypes.c_double * len(f))(*f)
+        r.frequencies = ctypes.cast(r._kept, ctypes.c_void_p)
+    return r
+
+
+def rotary_frequencies(rotary_dim: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0, high: float = 32.0,
+                       original: float = 0.0) -> list:
+    """Radians per token of each pair, as ICPagedKV.set_rotary with these arguments takes them (include/ic_kv.h has the formulas)."""
+    r = _rotary(rotary_dim, base, False, scaling, factor, low, high, original, 1.0, None)
+    out = (ctypes.c_double * max(1, rotary_dim // 2))()
+    rc = _library().ic_kv_rotary_frequencies(ctypes.byref(r), out)
+    if rc != IC_OK:
+        raise ICCacheError(rc, ic_cache_last_error())
+    return list(out)
 
 
 class ICPagedKV:
@@ -144,6 +194,9 @@ class ICPagedKV:
         self._a = ic_kv_attend_t()
         self._a.struct_size = ctypes.sizeof(ic_kv_attend_t)
         self._ref = ctypes.byref(self._a)
+        self._r = ic_kv_rotate_t()
+        self._r.struct_size = ctypes.sizeof(ic_kv_rotate_t)
+        self._r_ref = ctypes.byref(self._r)
         self._scale = 1.0 / math.sqrt(head_dim)
 
     # -- lifetime
@@ -258,6 +311,78 @@ class ICPagedKV:
         decode."""
         self._ints(starts, seqs.shape[0] + 1, "starts")
         return self._attend(layer, q, seqs, starts, window, sinks, scale, out)
+
+    def set_rotary(self, rotary_dim: Optional[int] = None, *, base: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                   factor: float = 1.0, low: float = 1.0, high: float = 32.0, original: float = 0.0, magnitude: float = 1.0,
+                   frequencies=None) -> None:
+        """How write_rotated, rotate and shift turn rows: the first rotary_dim elements of a head (None: all), pairs
+        (i, i + rotary_dim / 2) or, interleaved, (2 i, 2 i + 1); pair i by base ** (-2 i / rotary_dim) radians per token, scaled "linear", by
+        the "base", or in "bands" (include/ic_kv.h), or by frequencies[i].  Later calls use it; a captured graph keeps what it had."""
+        if self._h is None:
+            raise ValueError("the cache is closed")
+        r = _rotary(self.head_dim if rotary_dim is None else rotary_dim, base, interleaved, scaling, factor, low, high, original, magnitude,
+                    frequencies)
+        rc = self._lib.ic_kv_set_rotary(self._h, ctypes.byref(r))
+        if rc != IC_OK:
+            raise ICCacheError(rc, ic_cache_last_error())
+
+    def _rotate(self, layer, q, k, v, seqs, starts, positions, out, inverse):
+        a = self._r
+        tokens = (q if q is not None else k).shape[0]
+        n = 0
+        if seqs is not None:
+            n = seqs.shape[0]
+            self._ints(seqs, n, "seqs")
+        if starts is not None:
+            self._ints(starts, n + 1, "starts")
+        if positions is not None:
+            self._ints(positions, tokens, "positions")
+        given = None
+        a.n_heads, a.q, a.out = 0, None, None
+        if q is not None:
+            q = self._rows(q, "q")
+            a.n_heads = q.shape[1]
+            if out is None:
+                given = out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            else:
+                if out.shape != q.shape:
+                    raise ValueError("out must have the shape of q")
+                given, out = out, self._rows(out, "out")
+            a.q, (a.q_token_stride, a.q_head_stride, _) = q.data_ptr(), q.stride()
+            a.out, (a.out_token_stride, a.out_head_stride, _) = out.data_ptr(), out.stride()
+        a.k = a.v = None
+        if k is not None:
+            k, v = self._rows(k, "k"), self._rows(v, "v")
+            if k.shape != (tokens, self.n_kv_heads, self.head_dim) or v.shape != k.shape:
+                raise ValueError(f"k and v must have the shape [{tokens}, {self.n_kv_heads}, {self.head_dim}]")
+            if k.stride() != v.stride():
+                k, v = (torch.empty(x.shape, dtype=x.dtype, device=x.device).copy_(x) for x in (k, v))
+            a.k, a.v, (a.kv_token_stride, a.kv_head_stride, _) = k.data_ptr(), v.data_ptr(), k.stride()
+        a.layer, a.n, a.n_tokens, a.inverse = layer, n, tokens, int(bool(inverse))
+        a.positions, a.seqs, a.starts = (t.data_ptr() if t is not None else None for t in (positions, seqs, starts))
+        self._call(self._lib.ic_kv_rotate, (self._r_ref,), q, out, k, v, seqs, starts, positions)
+        if out is not given:
+            given.copy_(out)
+        return given
+
+    def write_rotated(self, layer: int, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, seqs: torch.Tensor,
+                      starts: Optional[torch.Tensor] = None, *, positions: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """write() with rotary positions: k turned and stored with v in one layer, and q [tokens, n_heads, head_dim] turned into out (None:
+        a new tensor; q itself is fine), which is returned.  A token's position is its place in the sequence, or positions[t] (int32)."""
+        return self._rotate(layer, q, k, v, seqs, starts, positions, out, False)
+
+    def rotate(self, x: torch.Tensor, positions: torch.Tensor, *, inverse: bool = False, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rows [tokens, heads, head_dim] turned as at these positions, or back (inverse).  out: as for write_rotated."""
+        return self._rotate(0, x, None, None, None, None, positions, out, inverse)
+
+    def shift(self, seqs: torch.Tensor, by: torch.Tensor) -> None:
+        """Move the cached keys of each sequence, in all layers, by by[i] positions (int32).  Its pages must not be shared: fork with
+        copy=True."""
+        n = seqs.shape[0]
+        self._ints(seqs, n, "seqs")
+        self._ints(by, n, "by")
+        self._call(self._lib.ic_kv_shift, (seqs.data_ptr(), by.data_ptr(), n), seqs, by)
 
     def fork(self, parents: torch.Tensor, children: torch.Tensor, upto: Optional[torch.Tensor] = None, *, copy: bool = False) -> None:
         """Sequence children[i] becomes the first upto[i] tokens (None: all) of parents[i], all at once; full pages are shared, or
