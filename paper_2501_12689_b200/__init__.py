@@ -12,3 +12,6 @@ from .binding import (  # noqa: F401
 from .paged_kv import (  # noqa: F401
     ICPagedKV, ic_kv_workspace_bytes, rotary_frequencies, IC_KV_BF16, IC_KV_F16, IC_KV_MAX_HEAD_DIM, IC_KV_MAX_PAGE, IC_KV_MAX_SEQS,
 )
+from .token_scores import (  # noqa: F401
+    ICTokenScores, TokenScores, ic_score_workspace_bytes, IC_SCORE_BF16, IC_SCORE_F16, IC_SCORE_F32, IC_SCORE_MAX_TOP, IC_SCORE_MAX_VOCAB,
+)

@@ -29,6 +29,13 @@ inline bool is_device_ptr(const void* p, int device) {
   return a.type == cudaMemoryTypeDevice && a.device == device;
 }
 
+// A mapped host word for a handle's error, zero; nullptr if there is no memory.
+int* take_status_word();
+void give_status_word(int* w);
+
+// The device that a handle is made for (wanted < 0: the current one), if this library runs on it: IC_OK, or the error's code.
+int usable_device(int wanted, int* dev, int* sms, int* smem);
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,

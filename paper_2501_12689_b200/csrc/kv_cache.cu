@@ -12,7 +12,9 @@
 
 using icc::DeviceGuard;
 using icc::fail;
+using icc::give_status_word;
 using icc::is_device_ptr;
+using icc::take_status_word;
 
 struct ic_kv {
   icc::KvView v;
@@ -34,46 +36,6 @@ struct ic_kv {
 };
 
 namespace {
-
-// Mapped host words for the handles' errors.  Allocating pinned memory takes longer than everything else in a
-// creation, so a block of words serves many handles of the process; blocks are never given back.
-struct StatusBlock {
-  static constexpr int WORDS = 1024;
-  int* words = nullptr;
-  bool used[WORDS] = {};
-  StatusBlock* next = nullptr;
-};
-std::mutex g_status_mutex;
-StatusBlock* g_status_blocks = nullptr;
-
-int* take_status_word() {
-  std::lock_guard<std::mutex> lock(g_status_mutex);
-  for (StatusBlock* b = g_status_blocks;; b = b->next) {
-    if (!b) {
-      void* p = nullptr;
-      b = new (std::nothrow) StatusBlock;
-      if (!b || cudaHostAlloc(&p, StatusBlock::WORDS * sizeof(int), cudaHostAllocMapped | cudaHostAllocPortable) != cudaSuccess) {
-        cudaGetLastError();
-        delete b;
-        return nullptr;
-      }
-      b->words = static_cast<int*>(p);
-      b->next = g_status_blocks;
-      g_status_blocks = b;
-    }
-    for (int i = 0; i < StatusBlock::WORDS; ++i)
-      if (!b->used[i]) {
-        b->used[i] = true;
-        b->words[i] = 0;
-        return b->words + i;
-      }
-  }
-}
-void give_status_word(int* w) {
-  std::lock_guard<std::mutex> lock(g_status_mutex);
-  for (StatusBlock* b = g_status_blocks; b; b = b->next)
-    if (w >= b->words && w < b->words + StatusBlock::WORDS) b->used[w - b->words] = false;
-}
 
 // The kernels' shared-memory limits, once per device.
 cudaError_t configure_kernels(int dev, int smem) {
@@ -303,36 +265,10 @@ size_t ic_kv_workspace_bytes(const ic_kv_opts_t* opts) {
 ic_kv_t* ic_kv_create(const ic_kv_opts_t* opts) {
   ic_kv_opts_t o;
   if (read_opts(opts, &o) != IC_OK) return nullptr;
-  int ndev = 0;
-  cudaError_t e = cudaGetDeviceCount(&ndev);
-  if (e != cudaSuccess || ndev == 0) {
-    cudaGetLastError();
-    fail(IC_ERR_CUDA, "no usable CUDA device (%s); this library has no CPU fallback", e != cudaSuccess ? cudaGetErrorString(e) : "device count is 0");
-    return nullptr;
-  }
-  int dev = o.device;
-  if (dev < 0 && cudaGetDevice(&dev) != cudaSuccess) {
-    fail(IC_ERR_CUDA, "cudaGetDevice failed");
-    return nullptr;
-  }
-  if (dev >= ndev) {
-    fail(IC_ERR_INVALID, "device %d does not exist (%d devices)", dev, ndev);
-    return nullptr;
-  }
+  int dev = 0, sms = 0, smem = 0;
+  if (icc::usable_device(o.device, &dev, &sms, &smem) != IC_OK) return nullptr;
   DeviceGuard guard(dev);
-  int major = 0, minor = 0, sms = 0, smem = 0;
-  if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess) {
-    cudaGetLastError();
-    fail(IC_ERR_CUDA, "reading the device's attributes failed");
-    return nullptr;
-  }
-  if (major != 10 || sms > icc::KV_MAX_CTAS) {
-    fail(IC_ERR_UNSUPPORTED, "device %d is sm_%d%d with %d multiprocessors; this library is built for sm_100a only", dev, major, minor, sms);
-    return nullptr;
-  }
+  cudaError_t e = cudaSuccess;
   ic_kv* kv = new (std::nothrow) ic_kv();
   if (!kv) {
     fail(IC_ERR_NOMEM, "host allocation failed");

@@ -200,23 +200,6 @@ __device__ __forceinline__ uint32_t bits_below(int n) { return n <= 0 ? 0u : (n 
 __device__ __forceinline__ void turn_wait(int warp) { asm volatile("bar.sync %0, 64;" ::"r"(3 + warp) : "memory"); }
 __device__ __forceinline__ void turn_pass(int warp) { asm volatile("bar.arrive %0, 64;" ::"r"(3 + (warp ^ 4)) : "memory"); }
 
-// ---------------------------------------------------------------- pairs of floats in one instruction
-__device__ __forceinline__ uint64_t pair_of(float a, float b) {
-  uint64_t d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
-  return d;
-}
-__device__ __forceinline__ void split_pair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma_pairs(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add_pairs(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 // Weights 2^(scale s - base) of 64 scores, packed to the cache's type; their sum is added to sum2.
 template <bool F16>
 __device__ __forceinline__ void weights(const uint32_t (&s)[64], uint64_t scale2, uint64_t base2, uint64_t (&sum2)[2], uint32_t (&w)[32]) {
