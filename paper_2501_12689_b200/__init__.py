@@ -15,3 +15,6 @@ from .paged_kv import (  # noqa: F401
 from .token_scores import (  # noqa: F401
     ICTokenScores, TokenScores, ic_score_workspace_bytes, IC_SCORE_BF16, IC_SCORE_F16, IC_SCORE_F32, IC_SCORE_MAX_TOP, IC_SCORE_MAX_VOCAB,
 )
+from .states import (  # noqa: F401
+    ICStates, ic_state_workspace_bytes, IC_STATE_BF16, IC_STATE_F16, IC_STATE_MAX_KEY_DIM, IC_STATE_MAX_SEQS, IC_STATE_MAX_VALUE_DIM,
+)

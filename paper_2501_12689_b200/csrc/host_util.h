@@ -29,6 +29,22 @@ inline bool is_device_ptr(const void* p, int device) {
   return a.type == cudaMemoryTypeDevice && a.device == device;
 }
 
+// Rows of `length` elements at t * token_stride + h * head_stride, t < tokens, h < heads: do two of them share an element?
+inline bool rows_overlap(int64_t tokens, int64_t heads, int64_t token_stride, int64_t head_stride, int64_t length) {
+  if (tokens > 1 && token_stride < length) return true;
+  if (heads > 1 && head_stride < length) return true;
+  if (tokens <= 1 || heads <= 1) return false;
+  // one within the other, as in a tensor of tokens and heads in either order
+  if ((token_stride - length) / head_stride >= heads - 1 || (head_stride - length) / token_stride >= tokens - 1) return false;
+  // otherwise: a head h further on is d tokens back, give or take less than a row
+  for (int64_t h = 1; h < heads; ++h) {
+    const int64_t d = h * head_stride / token_stride, rest = h * head_stride - d * token_stride;
+    if (d < tokens && d > 0 && rest < length) return true;
+    if (d + 1 < tokens && token_stride - rest < length) return true;
+  }
+  return false;
+}
+
 // A mapped host word for a handle's error, zero; nullptr if there is no memory.
 int* take_status_word();
 void give_status_word(int* w);

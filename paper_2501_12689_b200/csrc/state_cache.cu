@@ -1,0 +1,269 @@
+// Host side of the C ABI declared in include/ic_state.h: argument checking, buffer ownership and kernel
+// sequencing of the state cache.
+#include <math.h>
+#include <string.h>
+
+#include <mutex>
+#include <new>
+
+#include "../../include/ic_state.h"
+#include "host_util.h"
+#include "kv.h"
+#include "state.h"
+
+using icc::DeviceGuard;
+using icc::fail;
+using icc::is_device_ptr;
+
+struct ic_state {
+  icc::StateView v;
+  int device = 0, sm_count = 0, smem_optin = 0;
+  bool f16 = false;
+  cudaStream_t stream = nullptr;
+  void* own_pool = nullptr;
+  void* own_workspace = nullptr;
+  int* h_status = nullptr;
+  int64_t launches = 0;
+};
+
+namespace {
+
+static_assert(IC_STATE_MAX_SEQS == icc::STATE_MAX_SEQS, "the checks have a bit for each");
+constexpr size_t WORDS = 256;             // error and plan, at the head of the workspace
+
+cudaError_t configure_kernels(int dev, int smem) {
+  static std::mutex mutex;
+  static bool done[64] = {};
+  std::lock_guard<std::mutex> lock(mutex);
+  if (dev < 64 && done[dev]) return cudaSuccess;
+  const cudaError_t e = icc::state_configure(smem);
+  if (e == cudaSuccess && dev < 64) done[dev] = true;
+  return e;
+}
+
+int read_opts(const ic_state_opts_t* opts, ic_state_opts_t* o) {
+  memset(o, 0, sizeof *o);
+  if (!opts) return fail(IC_ERR_INVALID, "NULL options");
+  if (opts->struct_size < sizeof(uint32_t) || opts->struct_size > sizeof *o)
+    return fail(IC_ERR_INVALID, "opts.struct_size %u not understood (this build: %zu)", opts->struct_size, sizeof *o);
+  memcpy(o, opts, opts->struct_size);
+  if (o->dtype != IC_STATE_BF16 && o->dtype != IC_STATE_F16) return fail(IC_ERR_INVALID, "unknown dtype %d", o->dtype);
+  if (o->n_layers < 1 || o->n_layers > 1024 || o->n_heads < 1 || o->n_heads > icc::STATE_MAX_HEADS)
+    return fail(IC_ERR_INVALID, "n_layers %d and n_heads %d must be in [1, 1024]", o->n_layers, o->n_heads);
+  if (o->key_dim < 8 || o->key_dim > IC_STATE_MAX_KEY_DIM || o->key_dim % 8)
+    return fail(IC_ERR_INVALID, "key_dim %d must be a multiple of 8 in [8, %d]", o->key_dim, IC_STATE_MAX_KEY_DIM);
+  if (o->value_dim < 8 || o->value_dim > IC_STATE_MAX_VALUE_DIM || o->value_dim % 8)
+    return fail(IC_ERR_INVALID, "value_dim %d must be a multiple of 8 in [8, %d]", o->value_dim, IC_STATE_MAX_VALUE_DIM);
+  if (o->max_seqs < 1 || o->max_seqs > IC_STATE_MAX_SEQS) return fail(IC_ERR_INVALID, "max_seqs %d must be in [1, %d]", o->max_seqs, IC_STATE_MAX_SEQS);
+  return IC_OK;
+}
+
+size_t workspace_need(const ic_state_opts_t& o) {
+  (void)o;
+  return WORDS;
+}
+
+int reported(int code) {
+  if (code == icc::KV_INVALID)
+    return fail(IC_ERR_INVALID, "an earlier call was given a bad sequence, start or rate on the device; call ic_state_sync to clear");
+  return fail(IC_ERR_TIMEOUT, "an earlier kernel gave up on a bounded wait (code %d); call ic_state_sync to clear", code);
+}
+
+int check_handle(ic_state* s) {
+  if (!s) return fail(IC_ERR_INVALID, "NULL handle");
+  const int code = *reinterpret_cast<volatile int*>(s->h_status);
+  return code == icc::KV_OK ? IC_OK : reported(code);
+}
+
+int check_rows(const ic_state* s, const void* p, int64_t token_stride, int64_t head_stride, const char* what) {
+  if (!p || !is_device_ptr(p, s->device)) return fail(IC_ERR_INVALID, "%s must be a device pointer on device %d", what, s->device);
+  constexpr int64_t most = 1ll << 46;
+  if ((reinterpret_cast<uintptr_t>(p) & 15) || token_stride % 8 || head_stride % 8 || token_stride < 0 || head_stride < 0 || token_stride > most ||
+      head_stride > most)
+    return fail(IC_ERR_INVALID, "%s must be 16-byte aligned, its strides (%lld, %lld) non-negative multiples of 8 elements", what,
+                (long long)token_stride, (long long)head_stride);
+  return IC_OK;
+}
+
+int check_list(const ic_state* s, const void* p, const char* what) {
+  if (!p || !is_device_ptr(p, s->device) || (reinterpret_cast<uintptr_t>(p) & 3))
+    return fail(IC_ERR_INVALID, "%s must be a device array on device %d", what, s->device);
+  return IC_OK;
+}
+
+int check_n(const ic_state* s, int32_t n) {
+  if (n < 0 || n > s->v.max_seqs) return fail(IC_ERR_INVALID, "n = %d outside [0, max_seqs = %d]", n, s->v.max_seqs);
+  return IC_OK;
+}
+
+int launched(ic_state* s, cudaError_t e, int n, const char* what) {
+  if (e != cudaSuccess) return fail(IC_ERR_CUDA, "%s launch failed: %s", what, cudaGetErrorString(e));
+  s->launches += n;
+  return IC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ic_state_workspace_bytes(const ic_state_opts_t* opts) {
+  ic_state_opts_t o;
+  return read_opts(opts, &o) == IC_OK ? workspace_need(o) : 0;
+}
+
+ic_state_t* ic_state_create(const ic_state_opts_t* opts) {
+  ic_state_opts_t o;
+  if (read_opts(opts, &o) != IC_OK) return nullptr;
+  int dev = 0, sms = 0, smem = 0;
+  if (icc::usable_device(o.device, &dev, &sms, &smem) != IC_OK) return nullptr;
+  DeviceGuard guard(dev);
+  const size_t need = workspace_need(o);
+  auto lent = [&](const void* p, const char* what) {
+    if (!p || (is_device_ptr(p, dev) && (reinterpret_cast<uintptr_t>(p) & 255) == 0)) return true;
+    fail(IC_ERR_INVALID, "opts.%s must be a 256-byte aligned device pointer on device %d", what, dev);
+    return false;
+  };
+  if (!lent(o.pool, "pool") || !lent(o.workspace, "workspace")) return nullptr;
+  if (o.workspace && o.workspace_bytes < need) {
+    fail(IC_ERR_NOMEM, "opts.workspace holds %zu bytes, %zu are needed", o.workspace_bytes, need);
+    return nullptr;
+  }
+  ic_state* s = new (std::nothrow) ic_state();
+  if (!s) {
+    fail(IC_ERR_NOMEM, "host allocation failed");
+    return nullptr;
+  }
+  memset(&s->v, 0, sizeof s->v);
+  s->device = dev;
+  s->sm_count = sms;
+  s->smem_optin = smem;
+  s->f16 = o.dtype == IC_STATE_F16;
+  s->stream = static_cast<cudaStream_t>(o.stream);
+  icc::StateView& v = s->v;
+  v.n_layers = o.n_layers;
+  v.n_heads = o.n_heads;
+  v.key_dim = o.key_dim;
+  v.value_dim = o.value_dim;
+  v.max_seqs = o.max_seqs;
+  cudaError_t e = cudaSuccess;
+  const size_t pool_bytes = v.seq_floats() * 4 * o.max_seqs;
+  if (!o.pool) {
+    e = cudaMalloc(&s->own_pool, pool_bytes);
+    if (e == cudaSuccess) e = cudaMemsetAsync(s->own_pool, 0, pool_bytes, s->stream);
+  }
+  v.pool = o.pool ? o.pool : static_cast<float*>(s->own_pool);
+  if (e == cudaSuccess && !o.workspace) e = cudaMalloc(&s->own_workspace, need);
+  v.err = static_cast<int*>(o.workspace ? o.workspace : s->own_workspace);
+  v.meta = v.err + 32;
+  if (e == cudaSuccess) e = cudaMemsetAsync(v.err, 0, WORDS, s->stream);
+  if (e == cudaSuccess && !(s->h_status = icc::take_status_word())) e = cudaErrorMemoryAllocation;
+  if (e == cudaSuccess) e = cudaHostGetDevicePointer(reinterpret_cast<void**>(&v.host_status), s->h_status, 0);
+  if (e == cudaSuccess) e = configure_kernels(dev, smem);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    ic_state_destroy(s);
+    fail(e == cudaErrorMemoryAllocation ? IC_ERR_NOMEM : IC_ERR_CUDA, "setting up the states (a pool of %zu bytes) failed: %s", pool_bytes,
+         cudaGetErrorString(e));
+    return nullptr;
+  }
+  return s;
+}
+
+void ic_state_destroy(ic_state_t* s) {
+  if (!s) return;
+  DeviceGuard guard(s->device);
+  cudaStreamSynchronize(s->stream);
+  if (s->own_pool) cudaFree(s->own_pool);
+  if (s->own_workspace) cudaFree(s->own_workspace);
+  if (s->h_status) icc::give_status_word(s->h_status);
+  delete s;
+}
+
+int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
+  int rc = check_handle(s);
+  if (rc != IC_OK) return rc;
+  if (!args) return fail(IC_ERR_INVALID, "NULL arguments");
+  ic_state_attend_t a;
+  memset(&a, 0, sizeof a);
+  if (args->struct_size < sizeof(uint32_t) || args->struct_size > sizeof a)
+    return fail(IC_ERR_INVALID, "struct_size %u not understood (this build: %zu)", args->struct_size, sizeof a);
+  memcpy(&a, args, args->struct_size);
+  if ((rc = check_n(s, a.n)) != IC_OK) return rc;
+  if (a.layer < 0 || a.layer >= s->v.n_layers) return fail(IC_ERR_INVALID, "layer %d outside [0, %d)", a.layer, s->v.n_layers);
+  if (!isfinite(a.scale)) return fail(IC_ERR_INVALID, "scale %g must be finite", a.scale);
+  if (a.n_tokens < 0 || a.n_tokens > 0x7fffffffll || (!a.starts && a.n_tokens != a.n))
+    return fail(IC_ERR_INVALID, "n_tokens = %lld does not fit n = %d", (long long)a.n_tokens, a.n);
+  if (a.n == 0 && a.n_tokens > 0) return fail(IC_ERR_INVALID, "tokens without sequences");
+  if (a.n_tokens == 0) return IC_OK;
+  if ((rc = check_rows(s, a.q, a.q_token_stride, a.q_head_stride, "q")) != IC_OK ||
+      (rc = check_rows(s, a.k, a.k_token_stride, a.k_head_stride, "k")) != IC_OK ||
+      (rc = check_rows(s, a.v, a.v_token_stride, a.v_head_stride, "v")) != IC_OK ||
+      (rc = check_rows(s, a.out, a.out_token_stride, a.out_head_stride, "out")) != IC_OK ||
+      (rc = check_list(s, a.rates, "rates")) != IC_OK || (rc = check_list(s, a.seqs, "seqs")) != IC_OK ||
+      (a.starts && (rc = check_list(s, a.starts, "starts")) != IC_OK))
+    return rc;
+  if (icc::rows_overlap(a.n_tokens, s->v.n_heads, a.out_token_stride, a.out_head_stride, s->v.value_dim))
+    return fail(IC_ERR_INVALID, "rows of out overlap with strides (%lld, %lld)", (long long)a.out_token_stride, (long long)a.out_head_stride);
+  icc::StateAttendParams p;
+  p.v = s->v;
+  p.q = {static_cast<const unsigned char*>(a.q), a.q_token_stride, a.q_head_stride};
+  p.k = {static_cast<const unsigned char*>(a.k), a.k_token_stride, a.k_head_stride};
+  p.val = {static_cast<const unsigned char*>(a.v), a.v_token_stride, a.v_head_stride};
+  p.out = {static_cast<const unsigned char*>(a.out), a.out_token_stride, a.out_head_stride};
+  p.rates = a.rates;
+  p.seqs = a.seqs;
+  p.starts = a.starts;
+  p.n = a.n;
+  p.layer = a.layer;
+  p.checked = a.n > icc::STATE_CHECK_THREADS;
+  p.n_tokens = a.n_tokens;
+  p.scale = a.scale;
+  DeviceGuard guard(s->device);
+  if (p.checked && (rc = launched(s, icc::state_check_launch(p, s->stream), 1, "check")) != IC_OK) return rc;
+  return launched(s, icc::state_step_launch(p, s->f16, s->sm_count, s->stream), 1, "state");
+}
+
+int ic_state_fork(ic_state_t* s, const int32_t* parents, const int32_t* children, int32_t n) {
+  int rc = check_handle(s);
+  if (rc == IC_OK) rc = check_n(s, n);
+  if (rc != IC_OK || n == 0) return rc;
+  if ((rc = check_list(s, parents, "parents")) != IC_OK || (rc = check_list(s, children, "children")) != IC_OK) return rc;
+  DeviceGuard guard(s->device);
+  int launches = 0;
+  const cudaError_t e = icc::state_fork_launch(s->v, parents, children, n, s->sm_count, &launches, s->stream);
+  return launched(s, e, launches, "fork");
+}
+
+int ic_state_clear(ic_state_t* s, const int32_t* seqs, int32_t n) {
+  int rc = check_handle(s);
+  if (rc != IC_OK) return rc;
+  if (n < 0) return fail(IC_ERR_INVALID, "n = %d is negative", n);
+  if (n == 0) return IC_OK;
+  if ((rc = check_list(s, seqs, "seqs")) != IC_OK) return rc;
+  DeviceGuard guard(s->device);
+  return launched(s, icc::state_clear_launch(s->v, seqs, n, s->sm_count, s->stream), 1, "clear");
+}
+
+int ic_state_sync(ic_state_t* s) {
+  if (!s) return fail(IC_ERR_INVALID, "NULL handle");
+  DeviceGuard guard(s->device);
+  cudaError_t e = cudaStreamSynchronize(s->stream);
+  if (e != cudaSuccess) return fail(IC_ERR_CUDA, "stream sync failed: %s", cudaGetErrorString(e));
+  const int code = *reinterpret_cast<volatile int*>(s->h_status);
+  if (code == icc::KV_OK) return IC_OK;
+  *s->h_status = icc::KV_OK;
+  e = cudaMemsetAsync(s->v.err, 0, WORDS, s->stream);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s->stream);
+  if (e != cudaSuccess) return fail(IC_ERR_CUDA, "clearing the error failed: %s", cudaGetErrorString(e));
+  return reported(code);
+}
+
+int ic_state_set_stream(ic_state_t* s, void* cuda_stream) {
+  if (!s) return fail(IC_ERR_INVALID, "NULL handle");
+  s->stream = static_cast<cudaStream_t>(cuda_stream);
+  return IC_OK;
+}
+
+int64_t ic_state_launch_count(const ic_state_t* s) { return s ? s->launches : IC_ERR_INVALID; }
+
+}  // extern "C"
