@@ -32,8 +32,14 @@ struct StateAttendParams {
   const int* seqs;
   const int* starts;        // null: one token per sequence
   int n, layer, checked;    // checked: a kernel before has looked over the arguments
+  int first_seq;            // of the call, where this launch's sequences begin (starts null: their first token)
   int64_t n_tokens;
   float scale;
+  // calls of many tokens: value slices of a head; states that CTAs publish for one another, and how much of each is there
+  int slices;
+  float* slots;
+  size_t slot_floats;       // of one CTA's
+  unsigned* flags;          // [CTAs + 1], zero between launches
 };
 
 cudaError_t state_configure(int smem_optin);
@@ -42,6 +48,11 @@ cudaError_t state_check_launch(const StateAttendParams& p, cudaStream_t st);
 cudaError_t state_step_launch(const StateAttendParams& p, bool f16, int sm_count, cudaStream_t st);
 cudaError_t state_fork_launch(const StateView& v, const int* parents, const int* children, int n, int sm_count, int* launches, cudaStream_t st);
 cudaError_t state_clear_launch(const StateView& v, const int* seqs, int n, int sm_count, cudaStream_t st);
+
+// Many tokens a sequence: chunks of them, on the tensor cores.  At most STATE_BATCH sequences a launch.
+cudaError_t state_chunk_configure(int smem_optin);
+size_t state_slot_floats(int key_dim, int value_dim);
+cudaError_t state_chunk_launch(StateAttendParams p, bool f16, int sm_count, int smem_optin, cudaStream_t st);
 
 constexpr int STATE_CHECK_THREADS = 256;  // sequences that every CTA looks over by itself
 

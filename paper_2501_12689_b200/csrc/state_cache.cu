@@ -10,6 +10,7 @@
 #include "host_util.h"
 #include "kv.h"
 #include "state.h"
+#include "state_schedule.cuh"
 
 using icc::DeviceGuard;
 using icc::fail;
@@ -29,14 +30,18 @@ struct ic_state {
 namespace {
 
 static_assert(IC_STATE_MAX_SEQS == icc::STATE_MAX_SEQS, "the checks have a bit for each");
-constexpr size_t WORDS = 256;             // error and plan, at the head of the workspace
+// The head of the workspace: error and plan, then the flags of published states.  Zeros to begin with, and again after an error.
+constexpr size_t FLAGS = 256, WORDS = FLAGS + 1024;
+static_assert((icc::KV_MAX_CTAS + 1) * 4 <= WORDS - FLAGS, "a flag for each CTA, and their count");
+static_assert(icc::STATE_CHECK_THREADS <= icc::STATE_BATCH, "calls of more sequences than a launch takes are checked before");
 
 cudaError_t configure_kernels(int dev, int smem) {
   static std::mutex mutex;
   static bool done[64] = {};
   std::lock_guard<std::mutex> lock(mutex);
   if (dev < 64 && done[dev]) return cudaSuccess;
-  const cudaError_t e = icc::state_configure(smem);
+  cudaError_t e = icc::state_configure(smem);
+  if (e == cudaSuccess) e = icc::state_chunk_configure(smem);
   if (e == cudaSuccess && dev < 64) done[dev] = true;
   return e;
 }
@@ -59,8 +64,7 @@ int read_opts(const ic_state_opts_t* opts, ic_state_opts_t* o) {
 }
 
 size_t workspace_need(const ic_state_opts_t& o) {
-  (void)o;
-  return WORDS;
+  return WORDS + icc::KV_MAX_CTAS * icc::state_slot_floats(o.key_dim, o.value_dim) * 4;
 }
 
 int reported(int code) {
@@ -220,7 +224,20 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
   p.scale = a.scale;
   DeviceGuard guard(s->device);
   if (p.checked && (rc = launched(s, icc::state_check_launch(p, s->stream), 1, "check")) != IC_OK) return rc;
-  return launched(s, icc::state_step_launch(p, s->f16, s->sm_count, s->stream), 1, "state");
+  p.first_seq = 0;
+  p.slices = 1;
+  p.flags = reinterpret_cast<unsigned*>(reinterpret_cast<unsigned char*>(s->v.err) + FLAGS);
+  p.slots = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS);
+  p.slot_floats = icc::state_slot_floats(s->v.key_dim, s->v.value_dim);
+  if (a.n_tokens <= 8 * (int64_t)a.n) return launched(s, icc::state_step_launch(p, s->f16, s->sm_count, s->stream), 1, "state");
+  for (int off = 0; off < a.n && rc == IC_OK; off += icc::STATE_BATCH) {
+    p.first_seq = off;
+    p.seqs = a.seqs + off;
+    p.starts = a.starts ? a.starts + off : nullptr;
+    p.n = a.n - off < icc::STATE_BATCH ? a.n - off : icc::STATE_BATCH;
+    rc = launched(s, icc::state_chunk_launch(p, s->f16, s->sm_count, s->smem_optin, s->stream), 1, "state");
+  }
+  return rc;
 }
 
 int ic_state_fork(ic_state_t* s, const int32_t* parents, const int32_t* children, int32_t n) {

@@ -68,9 +68,11 @@ def close(got, state, want, t, several):
     steps = (4 * t + 64) * 2.0 ** -24
     bound = u * out.abs() + (1.01 * u * rounded if several else 0.0) + 2 * steps * summed + 2.0 ** -25
     off = (got.double() - out).abs()
-    assert torch.isfinite(got).all() and (off <= bound).all(), f"out: {(off / bound).max().item():.2f} times the bound"
+    worst = (off / bound).max().item()
+    assert worst <= 1.0, f"out: {worst:.2f} times the bound"
     off = (state.double() - s).abs()
-    assert (off <= steps * size + 1e-30).all(), f"state: {(off / (steps * size + 1e-30)).max().item():.2f} times the bound"
+    worst = (off / (steps * size + 1e-30)).max().item()
+    assert worst <= 1.0, f"state: {worst:.2f} times the bound"
     # roundings are as often up as down: far from adding up
     for h in range(s.shape[0]):
         assert (state[h].double() - s[h]).norm() <= 2.0 ** -19 * s[h].norm() + 1e-30
@@ -102,7 +104,7 @@ def run(counts, *, heads=2, dk=64, dv=64, dtype=BF16, layers=2, layer=1, max_seq
         if c:
             part = slice(a, a + c)
             want = formula(q[part], k[part], v[part], rates, before[x, layer], 1.0 / math.sqrt(dk) if scale is None else scale)
-            close(got[part], s.pool[x, layer], want, c, c > 1)
+            close(got[part], s.pool[x, layer], want, c, max(counts) > 1)
         else:
             assert torch.equal(s.pool[x], before[x])
         a += c
