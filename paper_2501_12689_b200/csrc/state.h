@@ -1,5 +1,6 @@
 // State cache: what its kernels are given, and the launch functions that state_cache.cu calls.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -52,7 +53,12 @@ cudaError_t state_clear_launch(const StateView& v, const int* seqs, int n, int s
 // Many tokens a sequence: chunks of them, on the tensor cores.  At most STATE_BATCH sequences a launch.
 cudaError_t state_chunk_configure(int smem_optin);
 size_t state_slot_floats(int key_dim, int value_dim);
-cudaError_t state_chunk_launch(StateAttendParams p, bool f16, int sm_count, int smem_optin, cudaStream_t st);
+// Rows of q, k and v as tensor maps [heads, tokens, dim] of boxes of 64 tokens and 64 elements; there: all three could be made.
+struct StateMaps {
+  CUtensorMap q, k, val;
+  int there;
+};
+cudaError_t state_chunk_launch(StateAttendParams p, const StateMaps& maps, bool f16, int sm_count, int smem_optin, cudaStream_t st);
 
 constexpr int STATE_CHECK_THREADS = 256;  // sequences that every CTA looks over by itself
 

@@ -100,6 +100,28 @@ int check_n(const ic_state* s, int32_t n) {
   return IC_OK;
 }
 
+// Rows of tokens and heads as a tensor map, if their strides allow one (a shared row, a stride of 0, does only among the heads).
+bool encode_rows(const ic_state* s, const icc::StateRows& r, int dim, int64_t tokens, CUtensorMap* map) {
+  static const icc::EncodeTiledFn encode = [] {
+    cudaDriverEntryPointQueryResult found;
+    void* fn = nullptr;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      fn = nullptr;
+    }
+    return reinterpret_cast<icc::EncodeTiledFn>(fn);
+  }();
+  const bool shared = r.head_stride == 0;
+  const int64_t token_bytes = r.token_stride * 2, head_bytes = shared ? (int64_t)dim * 2 : r.head_stride * 2;
+  if (!encode || token_bytes < (int64_t)dim * 2 || head_bytes < (int64_t)dim * 2 || token_bytes >= 1ll << 40 || head_bytes >= 1ll << 40) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)tokens, shared ? 1u : (cuuint64_t)s->v.n_heads};
+  const cuuint64_t strides[2] = {(cuuint64_t)token_bytes, (cuuint64_t)head_bytes};
+  const cuuint32_t box[3] = {64, icc::STATE_CHUNK, 1}, steps[3] = {1, 1, 1};
+  return encode(map, s->f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<unsigned char*>(r.at), dims, strides, box,
+                steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int launched(ic_state* s, cudaError_t e, int n, const char* what) {
   if (e != cudaSuccess) return fail(IC_ERR_CUDA, "%s launch failed: %s", what, cudaGetErrorString(e));
   s->launches += n;
@@ -230,12 +252,15 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
   p.slots = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS);
   p.slot_floats = icc::state_slot_floats(s->v.key_dim, s->v.value_dim);
   if (a.n_tokens <= 8 * (int64_t)a.n) return launched(s, icc::state_step_launch(p, s->f16, s->sm_count, s->stream), 1, "state");
+  icc::StateMaps maps;
+  maps.there = encode_rows(s, p.q, s->v.key_dim, a.n_tokens, &maps.q) && encode_rows(s, p.k, s->v.key_dim, a.n_tokens, &maps.k) &&
+               encode_rows(s, p.val, s->v.value_dim, a.n_tokens, &maps.val);
   for (int off = 0; off < a.n && rc == IC_OK; off += icc::STATE_BATCH) {
     p.first_seq = off;
     p.seqs = a.seqs + off;
     p.starts = a.starts ? a.starts + off : nullptr;
     p.n = a.n - off < icc::STATE_BATCH ? a.n - off : icc::STATE_BATCH;
-    rc = launched(s, icc::state_chunk_launch(p, s->f16, s->sm_count, s->smem_optin, s->stream), 1, "state");
+    rc = launched(s, icc::state_chunk_launch(p, maps, s->f16, s->sm_count, s->smem_optin, s->stream), 1, "state");
   }
   return rc;
 }
