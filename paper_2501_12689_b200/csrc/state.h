@@ -37,7 +37,7 @@ struct StateAttendParams {
   int64_t n_tokens;
   float scale;
   // calls of many tokens: value slices of a head; states that CTAs publish for one another, and how much of each is there
-  int slices;
+  int slices, first_item, n_items;        // (heads times slices) items of a launch
   float* slots;
   size_t slot_floats;       // of one CTA's
   unsigned* flags;          // [CTAs + 1], zero between launches

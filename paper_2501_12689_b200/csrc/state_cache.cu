@@ -247,7 +247,7 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
   DeviceGuard guard(s->device);
   if (p.checked && (rc = launched(s, icc::state_check_launch(p, s->stream), 1, "check")) != IC_OK) return rc;
   p.first_seq = 0;
-  p.slices = 1;
+  p.slices = (s->v.value_dim + 127) / 128;
   p.flags = reinterpret_cast<unsigned*>(reinterpret_cast<unsigned char*>(s->v.err) + FLAGS);
   p.slots = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS);
   p.slot_floats = icc::state_slot_floats(s->v.key_dim, s->v.value_dim);
@@ -260,7 +260,11 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
     p.seqs = a.seqs + off;
     p.starts = a.starts ? a.starts + off : nullptr;
     p.n = a.n - off < icc::STATE_BATCH ? a.n - off : icc::STATE_BATCH;
-    rc = launched(s, icc::state_chunk_launch(p, maps, s->f16, s->sm_count, s->smem_optin, s->stream), 1, "state");
+    const int items = s->v.n_heads * ((s->v.value_dim + 127) / 128), most = icc::state_items(a.n_tokens, p.n);
+    for (p.first_item = 0; p.first_item < items && rc == IC_OK; p.first_item += most) {
+      p.n_items = items - p.first_item < most ? items - p.first_item : most;
+      rc = launched(s, icc::state_chunk_launch(p, maps, s->f16, s->sm_count, s->smem_optin, s->stream), 1, "state");
+    }
   }
   return rc;
 }

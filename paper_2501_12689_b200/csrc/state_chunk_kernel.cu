@@ -20,11 +20,11 @@
 //   warps 0-3    results: out = scale (O1 + l^(t+1) O2), rounded and stored
 //   warps 4-7    the state: loaded, copied for the queries, S <- l^n S + U, and stored in the end
 //   warps 8-11   W
-//   warps 12-13  P
-//   warp 14      issues the products: U(c), O2(c), O1(c), P(c + 1), ...
-//   warp 15      loads of K, V and Q into a ring of stages: boxes of tensor maps; of a sequence's last, shorter chunk (and where the strides
-//                allow no map) 16-byte copies, with zeros behind the end
-//
+//   warps 12-13  P; warp 12 also loads K, V and Q into a ring of stages: boxes of tensor maps (where the strides allow none, 16-byte copies)
+//   warp 14      issues the products U(c), O2(c)
+//   warp 15      issues P(c + 1), O1(c)
+// Two warps issue because a product takes one about 100 cycles, more than the tensor cores.  The rows of a sequence's last chunk that
+// lie behind its end (another sequence's) are set to zeros in shared memory, by the warps of W.
 // Bound: HBM, 1 KB a token and head of 128 x 128; a chunk is 64 KB, 2,750 cycles of an SM's share.  The products take 1,600.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -46,7 +46,7 @@ constexpr int THREADS = 512;
 constexpr int MAX_STAGES = 6;
 constexpr int OUT_BYTES = 4 * 32 * 64;
 constexpr int ROW_CHUNK = C * 128;                    // bytes of 64 tokens' 64 elements
-enum : int { W_OUT = 0, W_STATE = 4, W_VALUES = 8, W_SCORES = 12, W_PRODUCTS = 14, W_LOADS = 15 };
+enum : int { W_OUT = 0, W_STATE = 4, W_VALUES = 8, W_SCORES = 12, W_STATE_PRODUCTS = 14, W_RESULT_PRODUCTS = 15 };
 // Registers of the four warpgroups' threads; they are launched with 128.
 constexpr int OUT_REGS = 96, STATE_REGS = 208, VALUE_REGS = 96, OTHER_REGS = 112;
 static_assert(OUT_REGS + STATE_REGS + VALUE_REGS + OTHER_REGS <= 4 * 128, "what some have more, others have less");
@@ -56,7 +56,7 @@ constexpr uint32_t T_P = 0, T_O1 = 64, T_O2 = 128, T_COPY = 192, T_U = 256, T_W 
 template <bool F16>
 constexpr int PARTS = F16 ? 2 : 3;                    // 16-bit numbers that hold one of W
 
-// A warp's powers of l.
+// A head's powers of l.
 constexpr int FALL = C;
 struct Fall {
   float at[2 * C + 4];                                // l^j at FALL + j, j = 0 .. 64, with zeros in front
@@ -64,18 +64,31 @@ struct Fall {
 
 struct Tail {
   StateLine line;
-  Fall fall[W_PRODUCTS];                              // of each warp that needs one
+  int starts[STATE_BATCH + 1];                        // of the call's tokens
+  StatePlan plan;
+  // published states that the last piece's is put together from: whose, and what is left of them after the chunks between
+  int slots, slot_cta[KV_MAX_CTAS];
+  float slot_weight[KV_MAX_CTAS];
+  Fall fall[2];                                       // of a piece and the next one
+  uint64_t fall_ready[2], fall_free[2];
   alignas(16) float token_scale[2][C];                      // fp16: what P's row was divided by, by the chunk's parity
   float lane_scale[2][128];                           // fp16: what W's column was multiplied by
   float copy_scale[2][128];                           // fp16: what the copy of S has to be multiplied by
   uint64_t full[MAX_STAGES], empty[MAX_STAGES];
-  uint64_t p_full, p_ready, w_ready, copy_ready, u_full, u_free, o2_done, o_full, o_free, drain;
+  uint64_t w_ready[2], w_free[2];                     // of a chunk's halves
+  uint64_t clean[MAX_STAGES];                         // of a stage with a sequence's last chunk: rows behind the end are zeros
+  uint64_t p_full, p_ready, copy_ready, u_full, u_free, o1_full, o2_full, o_free, drain[2];
   uint64_t slots_read[MAX_STAGES];
   uint32_t seen[STATE_MAX_SEQS / 32];
   uint32_t tmem_base;
   int abort_flag, holds;
 };
 
+__device__ __forceinline__ float ld_shared(uint32_t addr) {
+  float x;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(x) : "r"(addr));
+  return x;
+}
 // The power of two that brings the largest magnitude m (>= 0, finite) into [2^13, 2^14); 1 for 0.
 __device__ __forceinline__ float lift_of(float m, int most) {
   if (m == 0.0f) return 1.0f;
@@ -84,9 +97,42 @@ __device__ __forceinline__ float lift_of(float m, int most) {
 }
 __device__ __forceinline__ float reciprocal_of_power(float p) { return __uint_as_float((254u << 23) - __float_as_uint(p)); }
 
+// Where a role is in the ring of stages.
+struct Ring {
+  int stage, n_stages;
+  uint32_t phase;
+  __device__ __forceinline__ explicit Ring(int n) : stage(0), n_stages(n), phase(0) {}
+  __device__ __forceinline__ void advance() {
+    if (++stage == n_stages) {
+      stage = 0;
+      phase ^= 1u;
+    }
+  }
+};
+
+// A wait of a whole warp, in few instructions (the roles' code together has to stay in the instruction cache): up to WAIT_TRIES looks at the
+// barrier, of 20 cycles or more each, so that it ends after a second or some.
+constexpr int WAIT_TRIES = 1 << 26;
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+#pragma unroll 1
+  for (int i = 0; i < WAIT_TRIES; ++i) {
+    if (__all_sync(FULL_MASK, mbar_try_wait(bar, parity))) return true;
+    if (__any_sync(FULL_MASK, *abort_flag != 0)) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+
 template <bool F16>
 __device__ __forceinline__ float2 pair16(uint32_t x) {
   return F16 ? __half22float2(*reinterpret_cast<const __half2*>(&x)) : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
+
+// e^(-rate * steps): the exponent in 64 bits, as it would be rounded to 1e-6 in 32, and what is left of it below a power of two in 32.
+__device__ __noinline__ float fall_of(float rate, int steps) {
+  if (steps == 0) return 1.0f;                       // (also of an infinite rate)
+  const double y = fmax(-(double)rate * steps * 1.4426950408889634, -200.0), whole = rint(y);
+  return ldexpf(exp2f((float)(y - whole)), (int)whole);
 }
 
 template <bool F16, int DK, int DV>
@@ -111,23 +157,32 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
   if (tid == 0) {
     for (int s = 0; s < n_stages; ++s) {
       mbar_init(&t->full[s], 32);
-      mbar_init(&t->empty[s], 1);
+      mbar_init(&t->empty[s], 2);                    // the two warps that issue products
       mbar_init(&t->slots_read[s], 2 * X::LANE_WARPS);
+      mbar_init(&t->clean[s], X::LANE_WARPS);
     }
     mbar_init(&t->p_full, 1);
     mbar_init(&t->p_ready, 2);
-    mbar_init(&t->w_ready, X::LANE_WARPS);
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(&t->w_ready[h], X::LANE_WARPS);
+      mbar_init(&t->w_free[h], 1);
+    }
     mbar_init(&t->copy_ready, X::LANE_WARPS);
     mbar_init(&t->u_full, 1);
     mbar_init(&t->u_free, X::LANE_WARPS);
-    mbar_init(&t->o2_done, 1);
-    mbar_init(&t->o_full, 1);
+    mbar_init(&t->o2_full, 1);
+    mbar_init(&t->o1_full, 1);
     mbar_init(&t->o_free, X::LANE_WARPS);
-    mbar_init(&t->drain, 1);
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(&t->fall_ready[h], 1);
+      mbar_init(&t->fall_free[h], 3 * X::LANE_WARPS + 2);
+    }
+    mbar_init(&t->drain[0], 1);
+    mbar_init(&t->drain[1], 1);
     t->abort_flag = 0;
     mbar_fence_init();
   }
-  if (warp == W_PRODUCTS) tmem_alloc(&t->tmem_base, 512);
+  if (warp == W_STATE_PRODUCTS) tmem_alloc(&t->tmem_base, 512);
   grid_dep_launch_dependents();
   grid_dep_wait();
   const bool holds = state_call_holds(p, t->seen);
@@ -136,7 +191,10 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     int sum = 0;
     for (int i0 = 0; i0 < p.n; i0 += 32) {
       const int i = i0 + lane;
-      const int mine = i < p.n ? (int)(((unsigned)(p.starts ? p.starts[i + 1] - p.starts[i] : 1) + C - 1) / C) : 0;
+      const int from = i <= p.n ? (p.starts ? p.starts[i] : p.first_seq + i) : 0, to = i < p.n ? (p.starts ? p.starts[i + 1] : from + 1) : from;
+      if (i < p.n) t->starts[i] = from;
+      if (i == p.n - 1) t->starts[p.n] = to;
+      const int mine = (int)(((unsigned)(to - from) + C - 1) / C);
       int inc = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -149,14 +207,35 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     if (lane == 0) {
       t->line.before[0] = 0;
       t->line.n = p.n;
-      t->line.per_chunk = v.n_heads * p.slices;
+      t->line.per_chunk = p.n_items;
       t->line.parts = gridDim.x;
+      t->line.set_per();
+      t->plan.make(t->line, blockIdx.x);
     }
+    __syncwarp();
+    int slots = 0;
+    if (t->plan.last.c1)
+      for (int j0 = t->plan.slot_first; j0 < (int)blockIdx.x; j0 += 32) {
+        const int j = j0 + lane;
+        const int to = j < (int)blockIdx.x ? t->line.cut(j + 1) : 0;
+        const bool some = j < (int)blockIdx.x && t->line.cut(j) < to;
+        const unsigned who = __ballot_sync(FULL_MASK, some);
+        if (some) {
+          const int at = slots + __popc(who & ((1u << lane) - 1u));
+          t->slot_cta[at] = j;
+          t->slot_weight[at] = fall_of(p.rates[(t->plan.last.item + p.first_item) / p.slices], C * (t->plan.begin - to));
+        }
+        slots += __popc(who);
+      }
+    if (lane == 0) t->slots = slots;
   } else if (!holds && tid == 0) {
     // nothing to do: a line without chunks
     t->line.before[0] = t->line.before[1] = 0;
     t->line.n = t->line.per_chunk = 1;
     t->line.parts = gridDim.x;
+    t->line.set_per();
+    t->plan.make(t->line, blockIdx.x);
+    t->slots = 0;
   }
   tc_fence_before_sync();
   __syncthreads();
@@ -166,46 +245,163 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
   volatile int* abort_flag = &t->abort_flag;
   bool ok = true;
   auto wait = [&](uint64_t* bar, uint32_t parity) {
-    if (ok) ok = mbar_warp_wait(bar, parity, abort_flag);
+    if (ok) ok = wait_for(bar, parity, abort_flag);
   };
-  StateWalk walk(&t->line, blockIdx.x);
+  Ring at(n_stages);                                  // of the roles that follow the stages
+  StateWalk walk(&t->line, &t->plan);
   StatePiece piece;
-  auto head_of = [&](const StatePiece& x) { return x.item / p.slices; };
-  auto slice_of = [&](const StatePiece& x) { return x.item % p.slices; };
-  auto first_token = [&](const StatePiece& x) { return p.starts ? p.starts[x.i] : p.first_seq + x.i; };
-  auto tokens_of = [&](const StatePiece& x) { return p.starts ? p.starts[x.i + 1] - p.starts[x.i] : 1; };
-  // How many published states a piece's own one is put together from.
-  auto slots_of = [&](const StatePiece& x) {
-    int n = 0;
-    if (x.from == StatePiece::PUBLISHED)
-      for (int j = x.first; j < (int)blockIdx.x; ++j) n += t->line.cut(j) < t->line.cut(j + 1);
-    return n;
-  };
-  // This warp's powers of the head's decay.
-  auto fill_falls = [&](const StatePiece& x) {
-    Fall& f = t->fall[warp];
-    const double rate = p.rates[head_of(x)];
-    __syncwarp();
-    for (int j = lane; j < 2 * C + 4; j += 32) f.at[j] = j < FALL ? 0.0f : j == FALL ? 1.0f : (float)exp(-rate * (j - FALL));
-    __syncwarp();
-  };
+  auto head_of = [&](const StatePiece& x) { return (x.item + p.first_item) / p.slices; };
+  auto slice_of = [&](const StatePiece& x) { return (x.item + p.first_item) % p.slices; };
+  auto first_token = [&](const StatePiece& x) { return t->starts[x.i]; };
+  auto tokens_of = [&](const StatePiece& x) { return t->starts[x.i + 1] - t->starts[x.i]; };
+  // Stages in front of a piece's chunks: the state that it begins with, or the published ones that this is put together from, 64 key dimensions each.
+  auto states_of = [&](const StatePiece& x) { return x.from == StatePiece::PUBLISHED ? t->slots : x.from == StatePiece::STORED ? 1 : 0; };
+  auto slots_of = [&](const StatePiece& x) { return DK * states_of(x); };
   auto tell = [&](uint64_t* bar) {
     __syncwarp();
     arrive_one(bar, on);
   };
 
-  if (warp == W_LOADS) {
-    // ------------------------------------------------------------ loads
+  // The powers of its head's decay are worked out by warp 13, a piece ahead.
+  int n_pieces = 0;
+  auto next_piece = [&]() {
+    if (!ok || !walk.next(&piece)) return false;
+    wait(&t->fall_ready[n_pieces & 1], (n_pieces >> 1) & 1);
+    return ok;
+  };
+  auto end_piece = [&]() {
+    tell(&t->fall_free[n_pieces & 1]);
+    ++n_pieces;
+  };
+  // products
+  const int key_steps = (v.key_dim + 15) / 16;
+  constexpr uint32_t CH = ROW_CHUNK >> 4, K_AT = X::K_BYTES >> 4, V_AT = 2 * X::K_BYTES >> 4;
+  // Nothing issued is still running when tensor memory is released.
+  auto drain = [&](uint64_t* bar) {
+    commit_products(bar, on);
+    const long long t0 = clock64();
+    while (!mbar_try_wait(bar, 0) && clock64() - t0 < WAIT_LIMIT_CYCLES) {
+    }
+  };
+
+  if (warp == W_STATE_PRODUCTS) {
+    // ------------------------------------------------------------ U, O2
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-    int n = 0;
-    auto begin = [&]() {
-      wait(&t->empty[n % n_stages], ((n / n_stages) & 1) ^ 1);
-      return ring + (n % n_stages) * X::STAGE;
+    const uint32_t id_o2 = idesc(F16, C, false), id_u = idesc(F16, key_steps * 16, true);
+    const uint64_t rows_desc = umma_desc_k_major_sw128(smem_u32(ring)), columns_desc = desc_mn_major_sw128(smem_u32(ring), ROW_CHUNK);
+    uint32_t ph = 0, out_ph = 0, slots_ph = 0;        // of the barriers that turn once a chunk, and once a chunk with results
+    while (ok && walk.next(&piece)) {
+      for (int j = slots_of(piece); j > 0 && ok; --j) {      // stages that hold published states
+        wait(&t->slots_read[at.stage], (slots_ph >> at.stage) & 1u);      // a stage's barrier turns at each such use
+        slots_ph ^= 1u << at.stage;
+        arrive_one(&t->empty[at.stage], on);
+        at.advance();
+      }
+      for (int c = piece.c0; c < piece.c1 && ok; ++c) {
+        const uint32_t stage = at.stage * (X::STAGE >> 4);
+        wait(&t->full[at.stage], at.phase);
+        wait(&t->u_free, ph ^ 1u);
+        // U by halves of the chunk, so that W's next is made while the other half is used; of each the least parts first: what is cut off of a
+        // sum is a part of what is there
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          wait(&t->w_ready[h], ph);
+          if (!ok) break;
+          if (h == 0 && !maps.there) fence_async_shared();         // the copies were ordinary writes
+          tc_fence_after_sync();
+          const uint64_t b = columns_desc + stage + K_AT + h * 256;
+          const uint32_t a = tmem + T_W + h * 16;
+#pragma unroll
+          for (int w = PARTS<F16> - 1; w >= 0; --w)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)               // 16 tokens further: 8 columns of W, 2048 bytes of K
+              product_tmem(tmem + T_U, a + w * (C / 2) + k * 8, b + k * 128, id_u, h != 0 || w + 1 < PARTS<F16> || k != 0, on);
+          commit_products(&t->w_free[h], on);
+        }
+        if (!ok) break;
+        commit_products(&t->u_full, on);
+        ph ^= 1u;
+        if (!piece.sum_only) {
+          wait(&t->copy_ready, out_ph);
+          wait(&t->o_free, out_ph ^ 1u);
+          out_ph ^= 1u;
+          if (!ok) break;
+          tc_fence_after_sync();
+#pragma unroll
+          for (int k = 0; k < DK * 4; ++k)
+            product_tmem(tmem + T_O2, tmem + T_COPY + k * 8, rows_desc + stage + (k >> 2) * CH + (k & 3) * 2, id_o2, k != 0, k < key_steps ? on : 0u);
+          commit_products(&t->o2_full, on);
+        }
+        commit_products(&t->empty[at.stage], on);
+        at.advance();
+      }
+    }
+    drain(&t->drain[0]);
+  } else if (warp == W_RESULT_PRODUCTS) {
+    // ------------------------------------------------------------ P, O1
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+    const uint32_t id_p = idesc(F16, C, false), id_o1 = idesc(F16, C, false, true);
+    const uint64_t rows_desc = umma_desc_k_major_sw128(smem_u32(ring)), p_desc = umma_desc_k_major_sw128(smem_u32(p_smem)),
+                   columns_desc = desc_mn_major_sw128(smem_u32(ring), ROW_CHUNK);
+    uint32_t ph = 0, clean_ph = 0;
+    int before = -1;                                  // the stage of the chunk whose P is under way
+    // O1 of that chunk, as soon as its P is ready; and with that there is room for the next one's
+    auto ready = [&]() {
+      wait(&t->p_ready, ph);
+      wait(&t->o_free, ph ^ 1u);
+      ph ^= 1u;
+      tc_fence_after_sync();
     };
-    auto end = [&]() {
-      cp_async_arrive(&t->full[n % n_stages]);
-      ++n;
+    auto values = [&]() {
+      const uint64_t a = columns_desc + before * (X::STAGE >> 4) + V_AT;
+#pragma unroll
+      for (int k = 0; k < C / 16; ++k) product_smem(tmem + T_O1, a + k * 128, p_desc + k * 2, id_o1, k != 0, on);
+      commit_products(&t->o1_full, on);
+      commit_products(&t->empty[before], on);
+      before = -1;
     };
+    while (ok && walk.next(&piece)) {
+      const int count = tokens_of(piece);
+      // (of stages that are not for this warp it says so when they are full, or it could lose count of the rounds)
+      for (int j = slots_of(piece) + (piece.sum_only ? piece.c1 - piece.c0 : 0); j > 0 && ok; --j) {
+        if (before >= 0) {
+          ready();
+          if (ok) values();
+        }
+        wait(&t->full[at.stage], at.phase);
+        arrive_one(&t->empty[at.stage], on);
+        at.advance();
+      }
+      for (int c = piece.c0; c < piece.c1 && ok && !piece.sum_only; ++c) {
+        wait(&t->full[at.stage], at.phase);
+        if (count < (c + 1) * C) {                    // rows behind the end have been cleared
+          wait(&t->clean[at.stage], (clean_ph >> at.stage) & 1u);      // a stage's barrier turns at each such use
+          clean_ph ^= 1u << at.stage;
+        }
+        if (before >= 0) ready();
+        if (!ok) break;
+        if (!maps.there) fence_async_shared();        // the copies were ordinary writes
+        tc_fence_after_sync();
+        const uint64_t a = rows_desc + at.stage * (X::STAGE >> 4), b = a + K_AT;
+#pragma unroll
+        for (int k = 0; k < DK * 4; ++k) {
+          const uint32_t step = (k >> 2) * CH + (k & 3) * 2;
+          product_smem(tmem + T_P, a + step, b + step, id_p, k != 0, k < key_steps ? on : 0u);
+        }
+        commit_products(&t->p_full, on);
+        if (before >= 0) values();
+        before = at.stage;
+        at.advance();
+      }
+    }
+    if (ok && before >= 0) {
+      ready();
+      if (ok) values();
+    }
+    drain(&t->drain[1]);
+  } else if (warp >= W_SCORES) {
+    // ------------------------------------------------------------ P, loads
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     // 64 rows of up to CH chunks of 64 elements; what is not there becomes zeros
     auto rows = [&](unsigned char* to, const StateRows& r, int64_t token, int head, int column, int dim, int there, auto ch) {
       constexpr int CH = decltype(ch)::value, LANES = CH * 8, AT_ONCE = 32 / LANES;
@@ -221,174 +417,115 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     };
     const std::integral_constant<int, DK> key_chunks;
     const std::integral_constant<int, DV> value_chunks;
-    while (ok && walk.next(&piece)) {
-      const int head = head_of(piece), count = tokens_of(piece);
-      const int64_t token0 = first_token(piece);
-      if (piece.from == StatePiece::PUBLISHED)
-        for (int h = 0; h < DK && ok; ++h)
-          for (int j = piece.first; j < (int)blockIdx.x && ok; ++j) {
-            if (t->line.cut(j) == t->line.cut(j + 1)) continue;
-            unsigned char* to = begin();
-            if (!ok) break;
-            const long long t0 = clock64();
-            while (ok && ld_acquire_gpu(p.flags + j) != X::LANE_WARPS) {
-              if (*abort_flag || clock64() - t0 > WAIT_LIMIT_CYCLES) ok = false;
-            }
-            ok = __all_sync(FULL_MASK, ok);
-            if (!ok) {
-              *abort_flag = 1;
-              break;
-            }
-            const unsigned char* from = reinterpret_cast<const unsigned char*>(p.slots + (size_t)j * p.slot_floats + h * X::SLOT_HALF);
-            for (int u = lane; u < X::SLOT_HALF / 4; u += 32) cp_async_16(smem_u32(to) + u * 16, from + u * 16, true);
-            end();
+    // What comes next into the ring: published states, 64 key dimensions at a time, and chunks.
+    StateWalk load_walk = walk;
+    StatePiece loading;
+    bool more = warp == W_SCORES;
+    int load_c = 0, load_end = 0, load_slot = 0, load_slots = 0, loads = 0;
+    auto load_one = [&]() {
+      while (more && load_slot >= load_slots && load_c >= load_end) {
+        more = load_walk.next(&loading);
+        if (!more) break;
+        load_c = loading.c0;
+        load_end = loading.c1;
+        load_slot = 0;
+        load_slots = slots_of(loading);
+      }
+      if (!more || !ok) return;
+      wait(&t->empty[at.stage], at.phase ^ 1u);
+      if (!ok) return;
+      unsigned char* to = ring + at.stage * X::STAGE;
+      uint64_t* bar = &t->full[at.stage];
+      if (load_slot < load_slots) {
+        const int of = states_of(loading), half = load_slot / of;
+        if (loading.from == StatePiece::PUBLISHED) {
+          const int j = t->slot_cta[load_slot - half * of];
+          const long long t0 = clock64();
+          bool told = true;
+          while (told && ld_acquire_gpu(p.flags + j) != X::LANE_WARPS) told = !*abort_flag && clock64() - t0 < WAIT_LIMIT_CYCLES;
+          ok = __all_sync(FULL_MASK, told);
+          if (!ok) {
+            *abort_flag = 1;
+            return;
           }
-      for (int c = piece.c0; c < piece.c1 && ok; ++c) {
-        unsigned char* to = begin();
-        if (!ok) break;
-        const int there = min(C, count - c * C);
-        const int64_t token = token0 + (int64_t)c * C;
-        if (there == C && maps.there) {
-          uint64_t* bar = &t->full[n % n_stages];
           if (lane == 0) {
-            const int y = (int)token;
-            mbar_arrive_expect_tx(bar, (piece.sum_only ? DK + DV : 2 * DK + DV) * ROW_CHUNK);
-#pragma unroll
-            for (int x = 0; x < DK; ++x) tma_load_3d(to + X::K_BYTES + x * ROW_CHUNK, &maps.k, x * 64, y, p.k.head_stride ? head : 0, bar);
-#pragma unroll
-            for (int x = 0; x < DV; ++x)
-              tma_load_3d(to + 2 * X::K_BYTES + x * ROW_CHUNK, &maps.val, slice_of(piece) * 128 + x * 64, y, p.val.head_stride ? head : 0, bar);
-            if (!piece.sum_only)
-#pragma unroll
-              for (int x = 0; x < DK; ++x) tma_load_3d(to + x * ROW_CHUNK, &maps.q, x * 64, y, p.q.head_stride ? head : 0, bar);
+            asm volatile("fence.proxy.async;" ::: "memory");     // what is copied was written by ordinary stores
+            mbar_arrive_expect_tx(bar, X::SLOT_HALF * 4);
+            bulk_load(to, p.slots + (size_t)j * p.slot_floats + half * X::SLOT_HALF, X::SLOT_HALF * 4, bar);
+          } else {
+            mbar_arrive(bar);
+          }
+        } else {
+          const int column = slice_of(loading) * 128, width = min(128, v.value_dim - column), there = min(64, v.key_dim - half * 64);
+          const float* from = v.pool + (((size_t)p.seqs[loading.i] * v.n_layers + p.layer) * v.n_heads + head_of(loading)) * v.head_floats() +
+                              (size_t)half * 64 * v.value_dim + column;
+          if (lane == 0) mbar_arrive_expect_tx(bar, there * width * 4);
+          __syncwarp();
+          for (int r = lane; r < there; r += 32) bulk_load(to + r * (DV * 256), from + (size_t)r * v.value_dim, width * 4, bar);
+          if (lane != 0) mbar_arrive(bar);
+        }
+        __syncwarp();
+        ++load_slot;
+      } else {
+        const int head = head_of(loading), column = slice_of(loading) * 128;
+        const int64_t token = first_token(loading) + (int64_t)load_c * C;
+        if (maps.there) {
+          if (lane == 0) {
+            const int y = (int)token, z = head;
+            mbar_arrive_expect_tx(bar, (loading.sum_only ? DK + DV : 2 * DK + DV) * ROW_CHUNK);
+#pragma unroll 1
+            for (int x = 0; x < DK; ++x) {
+              tma_load_3d(to + X::K_BYTES + x * ROW_CHUNK, &maps.k, x * 64, y, p.k.head_stride ? z : 0, bar);
+              if (!loading.sum_only) tma_load_3d(to + x * ROW_CHUNK, &maps.q, x * 64, y, p.q.head_stride ? z : 0, bar);
+            }
+#pragma unroll 1
+            for (int x = 0; x < DV; ++x) tma_load_3d(to + 2 * X::K_BYTES + x * ROW_CHUNK, &maps.val, column + x * 64, y, p.val.head_stride ? z : 0, bar);
           } else {
             mbar_arrive(bar);
           }
           __syncwarp();
-          ++n;
-          continue;
-        }
-        rows(to + X::K_BYTES, p.k, token, head, 0, v.key_dim, there, key_chunks);
-        rows(to + 2 * X::K_BYTES, p.val, token, head, slice_of(piece) * 128, v.value_dim, there, value_chunks);
-        if (!piece.sum_only) rows(to, p.q, token, head, 0, v.key_dim, there, key_chunks);
-        end();
-      }
-    }
-    // what is in flight lands before the CTA leaves
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    if (!ok)
-      for (int j = max(0, n - n_stages); j < n; ++j) {
-        const long long t0 = clock64();
-        while (!mbar_try_wait(&t->full[j % n_stages], (uint32_t)((j / n_stages) & 1)) && clock64() - t0 < WAIT_LIMIT_CYCLES) {
-        }
-      }
-  } else if (warp == W_PRODUCTS) {
-    // ------------------------------------------------------------ products
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
-    const int key_steps = (v.key_dim + 15) / 16;
-    const uint32_t id_p = idesc(F16, C, false), id_o1 = idesc(F16, C, false, true), id_o2 = idesc(F16, C, false), id_u = idesc(F16, key_steps * 16, true);
-    const uint64_t rows_desc = umma_desc_k_major_sw128(smem_u32(ring)), p_desc = umma_desc_k_major_sw128(smem_u32(p_smem)),
-                   columns_desc = desc_mn_major_sw128(smem_u32(ring), ROW_CHUNK);
-    constexpr uint32_t CH = ROW_CHUNK >> 4, K_AT = X::K_BYTES >> 4, V_AT = 2 * X::K_BYTES >> 4;
-    int n = 0;                                        // stages used before the present chunk's
-    uint32_t sum_ph = 0, out_ph = 0, slots_ph = 0;    // of the barriers that turn once a chunk, and once a chunk with results
-    bool scored = false;                              // the present chunk's P is under way
-    auto at = [&](int stage) { return (uint32_t)((stage % n_stages) * (X::STAGE >> 4)); };
-    auto loaded = [&](int stage, int there) {
-      wait(&t->full[stage % n_stages], (stage / n_stages) & 1);
-      if (!maps.there || there < C) fence_async_shared();       // the copies were ordinary writes
-      tc_fence_after_sync();
-    };
-    auto scores = [&](int stage) {
-      const uint64_t a = rows_desc + at(stage), b = a + K_AT;
-      // (unrolled: a product whose operands have to be worked out first takes 130 cycles to issue)
-#pragma unroll
-      for (int k = 0; k < DK * 4; ++k) {
-        const uint32_t step = (k >> 2) * CH + (k & 3) * 2;
-        product_smem(tmem + T_P, a + step, b + step, id_p, k != 0, k < key_steps ? on : 0u);
-      }
-      commit_products(&t->p_full, on);
-    };
-    bool more = walk.next(&piece);
-    int count = more ? tokens_of(piece) : 0;
-    while (more && ok) {
-      StateWalk after = walk;
-      StatePiece next;
-      const bool more_after = after.next(&next);
-      const int count_after = more_after ? tokens_of(next) : 0;
-      const int slots = DK * slots_of(piece);
-      for (int j = 0; j < slots && ok; ++j) {         // stages that held published states
-        wait(&t->slots_read[n % n_stages], (slots_ph >> (n % n_stages)) & 1u);      // a stage's barrier turns at each such use
-        slots_ph ^= 1u << (n % n_stages);
-        arrive_one(&t->empty[n % n_stages], on);
-        ++n;
-      }
-      for (int c = piece.c0; c < piece.c1 && ok; ++c) {
-        const uint32_t stage = at(n);
-        if (!scored) loaded(n, count - c * C);
-        if (!piece.sum_only && !scored && ok) scores(n);
-        scored = false;
-        wait(&t->w_ready, sum_ph);
-        wait(&t->u_free, sum_ph ^ 1u);
-        sum_ph ^= 1u;
-        if (!ok) break;
-        tc_fence_after_sync();
-#pragma unroll 1
-        for (int w = PARTS<F16> - 1; w >= 0; --w)     // the least parts first: what is cut off of a sum is a part of what is there
-#pragma unroll
-          for (int k = 0; k < C / 16; ++k)            // 16 tokens further: 8 columns of W, 2048 bytes of K
-            product_tmem(tmem + T_U, tmem + T_W + w * (C / 2) + k * 8, columns_desc + stage + K_AT + k * 128, id_u, w + 1 < PARTS<F16> || k != 0, on);
-        commit_products(&t->u_full, on);
-        if (piece.sum_only) {
-          commit_products(&t->empty[n % n_stages], on);
         } else {
-          wait(&t->copy_ready, out_ph);
-          wait(&t->o_free, out_ph ^ 1u);
-          if (!ok) break;
-          tc_fence_after_sync();
-#pragma unroll
-          for (int k = 0; k < DK * 4; ++k)
-            product_tmem(tmem + T_O2, tmem + T_COPY + k * 8, rows_desc + stage + (k >> 2) * CH + (k & 3) * 2, id_o2, k != 0, k < key_steps ? on : 0u);
-          commit_products(&t->o2_done, on);
-          wait(&t->p_ready, out_ph);
-          out_ph ^= 1u;
-          if (!ok) break;
-          tc_fence_after_sync();
-#pragma unroll
-          for (int k = 0; k < C / 16; ++k)
-            product_smem(tmem + T_O1, columns_desc + stage + V_AT + k * 128, p_desc + k * 2, id_o1, k != 0, on);
-          commit_products(&t->o_full, on);
-          commit_products(&t->empty[n % n_stages], on);
+          const int there = min(C, tokens_of(loading) - load_c * C);
+          rows(to + X::K_BYTES, p.k, token, head, 0, v.key_dim, there, key_chunks);
+          rows(to + 2 * X::K_BYTES, p.val, token, head, column, v.value_dim, there, value_chunks);
+          if (!loading.sum_only) rows(to, p.q, token, head, 0, v.key_dim, there, key_chunks);
+          cp_async_arrive(bar);
         }
-        ++n;
-        // the next chunk's scores, unless published states lie between in the ring
-        const bool last = c + 1 == piece.c1;
-        if (last ? more_after && !next.sum_only && next.from != StatePiece::PUBLISHED : !piece.sum_only) {
-          loaded(n, last ? count_after - next.c0 * C : count - (c + 1) * C);
-          if (ok) scores(n);
-          scored = true;
-        }
+        ++load_c;
       }
-      walk = after;
-      piece = next;
-      count = count_after;
-      more = more_after;
-    }
-    // nothing issued is still running when tensor memory is released
-    commit_products(&t->drain, on);
-    const long long t0 = clock64();
-    while (!mbar_try_wait(&t->drain, 0) && clock64() - t0 < WAIT_LIMIT_CYCLES) {
-    }
-  } else if (warp >= W_SCORES) {
-    // ------------------------------------------------------------ P
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+      at.advance();
+      ++loads;
+    };
+    for (int i = 0; i < n_stages; ++i) load_one();
+    bool begun = false;
+    // One more load for each stage that has been passed.
+    auto passed = [&]() {
+      if (begun) load_one();
+      begun = true;
+    };
     const int row = tid - W_SCORES * 32;              // token of the chunk
     uint32_t ph = 0;
     const uint32_t to = smem_u32(p_smem) + row * 128;
-    while (ok && walk.next(&piece)) {
-      if (piece.sum_only) continue;
-      fill_falls(piece);
-      const float* fall = t->fall[warp].at + FALL + row;                // fall[-s]: l^(row - s), 0 for s > row
+    int served = 0;
+    auto serve = [&]() {                              // the next piece's powers
+      if (warp == W_SCORES || !ok || !load_walk.next(&loading)) return;
+      const float rate = p.rates[head_of(loading)];
+      wait(&t->fall_free[served & 1], ((served >> 1) & 1) ^ 1);
+      for (int j = lane; j < 2 * C + 4; j += 32) t->fall[served & 1].at[j] = j < FALL ? 0.0f : fall_of(rate, j - FALL);
+      tell(&t->fall_ready[served & 1]);
+      ++served;
+    };
+    serve();
+    serve();
+    while (next_piece()) {
+      if (warp == W_SCORES)
+        for (int j = slots_of(piece) + (piece.sum_only ? piece.c1 - piece.c0 : 0); j > 0 && ok; --j) passed();
+      if (piece.sum_only) {
+        end_piece();
+        if (n_pieces > 1) serve();
+        continue;
+      }
+      const float* fall = t->fall[n_pieces & 1].at + FALL + row;        // fall[-s]: l^(row - s), 0 for s > row
       for (int c = piece.c0; c < piece.c1; ++c) {
         wait(&t->p_full, ph);
         if (!ok) break;
@@ -405,8 +542,10 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
             for (int s = 0; s < 32; ++s) m = fmaxf(m, fabsf(__uint_as_float(x[s]) * fall[-h - s]));
           }
           lift = lift_of(m, 100);
-          t->token_scale[ph][row] = reciprocal_of_power(lift);
         }
+        wait(&t->o1_full, ph ^ 1u);                   // the last chunk's has been used, and the factors of the one before
+        if (!ok) break;
+        if (F16) t->token_scale[ph][row] = reciprocal_of_power(lift);
 #pragma unroll 1
         for (int h = 0; h < C; h += 32) {
           uint32_t x[32];
@@ -430,8 +569,19 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
         fence_async_shared();
         tc_fence_before_sync();
         tell(&t->p_ready);
+        passed();
+        if (c == piece.c0 && n_pieces > 0) serve();
       }
+      end_piece();
     }
+    // what is in flight lands before the CTA leaves
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!ok)
+      for (int j = max(0, loads - n_stages); j < loads; ++j) {
+        const long long t0 = clock64();
+        while (!mbar_try_wait(&t->full[j % n_stages], (uint32_t)((j / n_stages) & 1)) && clock64() - t0 < WAIT_LIMIT_CYCLES) {
+        }
+      }
   } else if (warp >= W_VALUES) {
     // ------------------------------------------------------------ W
     // A thread has the tokens 8 j + 2 (lane % 4) and the next, of the value columns lane / 4 + 8 i: as matrices come out of shared memory
@@ -445,22 +595,38 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
       return (uint32_t)((column0 >> 6) * ROW_CHUNK + ((lane >> 4) * 8 + (lane & 7)) * 128 + ((eight ^ (lane & 7)) << 4));
     };
     const uint32_t from0 = smem_u32(ring) + 2 * X::K_BYTES, row_of[2] = {matrix_row(0), matrix_row(1)};
-    int n = 0;
     uint32_t ph = 0;
     // (warps whose value columns there are none of have nothing to do)
-    while (ok && (warp & 3) < X::LANE_WARPS && walk.next(&piece)) {
-      fill_falls(piece);
+    while ((warp & 3) < X::LANE_WARPS && next_piece()) {
       const int count = tokens_of(piece);
       // (stages that hold published states are not for these warps, but they follow them, or they could lose count of the rounds)
-      for (int j = DK * slots_of(piece); j > 0 && ok; --j, ++n) {
-        wait(&t->full[n % n_stages], (n / n_stages) & 1);
-        tell(&t->slots_read[n % n_stages]);
+      for (int j = slots_of(piece); j > 0 && ok; --j) {
+        wait(&t->full[at.stage], at.phase);
+        tell(&t->slots_read[at.stage]);
+        at.advance();
       }
       for (int c = piece.c0; c < piece.c1; ++c) {
-        const float* weight = t->fall[warp].at + FALL + min(C, count - c * C) - 1 - pair;       // weight[-s]: l^(n-1-s-pair), 0 behind the end
-        wait(&t->full[n % n_stages], (n / n_stages) & 1);
+        const float* weight = t->fall[n_pieces & 1].at + FALL + min(C, count - c * C) - 1 - pair;       // weight[-s]: l^(n-1-s-pair), 0 behind the end
+        wait(&t->full[at.stage], at.phase);
         if (!ok) break;
-        const uint32_t from = from0 + (n % n_stages) * X::STAGE;
+        const uint32_t from = from0 + at.stage * X::STAGE;
+        if (count < (c + 1) * C) {
+          // rows behind the end: of V what this warp reads, of K a share.  (A weight of zero would not undo an infinity.)
+          const int there = count - c * C;
+          unsigned char* stage = ring + at.stage * X::STAGE + X::K_BYTES;
+#pragma unroll 1
+          for (int u = lane; u < (C - there) * 4; u += 32) {
+            const int r = there + (u >> 2), x = column0 / 8 + (u & 3);
+            *reinterpret_cast<uint4*>(stage + X::K_BYTES + (x >> 3) * ROW_CHUNK + r * 128 + ((x & 7) ^ (r & 7)) * 16) = make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll 1
+          for (int u = tid - W_VALUES * 32; u < (C - there) * DK * 8; u += X::LANE_WARPS * 32) {
+            const int r = there + u / (DK * 8), x = u % (DK * 8);
+            *reinterpret_cast<uint4*>(stage + (x >> 3) * ROW_CHUNK + r * 128 + (x & 7) * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_async_shared();
+          tell(&t->clean[at.stage]);
+        }
         // (loops that are not unrolled: the roles' code together has to stay in the instruction cache.  Unrolled, warps waited for
         // instructions more than for anything else, and a chunk took 6,500 cycles.)
         float lift[4] = {1.0f, 1.0f, 1.0f, 1.0f};
@@ -486,105 +652,129 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
             lift[i] = lift_of(fmaxf(m[i], __shfl_xor_sync(FULL_MASK, m[i], 2)), 38);
           }
         }
-        wait(&t->u_full, ph ^ 1u);                    // the last chunk's W has been used, and the factors of the one before
-        if (!ok) break;
-        tc_fence_after_sync();
-        if (F16 && (lane & 3) == 0) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) t->lane_scale[ph][column0 + (lane >> 2) + 8 * i] = lift[i];
-        }
 #pragma unroll 1
-        for (int s = 0; s < C; s += 32) {
-          float f[8];
+        for (int x = 0; x < 4; ++x) {                 // halves of the chunk, and of these halves of the warp's value columns
+          const int half = x >> 1, g = x & 1, s = half * 32;
+          if (g == 0) {
+            wait(&t->w_free[half], ph ^ 1u);          // the last chunk's has been used
+            if (!ok) break;
+            tc_fence_after_sync();
+          }
+          uint32_t raw[2][4], out[PARTS<F16>][8];
+          const uint32_t matrix = from + (g ? row_of[1] : row_of[0]) + s * 128;
+          ldmatrix_x4_trans(raw[0], matrix);
+          ldmatrix_x4_trans(raw[1], matrix + 16 * 128);
+          const uint64_t lift2[2] = {F16 ? pair_of(g ? lift[2] : lift[0], g ? lift[2] : lift[0]) : 0, F16 ? pair_of(g ? lift[3] : lift[1], g ? lift[3] : lift[1]) : 0};
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = weight[-s - (j >> 1) * 8 - (j & 1)];
+          for (int u = 0; u < 8; ++u) {
+            const float* f = weight - s - (u >> 1) * 8;
+            const float2 y = pair16<F16>(raw[u >> 2][u & 3]);
+            uint64_t x2 = mul_pairs(pair_of(y.x, y.y), pair_of(f[0], f[-1]));
+            if (F16) x2 = mul_pairs(x2, lift2[u & 1]);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {               // 16 value columns
-            uint32_t raw[2][4], out[PARTS<F16>][8];
-            ldmatrix_x4_trans(raw[0], from + row_of[g] + s * 128);
-            ldmatrix_x4_trans(raw[1], from + row_of[g] + (s + 16) * 128);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const float2 y = pair16<F16>(raw[u >> 2][u & 3]);
-              float a = y.x * f[2 * (u >> 1)], b = y.y * f[2 * (u >> 1) + 1];
-              if (F16) {
-                a *= lift[2 * g + (u & 1)];
-                b *= lift[2 * g + (u & 1)];
-              }
-#pragma unroll
-              for (int w = 0; w < PARTS<F16>; ++w) {
-                out[w][u] = pack2<F16>(a, b);
+            for (int w = 0; w < PARTS<F16>; ++w) {
+              float a, b;
+              split_pair(x2, &a, &b);
+              out[w][u] = pack2<F16>(a, b);
+              if (w + 1 < PARTS<F16>) {               // what the rounding left over, exactly
                 const float2 e = pair16<F16>(out[w][u]);
-                a -= e.x;
-                b -= e.y;
+                x2 = fma_pairs(pair_of(e.x, e.y), pair_of(-1.0f, -1.0f), x2);
               }
             }
+          }
 #pragma unroll
-            for (int w = 0; w < PARTS<F16>; ++w)
-              tmem_st_16x16(tmem + lane_base + ((uint32_t)(g * 16) << 16) + T_W + w * (C / 2) + s / 2, out[w]);
+          for (int w = 0; w < PARTS<F16>; ++w)
+            tmem_st_16x16(tmem + lane_base + ((uint32_t)(g * 16) << 16) + T_W + w * (C / 2) + s / 2, out[w]);
+          if (g == 1) {
+            if (F16 && half == 1 && (lane & 3) == 0) {      // (the factors of the chunk before the last have been read)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) t->lane_scale[ph][column0 + (lane >> 2) + 8 * i] = lift[i];
+            }
+            tmem_st_wait();
+            tc_fence_before_sync();
+            tell(&t->w_ready[half]);
           }
         }
-        tmem_st_wait();
-        tc_fence_before_sync();
-        tell(&t->w_ready);
+        if (!ok) break;
         ph ^= 1u;
-        ++n;
+        at.advance();
       }
+      end_piece();
     }
   } else if (warp >= W_STATE) {
     // ------------------------------------------------------------ the state
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(STATE_REGS));
     if ((warp & 3) < X::LANE_WARPS) {
       const int column = tid - W_STATE * 32;
-      int n = 0;
       uint32_t ph = 0, out_ph = 0;                    // chunks, and chunks with results, before this one
       const uint32_t u_at = tmem + lane_base + T_U, copy_at = tmem + lane_base + T_COPY;
-      float s[DK * 64];
-      while (ok && walk.next(&piece)) {
-        fill_falls(piece);
+      uint64_t s[DK * 32];                            // key dimensions in pairs
+      bool to_tell = false;
+      while (next_piece()) {
         const int count = tokens_of(piece), head = head_of(piece), global_column = slice_of(piece) * 128 + column;
-        const bool here = global_column < v.value_dim;
-        float* stored = v.pool + (((size_t)p.seqs[piece.i] * v.n_layers + p.layer) * v.n_heads + head) * v.head_floats() + global_column;
         // the state in front of the piece
+        const int states = states_of(piece);
+        const bool published = piece.from == StatePiece::PUBLISHED;
 #pragma unroll
-        for (int k = 0; k < DK * 64; ++k)
-          s[k] = piece.from == StatePiece::STORED && here && k < v.key_dim ? stored[(size_t)k * v.value_dim] : 0.0f;
-        if (piece.from == StatePiece::PUBLISHED) {
-          const double rate = p.rates[head];
-          const long long start = t->line.cut(blockIdx.x) - piece.c0;
+        for (int h = 0; h < DK; ++h) {
 #pragma unroll
-          for (int h = 0; h < DK; ++h)
-            for (int j = piece.first; j < (int)blockIdx.x; ++j) {
-              const long long to = t->line.cut(j + 1);
-              if (t->line.cut(j) == to) continue;
-              const int chunks = piece.c0 - (int)(to - start);           // between its end and this piece
-              const float w = chunks == 0 ? 1.0f : (float)exp(-rate * C * chunks);
-              wait(&t->full[n % n_stages], (n / n_stages) & 1);
-              if (!ok) break;
-              const float* from = reinterpret_cast<const float*>(ring + (n % n_stages) * X::STAGE) + column;
+          for (int k = 0; k < 32; ++k) s[h * 32 + k] = 0;
+#pragma unroll 1
+          for (int j = 0; j < states; ++j) {
+            const float w = published ? t->slot_weight[j] : 1.0f;
+            const int there = published ? 64 : v.key_dim - h * 64;
+            wait(&t->full[at.stage], at.phase);
+            if (!ok) break;
+            const uint32_t from = smem_u32(ring) + at.stage * X::STAGE + column * 4;
+            const uint64_t w2 = pair_of(w, w);
+            // (code that runs once a piece comes from far away: the whole case has no more of it than it needs)
+            if (there >= 64) {
 #pragma unroll
-              for (int k = 0; k < 64; ++k) s[h * 64 + k] = fmaf(w, from[k * DV * 64], s[h * 64 + k]);
-              tell(&t->slots_read[n % n_stages]);
-              ++n;
+              for (int k = 0; k < 64; k += 2)
+                s[h * 32 + k / 2] = fma_pairs(w2, pair_of(ld_shared(from + k * (DV * 256)), ld_shared(from + (k + 1) * (DV * 256))), s[h * 32 + k / 2]);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 64; k += 2)         // (key_dim is even)
+                if (k < there)
+                  s[h * 32 + k / 2] = fma_pairs(w2, pair_of(ld_shared(from + k * (DV * 256)), ld_shared(from + (k + 1) * (DV * 256))), s[h * 32 + k / 2]);
             }
+            tell(&t->slots_read[at.stage]);
+            at.advance();
+          }
         }
-        for (int c = piece.c0; c < piece.c1; ++c, ++n) {
+        if (!ok) break;
+        if (to_tell) {
+          // the state that was published last: now that what was stored has been read (another CTA writes there when it has ended the item)
+          to_tell = false;
+          __threadfence();
+          __syncwarp();
+          if (lane == 0) atomicAdd(p.flags + blockIdx.x, 1u);
+        }
+        for (int c = piece.c0; c < piece.c1; ++c, at.advance()) {
           if (!piece.sum_only) {
             float lift = 1.0f;
             if (F16) {
               float m = 0.0f;
 #pragma unroll
-              for (int k = 0; k < DK * 64; ++k) m = fmaxf(m, fabsf(s[k]));
+              for (int k = 0; k < DK * 32; ++k) {
+                float a, b;
+                split_pair(s[k], &a, &b);
+                m = fmaxf(m, fmaxf(fabsf(a), fabsf(b)));
+              }
               lift = lift_of(m, 100);
             }
-            wait(&t->o2_done, out_ph ^ 1u);           // the copy before has been used, and the results before that have their factors
+            wait(&t->o2_full, out_ph ^ 1u);           // the copy before has been used, and the results before that have their factors
             if (!ok) break;
             if (F16) t->copy_scale[out_ph][column] = reciprocal_of_power(lift);
 #pragma unroll
             for (int h = 0; h < DK; ++h) {
               uint32_t w[32];
 #pragma unroll
-              for (int k = 0; k < 32; ++k) w[k] = pack2<F16>(s[h * 64 + 2 * k] * lift, s[h * 64 + 2 * k + 1] * lift);
+              for (int k = 0; k < 32; ++k) {
+                float a, b;
+                split_pair(F16 ? mul_pairs(s[h * 32 + k], pair_of(lift, lift)) : s[h * 32 + k], &a, &b);
+                w[k] = pack2<F16>(a, b);
+              }
               tmem_st_32x32(copy_at + h * 32, w);
             }
             tmem_st_wait();
@@ -592,7 +782,7 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
             tell(&t->copy_ready);
             out_ph ^= 1u;
           }
-          const float decay = t->fall[warp].at[FALL + min(C, count - c * C)];
+          const float decay = t->fall[n_pieces & 1].at[FALL + min(C, count - c * C)];
           wait(&t->u_full, ph);
           if (!ok) break;
           tc_fence_after_sync();
@@ -608,24 +798,51 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
             }
             // (columns beyond key_dim rounded up to 16 are not written by the products)
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (h * 32 + (k & ~15) < v.key_dim) s[h * 32 + k] = fmaf(decay, s[h * 32 + k], F16 ? __uint_as_float(u[k]) * back : __uint_as_float(u[k]));
+            for (int k = 0; k < 32; k += 2)
+              if (h * 32 + (k & ~15) < v.key_dim) {
+                uint64_t y = pair_of(__uint_as_float(u[k]), __uint_as_float(u[k + 1]));
+                if (F16) y = mul_pairs(y, pair_of(back, back));
+                s[h * 16 + k / 2] = fma_pairs(pair_of(decay, decay), s[h * 16 + k / 2], y);
+              }
           }
           ph ^= 1u;
         }
         if (!ok) break;
+        end_piece();
         // the state behind it
-        if (piece.to == StatePiece::STORED) {
+        if (piece.to != StatePiece::NOTHING) {
+          const bool publish = piece.to == StatePiece::PUBLISHED;
+          const int stride = publish ? DV * 64 : v.value_dim, there = publish ? DK * 64 : v.key_dim;
+          float* to = publish ? p.slots + (size_t)blockIdx.x * p.slot_floats + column
+                              : v.pool + (((size_t)p.seqs[piece.i] * v.n_layers + p.layer) * v.n_heads + head) * v.head_floats() + global_column;
+          const bool here = publish || global_column < v.value_dim;
+          if (stride == DV * 64 && there == DK * 64) {
 #pragma unroll
-          for (int k = 0; k < DK * 64; ++k)
-            if (here && k < v.key_dim) stored[(size_t)k * v.value_dim] = s[k];
-        } else if (piece.to == StatePiece::PUBLISHED) {
-          float* slot = p.slots + (size_t)blockIdx.x * p.slot_floats + column;
+            for (int k = 0; k < DK * 64; k += 2) {
+              float a, b;
+              split_pair(s[k / 2], &a, &b);
+              to[k * (DV * 64)] = a;
+              to[(k + 1) * (DV * 64)] = b;
+            }
+          } else {
 #pragma unroll
-          for (int k = 0; k < DK * 64; ++k) slot[k * (DV * 64)] = s[k];
-          __threadfence();
-          __syncwarp();
-          if (lane == 0) atomicAdd(p.flags + blockIdx.x, 1u);
+            for (int k = 0; k < DK * 64; k += 2) {
+              float a, b;
+              split_pair(s[k / 2], &a, &b);
+              if (here && k < there) {
+                to[0] = a;
+                to[stride] = b;
+              }
+              to += 2 * stride;
+            }
+          }
+          if (publish && t->plan.again.c1) {
+            to_tell = true;
+          } else if (publish) {
+            __threadfence();
+            __syncwarp();
+            if (lane == 0) atomicAdd(p.flags + blockIdx.x, 1u);
+          }
         }
       }
     }
@@ -637,83 +854,91 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     const int pair = (lane & 3) * 2;
     uint32_t ph = 0;
     const uint32_t mine = smem_u32(out_smem) + warp * 32 * 64;
+    const uint64_t scale2 = pair_of(p.scale, p.scale);
     auto place = [&](int token, int eight) { return mine + token * 64 + ((eight ^ ((token >> 1) & 3)) << 4); };
-    while (ok && (warp & 3) < X::LANE_WARPS && walk.next(&piece)) {
-      if (piece.sum_only) continue;
-      fill_falls(piece);
-      const float* fall = t->fall[warp].at + FALL + 1 + pair;          // fall[t]: l^(t+pair+1)
+    while ((warp & 3) < X::LANE_WARPS && next_piece()) {
+      if (piece.sum_only) {
+        end_piece();
+        continue;
+      }
+      const float* fall = t->fall[n_pieces & 1].at + FALL + 1 + pair;          // fall[t]: l^(t+pair+1)
       const int count = tokens_of(piece), first_column = slice_of(piece) * 128 + warp * 32;
       const int64_t token0 = first_token(piece);
       uint16_t* out = reinterpret_cast<uint16_t*>(const_cast<unsigned char*>(p.out.at)) + token0 * p.out.token_stride + head_of(piece) * p.out.head_stride +
                       first_column + (lane & 3) * 8;
       const bool here = first_column + (lane & 3) * 8 < v.value_dim;
       for (int c = piece.c0; c < piece.c1; ++c) {
-        wait(&t->o_full, ph);
+        wait(&t->o1_full, ph);
+        wait(&t->o2_full, ph);
         if (!ok) break;
         tc_fence_after_sync();
         const int there = here ? min(C, count - c * C) : 0;
         uint16_t* to = out + (int64_t)c * C * p.out.token_stride;
-        float copy[4];
-        if (F16)
+        auto flush = [&](int h) {                     // 32 tokens from shared memory to the result
+          __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 4; ++i) copy[i] = t->copy_scale[ph][warp * 32 + (lane >> 2) + 8 * i];
+          for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + (lane >> 2);
+            uint4 y;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w) : "r"(place(row, lane & 3)));
+            if (h * 32 + row < there) *reinterpret_cast<uint4*>(to + (h * 32 + row) * p.out.token_stride) = y;
+          }
+          __syncwarp();
+        };
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {                 // 32 tokens
-          float f[8];
-          float2 one[4];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = p.scale * fall[h * 32 + (j >> 1) * 8 + (j & 1)];
-          if (F16)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) one[j] = *reinterpret_cast<const float2*>(&t->token_scale[ph][h * 32 + j * 8 + pair]);
+          uint32_t w[2][8];
 #pragma unroll
           for (int g = 0; g < 2; ++g) {               // 16 value columns
-            uint32_t a[16], b[16], w[8];
+            uint32_t a[16], b[16];
             const uint32_t from = tmem + lane_base + ((uint32_t)(g * 16) << 16) + h * 32;
             tmem_ld_16x32(from + T_O1, a);
             tmem_ld_16x32(from + T_O2, b);
             tmem_ld_wait_for16(a);
             tmem_ld_wait_for16(b);
-            if (g == 1 && h == 1) {
-              tc_fence_before_sync();
-              tell(&t->o_free);
-            }
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j) {
+              const float* f = fall + h * 32 + j * 8;
+              const uint64_t fall2 = mul_pairs(pair_of(f[0], f[1]), scale2);
+              const uint64_t one = F16 ? mul_pairs(*reinterpret_cast<const uint64_t*>(&t->token_scale[ph][h * 32 + j * 8 + pair]), scale2) : scale2;
 #pragma unroll
               for (int r = 0; r < 2; ++r) {
-                float y[2];
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                  float o = p.scale;
-                  if (F16) o *= x ? one[j].y : one[j].x;
-                  y[x] = fmaf(F16 ? f[j * 2 + x] * copy[2 * g + r] : f[j * 2 + x], __uint_as_float(b[4 * j + 2 * r + x]),
-                              o * __uint_as_float(a[4 * j + 2 * r + x]));
+                const int x = 4 * j + 2 * r;
+                uint64_t y = pair_of(__uint_as_float(b[x]), __uint_as_float(b[x + 1]));
+                if (F16) {
+                  const float copy = t->copy_scale[ph][warp * 32 + (lane >> 2) + 8 * (2 * g + r)];
+                  y = mul_pairs(y, pair_of(copy, copy));
                 }
-                w[2 * j + r] = pack2<F16>(y[0], y[1]);
+                y = fma_pairs(fall2, y, mul_pairs(one, pair_of(__uint_as_float(a[x]), __uint_as_float(a[x + 1]))));
+                float u, v;
+                split_pair(y, &u, &v);
+                w[g][2 * j + r] = pack2<F16>(u, v);
               }
+            }
+          }
+          if (h == 1) {
+            // all of the chunk's has been read, its factors too: the products of the next one wait for this
+            tc_fence_before_sync();
+            tell(&t->o_free);
+            flush(0);
+          }
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int j = 0; j < 4; j += 2)
-              stmatrix_x4_trans(place(8 * (j + (lane >> 4)) + (lane & 7), g * 2 + ((lane >> 3) & 1)), w[2 * j], w[2 * j + 1], w[2 * j + 2], w[2 * j + 3]);
-          }
-          __syncwarp();
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int row = i * 8 + (lane >> 2);
-            uint4 w;
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(place(row, lane & 3)));
-            if (h * 32 + row < there) *reinterpret_cast<uint4*>(to + (h * 32 + row) * p.out.token_stride) = w;
-          }
-          __syncwarp();
+              stmatrix_x4_trans(place(8 * (j + (lane >> 4)) + (lane & 7), g * 2 + ((lane >> 3) & 1)), w[g][2 * j], w[g][2 * j + 1], w[g][2 * j + 2],
+                                w[g][2 * j + 3]);
         }
+        flush(1);
         ph ^= 1u;
       }
+      end_piece();
     }
   }
   if (!ok && lane == 0) state_report(v, KV_TIMEOUT);
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == W_PRODUCTS) tmem_dealloc(tmem, 512);
+  if (warp == W_STATE_PRODUCTS) tmem_dealloc(tmem, 512);
   // the last CTA leaves the flags as it found them
   if (holds && tid == 0) {
     __threadfence();
@@ -758,7 +983,6 @@ cudaError_t state_chunk_configure(int smem_optin) {
 
 cudaError_t state_chunk_launch(StateAttendParams p, const StateMaps& maps, bool f16, int sm_count, int smem_optin, cudaStream_t st) {
   const bool k2 = p.v.key_dim > 64, v2 = p.v.value_dim > 64;
-  p.slices = (p.v.value_dim + 127) / 128;
   auto* go = f16 ? (k2 ? (v2 ? launch<true, 2, 2> : launch<true, 2, 1>) : (v2 ? launch<true, 1, 2> : launch<true, 1, 1>))
                  : (k2 ? (v2 ? launch<false, 2, 2> : launch<false, 2, 1>) : (v2 ? launch<false, 1, 2> : launch<false, 1, 1>));
   return go(p, maps, sm_count, smem_optin, st);
