@@ -284,9 +284,10 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     }
   };
 
+  // (one place for the warps of a warpgroup: the instruction is theirs together)
+  if (warp >= W_SCORES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
   if (warp == W_STATE_PRODUCTS) {
     // ------------------------------------------------------------ U, O2
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     const uint32_t id_o2 = idesc(F16, C, false), id_u = idesc(F16, key_steps * 16, true);
     const uint64_t rows_desc = umma_desc_k_major_sw128(smem_u32(ring)), columns_desc = desc_mn_major_sw128(smem_u32(ring), ROW_CHUNK);
     uint32_t ph = 0, out_ph = 0, slots_ph = 0;        // of the barriers that turn once a chunk, and once a chunk with results
@@ -339,7 +340,6 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     drain(&t->drain[0]);
   } else if (warp == W_RESULT_PRODUCTS) {
     // ------------------------------------------------------------ P, O1
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     const uint32_t id_p = idesc(F16, C, false), id_o1 = idesc(F16, C, false, true);
     const uint64_t rows_desc = umma_desc_k_major_sw128(smem_u32(ring)), p_desc = umma_desc_k_major_sw128(smem_u32(p_smem)),
                    columns_desc = desc_mn_major_sw128(smem_u32(ring), ROW_CHUNK);
@@ -401,7 +401,6 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     drain(&t->drain[1]);
   } else if (warp >= W_SCORES) {
     // ------------------------------------------------------------ P, loads
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     // 64 rows of up to CH chunks of 64 elements; what is not there becomes zeros
     auto rows = [&](unsigned char* to, const StateRows& r, int64_t token, int head, int column, int dim, int there, auto ch) {
       constexpr int CH = decltype(ch)::value, LANES = CH * 8, AT_ONCE = 32 / LANES;
@@ -690,6 +689,7 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
 #pragma unroll
               for (int i = 0; i < 4; ++i) t->lane_scale[ph][column0 + (lane >> 2) + 8 * i] = lift[i];
             }
+            __syncwarp();
             tmem_st_wait();
             tc_fence_before_sync();
             tell(&t->w_ready[half]);
