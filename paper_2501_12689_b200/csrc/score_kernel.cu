@@ -6,10 +6,12 @@
 // function units do 16 a cycle and SM: in 16 bits three quarters of their rate at the copy's bandwidth), and about six other
 // instructions, pairs of floats at a time, where the bandwidth leaves room for eleven.
 //
-// Top alternatives: a warp keeps its 32 best keys (value, lowest index first) one a lane, sorted.  A block of elements is looked at more closely
-// only if its maximum reaches the list: the largest known lower bound of the row's n-th best, shared by the CTA, starts as
-// the n-th largest of the lanes' maxima over their first blocks, so that even then few elements pass.  A warp's steps, a vector a lane,
-// ascend in their indices, so an element equal to the list's last one of an earlier step never enters.
+// Top alternatives: a lower bound of the row's n-th best is the n-th largest of the maxima of 64 groups of threads, as these are n different
+// elements.  So all that the pass over the row does for them is to note the maximum of each thread's blocks (or of groups of them, in long
+// rows).  At the end few blocks reach the bound, a little more than n; those are read again, and the elements that reach it go to a buffer of the
+// warp, where the rank of each is the number of larger ones.  A buffer that fills up is taken into the warp's list of its 32 best keys (value,
+// lowest index first), one a lane, sorted.  A warp's steps, a vector a lane, ascend in their indices, so an element equal to the list's
+// last one never enters later: rows of equal or banned tokens are no slower.
 //
 // Rows are split over CTAs when there are few of them; the CTA that finishes last joins the pieces, in their order.
 #include <cuda_bf16.h>
@@ -28,6 +30,10 @@ namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int VECTORS = 4;                // 16-byte vectors of a thread's block
+constexpr int CTAS = 4;                   // an SM
+constexpr int GROUPS = 16;                // of a thread's blocks, each with its maximum
+constexpr int BUFFER = 384;               // keys of a warp that have passed the bound: more than a step's 256, so that it is seldom emptied
+static_assert(WARPS * BUFFER >= SCORE_MAX_SPLIT * SCORE_MAX_TOP, "the pieces' keys are joined there");
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LEAST = -150.0f;          // e^LEAST is 0 in fp32; keeps banned tokens' differences finite
 constexpr float INF = __builtin_huge_valf();
@@ -51,16 +57,27 @@ struct Elements {
     if (T == F16) return __half22float2(*reinterpret_cast<const __half2*>(x + i));
     return make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u));
   }
+  // Element e, which the compiler does not know.
+  __device__ __forceinline__ static float any(const uint4& v, int e) {
+    const int i = T == F32 ? e : e >> 1;
+    const uint32_t x = i & 2 ? (i & 1 ? v.w : v.z) : (i & 1 ? v.y : v.x);
+    if (T == F32) return __uint_as_float(x);
+    const uint16_t h = (uint16_t)(e & 1 ? x >> 16 : x);
+    return T == F16 ? __half2float(__ushort_as_half(h)) : __bfloat162float(__ushort_as_bfloat16(h));
+  }
   // Largest element; NaN if there is one.
-  __device__ __forceinline__ static float largest(const uint4& v) {
-    if (T == F32) return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)), max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
-    if (T == F16) {
-      const __half2* x = reinterpret_cast<const __half2*>(&v.x);
-      const float2 m = __half22float2(__hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3])));
-      return max_nan(m.x, m.y);
-    }
-    const __nv_bfloat162* x = reinterpret_cast<const __nv_bfloat162*>(&v.x);
-    const float2 m = __bfloat1622float2(__hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3])));
+  __device__ __forceinline__ static float largest(const uint4& v) { return widest(larger(larger(v.x, v.y), larger(v.z, v.w))); }
+  // The same by words, of one element or two.
+  __device__ __forceinline__ static uint32_t larger(uint32_t a, uint32_t b) {
+    if (T == F32) return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
+    uint32_t d;
+    if (T == F16) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+  }
+  __device__ __forceinline__ static float widest(uint32_t x) {
+    if (T == F32) return __uint_as_float(x);
+    const float2 m = T == F16 ? __half22float2(*reinterpret_cast<const __half2*>(&x)) : make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
     return max_nan(m.x, m.y);
   }
   __device__ __forceinline__ static float one(const unsigned char* row, int i) {
@@ -85,9 +102,9 @@ struct Sums {
     top = now;
     return at;
   }
-  __device__ __forceinline__ void add(uint64_t y2, uint64_t minus2) {
+  __device__ __forceinline__ void add(uint64_t x2, uint64_t scale2, uint64_t minus2) {
     float a, b;
-    split_pair(add_pairs(y2, minus2), &a, &b);
+    split_pair(fma_pairs(x2, scale2, minus2), &a, &b);
     const uint64_t d = pair_of(fmaxf(a, LEAST), fmaxf(b, LEAST));
     split_pair(mul_pairs(d, pair_of(LOG2E, LOG2E)), &a, &b);
     const uint64_t e = pair_of(exp2_fast(a), exp2_fast(b));
@@ -117,34 +134,47 @@ struct Joined {
 // The warp's best keys, one a lane in descending order; the first n of them count.
 struct TopList {
   uint64_t mine, last;      // last: the n-th, KEY_EMPTY until there are n
-  float above;              // its value
-  __device__ __forceinline__ TopList() : mine(KEY_EMPTY), last(KEY_EMPTY), above(-INF) {}
-  // Whether an element x may be among the row's n best; `bound`: a value that n elements of the row reach.
-  __device__ __forceinline__ bool admits(float x, float bound) const { return x >= bound && (x > above || last == KEY_EMPTY); }
+  __device__ __forceinline__ TopList() : mine(KEY_EMPTY), last(KEY_EMPTY) {}
+  // What an element of a later step has to reach to enter: the next number after the last one's (NaN, which nothing reaches, after infinity).
+  __device__ __forceinline__ float least() const { return last == KEY_EMPTY ? -INF : ord_to_score((uint32_t)(last >> 32) + 1); }
   // A key per lane, KEY_EMPTY for none.
   __device__ __forceinline__ void offer(uint64_t key, int n, int lane) {
     unsigned who = __ballot_sync(FULL_MASK, key > last);
-    while (who) {
-      const uint64_t k = __shfl_sync(FULL_MASK, key, __ffs(who) - 1);
+    while (who) {           // the highest lane's first: of elements that ascend, all but n are out at once
+      const uint64_t k = __shfl_sync(FULL_MASK, key, 31 - __clz(who));
       const int at = __popc(__ballot_sync(FULL_MASK, mine > k));
       const uint64_t up = __shfl_up_sync(FULL_MASK, mine, 1);
       if (lane == at) mine = k;
       else if (lane > at) mine = up;
       last = __shfl_sync(FULL_MASK, mine, n - 1);
-      who &= who - 1;
+      who &= ~(0x80000000u >> __clz(who));
       who &= __ballot_sync(FULL_MASK, key > last);
     }
-    if (last != KEY_EMPTY) above = key_score(last);
   }
 };
 
+// The n-th largest of the maxima of 64 groups of threads, without what is behind its first BITS bits.
+template <int BITS>
+__device__ __forceinline__ uint32_t nth_largest(const volatile uint32_t* words, int n, int lane) {
+  uint32_t x[2] = {0, 0}, y = 0;
+#pragma unroll
+  for (int i = 0; i < WARPS; ++i) x[i & 1] = max(x[i & 1], words[i * 32 + lane]);
+#pragma unroll 1
+  for (uint32_t bit = 0x80000000u; bit >> (32 - BITS); bit >>= 1) {
+    const uint32_t t = y | bit;
+    if (__popc(__ballot_sync(FULL_MASK, x[0] >= t)) + __popc(__ballot_sync(FULL_MASK, x[1] >= t)) >= n) y = t;
+  }
+  return y;
+}
+
 template <int T, bool TOP>
-__global__ void __launch_bounds__(THREADS, 3) score_kernel(const ScoreParams p) {
+__global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams p) {
   using E = Elements<T>;
   __shared__ Joined of_warp[WARPS];
-  __shared__ uint64_t lists[SCORE_MAX_SPLIT * SCORE_MAX_TOP], best[SCORE_MAX_TOP];
-  __shared__ uint32_t bound_word;
-  __shared__ int last_one;
+  __shared__ uint64_t passed[TOP ? WARPS * BUFFER : 1], best[SCORE_MAX_TOP];
+  __shared__ float group_max[TOP ? GROUPS * THREADS : 1];
+  __shared__ uint32_t maxima[THREADS];
+  __shared__ int n_passed[WARPS], last_one;
   grid_dep_launch_dependents();
   grid_dep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_top;
@@ -156,39 +186,70 @@ __global__ void __launch_bounds__(THREADS, 3) score_kernel(const ScoreParams p) 
   const int vectors = (p.vocab - head) / E::PER, tail = p.vocab - head - vectors * E::PER;
   const uint4* xv = reinterpret_cast<const uint4*>(x + head * E::SIZE);
   const int per = (vectors + p.split - 1) / p.split, v0 = min(vectors, per * piece), v1 = min(vectors, v0 + per);
-  if (TOP && tid == 0) bound_word = score_to_ord(-INF);
-  if (TOP) __syncthreads();
-  volatile uint32_t* bound_at = &bound_word;
+  float largest = -INF, of_group = -INF, least = -INF;         // the thread's so far, its group's; what elements have to reach
   const uint64_t scale2 = pair_of(p.scale, p.scale);
+  // what the end needs, on its way from the start
+  const int target = p.targets && warp == 0 ? p.targets[row] : -1;
+  const float of_target = target >= 0 && target < p.vocab ? E::one(x, target) : 0.0f;
   Sums sums;
   TopList list;
 
-  auto single = [&](int i, bool there) {             // an element per lane
-    const float v = there ? E::one(x, i) : -INF, y = __fmul_rn(v, p.scale), at = sums.raise(y);
-    sums.add(pair_of(y, -INF), pair_of(-at, -at));
-    if (TOP) list.offer(there && list.admits(v, ord_to_score(*bound_at)) ? make_key(v, i) : KEY_EMPTY, n, lane);
+  uint64_t* const mine_passed = passed + (TOP ? warp * BUFFER : 0);
+  int count = 0;                                      // of the warp's keys there
+  auto push = [&](uint32_t mask, auto key_of) {       // a bit for each element of the lane's that has passed
+    for (unsigned who; (who = __ballot_sync(FULL_MASK, mask != 0)) != 0; count += __popc(who))
+      if (mask) {
+        mine_passed[count + __popc(who & ((1u << lane) - 1u))] = key_of(__ffs(mask) - 1);
+        mask &= mask - 1;
+      }
+    __syncwarp();
   };
-  if (piece == 0 && warp == 0 && head) single(lane, lane < head);
+  auto take_in = [&]() {                              // what has passed, into the list
+    for (int i = 0; i < count; i += 32) list.offer(i + lane < count ? mine_passed[i + lane] : KEY_EMPTY, n, lane);
+    count = 0;
+    __syncwarp();
+  };
+  // single elements, of the first warp's lanes
+  auto single_value = [&](int i, int end) { return i < end ? E::one(x, i) : -INF; };
+  auto single_sums = [&](float y) {
+    const float at = sums.raise(__fmul_rn(y, p.scale));
+    sums.add(pair_of(y, -INF), scale2, pair_of(-at, -at));
+  };
+  auto single_key = [&](float y, int i, int end) { push(i < end && y >= least, [&](int) { return make_key(y, i); }); };
+  const bool has_head = piece == 0 && warp == 0 && head, has_tail = piece == p.split - 1 && warp == 0 && tail;
+  float of_head = -INF, of_tail = -INF;
+  if (has_head) single_sums(of_head = single_value(lane, head));
+  if (has_tail) single_sums(of_tail = single_value(p.vocab - tail + lane, p.vocab));
 
-  uint4 next[VECTORS];
+  uint4 v[VECTORS];
   auto load = [&](int base) {
+    const uint4* from = xv + base + tid;
+    if (base + VECTORS * THREADS <= v1) {
 #pragma unroll
-    for (int j = 0; j < VECTORS; ++j) {
-      const int i = base + j * THREADS + tid;
-      next[j] = i < v1 ? ld_stream_16B(xv + i) : make_uint4(E::BANNED, E::BANNED, E::BANNED, E::BANNED);
+      for (int j = 0; j < VECTORS; ++j) v[j] = ld_stream_16B(from + j * THREADS);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VECTORS; ++j)
+        v[j] = base + j * THREADS + tid < v1 ? ld_stream_16B(from + j * THREADS) : make_uint4(E::BANNED, E::BANNED, E::BANNED, E::BANNED);
     }
   };
-  load(v0);
-  for (int base = v0; base < v1; base += VECTORS * THREADS) {
-    uint4 v[VECTORS];
-    float most[VECTORS], all = -INF;
+  const int blocks = (v1 - v0 + VECTORS * THREADS - 1) / (VECTORS * THREADS);
+  int shift = 0;                                      // 2^shift blocks are a group
+  while (blocks > GROUPS << shift) ++shift;
+  for (int block = 0; block < blocks; ++block) {
+    load(v0 + block * VECTORS * THREADS);
+    uint32_t words[4];
 #pragma unroll
-    for (int j = 0; j < VECTORS; ++j) v[j] = next[j];
-    load(base + VECTORS * THREADS);
+    for (int i = 0; i < 4; ++i) {
+      words[i] = (&v[0].x)[i];
 #pragma unroll
-    for (int j = 0; j < VECTORS; ++j) {
-      most[j] = E::largest(v[j]);
-      all = max_nan(all, most[j]);
+      for (int j = 1; j < VECTORS; ++j) words[i] = E::larger(words[i], (&v[j].x)[i]);
+    }
+    const float all = E::widest(E::larger(E::larger(words[0], words[1]), E::larger(words[2], words[3])));
+    if (TOP) {
+      of_group = block & ((1 << shift) - 1) ? max_nan(of_group, all) : all;
+      group_max[(block >> shift) * THREADS + tid] = of_group;
+      largest = max_nan(largest, all);
     }
     const float at = sums.raise(__fmul_rn(all, p.scale));
     const uint64_t minus2 = pair_of(-at, -at);
@@ -197,40 +258,9 @@ __global__ void __launch_bounds__(THREADS, 3) score_kernel(const ScoreParams p) 
 #pragma unroll
       for (int i = 0; i < E::PER / 2; ++i) {
         const float2 u = E::pair(v[j], i);
-        sums.add(mul_pairs(pair_of(u.x, u.y), scale2), minus2);
+        sums.add(pair_of(u.x, u.y), scale2, minus2);
       }
-    if (TOP) {
-      if (base == v0) {
-        // the n-th largest of the lanes' maxima: n elements reach it
-        const uint32_t o = base + tid < v1 && all == all ? score_to_ord(all) : 0u;
-        int rank = 0;
-#pragma unroll 8
-        for (int i = 0; i < 32; ++i) {
-          const uint32_t other = __shfl_sync(FULL_MASK, o, i);
-          rank += other > o || (other == o && i < lane);
-        }
-        if (rank == n - 1 && o) atomicMax(&bound_word, o);
-        __syncwarp();
-      }
-      const float bound = ord_to_score(*bound_at);
-      if (__any_sync(FULL_MASK, list.admits(all, bound))) {
-#pragma unroll
-        for (int j = 0; j < VECTORS; ++j) {
-          if (!__any_sync(FULL_MASK, list.admits(most[j], bound))) continue;
-          const int i = base + j * THREADS + tid;
-          const TopList before = list;               // of lower indices all; among this step's own, the keys decide
-#pragma unroll
-          for (int e = 0; e < E::PER; ++e) {
-            const float2 u = E::pair(v[j], e / 2);
-            const float one = e & 1 ? u.y : u.x;
-            list.offer(i < v1 && before.admits(one, bound) ? make_key(one, head + i * E::PER + e) : KEY_EMPTY, n, lane);
-          }
-        }
-        if (lane == 0 && list.last != KEY_EMPTY) atomicMax(&bound_word, (uint32_t)(list.last >> 32));
-      }
-    }
   }
-  if (piece == p.split - 1 && warp == 0 && tail) single(p.vocab - tail + lane, lane < tail);
 
   // the CTA's result
   float sa, sb, wa, wb;
@@ -239,16 +269,63 @@ __global__ void __launch_bounds__(THREADS, 3) score_kernel(const ScoreParams p) 
   Joined mine{sums.top, sa + sb, wa + wb};
   mine.over_warp();
   if (lane == 0) of_warp[warp] = mine;
-  if (TOP && lane < n) lists[warp * SCORE_MAX_TOP + lane] = list.mine;
+  if (TOP) {
+    maxima[tid] = largest == largest ? score_to_ord(largest) : 0u;
+    __syncthreads();
+    least = fmaxf(ord_to_score(nth_largest<T == BF16 ? 16 : 20>(maxima, n, lane)), -INF);        // (NaN where less than n threads have something)
+    if (has_head) single_key(of_head, lane, head);
+    for (int first = 0; first < blocks; first += 1 << shift) {
+      const bool reaches = group_max[(first >> shift) * THREADS + tid] >= least;
+      if (!__any_sync(FULL_MASK, reaches)) continue;
+      for (int block = first; block < min(blocks, first + (1 << shift)); ++block) {
+        const int i0 = v0 + block * VECTORS * THREADS + tid;
+#pragma unroll
+        for (int j = 0; j < VECTORS; ++j)
+          v[j] = reaches && i0 + j * THREADS < v1 ? ld_stream_16B(xv + i0 + j * THREADS) : make_uint4(E::BANNED, E::BANNED, E::BANNED, E::BANNED);
+#pragma unroll
+        for (int j = 0; j < VECTORS; ++j) {
+          const bool some = reaches && i0 + j * THREADS < v1 && E::largest(v[j]) >= least;
+          if (!__any_sync(FULL_MASK, some)) continue;
+          uint32_t mask = 0;
+#pragma unroll
+          for (int e = 0; e < E::PER; ++e) {
+            const float2 u = E::pair(v[j], e / 2);
+            mask |= ((e & 1 ? u.y : u.x) >= least ? 1u : 0u) << e;
+          }
+          push(some ? mask : 0u, [&](int e) { return make_key(E::any(v[j], e), head + (i0 + j * THREADS) * E::PER + e); });
+          if (count > BUFFER - 32 * E::PER) {
+            take_in();
+            least = max_nan(least, list.least());
+          }
+        }
+      }
+    }
+    if (has_tail) single_key(of_tail, p.vocab - tail + lane, p.vocab);
+    if (count > 32 || __any_sync(FULL_MASK, list.mine != KEY_EMPTY)) {
+      take_in();
+      count = __popc(__ballot_sync(FULL_MASK, lane < n && list.mine != KEY_EMPTY));
+      if (lane < count) mine_passed[lane] = list.mine;
+    }
+    if (lane == 0) n_passed[warp] = count;
+  }
   __syncthreads();
+  int found = 0;
+  if (TOP) {                                          // a key a thread: its rank is the number of larger ones
+    const uint64_t key = lane < count ? mine_passed[lane] : KEY_EMPTY;
+    int rank = 0;
+    for (int i = 0; i < WARPS; ++i) {
+      const int keys = n_passed[i];
+      found += keys;
+#pragma unroll 4
+      for (int k = 0; k < keys; ++k) rank += passed[i * BUFFER + k] > key;
+    }
+    if (found > n) found = n;
+    if (lane < count && rank < n) best[rank] = key;
+    __syncthreads();
+  }
   if (warp != 0) return;
   mine = lane < WARPS ? of_warp[lane] : Joined{-INF, 0.0f, 0.0f};
   mine.over_warp();
-  int found = 0;
-  if (TOP) {
-    found = tournament_in_registers<1>(lists, SCORE_MAX_TOP, WARPS, n, lane, best);
-    __syncwarp();
-  }
   if (p.split > 1) {
     ScorePartial* to = p.partials + row * p.split + piece;
     if (lane == 0) {
@@ -271,24 +348,24 @@ __global__ void __launch_bounds__(THREADS, 3) score_kernel(const ScoreParams p) 
     if (lane < p.split) mine = Joined{__ldcg(&all[lane].top), __ldcg(&all[lane].sum), __ldcg(&all[lane].weighted)};
     mine.over_warp();
     if (TOP) {
+#pragma unroll 8
       for (int i = 0; i < p.split; ++i)
-        if (lane < n) lists[i * SCORE_MAX_TOP + lane] = __ldcg(&all[i].keys[lane]);
+        if (lane < n) passed[i * SCORE_MAX_TOP + lane] = __ldcg(&all[i].keys[lane]);
       __syncwarp();
-      found = tournament_in_registers<1>(lists, SCORE_MAX_TOP, p.split, n, lane, best);
+      found = tournament_in_registers<1>(passed, SCORE_MAX_TOP, p.split, n, lane, best);
       __syncwarp();
     }
   }
   // the row's
   const bool none = !(mine.top < INF), banned = mine.top == -INF;
   const float log_sum = banned ? 0.0f : logf(mine.sum), top = banned ? 0.0f : mine.top, nan = __int_as_float(0x7fffffff);
-  auto log_prob = [&](float v) { return none ? nan : __fmul_rn(v, p.scale) - top - log_sum; };
+  auto log_prob = [&](float v) { return none ? nan : fmaf(v, p.scale, -top) - log_sum; };
   if (lane == 0 && p.entropy) p.entropy[row] = none ? nan : banned ? 0.0f : log_sum - mine.weighted / mine.sum;
   if (lane == 0 && p.targets) {
-    const int t = p.targets[row];
     float r = 0.0f;
-    if (t >= 0 && t < p.vocab) {
-      r = log_prob(E::one(x, t));
-    } else if (t != -1) {
+    if (target >= 0 && target < p.vocab) {
+      r = log_prob(of_target);
+    } else if (target != -1) {
       r = nan;
       report_status(p.host_status, KV_INVALID);
     }
@@ -309,8 +386,8 @@ cudaError_t launch(const ScoreParams& p, cudaStream_t st) {
 }  // namespace
 
 cudaError_t score_launch(ScoreParams p, int dtype, int sm_count, cudaStream_t st) {
-  // few rows are split until three CTAs an SM have something to do, down to a block per thread
-  const int64_t wanted = (3 * sm_count + p.n_rows - 1) / p.n_rows, blocks = (int64_t)p.vocab * (dtype == F32 ? 4 : 2) / (16 * VECTORS * THREADS);
+  // few rows are split until CTAS an SM have something to do, down to a block per thread
+  const int64_t wanted = CTAS * sm_count / p.n_rows, blocks = (int64_t)p.vocab * (dtype == F32 ? 4 : 2) / (16 * VECTORS * THREADS);
   p.split = (int)(wanted < SCORE_MAX_SPLIT ? wanted : SCORE_MAX_SPLIT);
   if (p.split > blocks) p.split = (int)blocks;
   if (p.split < 1) p.split = 1;
