@@ -159,10 +159,16 @@ __device__ __forceinline__ uint32_t nth_largest(const volatile uint32_t* words, 
   uint32_t x[2] = {0, 0}, y = 0;
 #pragma unroll
   for (int i = 0; i < WARPS; ++i) x[i & 1] = max(x[i & 1], words[i * 32 + lane]);
+  static_assert(BITS % 2 == 0, "two bits a round: half as many rounds, each waiting for the last, as with one");
 #pragma unroll 1
-  for (uint32_t bit = 0x80000000u; bit >> (32 - BITS); bit >>= 1) {
-    const uint32_t t = y | bit;
-    if (__popc(__ballot_sync(FULL_MASK, x[0] >= t)) + __popc(__ballot_sync(FULL_MASK, x[1] >= t)) >= n) y = t;
+  for (int at = 30; at >= 32 - BITS; at -= 2) {
+    uint32_t more = 0;
+#pragma unroll
+    for (uint32_t d = 1; d < 4; ++d) {
+      const uint32_t t = y | d << at;
+      more += __popc(__ballot_sync(FULL_MASK, x[0] >= t)) + __popc(__ballot_sync(FULL_MASK, x[1] >= t)) >= n;
+    }
+    y |= more << at;
   }
   return y;
 }
@@ -171,10 +177,10 @@ template <int T, bool TOP>
 __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams p) {
   using E = Elements<T>;
   __shared__ Joined of_warp[WARPS];
-  __shared__ uint64_t passed[TOP ? WARPS * BUFFER : 1], best[SCORE_MAX_TOP];
+  __shared__ uint64_t passed[TOP ? WARPS * BUFFER : 1], keys[TOP ? THREADS : 1], best[SCORE_MAX_TOP];
   __shared__ float group_max[TOP ? GROUPS * THREADS : 1];
   __shared__ uint32_t maxima[THREADS];
-  __shared__ int n_passed[WARPS], last_one;
+  __shared__ int n_passed, last_one;
   grid_dep_launch_dependents();
   grid_dep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = p.n_top;
@@ -271,12 +277,16 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
   if (lane == 0) of_warp[warp] = mine;
   if (TOP) {
     maxima[tid] = largest == largest ? score_to_ord(largest) : 0u;
+    if (tid == 0) n_passed = 0;
     __syncthreads();
     least = fmaxf(ord_to_score(nth_largest<T == BF16 ? 16 : 20>(maxima, n, lane)), -INF);        // (NaN where less than n threads have something)
     if (has_head) single_key(of_head, lane, head);
-    for (int first = 0; first < blocks; first += 1 << shift) {
-      const bool reaches = group_max[(first >> shift) * THREADS + tid] >= least;
-      if (!__any_sync(FULL_MASK, reaches)) continue;
+    uint32_t mine_reach = 0;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) mine_reach |= (g << shift < blocks && group_max[g * THREADS + tid] >= least ? 1u : 0u) << g;
+    for (uint32_t groups = __reduce_or_sync(FULL_MASK, mine_reach); groups; groups &= groups - 1) {
+      const int first = (__ffs(groups) - 1) << shift;
+      const bool reaches = mine_reach & groups & -groups;
       for (int block = first; block < min(blocks, first + (1 << shift)); ++block) {
         const int i0 = v0 + block * VECTORS * THREADS + tid;
 #pragma unroll
@@ -306,22 +316,26 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
       count = __popc(__ballot_sync(FULL_MASK, lane < n && list.mine != KEY_EMPTY));
       if (lane < count) mine_passed[lane] = list.mine;
     }
-    if (lane == 0) n_passed[warp] = count;
+    // all warps' keys, one behind the other
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&n_passed, count);
+    at = __shfl_sync(FULL_MASK, at, 0);
+    if (lane < count) keys[at + lane] = mine_passed[lane];
   }
   __syncthreads();
   int found = 0;
   if (TOP) {                                          // a key a thread: its rank is the number of larger ones
-    const uint64_t key = lane < count ? mine_passed[lane] : KEY_EMPTY;
-    int rank = 0;
-    for (int i = 0; i < WARPS; ++i) {
-      const int keys = n_passed[i];
-      found += keys;
-#pragma unroll 4
-      for (int k = 0; k < keys; ++k) rank += passed[i * BUFFER + k] > key;
+    found = n_passed;
+    if (tid < found) {
+      const uint64_t key = keys[tid];
+      int rank = 0;
+#pragma unroll 8
+      for (int k = 0; k < found; ++k) rank += keys[k] > key;
+      if (rank < n) best[rank] = key;
     }
+    if (found > 32) __syncthreads();
     if (found > n) found = n;
-    if (lane < count && rank < n) best[rank] = key;
-    __syncthreads();
+    __syncwarp();
   }
   if (warp != 0) return;
   mine = lane < WARPS ? of_warp[lane] : Joined{-INF, 0.0f, 0.0f};
