@@ -131,6 +131,25 @@ struct Joined {
   }
 };
 
+// The 32 best of two sets of 32 keys, one a lane, in descending order; the first set is in that order.
+__device__ __noinline__ uint64_t merge_sorted(uint64_t sorted, uint64_t key, int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32; k *= 2)
+#pragma unroll
+    for (int j = k / 2; j; j /= 2) {
+      const uint64_t other = __shfl_xor_sync(FULL_MASK, key, j);
+      if (((lane & k) == 0) == ((lane & j) == 0) ? other > key : other < key) key = other;
+    }
+  const uint64_t turned = __shfl_sync(FULL_MASK, key, 31 - lane);
+  if (turned > sorted) sorted = turned;
+#pragma unroll
+  for (int j = 16; j; j /= 2) {
+    const uint64_t other = __shfl_xor_sync(FULL_MASK, sorted, j);
+    if ((lane & j) == 0 ? other > sorted : other < sorted) sorted = other;
+  }
+  return sorted;
+}
+
 // The warp's best keys, one a lane in descending order; the first n of them count.
 struct TopList {
   uint64_t mine, last;      // last: the n-th, KEY_EMPTY until there are n
@@ -140,14 +159,19 @@ struct TopList {
   // A key per lane, KEY_EMPTY for none.
   __device__ __forceinline__ void offer(uint64_t key, int n, int lane) {
     unsigned who = __ballot_sync(FULL_MASK, key > last);
-    while (who) {           // the highest lane's first: of elements that ascend, all but n are out at once
-      const uint64_t k = __shfl_sync(FULL_MASK, key, 31 - __clz(who));
+    if (__popc(who) > 6) {  // some 20 exchanges between lanes, as in three to six insertions that wait for one another
+      mine = merge_sorted(mine, key, lane);
+      last = __shfl_sync(FULL_MASK, mine, n - 1);
+      return;
+    }
+    while (who) {
+      const uint64_t k = __shfl_sync(FULL_MASK, key, __ffs(who) - 1);
       const int at = __popc(__ballot_sync(FULL_MASK, mine > k));
       const uint64_t up = __shfl_up_sync(FULL_MASK, mine, 1);
       if (lane == at) mine = k;
       else if (lane > at) mine = up;
       last = __shfl_sync(FULL_MASK, mine, n - 1);
-      who &= ~(0x80000000u >> __clz(who));
+      who &= who - 1;
       who &= __ballot_sync(FULL_MASK, key > last);
     }
   }
