@@ -250,8 +250,9 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
   Ring at(n_stages);                                  // of the roles that follow the stages
   StateWalk walk(&t->line, &t->plan);
   StatePiece piece;
-  auto head_of = [&](const StatePiece& x) { return (x.item + p.first_item) / p.slices; };
-  auto slice_of = [&](const StatePiece& x) { return (x.item + p.first_item) % p.slices; };
+  // (one slice or two: value_dim is 256 at most)
+  auto head_of = [&](const StatePiece& x) { return (x.item + p.first_item) >> (p.slices - 1); };
+  auto slice_of = [&](const StatePiece& x) { return (x.item + p.first_item) & (p.slices - 1); };
   auto first_token = [&](const StatePiece& x) { return t->starts[x.i]; };
   auto tokens_of = [&](const StatePiece& x) { return t->starts[x.i + 1] - t->starts[x.i]; };
   // Stages in front of a piece's chunks: the state that it begins with, or the published ones that this is put together from, 64 key dimensions each.
@@ -495,13 +496,6 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
       at.advance();
       ++loads;
     };
-    for (int i = 0; i < n_stages; ++i) load_one();
-    bool begun = false;
-    // One more load for each stage that has been passed.
-    auto passed = [&]() {
-      if (begun) load_one();
-      begun = true;
-    };
     const int row = tid - W_SCORES * 32;              // token of the chunk
     uint32_t ph = 0;
     const uint32_t to = smem_u32(p_smem) + row * 128;
@@ -514,64 +508,81 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
       tell(&t->fall_ready[served & 1]);
       ++served;
     };
-    serve();
-    serve();
-    while (next_piece()) {
-      if (warp == W_SCORES)
-        for (int j = slots_of(piece) + (piece.sum_only ? piece.c1 - piece.c0 : 0); j > 0 && ok; --j) passed();
-      if (piece.sum_only) {
-        end_piece();
-        if (n_pieces > 1) serve();
+    // Loads and powers are called for at one place, as their code is long: a load for each stage of the ring and then one more for each that has
+    // been passed (the first one is kept back), powers two pieces ahead.
+    int to_load = warp == W_SCORES ? n_stages : 0, to_serve = 2, to_pass = 0, c = 0, c1 = 0;
+    bool begun = false, open = false;
+    const float* fall = nullptr;
+    auto passed = [&]() {
+      if (warp == W_SCORES && begun) ++to_load;
+      begun = true;
+    };
+    for (;;) {
+#pragma unroll 1
+      for (; to_load > 0; --to_load) load_one();
+#pragma unroll 1
+      for (; to_serve > 0; --to_serve) serve();
+      if (!ok) break;
+      if (to_pass > 0) {
+        --to_pass;
+        passed();
         continue;
       }
-      const float* fall = t->fall[n_pieces & 1].at + FALL + row;        // fall[-s]: l^(row - s), 0 for s > row
-      for (int c = piece.c0; c < piece.c1; ++c) {
-        wait(&t->p_full, ph);
-        if (!ok) break;
-        tc_fence_after_sync();
-        float lift = 1.0f;
-        if (F16) {
-          float m = 0.0f;
-#pragma unroll 1
-          for (int h = 0; h < C; h += 32) {
-            uint32_t x[32];
-            tmem_ld_32x32(tmem + lane_base + T_P + h, x);
-            tmem_ld_wait_for32(x);
-#pragma unroll
-            for (int s = 0; s < 32; ++s) m = fmaxf(m, fabsf(__uint_as_float(x[s]) * fall[-h - s]));
-          }
-          lift = lift_of(m, 100);
-        }
-        wait(&t->o1_full, ph ^ 1u);                   // the last chunk's has been used, and the factors of the one before
-        if (!ok) break;
-        if (F16) t->token_scale[ph][row] = reciprocal_of_power(lift);
+      if (c == c1) {
+        if (open) end_piece();
+        open = next_piece();
+        if (!open) break;
+        to_pass = slots_of(piece) + (piece.sum_only ? piece.c1 - piece.c0 : 0);
+        c = piece.sum_only ? piece.c1 : piece.c0;
+        c1 = piece.c1;
+        fall = t->fall[n_pieces & 1].at + FALL + row;       // fall[-s]: l^(row - s), 0 for s > row
+        continue;
+      }
+      wait(&t->p_full, ph);
+      if (!ok) break;
+      tc_fence_after_sync();
+      float lift = 1.0f;
+      if (F16) {
+        float m = 0.0f;
 #pragma unroll 1
         for (int h = 0; h < C; h += 32) {
           uint32_t x[32];
           tmem_ld_32x32(tmem + lane_base + T_P + h, x);
           tmem_ld_wait_for32(x);
 #pragma unroll
-          for (int s = 0; s < 32; ++s) {
-            const float y = __uint_as_float(x[s]) * fall[-h - s];
-            x[s] = __float_as_uint(F16 ? y * lift : y);
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = pack2<F16>(__uint_as_float(x[8 * j + 2 * i]), __uint_as_float(x[8 * j + 2 * i + 1]));
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((h / 8 + j) ^ (row & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
-                         : "memory");
-          }
+          for (int s = 0; s < 32; ++s) m = fmaxf(m, fabsf(__uint_as_float(x[s]) * fall[-h - s]));
         }
-        ph ^= 1u;
-        fence_async_shared();
-        tc_fence_before_sync();
-        tell(&t->p_ready);
-        passed();
-        if (c == piece.c0 && n_pieces > 0) serve();
+        lift = lift_of(m, 100);
       }
-      end_piece();
+      wait(&t->o1_full, ph ^ 1u);                   // the last chunk's has been used, and the factors of the one before
+      if (!ok) break;
+      if (F16) t->token_scale[ph][row] = reciprocal_of_power(lift);
+#pragma unroll 1
+      for (int h = 0; h < C; h += 32) {
+        uint32_t x[32];
+        tmem_ld_32x32(tmem + lane_base + T_P + h, x);
+        tmem_ld_wait_for32(x);
+#pragma unroll
+        for (int s = 0; s < 32; ++s) {
+          const float y = __uint_as_float(x[s]) * fall[-h - s];
+          x[s] = __float_as_uint(F16 ? y * lift : y);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = pack2<F16>(__uint_as_float(x[8 * j + 2 * i]), __uint_as_float(x[8 * j + 2 * i + 1]));
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((h / 8 + j) ^ (row & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                       : "memory");
+        }
+      }
+      ph ^= 1u;
+      fence_async_shared();
+      tc_fence_before_sync();
+      tell(&t->p_ready);
+      passed();
+      if (c == piece.c0 && n_pieces > 0) to_serve = 1;
+      ++c;
     }
     // what is in flight lands before the CTA leaves
     asm volatile("cp.async.wait_all;" ::: "memory");
