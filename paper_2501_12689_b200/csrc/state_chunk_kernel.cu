@@ -970,7 +970,15 @@ template <bool F16, int DK, int DV>
 cudaError_t launch(const StateAttendParams& p, const StateMaps& maps, int sm_count, int smem_optin, cudaStream_t st) {
   int stages = MAX_STAGES;
   while (stages > 2 && smem_bytes<F16, DK, DV>(stages) > smem_optin) --stages;
-  return launch_overlapped(state_chunk_kernel<F16, DK, DV>, dim3((unsigned)sm_count), dim3(THREADS), (size_t)smem_bytes<F16, DK, DV>(stages), st, 1, p, maps,
+  // A CTA with a part of an item waits for the states of all the parts before it and adds them up, so that beyond some number more parts cost more than
+  // they give: with an item of M chunks, about sqrt(2 M) (30,000 tokens, one head of 128 x 128: 141 us; with sqrt(M) 142, with sqrt(4 M) 155, with an SM
+  // each 314).  (Sequences of the mean length: what there is is not known here.)
+  const int64_t chunks = (p.n_tokens - 1) / C + p.n, mean = (chunks + p.n - 1) / p.n;
+  int64_t parts = 1;
+  while (parts * parts < 2 * mean) ++parts;
+  parts *= (int64_t)p.n * p.n_items;
+  if (parts > sm_count) parts = sm_count;
+  return launch_overlapped(state_chunk_kernel<F16, DK, DV>, dim3((unsigned)parts), dim3(THREADS), (size_t)smem_bytes<F16, DK, DV>(stages), st, 1, p, maps,
                            stages);
 }
 
