@@ -362,3 +362,45 @@ def test_rows_behind_the_last_sequence_stay():
     with pytest.raises(ICCacheError):
         s.sync()
     assert (out == 7).all()
+
+
+@pytest.mark.parametrize("counts", [[9000], [700, 30, 2500]])
+def test_two_handles_at_once(counts):
+    """Calls of two handles on two streams, not waited for in between: CTAs of one wait for the states that others of the same call publish."""
+    n, t = len(counts), sum(counts)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    q, k, v = (draw(30 + i, t, 2, 64) for i in range(3))
+    rates, seqs, starts = rates_of(2), ints(list(range(n))), starts_of(counts)
+    alone = ICStates(1, 2, 64, 64, n)
+    wants = [alone.extend(0, q, k, v, rates, seqs, starts) for _ in range(4)]
+    alone.sync()
+    torch.cuda.synchronize()
+    held = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            held.append(ICStates(1, 2, 64, 64, n, stream=s))
+    torch.cuda.synchronize()
+    gots = [[], []]
+    for _ in range(4):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                gots[i].append(held[i].extend(0, q, k, v, rates, seqs, starts))
+    torch.cuda.synchronize()
+    for i in range(2):
+        held[i].sync()
+        assert torch.equal(held[i].pool, alone.pool)
+        assert all(torch.equal(a, b) for a, b in zip(gots[i], wants))
+
+
+@pytest.mark.parametrize("counts", [[8192], [64 * 31, 64 * 33 + 1], [4000, 1, 0, 17]])
+@pytest.mark.parametrize("heads", [1, 3])
+def test_parts_of_an_item(counts, heads):
+    """Few heads and long sequences: an item is divided among fewer CTAs than there are."""
+    run(counts, heads=heads, dk=128, dv=64, layers=1, layer=0, seed=40)
+
+
+@pytest.mark.parametrize("each", [8, 9, 16, 17, 32, 33])
+def test_around_the_change_of_kernels(each):
+    run([each], heads=4, seed=50)
+    run([each] * 3, heads=2, dk=72, dv=136, dtype=F16, seed=51)
+    run([each] * 40, heads=16, dk=16, dv=16, seed=52)

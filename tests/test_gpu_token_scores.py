@@ -267,3 +267,36 @@ def test_more_than_two_to_the_32_bytes():
         part = check(x[a:a + 100], 2, targets=t[a:a + 100].contiguous(), scores=s)
         assert torch.equal(part.top_ids, got.top_ids[a:a + 100])
         assert (part.log_probs - got.log_probs[a:a + 100]).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("kind", ["drawn", "banned", "rising", "falling", "two values"])
+@pytest.mark.parametrize("rows,vocab,dtype", [(1, 16777216, BF16), (600, 262145, BF16), (3, 1500001, F32), (600, 130001, F32)])
+def test_rows_of_many_blocks(rows, vocab, dtype, kind):
+    """Rows so long that a thread's blocks are put together in groups, whole and split, with 32 alternatives."""
+    x = torch.empty(rows, vocab, dtype=dtype, device=DEV)
+    ramp = torch.arange(vocab, device=DEV).to(F32) / vocab
+    if kind == "drawn":
+        x[:] = draw(rows, vocab, dtype, 5)
+    elif kind == "banned":          # fewer left than are asked for
+        x[:] = -INF
+        x[:, vocab // 3:: vocab // 7] = 1.5
+        x[:, -1] = 2.5
+    elif kind == "rising":
+        x[:] = (8 * ramp).to(dtype)
+    elif kind == "falling":
+        x[:] = (-8 * ramp).to(dtype)
+    else:
+        x[:] = 0
+        x[:, 7:: max(1, vocab // 40)] = 1.0
+    s = ICTokenScores(vocab, dtype=dtype)
+    t = torch.randint(-1, vocab, (rows,), device=DEV, generator=gen(8), dtype=torch.int32)
+    got = s.score(x, t, n_top=32)
+    s.sync()
+    for a in range(0, rows, 100):       # (a part at a time: 64 bits a logit)
+        part = x[a:a + 100]
+        assert torch.equal(got.top_ids[a:a + 100].long(), torch.sort(part, dim=-1, descending=True, stable=True).indices[:, :32])
+    last = x[-1:].contiguous()
+    again = check(last, 32, targets=t[-1:].contiguous(), scores=ICTokenScores(vocab, dtype=dtype))
+    assert torch.equal(again.top_ids[0], got.top_ids[-1])
+    # (another division into pieces: the same sums in another order, each within the bound that check() holds)
+    assert torch.allclose(again.entropy[0], got.entropy[-1], rtol=2.0 ** -10, atol=2.0 ** -10)
