@@ -251,12 +251,10 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
   p.flags = reinterpret_cast<unsigned*>(reinterpret_cast<unsigned char*>(s->v.err) + FLAGS);
   p.slots = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS);
   p.slot_floats = icc::state_slot_floats(s->v.key_dim, s->v.value_dim);
-  // Token by token or in chunks: the chunks take 23 to 39 us for up to 64 tokens a sequence while there is an SM for each of two sequences' heads, the
-  // tokens 0.5 to 1.7 us each (1 sequence, 32 heads of 128 x 128: 32 us against 30 for 32 tokens, 43 for 48; 8 of them: 39 against 37 for 16, 51 for 24);
-  // beyond that they are bound by their sums (64 of them: 142 us against 128 for 8, 171 for 12).  Of several sequences only the mean length is known
-  // here, and the longest decides.
-  const int64_t items = (int64_t)a.n * s->v.n_heads;
-  const int few = items > 2 * s->sm_count ? 8 : a.n > 1 ? 16 : 32;
+  // Token by token or in chunks: up to 64 tokens a sequence, chunks take 9 to 23 us while there are few states, and a token 0.5 to 1.7 us (1 sequence, 4 heads
+  // of 64 x 64: 9.4 us against 8.8 for 12 tokens, 11.0 for 16; 32 heads of 128 x 128: 12.7 against 13.5 and 16.8); with an SM's share of two and more
+  // they are bound by the states and by their sums (8 such sequences: 23 us against 23 for 8, 29 for 12; 64 of them: 111 against 85 for 4, 128 for 8).
+  const int few = (int64_t)a.n * s->v.n_heads > s->sm_count ? 7 : 12;
   if (a.n_tokens <= few * (int64_t)a.n) return launched(s, icc::state_step_launch(p, s->f16, s->sm_count, s->stream), 1, "state");
   icc::StateMaps maps;
   maps.there = encode_rows(s, p.q, s->v.key_dim, a.n_tokens, &maps.q) && encode_rows(s, p.k, s->v.key_dim, a.n_tokens, &maps.k) &&

@@ -28,7 +28,12 @@ struct StateLine {
   __host__ __device__ int chunks(int i) const { return before[i + 1] - before[i]; }
   __host__ __device__ void set_per() {
     per = (int)(((unsigned)length() + parts - 1) / parts);
-    if (per < STATE_LEAST) per = STATE_LEAST;
+    if (per >= STATE_LEAST) return;
+    // (few chunks: items that are not cut may go one to a CTA)
+    bool cut_some = false;
+    for (int i = 0; i < n; ++i) cut_some |= chunks(i) > STATE_WHOLE;
+    if (cut_some) per = STATE_LEAST;
+    else if (per < 1) per = 1;
   }
   // The item that position x (below length()) lies in: its sequence, which of its items, and where that begins.
   struct At {
