@@ -15,8 +15,11 @@ namespace icc {
 
 constexpr int STATE_CHUNK = 64;           // tokens
 constexpr int STATE_BATCH = 256;          // sequences of a launch
-constexpr int STATE_WHOLE = 6;            // items of at most so many chunks are not cut,
-constexpr int STATE_LEAST = 3;            // and no piece has fewer
+// Items of at most STATE_WHOLE chunks are not cut (8 sequences of 700 tokens, 32 heads of 128 x 128: 73 us, with 6 90; 5 sequences, 16 heads of 64 x 128:
+// 31 and 51; 8 of 1,000 tokens 110, with 16 95, but one sequence, 4 heads of 64 x 64, 32 in place of 28), and no piece has fewer than STATE_LEAST (2: 75
+// in place of 68 us for 8 sequences of 500 tokens).
+constexpr int STATE_WHOLE = 12;
+constexpr int STATE_LEAST = 3;
 
 struct StateLine {
   int before[STATE_BATCH + 1];            // chunks of the sequences before this one
