@@ -190,13 +190,14 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
   const bool holds = state_call_holds(p, t->seen);
   if (holds && warp == 0) {
     // chunks before each sequence
-    int sum = 0;
+    int sum = 0, longest = 0;
     for (int i0 = 0; i0 < p.n; i0 += 32) {
       const int i = i0 + lane;
       const int from = i <= p.n ? (p.starts ? p.starts[i] : p.first_seq + i) : 0, to = i < p.n ? (p.starts ? p.starts[i + 1] : from + 1) : from;
       if (i < p.n) t->starts[i] = from;
       if (i == p.n - 1) t->starts[p.n] = to;
       const int mine = (int)(((unsigned)(to - from) + C - 1) / C);
+      longest = max(longest, mine);
       int inc = mine;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -206,12 +207,13 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
       if (i < p.n) t->line.before[i + 1] = sum + inc;
       sum += __shfl_sync(FULL_MASK, inc, 31);
     }
+    longest = __reduce_max_sync(FULL_MASK, longest);
     if (lane == 0) {
       t->line.before[0] = 0;
       t->line.n = p.n;
       t->line.per_chunk = p.n_items;
       t->line.parts = gridDim.x;
-      t->line.set_per();
+      t->line.set_per(longest);
       t->plan.make(t->line, blockIdx.x);
     }
     __syncwarp();
@@ -235,7 +237,7 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     t->line.before[0] = t->line.before[1] = 0;
     t->line.n = t->line.per_chunk = 1;
     t->line.parts = gridDim.x;
-    t->line.set_per();
+    t->line.set_per(0);
     t->plan.make(t->line, blockIdx.x);
     t->slots = 0;
   }

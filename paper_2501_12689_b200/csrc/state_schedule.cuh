@@ -29,13 +29,12 @@ struct StateLine {
   // (the line has fewer than 2^31 chunks: state_items() sees to it)
   __host__ __device__ int length() const { return before[n] * per_chunk; }
   __host__ __device__ int chunks(int i) const { return before[i + 1] - before[i]; }
-  __host__ __device__ void set_per() {
+  // longest: chunks of the longest sequence
+  __host__ __device__ void set_per(int longest) {
     per = (int)(((unsigned)length() + parts - 1) / parts);
     if (per >= STATE_LEAST) return;
     // (few chunks: items that are not cut may go one to a CTA)
-    bool cut_some = false;
-    for (int i = 0; i < n; ++i) cut_some |= chunks(i) > STATE_WHOLE;
-    if (cut_some) per = STATE_LEAST;
+    if (longest > STATE_WHOLE) per = STATE_LEAST;
     else if (per < 1) per = 1;
   }
   // The item that position x (below length()) lies in: its sequence, which of its items, and where that begins.
