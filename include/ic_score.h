@@ -8,9 +8,9 @@
  * For a row x[0..vocab) of logits, y = scale * x:
  *     log_prob(t) = y_t - log sum_j e^(y_j)         entropy = - sum_j p_j log p_j,  p_j = e^(log_prob(j))
  *     top alternatives: the n_top largest logits, in order, the lowest index first among equal ones (-0 equals 0)
- * Products, sums and maxima are held in fp32.  A logit of minus infinity is a banned token: probability 0, and nothing to the entropy.  A row
- * that bans every token has log-probabilities of minus infinity and an entropy of 0.  A row with a NaN, or whose largest y is plus
- * infinity, has none: log-probabilities and entropy are NaN, its top ids -1.
+ * Differences to a row's largest logit, products, sums and maxima are held in fp32.  A logit of minus infinity is a banned token:
+ * probability 0, and nothing to the entropy.  A row that bans every token has log-probabilities of minus infinity and an entropy of 0.
+ * A row with a NaN, or whose largest y is plus infinity, has none: log-probabilities and entropy are NaN, its top ids -1.
  *
  * Conventions as in ic_kv.h: device arrays, work enqueued on the handle's stream without synchronising, one handle per stream, not
  * thread-safe.  A call needs no more memory than the handle has, whatever its size.  Graphs captured from one handle share its
@@ -53,7 +53,7 @@ typedef struct ic_score_args {
   uint32_t struct_size; /* sizeof(ic_score_args_t) of the caller's build                      */
   int32_t n_top;        /* 0 .. IC_SCORE_MAX_TOP, at most vocab                               */
   int64_t n_rows;       /* 0 .. 2^26                                                          */
-  float scale;          /* of the logits, above 0 (one over the temperature)                  */
+  float scale;          /* of the logits, above 0 (one over the temperature); finite, also times log2(e) */
   int32_t reserved;     /* 0                                                                  */
   const void* logits;   /* row r at element r * row_stride, `vocab` contiguous values; any    */
   int64_t row_stride;   /*   stride >= 0, aligned to an element                               */

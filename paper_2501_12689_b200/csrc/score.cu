@@ -123,7 +123,9 @@ int ic_score_tokens(ic_score_t* s, const ic_score_args_t* args) {
   if (a.n_top < 0 || a.n_top > IC_SCORE_MAX_TOP || a.n_top > s->vocab)
     return fail(IC_ERR_INVALID, "n_top %d must be in [0, %d] and at most vocab %d", a.n_top, IC_SCORE_MAX_TOP, s->vocab);
   if (a.n_rows < 0 || a.n_rows > 1 << 26) return fail(IC_ERR_INVALID, "n_rows = %lld outside [0, 2^26]", (long long)a.n_rows);
-  if (!isfinite(a.scale) || a.scale <= 0.0f) return fail(IC_ERR_INVALID, "scale %g must be finite and above 0", a.scale);
+  const float scale_log2 = (float)((double)a.scale * 1.4426950408889634);
+  if (!isfinite(a.scale) || a.scale <= 0.0f || !isfinite(scale_log2))
+    return fail(IC_ERR_INVALID, "scale %g must be above 0 and finite, also times log2(e)", a.scale);
   if (a.row_stride < 0 || a.row_stride > 1ll << 36) return fail(IC_ERR_INVALID, "row_stride %lld must not be negative", (long long)a.row_stride);
   if (a.n_rows == 0) return IC_OK;
   if (!a.targets && !a.entropy && !a.n_top) return fail(IC_ERR_INVALID, "nothing is asked for");
@@ -145,6 +147,7 @@ int ic_score_tokens(ic_score_t* s, const ic_score_args_t* args) {
   p.n_top = a.n_top;
   p.split = 1;
   p.scale = a.scale;
+  p.scale_log2 = scale_log2;
   p.partials = s->partials;
   p.arrivals = s->arrivals;
   p.host_status = s->d_status;

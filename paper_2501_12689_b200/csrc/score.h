@@ -10,7 +10,7 @@ constexpr int SCORE_MAX_TOP = 32;
 constexpr int SCORE_MAX_SPLIT = 32;       // pieces of a row
 constexpr int SCORE_SLOTS = 1024;         // partial results, and rows that are split, of a launch
 
-// What one CTA knows of its piece of a row: maximum y, sum of e^(y - max), sum of e^(y - max) (y - max), and the best keys.
+// What one CTA knows of its piece of a row: largest logit m, sum of 2^d and of 2^d d with d = (x - m) scale log2(e), and the best keys.
 struct ScorePartial {
   float top, sum, weighted, unused;
   uint64_t keys[SCORE_MAX_TOP];
@@ -26,7 +26,7 @@ struct ScoreParams {
   int* top_ids;
   float* top_log_probs;
   int vocab, n_top, split;  // pieces of a row
-  float scale;
+  float scale, scale_log2;  // scale_log2 = scale * log2(e)
   ScorePartial* partials;   // [rows, split] where split > 1
   int* arrivals;            // [rows]: pieces that have arrived, zero between launches
   int* host_status;         // mapped host word

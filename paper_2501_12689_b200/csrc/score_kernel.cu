@@ -1,7 +1,10 @@
 // Log-probabilities of given tokens, entropy and the top alternatives of rows of logits, in one pass.
 //
-// A thread walks over its part of a row with a running maximum m and the sums  s = sum e^(y - m)  and  w = sum e^(y - m) (y - m):  at a new
-// maximum m' both are rescaled, w <- f (w + s (m - m')), s <- f s, f = e^(m - m').  Then  log_prob(t) = y_t - m - log s,  entropy = log s - w / s.
+// A thread walks over its part of a row with a running maximum m of the logits x and the sums  s = sum 2^d  and  w = sum 2^d d,
+// d = (x - m) scale log2(e):  at a new maximum m' both are rescaled, w <- f (w + s c), s <- f s, f = 2^c, c = (m - m') scale log2(e).  Then
+// log_prob(t) = (x_t - m) scale - log s,  entropy = log s - log(2) w / s.  The difference is taken before the product: that of the largest logit is 0 and
+// none is above it, however large the logits are.  (scale x rounded for the maximum and not for the difference would leave the product's rounding error,
+// 10^30 for rows masked with the type's lowest value.)
 // Every logit is read once, as 16-byte vectors, VECTORS of them at a time.  Per logit: one exponential (the special
 // function units do 16 a cycle and SM: in 16 bits three quarters of their rate at the copy's bandwidth), and about six other
 // instructions, pairs of floats at a time, where the bandwidth leaves room for eleven.  4,001 rows of 128,256 in bf16: 164 us, 6.3 TB/s; with five
@@ -35,8 +38,8 @@ constexpr int CTAS = 4;                   // an SM
 constexpr int GROUPS = 16;                // of a thread's blocks, each with its maximum
 constexpr int BUFFER = 384;               // keys of a warp that have passed the bound: more than a step's 256, so that it is seldom emptied
 static_assert(WARPS * BUFFER >= SCORE_MAX_SPLIT * SCORE_MAX_TOP, "the pieces' keys are joined there");
-constexpr float LOG2E = 1.4426950408889634f;
-constexpr float LEAST = -150.0f;          // e^LEAST is 0 in fp32; keeps banned tokens' differences finite
+constexpr float LOG_OF_2 = 0.6931471805599453f;
+constexpr float LEAST = -217.0f;          // 2^LEAST is 0 in fp32; keeps banned tokens' differences finite
 constexpr float INF = __builtin_huge_valf();
 
 enum : int { BF16 = 0, F16 = 1, F32 = 2 };
@@ -88,46 +91,46 @@ struct Elements {
   }
 };
 
-// Maximum and sums, by halves: even and odd elements are summed apart.
+// Maximum and sums, by halves: even and odd elements are summed apart.  c: scale log2(e).
 struct Sums {
   float top;                // -infinity: nothing yet
   uint64_t s, w;
   __device__ __forceinline__ Sums() : top(-INF), s(0), w(0) {}
-  // Raise the maximum to cover y; returns what differences are taken against.
-  __device__ __forceinline__ float raise(float y) {
-    const float now = max_nan(top, y), at = now == -INF ? 0.0f : now;
-    const float d = fmaxf(top - at, LEAST), f = exp2_fast(d * LOG2E);
+  // Raise the maximum to cover x; returns what differences are taken against.
+  __device__ __forceinline__ float raise(float x, float c) {
+    const float now = max_nan(top, x), at = now == -INF ? 0.0f : now;
+    const float d = fmaxf((top - at) * c, LEAST), f = exp2_fast(d);
     const uint64_t f2 = pair_of(f, f);
     w = mul_pairs(fma_pairs(s, pair_of(d, d), w), f2);
     s = mul_pairs(s, f2);
     top = now;
     return at;
   }
-  __device__ __forceinline__ void add(uint64_t x2, uint64_t scale2, uint64_t minus2) {
+  __device__ __forceinline__ void add(uint64_t x2, uint64_t minus2, uint64_t c2) {
     float a, b;
-    split_pair(fma_pairs(x2, scale2, minus2), &a, &b);
-    const uint64_t d = pair_of(fmaxf(a, LEAST), fmaxf(b, LEAST));
-    split_pair(mul_pairs(d, pair_of(LOG2E, LOG2E)), &a, &b);
+    split_pair(mul_pairs(add_pairs(x2, minus2), c2), &a, &b);
+    a = fmaxf(a, LEAST);
+    b = fmaxf(b, LEAST);
     const uint64_t e = pair_of(exp2_fast(a), exp2_fast(b));
     s = add_pairs(s, e);
-    w = fma_pairs(e, d, w);
+    w = fma_pairs(e, pair_of(a, b), w);
   }
 };
 
 struct Joined {
   float top, sum, weighted;
-  __device__ __forceinline__ void join(const Joined& o) {
+  __device__ __forceinline__ void join(const Joined& o, float c) {
     const float now = max_nan(top, o.top), at = now == -INF ? 0.0f : now;
-    const float da = fmaxf(top - at, LEAST), db = fmaxf(o.top - at, LEAST), fa = exp2_fast(da * LOG2E), fb = exp2_fast(db * LOG2E);
+    const float da = fmaxf((top - at) * c, LEAST), db = fmaxf((o.top - at) * c, LEAST), fa = exp2_fast(da), fb = exp2_fast(db);
     weighted = fa * (weighted + sum * da) + fb * (o.weighted + o.sum * db);
     sum = fa * sum + fb * o.sum;
     top = now;
   }
-  __device__ __forceinline__ void over_warp() {
+  __device__ __forceinline__ void over_warp(float c) {
 #pragma unroll
     for (int x = 16; x; x >>= 1) {
       const Joined o{__shfl_xor_sync(FULL_MASK, top, x), __shfl_xor_sync(FULL_MASK, sum, x), __shfl_xor_sync(FULL_MASK, weighted, x)};
-      join(o);
+      join(o, c);
     }
   }
 };
@@ -218,7 +221,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
   const uint4* xv = reinterpret_cast<const uint4*>(x + head * E::SIZE);
   const int per = (vectors + p.split - 1) / p.split, v0 = min(vectors, per * piece), v1 = min(vectors, v0 + per);
   float largest = -INF, of_group = -INF, least = -INF;         // the thread's so far, its group's; what elements have to reach
-  const uint64_t scale2 = pair_of(p.scale, p.scale);
+  const float c = p.scale_log2;
+  const uint64_t c2 = pair_of(c, c);
   // what the end needs, on its way from the start
   const int target = p.targets && warp == 0 ? p.targets[row] : -1;
   const float of_target = target >= 0 && target < p.vocab ? E::one(x, target) : 0.0f;
@@ -243,8 +247,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
   // single elements, of the first warp's lanes
   auto single_value = [&](int i, int end) { return i < end ? E::one(x, i) : -INF; };
   auto single_sums = [&](float y) {
-    const float at = sums.raise(__fmul_rn(y, p.scale));
-    sums.add(pair_of(y, -INF), scale2, pair_of(-at, -at));
+    const float at = sums.raise(y, c);
+    sums.add(pair_of(y, -INF), pair_of(-at, -at), c2);
   };
   auto single_key = [&](float y, int i, int end) { push(i < end && y >= least, [&](int) { return make_key(y, i); }); };
   const bool has_head = piece == 0 && warp == 0 && head, has_tail = piece == p.split - 1 && warp == 0 && tail;
@@ -282,14 +286,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
       group_max[(block >> shift) * THREADS + tid] = of_group;
       largest = max_nan(largest, all);
     }
-    const float at = sums.raise(__fmul_rn(all, p.scale));
+    const float at = sums.raise(all, c);
     const uint64_t minus2 = pair_of(-at, -at);
 #pragma unroll
     for (int j = 0; j < VECTORS; ++j)
 #pragma unroll
       for (int i = 0; i < E::PER / 2; ++i) {
         const float2 u = E::pair(v[j], i);
-        sums.add(pair_of(u.x, u.y), scale2, minus2);
+        sums.add(pair_of(u.x, u.y), minus2, c2);
       }
   }
 
@@ -298,7 +302,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
   split_pair(sums.s, &sa, &sb);
   split_pair(sums.w, &wa, &wb);
   Joined mine{sums.top, sa + sb, wa + wb};
-  mine.over_warp();
+  mine.over_warp(c);
   if (lane == 0) of_warp[warp] = mine;
   if (TOP) {
     maxima[tid] = largest == largest ? score_to_ord(largest) : 0u;
@@ -364,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
   }
   if (warp != 0) return;
   mine = lane < WARPS ? of_warp[lane] : Joined{-INF, 0.0f, 0.0f};
-  mine.over_warp();
+  mine.over_warp(c);
   if (p.split > 1) {
     ScorePartial* to = p.partials + row * p.split + piece;
     if (lane == 0) {
@@ -385,7 +389,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
     const ScorePartial* all = p.partials + row * p.split;
     mine = Joined{-INF, 0.0f, 0.0f};
     if (lane < p.split) mine = Joined{__ldcg(&all[lane].top), __ldcg(&all[lane].sum), __ldcg(&all[lane].weighted)};
-    mine.over_warp();
+    mine.over_warp(c);
     if (TOP) {
 #pragma unroll 8
       for (int i = 0; i < p.split; ++i)
@@ -396,10 +400,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) score_kernel(const ScoreParams 
     }
   }
   // the row's
-  const bool none = !(mine.top < INF), banned = mine.top == -INF;
+  const float y_top = __fmul_rn(mine.top, p.scale);
+  const bool none = !(y_top < INF), banned = y_top == -INF;
   const float log_sum = banned ? 0.0f : logf(mine.sum), top = banned ? 0.0f : mine.top, nan = __int_as_float(0x7fffffff);
-  auto log_prob = [&](float v) { return none ? nan : fmaf(v, p.scale, -top) - log_sum; };
-  if (lane == 0 && p.entropy) p.entropy[row] = none ? nan : banned ? 0.0f : log_sum - mine.weighted / mine.sum;
+  // (halves: the difference of two finite logits may leave fp32 where scale brings it back)
+  auto log_prob = [&](float v) { return none ? nan : fmaf(0.5f * v - 0.5f * top, p.scale, -0.5f * log_sum) * 2.0f; };
+  if (lane == 0 && p.entropy) p.entropy[row] = none ? nan : banned ? 0.0f : log_sum - LOG_OF_2 * (mine.weighted / mine.sum);
   if (lane == 0 && p.targets) {
     float r = 0.0f;
     if (target >= 0 && target < p.vocab) {

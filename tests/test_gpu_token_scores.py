@@ -300,3 +300,52 @@ def test_rows_of_many_blocks(rows, vocab, dtype, kind):
     assert torch.equal(again.top_ids[0], got.top_ids[-1])
     # (another division into pieces: the same sums in another order, each within the bound that check() holds)
     assert torch.allclose(again.entropy[0], got.entropy[-1], rtol=2.0 ** -10, atol=2.0 ** -10)
+
+
+@pytest.mark.parametrize("scale", [0.7, 0.9, 1 / 1.3, 1.1, 1.4])
+@pytest.mark.parametrize("mask", ["lowest", -1e30, -1e10])
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+def test_masked_rows_at_a_temperature(dtype, mask, scale):
+    """Rows masked with large finite numbers, all but a few tokens (row 0: all of them), where scale * x is not exact."""
+    vocab, rows = 9001, 5
+    mask = torch.finfo(dtype).min if mask == "lowest" else max(mask, torch.finfo(dtype).min)
+    x = torch.full((rows, vocab), mask, dtype=dtype, device=DEV)
+    for r in range(1, rows):
+        x[r, 37 * r::900] = draw(1, 10, dtype, r)[0]
+    finite = mask * scale > -torch.finfo(F32).max       # (otherwise y of a masked token is minus infinity in fp32)
+    check(x[1:], 10, scale, targets=torch.tensor([37 * r for r in range(1, rows)], dtype=torch.int32, device=DEV))
+    if finite:
+        check(x[1:], 20, scale)
+    s = ICTokenScores(vocab, dtype=dtype)
+    got = s.score(x, ints_of(rows, 8000), n_top=20, scale=scale)
+    s.sync()
+    assert torch.equal(got.top_ids[0], torch.arange(20, dtype=torch.int32, device=DEV))
+    if finite:
+        # every weight is 1 and the sum the exact vocab: what is left is the logarithm's error and a rounding, 2 units
+        want = math.log(vocab)
+        for value in (-got.log_probs[0], got.entropy[0], *-got.top_log_probs[0]):
+            assert abs(float(value) - want) <= 2.0 ** -22 * want
+    else:           # banned
+        assert got.log_probs[0] == -INF and got.entropy[0] == 0
+
+
+def ints_of(n, value):
+    return torch.full((n,), value, dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("rows", [2, 700])
+def test_logits_far_apart(rows):
+    """Differences beyond fp32's largest number, brought back by the scale, and the largest scale there is."""
+    x = draw(rows, 3001, F32, 6)
+    x[:, 5], x[:, 9], x[:, 11] = 3e38, -3e38, 2.9e38
+    s = ICTokenScores(3001, dtype=F32)
+    got = s.score(x, ints_of(rows, 9), scale=1e-36)
+    s.sync()
+    want = (-6e38 * 1e-36) - math.log(1 + math.exp(-10.0) + 0.0)          # (the others are e^-300 and less)
+    assert (got.log_probs.double() - want).abs().max() <= 2.0 ** -22 * abs(want)
+    with pytest.raises(ICCacheError):
+        s.score(x, scale=3e38)          # times log2(e) not finite
+    got = s.score(torch.tensor([0.0, -1e-30], device=DEV).repeat(rows, 1501)[:, :3001].contiguous(), ints_of(rows, 1), scale=1e30)
+    s.sync()
+    want = -1.0 - math.log(1501 + 1500 * math.exp(-1.0))
+    assert (got.log_probs.double() - want).abs().max() <= 2.0 ** -18 * abs(want)      # (seven additions a thread, and those of threads and warps)
