@@ -36,11 +36,11 @@ __device__ __forceinline__ bool state_check_attend(const StateAttendParams& p, u
   return state_check_seqs(p.v, p.seqs, p.n, seen) & __syncthreads_and(fine);
 }
 
-// Whether the call goes on: nothing was wrong before it, and its arguments hold.  Whole CTA.
+// Whether the call goes on: nothing was wrong before it, and its arguments hold.  Whole CTA; ends with a barrier.
+// (Another CTA of the launch may set the error while this one's threads look at it: they decide together, no thread leaves by itself.)
 __device__ __forceinline__ bool state_call_holds(const StateAttendParams& p, uint32_t* seen) {
-  if (*p.v.err != KV_OK) return false;
-  if (p.checked) return true;
-  if (state_check_attend(p, seen)) return true;
+  if (__syncthreads_or(*p.v.err != KV_OK)) return false;
+  if (p.checked || state_check_attend(p, seen)) return true;
   if (threadIdx.x == 0) state_report(p.v, KV_INVALID);
   return false;
 }

@@ -404,3 +404,25 @@ def test_around_the_change_of_kernels(each):
     run([each], heads=4, seed=50)
     run([each] * 3, heads=2, dk=72, dv=136, dtype=F16, seed=51)
     run([each] * 40, heads=16, dk=16, dv=16, seed=52)
+
+
+@pytest.mark.parametrize("bad", [0, 33, 100, 199])
+@pytest.mark.parametrize("each", [1, 30])
+def test_refused_calls_of_many_ctas(each, bad):
+    """Some CTAs begin when others have already reported the call: whole CTAs refuse it, wherever the bad number stands."""
+    n, heads = 200, 16
+    s = ICStates(1, heads, 16, 16, n, pool=draw(1, n, 1, heads, 16, 16, dtype=torch.float32))
+    q, before = draw(2, n * each, heads, 16), s.pool.clone()
+    seqs, starts = list(range(n)), starts_of([each] * n)
+    good = ints(seqs)
+    for number in (n, -1, (bad + 1) % n):
+        seqs[bad] = number
+        wrong = ints(seqs)
+        for _ in range(5):
+            out = torch.zeros_like(q)
+            s.extend(0, q, q, q, rates_of(heads), wrong, starts, out=out)
+            with pytest.raises(ICCacheError):
+                s.sync()
+            assert torch.equal(s.pool, before) and not out.any()
+    s.extend(0, q, q, q, rates_of(heads), good, starts)
+    s.sync()
