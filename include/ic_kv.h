@@ -185,7 +185,8 @@ int ic_kv_rotary_frequencies(const ic_kv_rotary_t* r, double* frequencies);
  * A token stands where it stands in its sequence (as for ic_kv_attend), or at positions[t] (any int32, also below 0);
  * where it is stored does not depend on positions.  Without k and v, and with positions, seqs may be NULL (n = 0).
  * inverse != 0 turns back: by minus the angle, still times the magnitude.
- * A bad sequence or start anywhere in the call means that nothing is turned or stored; a bad table entry is met when others are done.
+ * A bad sequence or start anywhere in the call means that nothing is turned or stored; where a table entry is bad, other tokens may have
+ * been turned and stored.
  */
 typedef struct ic_kv_rotate {
   uint32_t struct_size; /* sizeof(ic_kv_rotate_t) of the caller's build                      */

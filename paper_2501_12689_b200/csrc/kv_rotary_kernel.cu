@@ -188,18 +188,18 @@ __global__ void __launch_bounds__(THREADS) kv_rotate_kernel(const __grid_constan
   const int tid = threadIdx.x;
   const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
   if (p.seqs) {
-    if (*v.err != KV_OK) return;
-    bool fine = true;
+    // (other CTAs may report a bad table entry meanwhile: whether this one goes on is its threads' common decision)
+    bool fine = *v.err == KV_OK;
     if (CHECKED) {
       const int64_t t = t0 + tid;
-      if (tid < TOKENS && t < p.n_tokens) {
+      if (fine && tid < TOKENS && t < p.n_tokens) {
         const WriteSeq seq(v, p.seqs, p.starts, p.starts ? owner_of(p.starts, p.n, (int)t) : (int)t, p.n, p.n_tokens);
         row_of[tid] = seq.s;
         pos_of[tid] = (int)(seq.length - seq.end + t);
       }
     } else if (tid < p.n) {
       const WriteSeq seq(v, p.seqs, p.starts, tid, p.n, p.n_tokens);
-      fine = seq.fine;
+      fine &= seq.fine;
       if (fine)
         for (int64_t t = max(seq.begin, t0); t < min(seq.end, t0 + TOKENS); ++t) {
           row_of[t - t0] = seq.s;

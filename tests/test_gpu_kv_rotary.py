@@ -400,3 +400,42 @@ def test_a_copied_example_behind_another_one():
     a, b = (kv.pool[kv.tables[s, at // 16].long(), 1, 0, :, at % 16].double() for s in (0, 1))
     assert (a - b).abs().max() <= 3 * 2.0 ** -8 * b.abs().max()
     assert (out[0].float() - out[1].float()).abs().max() < 0.06
+
+
+@pytest.mark.parametrize("n", [40, 300])
+def test_bad_pages_among_many_tokens(n):
+    """Entries that name no page all over the call: CTAs report them while others begin.  A token is stored and turned as a whole or not at all, and
+    nothing else is touched."""
+    counts = [50] * n
+    f = rotary_frequencies(64)
+    q, k, v = draw(1, 50 * n, 4, 64), draw(2, 50 * n, 2, 64), draw(3, 50 * n, 2, 64)
+    at = torch.arange(50, device=DEV).repeat(n)
+    want_q, size_q = turned(q, at, f, 64, False)
+    want_k, size_k = turned(k, at, f, 64, False)
+    for seed in range(5):
+        kv = make([0] * n, counts)
+        kv.set_rotary()
+        rng = random.Random(seed)
+        i = torch.repeat_interleave(torch.arange(n), 50).to(DEV)
+        page = kv.tables[i, at // 16].long()
+        bad = torch.zeros(n, 4, dtype=torch.bool, device=DEV)
+        for s in rng.sample(range(n), n // 8):
+            col = rng.randrange(4)
+            bad[s, col] = True
+            kv.tables[s, col] = rng.choice([-1, 10 ** 6, 2 ** 31 - 1])
+        before, out = kv.pool.clone(), torch.zeros_like(q)
+        kv.write_rotated(1, q, k, v, ints(list(range(n))), starts_of(counts), out=out)
+        with pytest.raises(ICCacheError):
+            kv.sync()
+        slot = at % 16
+        stored = ~kv.pool[page, 1, 0, :, slot].isnan().flatten(1).any(1)
+        assert not (stored & bad[i, at // 16]).any()
+        close(kv.pool[page, 1, 0, :, slot][stored], want_k[stored], size_k[stored])
+        assert torch.equal(kv.pool[page, 1, 1, :, slot][stored], v[stored])
+        done = (out != 0).flatten(1).any(1)
+        assert not (stored & ~done).any()
+        close(out[done], want_q[done], size_q[done])
+        rest = torch.ones_like(before, dtype=torch.bool)
+        rest[page[stored], 1, :, :, slot[stored]] = False
+        raw = lambda x: x.view(torch.int16)  # noqa: E731
+        assert torch.equal(raw(kv.pool)[rest], raw(before)[rest])
