@@ -141,24 +141,25 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, 
   __shared__ int row_of[TOKENS], pos_of[TOKENS];
   grid_dep_launch_dependents();
   grid_dep_wait();
-  if (*v.err != KV_OK) return;
+  // (other CTAs may report a bad table entry meanwhile: whether this one goes on is its threads' common decision)
+  bool fine = *v.err == KV_OK;
   const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
   if (CHECKED) {
     const int64_t t = t0 + threadIdx.x;
     if (threadIdx.x < TOKENS) {
       unsigned char* at = nullptr;
-      if (t < n_tokens) {
+      if (fine && t < n_tokens) {
         const WriteSeq seq(v, seqs, starts, starts ? owner_of(starts, n, (int)t) : (int)t, n, n_tokens);
         at = token_place(v, layer, seq.s, (int)(seq.length - seq.end + t));
       }
       place[threadIdx.x] = at;
     }
+    __syncthreads();                      // (a token whose place is null is left out: nothing else has to be agreed on)
   } else {
-    bool fine = true;
     const int i = threadIdx.x;
     if (i < n) {
       const WriteSeq seq(v, seqs, starts, i, n, n_tokens);
-      fine = seq.fine;
+      fine &= seq.fine;
       if (fine)
         for (int64_t t = max(seq.begin, t0); t < min(seq.end, t0 + TOKENS); ++t) {
           const int pos = (int)(seq.length - seq.end + t);
@@ -174,9 +175,11 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_write_kernel(const KvView v, 
       if (threadIdx.x == 0) kv_report(v, KV_INVALID);
       return;
     }
-    if (TOKENS > 1 && i < TOKENS) place[i] = t0 + i < n_tokens ? token_place(v, layer, row_of[i], pos_of[i]) : nullptr;
+    if (TOKENS > 1) {
+      if (i < TOKENS) place[i] = t0 + i < n_tokens ? token_place(v, layer, row_of[i], pos_of[i]) : nullptr;
+      __syncthreads();
+    }
   }
-  if (CHECKED || TOKENS > 1) __syncthreads();
   // a thread takes one place in the tokens (keys or values, head, piece) at a time and all TOKENS tokens there: their
   // loads are under way together
   const int pieces = v.head_dim >> 3, per_token = v.n_kv_heads * pieces;

@@ -501,3 +501,35 @@ def test_extend_in_a_graph():
         want, size = attention(kv, 1, q, [0, 1, 2], [9, 9, 9])
         close(out, want, size)
     kv.sync()
+
+
+@pytest.mark.parametrize("n", [40, 300])                 # (looked over by the kernel itself, and by one before it)
+@pytest.mark.parametrize("each", [1, 50])                # (a token a CTA, and eight)
+def test_writes_that_meet_many_bad_pages(n, each):
+    """Entries that name no page all over the call: CTAs report them while others begin.  A token is stored as a whole or not at all, and nothing
+    else is touched."""
+    from paper_2501_12689_b200 import IC_ERR_INVALID, ICPagedKV
+    t, page = n * each, 16
+    k, v = (torch.randn(t, 2, 64, device=DEV, generator=torch.Generator(device=DEV).manual_seed(i)).to(BF16) for i in (1, 2))
+    i = torch.arange(n, device=DEV).repeat_interleave(each)
+    at = torch.arange(each, device=DEV).repeat(n)
+    for seed in range(5):
+        g = torch.Generator().manual_seed(seed)
+        pool = torch.full((4 * n, 1, 2, 2, page, 64), float("nan"), dtype=BF16, device=DEV)
+        kv = ICPagedKV(4 * n, 1, 2, page, 64, n, 4, pool=pool)
+        kv.reserve(ints(list(range(n))), ints([each] * n))
+        kv.sync()
+        where = kv.tables[i, at // page].long()
+        wrong = torch.randperm(n, generator=g)[:n // 8].to(DEV)
+        col = torch.randint(0, -(-each // page), (len(wrong),), generator=g).to(DEV)
+        bad = torch.zeros(n, 4, dtype=torch.bool, device=DEV)
+        bad[wrong, col] = True
+        kv.tables[wrong, col] = torch.tensor([-1, 10 ** 6, 2 ** 31 - 1], dtype=torch.int32, device=DEV)[col % 3]
+        kv.write(0, k, v, ints(list(range(n))), starts_of([each] * n))
+        assert reported(kv) == IC_ERR_INVALID
+        slot = at % page
+        stored = ~pool[where, 0, :, :, slot].isnan().flatten(1).any(1)
+        assert not (stored & bad[i, at // page]).any()
+        assert torch.equal(pool[where, 0, 0, :, slot][stored], k[stored]) and torch.equal(pool[where, 0, 1, :, slot][stored], v[stored])
+        pool[where[stored], 0, :, :, slot[stored]] = float("nan")
+        assert pool.isnan().all()
