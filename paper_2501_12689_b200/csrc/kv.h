@@ -23,7 +23,8 @@ struct KvView {
   // scratch of the page operations
   int* err;                 // first error since the last ic_kv_sync
   int* host_status;         // mapped host word, the same
-  int* meta;                // [0] 1 = the plan of this call holds, [1] pages to copy, [2] live pages
+  int* meta;                // [0] 1 = the plan of this call holds, [1] pages to copy, [2] live pages;
+                            // zero between calls: [3] free: something was bad, [4] its CTAs that have finished
   int* had;                 // [max_seqs] fork: a child's tokens before the call
   int* upto;                // [max_seqs] fork: its tokens after the call; -1 = nothing to do
   int* shared;              // [max_seqs] fork: leading pages shared with the parent

@@ -368,25 +368,38 @@ __global__ void __launch_bounds__(COPY_THREADS) kv_fork_apply_kernel(const KvVie
 }
 
 // ---------------------------------------------------------------- free
-// A CTA per sequence.  Whoever takes the length away owns the release, so a number that comes twice counts once.
+// A CTA per sequence.  Whoever takes the length away owns the release, so a number that comes twice counts once.  What is bad is passed over and
+// the rest done, so it is reported by the CTA that finishes last: an error that stood while others begin would stop them.
 __global__ void __launch_bounds__(COPY_THREADS) kv_free_kernel(const KvView v, const int* __restrict__ seqs, int n) {
-  __shared__ int had;
+  __shared__ int had, bad;
   grid_dep_launch_dependents();
   grid_dep_wait();
   if (*v.err != KV_OK) return;
+  if (threadIdx.x == 0) bad = 0;
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const int s = seqs[i];
     if (threadIdx.x == 0) {
       had = 0;
-      if (s < 0 || s >= v.max_seqs || !length_fits(v, v.lengths[s])) kv_report(v, KV_INVALID);
+      if (s < 0 || s >= v.max_seqs || !length_fits(v, v.lengths[s])) bad = 1;
       else had = atomicExch(&v.lengths[s], 0);
     }
     __syncthreads();
     const int pages = kv_pages_of(had, v.page_shift);
     const int* row = v.tables + (size_t)s * v.max_pages;
-    for (int c = threadIdx.x; c < pages; c += COPY_THREADS)
-      if (page_exists(v, row[c])) atomicSub(&v.refs[row[c]], 1);
+    for (int c = threadIdx.x; c < pages; c += COPY_THREADS) {
+      const int page = row[c];
+      if ((unsigned)page < (unsigned)v.n_pages) atomicSub(&v.refs[page], 1);
+      else bad = 1;
+    }
     __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    if (bad) atomicExch(&v.meta[3], 1);
+    __threadfence();
+    if (atomicAdd(&v.meta[4], 1) == (int)gridDim.x - 1) {
+      v.meta[4] = 0;
+      if (atomicExch(&v.meta[3], 0) != 0) kv_report(v, KV_INVALID);
+    }
   }
 }
 

@@ -533,3 +533,35 @@ def test_writes_that_meet_many_bad_pages(n, each):
         assert torch.equal(pool[where, 0, 0, :, slot][stored], k[stored]) and torch.equal(pool[where, 0, 1, :, slot][stored], v[stored])
         pool[where[stored], 0, :, :, slot[stored]] = float("nan")
         assert pool.isnan().all()
+
+
+@pytest.mark.parametrize("n", [3, 1000, 6000])           # (a CTA a sequence, and several sequences to a CTA)
+@pytest.mark.parametrize("kind", ["number", "length", "entry"])
+def test_a_bad_number_does_not_keep_the_others(n, kind):
+    """What is bad comes first: the CTAs that begin after it has been met free their sequences all the same."""
+    from paper_2501_12689_b200 import IC_ERR_INVALID, ICPagedKV
+    for _ in range(3):
+        kv = ICPagedKV(2 * n, 1, 1, 8, 8, n, 2)
+        kv.reserve(ints(list(range(n))), ints([9] * n))
+        kv.sync()
+        order = list(range(n))
+        if kind == "number":
+            order = [n, -1, 2 ** 31 - 1] + order
+        elif kind == "length":
+            kv.lengths[0] = 17
+        else:
+            kv.tables[0, 1] = 2 * n
+        kv.free(ints(order[:n]))
+        assert reported(kv) == IC_ERR_INVALID
+        freed = set(order[:n])
+        want = torch.tensor([0 if s in freed else 9 for s in range(n)], dtype=torch.int32, device=DEV)
+        if kind == "length":
+            want[0] = 17
+        assert torch.equal(kv.lengths, want)
+        held = {s for s in range(n) if s not in freed}
+        left = 2 * len(held) + (2 if kind == "length" else 1 if kind == "entry" else 0)
+        assert int(kv.refs.sum()) == left and int(kv.refs.min()) >= 0
+        if kind == "number":
+            kv.free(ints(order[n:]))                     # nothing is left behind in the scratch
+            kv.sync()
+            assert not kv.refs.any()
