@@ -15,7 +15,7 @@ struct StateView {
   int n_layers, n_heads, key_dim, value_dim, max_seqs;
   int* err;                 // first error since the last ic_state_sync (codes as in kv.h)
   int* host_status;         // mapped host word, the same
-  int* meta;                // [0] 1 = the arguments of this call hold
+  int* meta;                // [0] 1 = the arguments of this call hold; zero between calls: [1] clear: a number was bad, [2] its CTAs that have finished
   __host__ __device__ size_t head_floats() const { return (size_t)key_dim * value_dim; }
   __host__ __device__ size_t seq_floats() const { return head_floats() * n_layers * n_heads; }
 };

@@ -168,20 +168,32 @@ __global__ void __launch_bounds__(THREADS) state_fork_kernel(const StateView v, 
   }
 }
 
+// A bad number is passed over and the others cleared, so it is reported by the CTA that finishes last: an error that stood while others begin would
+// stop them.
 __global__ void __launch_bounds__(THREADS) state_clear_kernel(const StateView v, const int* __restrict__ seqs, int n) {
   grid_dep_launch_dependents();
   grid_dep_wait();
   if (*v.err != KV_OK) return;
   const size_t vectors = v.seq_floats() / 4;
   uint4* pool = reinterpret_cast<uint4*>(v.pool);
+  bool bad = false;
   for (int i = blockIdx.y; i < n; i += gridDim.y) {
     const int s = seqs[i];
     if (s < 0 || s >= v.max_seqs) {
-      if (threadIdx.x == 0 && blockIdx.x == 0) state_report(v, KV_INVALID);
+      bad = true;
       continue;
     }
     for (size_t c = (size_t)blockIdx.x * THREADS + threadIdx.x; c < vectors; c += (size_t)gridDim.x * THREADS)
       pool[s * vectors + c] = make_uint4(0, 0, 0, 0);
+  }
+  __syncthreads();                         // all threads have looked at the error
+  if (threadIdx.x == 0) {
+    if (bad) atomicExch(&v.meta[1], 1);
+    __threadfence();
+    if (atomicAdd(&v.meta[2], 1) == (int)(gridDim.x * gridDim.y) - 1) {
+      v.meta[2] = 0;
+      if (atomicExch(&v.meta[1], 0) != 0) state_report(v, KV_INVALID);
+    }
   }
 }
 

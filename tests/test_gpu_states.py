@@ -426,3 +426,19 @@ def test_refused_calls_of_many_ctas(each, bad):
             assert torch.equal(s.pool, before) and not out.any()
     s.extend(0, q, q, q, rates_of(heads), good, starts)
     s.sync()
+
+
+@pytest.mark.parametrize("n,heads,dk", [(3, 1, 8), (2000, 32, 64), (8192, 1, 8)])
+def test_a_bad_number_does_not_keep_the_others(n, heads, dk):
+    """Bad numbers come first: the CTAs that begin after they have been met clear their sequences all the same."""
+    s = ICStates(1, heads, dk, 16, n)
+    for _ in range(3):
+        s.pool.fill_(1.0)
+        s.clear(ints([n, -1, 2 ** 31 - 1] + list(range(1, n))))
+        with pytest.raises(ICCacheError) as e:
+            s.sync()
+        assert e.value.status == IC_ERR_INVALID
+        assert not s.pool[1:].any() and (s.pool[0] == 1).all()
+    s.clear(ints([0]))
+    s.sync()
+    assert not s.pool.any()
