@@ -48,23 +48,15 @@ template <int KIND>
 __device__ __forceinline__ int table_at(int i, int turned) {
   return KIND == HALVES ? ((i >> 2) & 1) * turned * 4 + (i >> 3) * 4 + (i & 3) : i;
 }
-// Sine and cosine of pair i at position pos, times the magnitude; beyond the last pair nothing turns.
+// Sine and cosine of pair i at position pos, times the magnitude.
 template <int KIND>
 __device__ __forceinline__ void make_entry(const KvRotary& r, int i, long long pos, float magnitude, int turned, float* cosv, float* sinv) {
-  float c = 1.0f, s = 0.0f;
-  if (i < r.dim / 2) {
-    const int turn = (int)(((unsigned long long)pos * r.turn[i]) >> 32);      // 2^-31 half turns
-    sincospif((float)turn * 4.656612873077393e-10f, &s, &c);
-    c *= magnitude;
-    s *= magnitude;
-  }
+  float c, s;
+  const int turn = (int)(((unsigned long long)pos * r.turn[i]) >> 32);        // 2^-31 half turns
+  sincospif((float)turn * 4.656612873077393e-10f, &s, &c);
   const int at = table_at<KIND>(i, turned);
-  cosv[at] = c;
-  sinv[at] = s;
-}
-template <int KIND>
-__device__ __forceinline__ int table_entries(const KvRotary& r, int turned) {
-  return KIND == HALVES ? turned * 8 : KIND == NEIGHBOURS ? turned * 4 : r.dim / 2;
+  cosv[at] = c * magnitude;
+  sinv[at] = s * magnitude;
 }
 
 // Streaming loads and stores of rows that may be turned in place (so not through the read-only path).
@@ -95,7 +87,7 @@ struct Piece {
     if (KIND == HALVES && place < turned) *reinterpret_cast<uint4*>(row + 2 * (8 * place + dim / 2)) = b;
   }
   // Computed in fp32 and rounded once.
-  __device__ __forceinline__ void turn(int place, int turned, const float* cosv, const float* sinv) {
+  __device__ __forceinline__ void turn(int place, int turned, int dim, const float* cosv, const float* sinv) {
     if (KIND == HALVES) {
       uint32_t* x = &a.x;
       uint32_t* y = &b.x;
@@ -116,6 +108,7 @@ struct Piece {
       uint32_t* x = &a.x;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
+        if (8 * place + 2 * j >= dim) break;          // what does not turn is not touched (an infinity times a sine of 0 is a NaN)
         const float2 u = unpack2<F16>(x[j]);
         x[j] = pack2<F16>(u.x * cs[j] - u.y * sn[j], u.x * sn[j] + u.y * cs[j]);
       }
@@ -150,7 +143,8 @@ struct Piece {
       }
       uint32_t* y = &a.x;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = pack2<F16>(out[2 * j], out[2 * j + 1]);
+      for (int j = 0; j < 4; ++j)
+        if (8 * place + 2 * j < dim) y[j] = pack2<F16>(out[2 * j], out[2 * j + 1]);
     }
   }
 };
@@ -213,7 +207,7 @@ __global__ void __launch_bounds__(THREADS) kv_rotate_kernel(const __grid_constan
     if (p.k && tid < TOKENS) place_of[tid] = t0 + tid < p.n_tokens ? token_place(v, p.layer, row_of[tid], pos_of[tid]) : nullptr;
   }
   const Places at(KIND, v.head_dim, p.r.dim);
-  const int entries = table_entries<KIND>(p.r, at.turned);
+  const int entries = p.r.dim / 2;
   for (int u = tid; u < TOKENS * entries; u += blockDim.x) {
     const int x = u / entries;
     if (t0 + x < p.n_tokens) {
@@ -252,7 +246,7 @@ __global__ void __launch_bounds__(THREADS) kv_rotate_kernel(const __grid_constan
     for (int x = 0; x < TOKENS; ++x) {
       const bool turns = to[x] && (query || key) && place < at.turned;
       if (KIND == ODD_HALVES) w[x].turn_staged(place, at.per_row, p.r.dim, stage + (tid & ~31), tid & 31, turns, cosv[x], sinv[x]);
-      else if (turns) w[x].turn(place, at.turned, cosv[x], sinv[x]);
+      else if (turns) w[x].turn(place, at.turned, p.r.dim, cosv[x], sinv[x]);
       if (to[x]) w[x].store(to[x], place, at.turned, p.r.dim);
     }
   }
@@ -345,7 +339,7 @@ __global__ void __launch_bounds__(THREADS) kv_shift_kernel(const KvView v, const
   if (v.meta[0] == 0 || *v.err != KV_OK) return;
   const int tid = threadIdx.x;
   const Places at(KIND, v.head_dim, rot.dim);
-  const int table = table_entries<KIND>(rot, at.turned), groups = (v.n_layers + layers - 1) / layers;
+  const int table = rot.dim / 2, groups = (v.n_layers + layers - 1) / layers;
   const int of_layer = v.n_kv_heads << v.page_shift, slots = (1 << v.page_shift) - 1;
   int place;
   const int mine = my_row<KIND>(at, &place), step = at.rows(KIND, THREADS);
@@ -395,7 +389,7 @@ __global__ void __launch_bounds__(THREADS) kv_shift_kernel(const KvView v, const
 #pragma unroll
       for (int x = 0; x < ROWS_AT_ONCE; ++x) {
         if (KIND == ODD_HALVES) w[x].turn_staged(place, at.per_row, rot.dim, stage + (tid & ~31), tid & 31, to[x] != nullptr, cosv, sinv);
-        else if (to[x]) w[x].turn(place, at.turned, cosv, sinv);
+        else if (to[x]) w[x].turn(place, at.turned, rot.dim, cosv, sinv);
         if (to[x]) w[x].store(to[x], place, at.turned, rot.dim);
       }
     }

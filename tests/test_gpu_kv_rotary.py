@@ -439,3 +439,43 @@ def test_bad_pages_among_many_tokens(n):
         rest[page[stored], 1, :, :, slot[stored]] = False
         raw = lambda x: x.view(torch.int16)  # noqa: E731
         assert torch.equal(raw(kv.pool)[rest], raw(before)[rest])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("d,dim,interleaved", SHAPES + [(16, 6, True), (16, 10, False), (256, 250, True), (40, 2, True)])
+@pytest.mark.parametrize("what", [float("inf"), float("nan"), -0.0])
+def test_elements_that_do_not_turn_are_left_as_they_are(d, dim, interleaved, dtype, what):
+    """Bit for bit, next to infinities, NaN and zeros of either sign; and what turns does not meet them."""
+    had, counts = [0, 17], [1, 40]
+    for single in (False, True):
+        kv = make(had, [1, 1] if single else counts, d=d, dtype=dtype)
+        kv.set_rotary(dim, interleaved=interleaved)
+        t = 2 if single else 41
+        q, k, v = (draw(i, t, h, d, dtype=dtype) for i, h in enumerate((4, 2, 2)))
+        for x in (q, k, v):
+            x[..., dim::2] = what
+            x[..., dim + 1::4] = 0.0
+        raw = lambda x: x.contiguous().view(torch.int16)  # noqa: E731
+        at = torch.tensor([0, 17] if single else [0] + list(range(17, 57)), device=DEV)
+        seqs = ints([0, 1])
+        got = kv.write_rotated(1, q, k, v, seqs, None if single else starts_of(counts))
+        inplace = q.clone()
+        kv.rotate(inplace, at.int(), out=inplace)
+        kv.sync()
+        i = ints([0, 1] if single else [0] + [1] * 40).long()
+        page, slot = kv.tables[i, at // 16].long(), at % 16
+        f = rotary_frequencies(dim)
+        stored = kv.pool[page, 1, 0, :, slot]
+        for now, was in ((got, q), (inplace, q), (stored, k)):
+            assert torch.equal(raw(now[..., dim:]), raw(was[..., dim:]))
+            want, size = turned(was[..., :dim], at, f, dim, interleaved)
+            close(now[..., :dim], want, size)
+        assert torch.equal(raw(kv.pool[page, 1, 1, :, slot]), raw(v))
+        # the cached keys moved
+        kv.pool.nan_to_num_(nan=1.0) if what == what else None
+        before = kv.pool.clone()
+        kv.shift(seqs, ints([5, -3]))
+        kv.sync()
+        assert torch.equal(raw(kv.pool[..., dim:]), raw(before[..., dim:])) and torch.equal(raw(kv.pool[:, :, 1]), raw(before[:, :, 1]))
+        want, size = turned(before[page, 1, 0, :, slot][..., :dim], torch.where(i == 0, 5, -3), f, dim, interleaved)
+        close(kv.pool[page, 1, 0, :, slot][..., :dim], want, size)
