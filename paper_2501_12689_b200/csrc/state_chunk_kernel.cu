@@ -112,14 +112,14 @@ struct Ring {
   }
 };
 
-// A wait of a whole warp, in few instructions (the roles' code together has to stay in the instruction cache): up to WAIT_TRIES looks at the
-// barrier, of 20 cycles or more each, so that it ends after a second or some.
-constexpr int WAIT_TRIES = 1 << 26;
+// A wait of a whole warp, in few instructions (the roles' code together has to stay in the instruction cache).  It ends after WAIT_LIMIT_CYCLES, about a
+// second, which 32 bits of the clock count.
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+  const uint32_t t0 = (uint32_t)clock();
 #pragma unroll 1
-  for (int i = 0; i < WAIT_TRIES; ++i) {
+  for (;;) {
     if (__all_sync(FULL_MASK, mbar_try_wait(bar, parity))) return true;
-    if (__any_sync(FULL_MASK, *abort_flag != 0)) return false;
+    if (__any_sync(FULL_MASK, *abort_flag != 0 || (uint32_t)clock() - t0 > (uint32_t)WAIT_LIMIT_CYCLES)) break;
   }
   *abort_flag = 1;
   return false;

@@ -442,3 +442,23 @@ def test_a_bad_number_does_not_keep_the_others(n, heads, dk):
     s.clear(ints([0]))
     s.sync()
     assert not s.pool.any()
+
+
+@pytest.mark.parametrize("counts,heads,dv", [([9000], 2, 64), ([3, 5000], 1, 128)])
+def test_a_wait_that_runs_out_is_reported(counts, heads, dv):
+    """A published state that nobody is told of (its word in the workspace is set to a number that it never leaves): the CTAs that wait for it give up after
+    a second, the call is reported, and the handle goes on."""
+    from paper_2501_12689_b200 import IC_ERR_TIMEOUT, ic_state_workspace_bytes
+    n, t, words = len(counts), sum(counts), 64
+    workspace = torch.empty(ic_state_workspace_bytes(1, heads, 64, dv, n), dtype=torch.uint8, device=DEV)
+    s = ICStates(1, heads, 64, dv, n, workspace=workspace)
+    s.sync()
+    q, k, v, rates = draw(1, t, heads, 64), draw(2, t, heads, 64), draw(3, t, heads, dv), rates_of(heads)
+    workspace.view(torch.int32)[words] = 1000          # of the first CTA
+    s.extend(0, q, k, v, rates, ints(list(range(n))), starts_of(counts))
+    with pytest.raises(ICCacheError) as e:
+        s.sync()
+    assert e.value.status == IC_ERR_TIMEOUT
+    s.sync()
+    s.clear(ints(list(range(n))))
+    run(counts, heads=heads, dk=64, dv=dv, layers=1, layer=0, states=s)
