@@ -33,7 +33,6 @@ struct StateAttendParams {
   const int* seqs;
   const int* starts;        // null: one token per sequence
   int n, layer, checked;    // checked: a kernel before has looked over the arguments
-  int first_seq;            // of the call, where this launch's sequences begin (starts null: their first token)
   int64_t n_tokens;
   float scale;
   // calls of many tokens: value slices of a head; states that CTAs publish for one another, and how much of each is there

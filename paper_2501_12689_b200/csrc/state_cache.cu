@@ -246,7 +246,6 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
   p.scale = a.scale;
   DeviceGuard guard(s->device);
   if (p.checked && (rc = launched(s, icc::state_check_launch(p, s->stream), 1, "check")) != IC_OK) return rc;
-  p.first_seq = 0;
   p.slices = (s->v.value_dim + 127) / 128;
   p.flags = reinterpret_cast<unsigned*>(reinterpret_cast<unsigned char*>(s->v.err) + FLAGS);
   p.slots = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS);
@@ -260,9 +259,8 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
   maps.there = encode_rows(s, p.q, s->v.key_dim, a.n_tokens, &maps.q) && encode_rows(s, p.k, s->v.key_dim, a.n_tokens, &maps.k) &&
                encode_rows(s, p.val, s->v.value_dim, a.n_tokens, &maps.val);
   for (int off = 0; off < a.n && rc == IC_OK; off += icc::STATE_BATCH) {
-    p.first_seq = off;
     p.seqs = a.seqs + off;
-    p.starts = a.starts ? a.starts + off : nullptr;
+    p.starts = a.starts + off;      // (without starts there is a token a sequence)
     p.n = a.n - off < icc::STATE_BATCH ? a.n - off : icc::STATE_BATCH;
     const int items = s->v.n_heads * ((s->v.value_dim + 127) / 128), most = icc::state_items(a.n_tokens, p.n);
     for (p.first_item = 0; p.first_item < items && rc == IC_OK; p.first_item += most) {

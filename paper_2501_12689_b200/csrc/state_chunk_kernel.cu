@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     int sum = 0, longest = 0;
     for (int i0 = 0; i0 < p.n; i0 += 32) {
       const int i = i0 + lane;
-      const int from = i <= p.n ? (p.starts ? p.starts[i] : p.first_seq + i) : 0, to = i < p.n ? (p.starts ? p.starts[i + 1] : from + 1) : from;
+      const int from = i <= p.n ? p.starts[i] : 0, to = i < p.n ? p.starts[i + 1] : from;
       if (i < p.n) t->starts[i] = from;
       if (i == p.n - 1) t->starts[p.n] = to;
       const int mine = (int)(((unsigned)(to - from) + C - 1) / C);

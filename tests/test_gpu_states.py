@@ -462,3 +462,50 @@ def test_a_wait_that_runs_out_is_reported(counts, heads, dv):
     s.sync()
     s.clear(ints(list(range(n))))
     run(counts, heads=heads, dk=64, dv=dv, layers=1, layer=0, states=s)
+
+
+@pytest.mark.parametrize("each", [6, 7, 8, 11, 12, 13])
+def test_where_the_kernels_change(each):
+    """7 | 8 tokens a sequence where there are many states, 12 | 13 where there are few."""
+    run([each], heads=4, seed=60)
+    run([each] * 3, heads=2, dk=72, dv=136, dtype=F16, seed=61)
+    run([each] * 60, heads=4, dk=16, dv=16, seed=62)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("shared", ["q", "k", "v", "qkv"])
+@pytest.mark.parametrize("counts,dk,dv", [([70, 3, 0, 200], 64, 64), ([1000, 130], 72, 136), ([3000], 128, 128)])
+def test_rows_shared_among_the_tokens(counts, dk, dv, shared, dtype):
+    """A stride of 0 between tokens, which no tensor map has: the rows come in 16-byte copies.  Whole items and cut ones, last chunks that are not full."""
+    t, heads, n = sum(counts), 2, len(counts)
+    s = ICStates(1, heads, dk, dv, n, dtype=dtype, pool=draw(9, n, 1, heads, dk, dv, dtype=torch.float32))
+    rates = torch.tensor([0.5, 0.01], device=DEV)
+    before = s.pool.clone()
+    x = {name: draw(i, 1 if name in shared else t, heads, d, dtype=dtype).expand(t, heads, d) for i, (name, d) in enumerate((("q", dk), ("k", dk), ("v", dv)))}
+    got = s.extend(0, x["q"], x["k"], x["v"], rates, ints(list(range(n))), starts_of(counts))
+    s.sync()
+    a = 0
+    for i, c in enumerate(counts):
+        part = slice(a, a + c)
+        close(got[part], s.pool[i, 0], formula(*(x[name][part] for name in "qkv"), rates, before[i, 0], 1 / math.sqrt(dk)), c, True) if c else None
+        a += c
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_what_lies_behind_a_short_chunk_is_not_read(dtype):
+    """The rows behind a sequence's last token belong to another one, whose infinities and NaN stay its own; by tensor maps and by copies."""
+    for shared in (False, True):
+        counts = [70, 5, 100]
+        t, heads = sum(counts), 2
+        s = ICStates(1, heads, 64, 64, 3, dtype=dtype)
+        q, k, v = (draw(i, t, heads, 64, dtype=dtype) for i in range(3))
+        if shared:
+            q = q[:1].expand(t, heads, 64)
+        else:
+            q[70:75] = math.nan
+        k[70:75], v[70:75] = math.inf, math.nan
+        got = s.extend(0, q, k, v, rates_of(heads), ints([0, 1, 2]), starts_of(counts))
+        s.sync()
+        for i, part in ((0, slice(0, 70)), (2, slice(75, 175))):
+            close(got[part], s.pool[i, 0], formula(q[part], k[part], v[part], rates_of(heads), torch.zeros(heads, 64, 64, device=DEV), 0.125), part.stop - part.start, True)
+        assert not got[70:75].isfinite().all()
