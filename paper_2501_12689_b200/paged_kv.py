@@ -328,6 +328,8 @@ class ICPagedKV:
 
     def _rotate(self, layer, q, k, v, seqs, starts, positions, out, inverse):
         a = self._r
+        if q is None and out is not None:
+            raise ValueError("out is for the turned queries: there is no q")
         tokens = (q if q is not None else k).shape[0]
         n = 0
         if seqs is not None:

@@ -61,3 +61,13 @@ def test_refused_arguments():
     assert lib.ic_kv_rotary_frequencies(ctypes.byref(r), None) == pkg.IC_ERR_INVALID
     r.struct_size = 1000
     assert lib.ic_kv_rotary_frequencies(ctypes.byref(r), (ctypes.c_double * 32)()) == pkg.IC_ERR_INVALID
+
+
+def test_a_result_without_queries_is_refused():
+    """Before anything is stored."""
+    import torch
+    kv = object.__new__(pkg.ICPagedKV)
+    kv._r, kv._h = paged_kv.ic_kv_rotate_t(), None
+    rows, one = torch.zeros(1, 2, 64, dtype=torch.bfloat16), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="there is no q"):
+        kv.write_rotated(0, None, rows, rows, one, out=rows)
