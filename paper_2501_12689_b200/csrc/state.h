@@ -33,6 +33,10 @@ struct StateAttendParams {
   const int* seqs;
   const int* starts;        // null: one token per sequence
   int n, layer, checked;    // checked: a kernel before has looked over the arguments
+  const int* ends;          // in chunks: where each sequence's tokens end
+  int most, least;          // token by token: sequences of up to `most` tokens; in chunks: of more than `least`
+  int n_long;               // sequences for the chunks, at most; 0 = none
+  int* long_ones;           // [3, max_seqs] their numbers, starts and ends, in their order, and empty ones up to n_long: made by the check ahead of a call
   int64_t n_tokens;
   float scale;
   // calls of many tokens: value slices of a head; states that CTAs publish for one another, and how much of each is there

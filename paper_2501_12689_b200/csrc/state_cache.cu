@@ -63,8 +63,16 @@ int read_opts(const ic_state_opts_t* opts, ic_state_opts_t* o) {
   return IC_OK;
 }
 
+// The mean says little of the longest, and one token after the other takes as long as the longest sequence has tokens.  So in calls of more than DIVIDED_FROM
+// tokens that go token by token, sequences of more than STEP_MOST are left to a launch of the chunks behind it.  As a rule that finds none and costs 1.3
+// to 3 us (64 sequences of 2 tokens, 32 heads of 128 x 128: 65 us, without it 63; 17 of 4, 4 heads of 64 x 64: 6.8 and 5.5); with 255 single tokens and
+// one sequence of 1,500 it takes 281 us, token by token 2,296; 31 and one of 352, 4 heads of 64 x 64: 23 and 192.  Where the two meet: 31 single tokens and one
+// sequence of 24, 32, 64 on those 4 heads 16, 21, 38 us token by token, the last divided 14; 255 and one of 33, 64, 128 on 32 heads 227, 273, 365 and 244 to 246.
+constexpr int STEP_MOST = 32, DIVIDED_FROM = 64;
+size_t list_bytes(int max_seqs) { return ((size_t)max_seqs * 3 * 4 + 255) & ~(size_t)255; }
+
 size_t workspace_need(const ic_state_opts_t& o) {
-  return WORDS + icc::KV_MAX_CTAS * icc::state_slot_floats(o.key_dim, o.value_dim) * 4;
+  return WORDS + list_bytes(o.max_seqs) + icc::KV_MAX_CTAS * icc::state_slot_floats(o.key_dim, o.value_dim) * 4;
 }
 
 int reported(int code) {
@@ -244,24 +252,44 @@ int ic_state_attend(ic_state_t* s, const ic_state_attend_t* args) {
   p.checked = a.n > icc::STATE_CHECK_THREADS;
   p.n_tokens = a.n_tokens;
   p.scale = a.scale;
-  DeviceGuard guard(s->device);
-  if (p.checked && (rc = launched(s, icc::state_check_launch(p, s->stream), 1, "check")) != IC_OK) return rc;
-  p.slices = (s->v.value_dim + 127) / 128;
-  p.flags = reinterpret_cast<unsigned*>(reinterpret_cast<unsigned char*>(s->v.err) + FLAGS);
-  p.slots = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS);
-  p.slot_floats = icc::state_slot_floats(s->v.key_dim, s->v.value_dim);
   // Token by token or in chunks: up to 64 tokens a sequence, chunks take 9 to 23 us while there are few states, and a token 0.5 to 1.7 us (1 sequence, 4 heads
   // of 64 x 64: 9.4 us against 8.8 for 12 tokens, 11.0 for 16; 32 heads of 128 x 128: 12.7 against 13.5 and 16.8); with an SM's share of two and more
   // they are bound by the states and by their sums (8 such sequences: 23 us against 23 for 8, 29 for 12; 64 of them: 111 against 85 for 4, 128 for 8).
   const int few = (int64_t)a.n * s->v.n_heads > s->sm_count ? 7 : 12;
-  if (a.n_tokens <= few * (int64_t)a.n) return launched(s, icc::state_step_launch(p, s->f16, s->sm_count, s->stream), 1, "state");
+  const bool by_token = a.n_tokens <= few * (int64_t)a.n, divided = by_token && a.starts && a.n_tokens > DIVIDED_FROM;
+  p.most = divided ? STEP_MOST : 0x7fffffff;
+  p.least = divided ? STEP_MOST : 0;
+  // sequences for the chunks, at most
+  const int n = divided && a.n_tokens / (STEP_MOST + 1) < a.n ? (int)(a.n_tokens / (STEP_MOST + 1)) : a.n;
+  p.long_ones = reinterpret_cast<int*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS);
+  p.n_long = divided ? n : 0;
+  DeviceGuard guard(s->device);
+  if (p.checked && (rc = launched(s, icc::state_check_launch(p, s->stream), 1, "check")) != IC_OK) return rc;
+  p.slices = (s->v.value_dim + 127) / 128;
+  p.flags = reinterpret_cast<unsigned*>(reinterpret_cast<unsigned char*>(s->v.err) + FLAGS);
+  p.slots = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(s->v.err) + WORDS + list_bytes(s->v.max_seqs));
+  p.slot_floats = icc::state_slot_floats(s->v.key_dim, s->v.value_dim);
+  if (by_token) rc = launched(s, icc::state_step_launch(p, s->f16, s->sm_count, s->stream), 1, "state");
+  if (rc != IC_OK || (by_token && !divided)) return rc;
+  // (a call without starts has a token a sequence and does not come here)
+  const int32_t *seqs = a.seqs, *starts = a.starts, *ends = a.starts + 1;
+  int among = a.n;                  // sequences that the launches look through
+  if (divided && p.checked) {       // the check has picked them
+    seqs = p.long_ones;
+    starts = p.long_ones + s->v.max_seqs;
+    ends = p.long_ones + 2 * s->v.max_seqs;
+    among = n;
+  }
+  p.checked |= by_token;
   icc::StateMaps maps;
   maps.there = encode_rows(s, p.q, s->v.key_dim, a.n_tokens, &maps.q) && encode_rows(s, p.k, s->v.key_dim, a.n_tokens, &maps.k) &&
                encode_rows(s, p.val, s->v.value_dim, a.n_tokens, &maps.val);
-  for (int off = 0; off < a.n && rc == IC_OK; off += icc::STATE_BATCH) {
-    p.seqs = a.seqs + off;
-    p.starts = a.starts + off;      // (without starts there is a token a sequence)
-    p.n = a.n - off < icc::STATE_BATCH ? a.n - off : icc::STATE_BATCH;
+  for (int off = 0; off < among && rc == IC_OK; off += icc::STATE_BATCH) {
+    p.seqs = seqs + off;
+    p.starts = starts + off;
+    p.ends = ends + off;
+    p.n = among - off < icc::STATE_BATCH ? among - off : icc::STATE_BATCH;
+    p.n_long = p.n < n ? p.n : n;
     const int items = s->v.n_heads * ((s->v.value_dim + 127) / 128), most = icc::state_items(a.n_tokens, p.n);
     for (p.first_item = 0; p.first_item < items && rc == IC_OK; p.first_item += most) {
       p.n_items = items - p.first_item < most ? items - p.first_item : most;

@@ -66,7 +66,10 @@ struct Fall {
 
 struct Tail {
   StateLine line;
-  int starts[STATE_BATCH + 1];                        // of the call's tokens
+  union {                                             // (the check comes first)
+    int starts[2 * STATE_BATCH];                      // of the call's tokens, and behind each where it ends
+    uint32_t seen[STATE_MAX_SEQS / 32];
+  };
   StatePlan plan;
   // published states that the last piece's is put together from: whose, and what is left of them after the chunks between
   int slots, slot_cta[KV_MAX_CTAS];
@@ -81,7 +84,6 @@ struct Tail {
   uint64_t clean[MAX_STAGES];                         // of a stage with a sequence's last chunk: rows behind the end are zeros
   uint64_t p_full, p_ready, copy_ready, u_full, u_free, o1_full, o2_full, o_free, drain[2];
   uint64_t slots_read[MAX_STAGES];
-  uint32_t seen[STATE_MAX_SEQS / 32];
   uint32_t tmem_base;
   int abort_flag, holds;
 };
@@ -156,6 +158,12 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
   Tail* t = reinterpret_cast<Tail*>(out_smem + OUT_BYTES);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const StateView& v = p.v;
+  if (p.least) {                                     // as a rule there is no sequence for this launch
+    grid_dep_wait();
+    bool some = false;
+    for (int i = tid; i < p.n; i += THREADS) some |= p.ends[i] - p.starts[i] > p.least;
+    if (!__syncthreads_or(some)) return;
+  }
   if (tid == 0) {
     for (int s = 0; s < n_stages; ++s) {
       mbar_init(&t->full[s], 32);
@@ -193,10 +201,12 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
     int sum = 0, longest = 0;
     for (int i0 = 0; i0 < p.n; i0 += 32) {
       const int i = i0 + lane;
-      const int from = i <= p.n ? p.starts[i] : 0, to = i < p.n ? p.starts[i + 1] : from;
-      if (i < p.n) t->starts[i] = from;
-      if (i == p.n - 1) t->starts[p.n] = to;
-      const int mine = (int)(((unsigned)(to - from) + C - 1) / C);
+      const int from = i < p.n ? p.starts[i] : 0, to = i < p.n ? p.ends[i] : 0;
+      if (i < p.n) {
+        t->starts[2 * i] = from;
+        t->starts[2 * i + 1] = to;
+      }
+      const int mine = to - from > p.least ? (int)(((unsigned)(to - from) + C - 1) / C) : 0;
       longest = max(longest, mine);
       int inc = mine;
 #pragma unroll
@@ -257,8 +267,8 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
   // (one slice or two: value_dim is 256 at most)
   auto head_of = [&](const StatePiece& x) { return (x.item + p.first_item) >> (p.slices - 1); };
   auto slice_of = [&](const StatePiece& x) { return (x.item + p.first_item) & (p.slices - 1); };
-  auto first_token = [&](const StatePiece& x) { return t->starts[x.i]; };
-  auto tokens_of = [&](const StatePiece& x) { return t->starts[x.i + 1] - t->starts[x.i]; };
+  auto first_token = [&](const StatePiece& x) { return t->starts[2 * x.i]; };
+  auto tokens_of = [&](const StatePiece& x) { return t->starts[2 * x.i + 1] - t->starts[2 * x.i]; };
   // Stages in front of a piece's chunks: the state that it begins with, or the published ones that this is put together from, 64 key dimensions each.
   auto states_of = [&](const StatePiece& x) { return x.from == StatePiece::PUBLISHED ? t->slots : x.from == StatePiece::STORED ? 1 : 0; };
   auto slots_of = [&](const StatePiece& x) { return DK * states_of(x); };
@@ -981,10 +991,10 @@ cudaError_t launch(const StateAttendParams& p, const StateMaps& maps, int sm_cou
   // A CTA with a part of an item waits for the states of all the parts before it and adds them up, so that beyond some number more parts cost more than
   // they give: with an item of M chunks, about sqrt(2 M) (30,000 tokens, one head of 128 x 128: 141 us; with sqrt(M) 142, with sqrt(4 M) 155, with an SM
   // each 314).  (Sequences of the mean length: what there is is not known here.)
-  const int64_t chunks = (p.n_tokens - 1) / C + p.n, mean = (chunks + p.n - 1) / p.n;
+  const int64_t chunks = (p.n_tokens - 1) / C + p.n_long, mean = (chunks + p.n_long - 1) / p.n_long;
   int64_t parts = 1;
   while (parts * parts < 2 * mean) ++parts;
-  parts *= (int64_t)p.n * p.n_items;
+  parts *= (int64_t)p.n_long * p.n_items;
   if (parts > sm_count) parts = sm_count;
   return launch_overlapped(state_chunk_kernel<F16, DK, DV>, dim3((unsigned)parts), dim3(THREADS), (size_t)smem_bytes<F16, DK, DV>(stages), st, 1, p, maps,
                            stages);

@@ -11,6 +11,7 @@
 
 #include "kernels.h"
 #include "kv_mma.cuh"
+#include "kv_pages.cuh"
 #include "pipeline.cuh"
 #include "state_check.cuh"
 
@@ -49,7 +50,7 @@ __global__ void __launch_bounds__(THREADS) state_step_kernel(const StateAttendPa
   const int r0 = tid / PER_ROW, col = slice * SLICE + tid % PER_ROW * 4;
   const bool here = col < v.value_dim;
   // the state is on its way while the call is looked over
-  const bool some = count > 0 && seq >= 0 && seq < v.max_seqs;
+  const bool some = count > 0 && count <= p.most && seq >= 0 && seq < v.max_seqs;
   float* state = v.pool + (((size_t)seq * v.n_layers + p.layer) * v.n_heads + head) * v.head_floats() + col;
   float4 s[ROUNDS];
 #pragma unroll
@@ -66,7 +67,7 @@ __global__ void __launch_bounds__(THREADS) state_step_kernel(const StateAttendPa
     const double decay = exp(-(double)p.rates[head]);
     decay_of = make_float2((float)decay, (float)(decay - (double)(float)decay));
   }
-  if (!state_call_holds(p, seen) || count == 0) return;
+  if (!state_call_holds(p, seen) || count == 0 || count > p.most) return;
   auto fetch = [&](int t) {
     for (int d = tid; d < 2 * RP * ROUNDS; d += THREADS) {
       const bool of_k = d >= RP * ROUNDS;
@@ -126,7 +127,27 @@ __global__ void __launch_bounds__(PLAN_THREADS) state_check_kernel(const StateAt
   grid_dep_launch_dependents();
   grid_dep_wait();
   if (*p.v.err != KV_OK) return;
-  if (!state_check_attend(p, seen) && threadIdx.x == 0) state_report(p.v, KV_INVALID);
+  if (!state_check_attend(p, seen)) {
+    if (threadIdx.x == 0) state_report(p.v, KV_INVALID);
+    return;
+  }
+  // the sequences that are left to the chunks
+  if (p.n_long == 0) return;
+  __shared__ unsigned sums[33];
+  int* const list[3] = {p.long_ones, p.long_ones + p.v.max_seqs, p.long_ones + 2 * p.v.max_seqs};
+  unsigned found = 0, total;
+  for (int i0 = 0; i0 < p.n; i0 += PLAN_THREADS) {
+    const int i = i0 + threadIdx.x;
+    const bool some = i < p.n && p.starts[i + 1] - p.starts[i] > p.most;
+    const unsigned at = found + block_scan(some, sums, &total);
+    if (some) {                           // (at most n_long, as each has more than `most` of the call's tokens)
+      list[0][at] = p.seqs[i];
+      list[1][at] = p.starts[i];
+      list[2][at] = p.starts[i + 1];
+    }
+    found += total;
+  }
+  for (int at = (int)found + threadIdx.x; at < p.n_long; at += PLAN_THREADS) list[0][at] = list[1][at] = list[2][at] = 0;
 }
 
 // ---------------------------------------------------------------- fork

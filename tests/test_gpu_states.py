@@ -509,3 +509,49 @@ def test_what_lies_behind_a_short_chunk_is_not_read(dtype):
         for i, part in ((0, slice(0, 70)), (2, slice(75, 175))):
             close(got[part], s.pool[i, 0], formula(q[part], k[part], v[part], rates_of(heads), torch.zeros(heads, 64, 64, device=DEV), 0.125), part.stop - part.start, True)
         assert not got[70:75].isfinite().all()
+
+
+MIXED = [[1] * 255 + [1500], [1] * 31 + [352], [0] * 10 + [70] + [1] * 10, [32, 33] + [1] * 20, [64] + [0] * 9, [65] + [0] * 9, [1] * 40 + [129, 31, 200] + [2] * 60,
+         [1, 200, 1] * 3 + [1] * 300 + [500] + [3] * 20 + [33] + [0] * 30]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("which", range(len(MIXED)))
+def test_a_prompt_among_single_tokens(which, dtype):
+    """Calls whose mean is short and whose longest is not: each sequence by its own length."""
+    counts = MIXED[which]
+    run(counts, heads=2, dk=64, dv=64, dtype=dtype, layers=1, layer=0, seed=70)
+    run(counts, heads=3, dk=72, dv=136, dtype=dtype, layers=1, layer=0, seed=71, order=random.Random(1).sample(range(len(counts) + 3), len(counts)),
+        max_seqs=len(counts) + 3)
+
+
+def test_many_prompts_among_many_single_tokens():
+    """More long sequences than a launch takes."""
+    counts = [1] * 2000 + [40, 33] * 150
+    random.Random(2).shuffle(counts)
+    run(counts, heads=1, dk=16, dv=16, layers=1, layer=0, seed=72)
+
+
+@pytest.mark.parametrize("bad", ["range", "twice", "starts", "end", "rate"])
+@pytest.mark.parametrize("n", [40, 300])
+def test_refused_calls_of_mixed_lengths(n, bad):
+    counts = [1] * (n - 1) + [120]
+    t, heads = sum(counts), 2
+    s = ICStates(1, heads, 16, 16, n, pool=draw(1, n, 1, heads, 16, 16, dtype=torch.float32))
+    q, rates, seqs, starts = draw(2, t, heads, 16), rates_of(heads), list(range(n)), starts_of(counts).tolist()
+    if bad == "range":
+        seqs[5] = n
+    elif bad == "twice":
+        seqs[-1] = 0
+    elif bad == "starts":
+        starts[3] = 10 ** 9
+    elif bad == "end":
+        starts[-1] -= 1
+    else:
+        rates[1] = -1.0
+    before, out = s.pool.clone(), torch.zeros_like(q)
+    s.extend(0, q, q, q, rates, ints(seqs), ints(starts), out=out)
+    with pytest.raises(ICCacheError) as e:
+        s.sync()
+    assert e.value.status == IC_ERR_INVALID
+    assert torch.equal(s.pool, before) and not out.any()
