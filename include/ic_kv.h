@@ -155,8 +155,9 @@ int ic_kv_attend(ic_kv_t* kv, const ic_kv_attend_t* a);
  *     BASE    with the base  base * factor^(rotary_dim / (rotary_dim - 2))  (rotary_dim 2: no change)
  *     BANDS   by how many turns r = original * f_i / 2 pi the pair makes over `original` tokens:  w f_i + (1 - w) f_i / factor
  *             with w = (r - low) / (high - low), between 0 and 1
- * or `frequencies` gives the f_i themselves.  Angles are exact to 2^-31 of a half turn at every position.  Rows are computed in fp32 and rounded
- * once to the cache's type.  The call changes the handle only: later calls use it, a captured graph keeps what it was captured with.
+ * or `frequencies` gives the f_i themselves (for instance where w is to go by the pair's number between rounded borders, as some checkpoints have it).
+ * Angles are off by less than 2^-24 of a half turn at every position (frequencies below 100).  Rows are computed in fp32 and rounded once to the cache's
+ * type; elements from rotary_dim on keep their bits.  The call changes the handle only: later calls use it, a captured graph keeps what it was captured with.
  * ic_kv_rotary_frequencies writes the f_i of these options to host memory (rotary_dim / 2 numbers).
  */
 enum ic_kv_rotary_layout { IC_KV_ROTARY_HALVES = 0, IC_KV_ROTARY_NEIGHBOURS = 1 };

@@ -64,7 +64,8 @@ size_t ic_state_workspace_bytes(const ic_state_opts_t* opts);
  * The newest tokens of sequences seqs[i], i < n (no sequence twice), through one layer: their states are brought up to date, and
  * every token's result is written.  Sums are held in fp32.  In calls of several tokens a sequence, products of two computed numbers
  * (scores with values, queries with states) round one of them to the 16-bit type first; the state itself is not rounded.
- * An infinite or NaN value may also reach its sequence and head's other tokens in the call.
+ * An infinite or NaN value may also reach its sequence and head's other tokens in the call, and where the formula gives an infinity the result
+ * may be a NaN.
  */
 typedef struct ic_state_attend {
   uint32_t struct_size; /* sizeof(ic_state_attend_t) of the caller's build                    */

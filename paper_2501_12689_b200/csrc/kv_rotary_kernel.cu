@@ -4,11 +4,11 @@
 // Pair i of a row at position p turns by the angle p f_i:  (a, b) -> m (a cos - b sin, a sin + b cos).  The frequency is kept as a
 // fraction of a turn, f_i / 2 pi modulo 1, in 64 bits after the point: p times it modulo 2^64 is the angle modulo a turn with an
 // error of p 2^-65 turns, at any position, by one integer product.  (p f_i in 32-bit floats is 0.008 radians off at p = 131,072.)  The
-// upper 32 bits of the product, as a signed number of half turns, go to sincospif.
+// upper 32 bits of the product, as a signed number of half turns, go to sincospif, as a float: off by up to 2^-25 half turns.
 //
 // Nothing is computed to speak of; the bound is the bytes: each row read once and written once.  Sines and cosines are worked out once per
 // token and CTA into shared memory, and a thread takes the same place in the rows of TOKENS tokens, so that their loads are
-// under way together.  8 prompts of up to 6000 tokens, 32 query and 8 kv heads of 128: 132 us, 6.0 TB/s; keys moved in place: 110 us, 5.2 TB/s.
+// under way together.  8 prompts of up to 6000 tokens, 32 query and 8 kv heads of 128: 132 us, 6.0 TB/s; keys moved in place: 111 us, 5.2 TB/s.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -52,7 +52,7 @@ __device__ __forceinline__ int table_at(int i, int turned) {
 template <int KIND>
 __device__ __forceinline__ void make_entry(const KvRotary& r, int i, long long pos, float magnitude, int turned, float* cosv, float* sinv) {
   float c, s;
-  const int turn = (int)(((unsigned long long)pos * r.turn[i]) >> 32);        // 2^-31 half turns
+  const int turn = (int)(((unsigned long long)pos * r.turn[i]) >> 32);        // in 2^-31 half turns
   sincospif((float)turn * 4.656612873077393e-10f, &s, &c);
   const int at = table_at<KIND>(i, turned);
   cosv[at] = c * magnitude;
@@ -429,7 +429,7 @@ cudaError_t shift_launch(const KvView& v, const KvRotary& rot, const int* seqs, 
   int layers = 128 / of_layer;             // about 128 rows to a unit
   if (layers < 1) layers = 1;
   if (layers > v.n_layers) layers = v.n_layers;
-  // (8 CTAs an SM, in turns: 48 sequences of up to 701 tokens, 8 layers of 8 heads of 128: 110 us, 5.2 TB/s; 4 an SM: 124)
+  // (8 CTAs an SM, in turns: 48 sequences of up to 701 tokens, 8 layers of 8 heads of 128: 111 us, 5.2 TB/s; 4 an SM: 124)
   const int64_t units = (int64_t)n * v.max_pages * ((v.n_layers + layers - 1) / layers), ctas = units < 8 * sm_count ? units : 8 * sm_count;
   return launch_overlapped(kv_shift_kernel<F16, KIND>, dim3((unsigned)ctas), dim3(THREADS), 0, st, 1, v, rot, seqs, by, n, layers);
 }

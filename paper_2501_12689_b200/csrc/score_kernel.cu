@@ -7,8 +7,8 @@
 // 10^30 for rows masked with the type's lowest value.)
 // Every logit is read once, as 16-byte vectors, VECTORS of them at a time.  Per logit: one exponential (the special
 // function units do 16 a cycle and SM: in 16 bits three quarters of their rate at the copy's bandwidth), and about six other
-// instructions, pairs of floats at a time, where the bandwidth leaves room for eleven.  4,001 rows of 128,256 in bf16: 164 us, 6.3 TB/s; with five
-// alternatives 191, with twenty 211.  VECTORS and CTAS an SM: 6 and 4; 8 and 3 take 166, 200 and 227, 4 and 4 171, 198 and 216, 4 and 5 161, 200 and 216.
+// instructions, pairs of floats at a time, where the bandwidth leaves room for eleven.  4,001 rows of 128,256 in bf16, in a graph: 163 us, 6.3 TB/s; with five
+// alternatives 192, with twenty 211.  VECTORS and CTAS an SM: 6 and 4; 8 and 3 take 166, 200 and 227, 4 and 4 171, 198 and 216, 4 and 5 161, 200 and 216.
 //
 // Top alternatives: a lower bound of the row's n-th best is the n-th largest of the maxima of 64 groups of threads, as these are n different
 // elements.  So all that the pass over the row does for them is to note the maximum of each thread's blocks (or of groups of them, in long

@@ -26,7 +26,7 @@
 // Two warps issue because a product takes one about 100 cycles, more than the tensor cores.  The rows of a sequence's last chunk that
 // lie behind its end (another sequence's) are set to zeros in shared memory, by the warps of W.
 // Bound: HBM, 1 KB a token and head of 128 x 128; a chunk is 64 KB, 2,750 cycles of an SM's share.  The products take 1,600, a chunk with all that waits
-// for them 3,800: 8 prompts of 2,800 tokens, 32 heads of 128 x 128, in bf16: 221 us, 3.3 TB/s.  Loops are rolled where registers allow: the roles'
+// for them 3,800: 8 prompts of 2,800 tokens, 32 heads of 128 x 128, in bf16: 219 us, 3.4 TB/s.  Loops are rolled where registers allow: the roles'
 // code has to stay in the instruction caches, and warps still wait for instructions more than for any unit.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
