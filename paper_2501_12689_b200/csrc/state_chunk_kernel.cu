@@ -26,7 +26,7 @@
 // Two warps issue because a product takes one about 100 cycles, more than the tensor cores.  The rows of a sequence's last chunk that
 // lie behind its end (another sequence's) are set to zeros in shared memory, by the warps of W.
 // Bound: HBM, 1 KB a token and head of 128 x 128; a chunk is 64 KB, 2,750 cycles of an SM's share.  The products take 1,600, a chunk with all that waits
-// for them 3,800: 8 prompts of 2,800 tokens, 32 heads of 128 x 128, in bf16: 219 us, 3.4 TB/s.  Loops are rolled where registers allow: the roles'
+// for them 3,800: 8 prompts of 2,800 tokens, 32 heads of 128 x 128, in bf16: 219 us, 3.3 TB/s.  Loops are rolled where registers allow: the roles'
 // code has to stay in the instruction caches, and warps still wait for instructions more than for any unit.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -58,10 +58,11 @@ constexpr uint32_t T_P = 0, T_O1 = 64, T_O2 = 128, T_COPY = 192, T_U = 256, T_W 
 template <bool F16>
 constexpr int PARTS = F16 ? 2 : 3;                    // 16-bit numbers that hold one of W
 
-// A head's powers of l.
-constexpr int FALL = C;
+// A head's powers of l.  What a chunk leaves of a state, l^64, rounded would be off the same way every time (1e-5 after 900 chunks of a slow decay), so the
+// chunks take turns with the two floats next to it: what TURNS of them leave is right to half a step of one.
+constexpr int FALL = C, TURN = 2 * C + 4, TURNS = 32;
 struct Fall {
-  float at[2 * C + 4];                                // l^j at FALL + j, j = 0 .. 64, with zeros in front
+  float at[TURN + TURNS];                             // l^j at FALL + j, j = 0 .. 64, with zeros in front; the turns at TURN
 };
 
 struct Tail {
@@ -137,6 +138,14 @@ __device__ __noinline__ float fall_of(float rate, int steps) {
   if (steps == 0) return 1.0f;                       // (also of an infinite rate)
   const double y = fmax(-(double)rate * steps * 1.4426950408889634, -200.0), whole = rint(y);
   return ldexpf(exp2f((float)(y - whole)), (int)whole);
+}
+
+// What chunk i, modulo TURNS, leaves of a state.
+__device__ __noinline__ float turn_of(float rate, int i) {
+  const double whole = exp(-(double)rate * C);
+  const float near = (float)whole, rest = (float)(whole - (double)near);
+  const float other = __uint_as_float(__float_as_uint(near) + (rest < 0.0f ? -1 : 1)), share = rest / (other - near);      // share: 0 .. 1 / 2
+  return rintf((i + 1) * share) != rintf(i * share) ? other : near;
 }
 
 template <bool F16, int DK, int DV>
@@ -522,7 +531,8 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
       if (warp == W_SCORES || !ok || !load_walk.next(&loading)) return;
       const float rate = p.rates[head_of(loading)];
       wait(&t->fall_free[served & 1], ((served >> 1) & 1) ^ 1);
-      for (int j = lane; j < 2 * C + 4; j += 32) t->fall[served & 1].at[j] = j < FALL ? 0.0f : fall_of(rate, j - FALL);
+      for (int j = lane; j < TURN; j += 32) t->fall[served & 1].at[j] = j < FALL ? 0.0f : fall_of(rate, j - FALL);
+      t->fall[served & 1].at[TURN + lane] = turn_of(rate, lane);
       tell(&t->fall_ready[served & 1]);
       ++served;
     };
@@ -811,7 +821,7 @@ __global__ void __launch_bounds__(THREADS, 1) state_chunk_kernel(const __grid_co
             tell(&t->copy_ready);
             out_ph ^= 1u;
           }
-          const float decay = t->fall[n_pieces & 1].at[FALL + min(C, count - c * C)];
+          const float decay = t->fall[n_pieces & 1].at[count - c * C < C ? FALL + count - c * C : TURN + (c & (TURNS - 1))];
           wait(&t->u_full, ph);
           if (!ok) break;
           tc_fence_after_sync();

@@ -555,3 +555,20 @@ def test_refused_calls_of_mixed_lengths(n, bad):
         s.sync()
     assert e.value.status == IC_ERR_INVALID
     assert torch.equal(s.pool, before) and not out.any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("t,n,heads", [(3840, 30, 8), (16384, 12, 8)])
+@pytest.mark.parametrize("rate", [0.0, 1e-6, 1e-5, 1e-4, 1e-3])
+def test_slow_decays_over_many_chunks(rate, t, n, heads, dtype):
+    """Items of many chunks that one CTA walks over: what a chunk leaves of the state is not off the same way every time.  fp32: a rounding a chunk of
+    2^-24 of the state at most, as often up as down, so sqrt(chunks) 2^-24 of it or less, and each chunk's own sums, 2e-7 = 2^-22.2."""
+    s = ICStates(1, heads, 64, 64, n, dtype=dtype)
+    q, k, v = (draw(i, t, heads, 64, dtype=dtype) for i in range(3))
+    rates = rate * torch.linspace(1.0, 1.7, heads, device=DEV)
+    s.extend(0, *(x.repeat(n, 1, 1) for x in (q, k, v)), rates, ints(list(range(n))), starts_of([t] * n))
+    s.sync()
+    want = formula(q, k, v, rates, torch.zeros(heads, 64, 64, device=DEV), 0.125)[3]
+    for i in (0, n // 2, n - 1):
+        for h in range(heads):
+            assert (s.pool[i, 0, h].double() - want[h]).norm() <= (math.sqrt(t / 64) * 2.0 ** -24 + 2.0 ** -22) * want[h].norm()
